@@ -68,6 +68,14 @@ extern "C" {
 #define LINFUSION_FLAG_FORCE_FUSED 4u  /* take the single-launch path whenever the shape allows it */
 #define LINFUSION_FLAG_FORCE_SOLO 8u   /* take the replicated-state launch whenever the shape allows it */
 
+/* flags for linfusion_rope */
+#define LINFUSION_FLAG_ROPE_NEIGHBOURS 1u /* channels 2i and 2i + 1 of a section are a pair; else i and i + half */
+#define LINFUSION_FLAG_ROPE_INVERSE 2u    /* turn back: the inverse, and the gradient */
+
+/* flags for linfusion_gate_norm_fwd / _bwd */
+#define LINFUSION_FLAG_NORM_RMS 1u  /* root mean square norms; else layer norms */
+#define LINFUSION_FLAG_NORM_POST 2u /* the block's output is normed before its gate */
+
 #define LINFUSION_OK 0
 #define LINFUSION_ERR_INVALID (-1)     /* NULL pointer, B/H/N/d <= 0, eps < 0 or NaN, bad flags */
 #define LINFUSION_ERR_UNSUPPORTED (-2) /* d, dtype or feature_map outside the supported sets */
@@ -412,6 +420,136 @@ int linfusion_init(void);
 int linfusion_attn_state(const void* k, const void* v, float* state_out,
                          int B, int H, long long N, int d, int dtype, int feature_map,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Around the mixer: positions, block boundaries, and a causal mixer with a state --------------------------------
+ *
+ * What a transformer block on image or video tokens needs beside its token mixer.  Conventions as above (device
+ * pointers, caller-owned buffers and workspaces, `stream`, status codes, nothing enqueued on an error, no allocation, no
+ * synchronisation, run-to-run identical results, may be recorded into a HIP graph), and these:
+ *   - Element types fp16, bf16, fp32 throughout; vectors, decays, corrections and states are fp32.  Arithmetic is fp32
+ *     (angles and sums of log decays fp64), every result is rounded once.
+ *   - [B, H, N, d] views: element strides {batch, head, token} as in linfusion_attn_fwd_strided; a NULL array is the
+ *     contiguous tensor.  [B, N, C] views: element strides {batch, token}.
+ *   - `lengths`: NULL, or a DEVICE array of B int32: only the first lengths[b] tokens (clamped to 0 .. N) of batch row b
+ *     count.  Tokens behind them are not read, whatever they hold, and what is written per token is left as it was there.
+ *   - Calls that share a workspace must be ordered on one stream, captured graphs that share one likewise.
+ */
+
+/*
+ * Rotary positions with several axes (height and width of an image; time, height and width of a video), on the queries
+ * and keys of one layer in one call.  Axis a owns the next channels[a] channels of a head and turns their pair i by
+ *
+ *     theta = positions[a] * scales[a] * bases[a]^(-2 i / channels[a]):
+ *     (x1, x2) -> (x1 cos theta - x2 sin theta, x2 cos theta + x1 sin theta)
+ *
+ * Channels behind the last axis keep their values.
+ *
+ *   q, q_out        [B, H, N, d] views; k, k_out: [B, H_k, N, d] views, or both NULL.  q_out == q (k_out == k) with the same
+ *                   strides works in place; else an output must not overlap an input.  Views whose spans interleave
+ *                   (columns of one projection) are accepted where their rows lie side by side in each token.
+ *   d               multiple of 8 up to 256.  axes: 1 .. 4.  channels, bases, scales: HOST arrays of `axes` values;
+ *                   channels even, positive, in all at most d; bases > 0; scales NULL = 1.
+ *   positions       DEVICE int32, element {b, a, n} at b * position_strides[0] + a * position_strides[1] + n; NULL strides:
+ *                   {0, N}, one [axes, N] table for the whole batch.
+ *   flags           LINFUSION_FLAG_ROPE_*.  The gradient with respect to q and k is the call with
+ *                   LINFUSION_FLAG_ROPE_INVERSE on the gradients of q_out and k_out.
+ * One kernel.
+ */
+int linfusion_rope(const void* q, const void* k, void* q_out, void* k_out, const int* positions, int axes,
+                   const int* channels, const double* bases, const double* scales, int B, int H, int H_k, long long N,
+                   int d, int dtype, unsigned flags, const int* lengths, const long long q_strides[3],
+                   const long long k_strides[3], const long long q_out_strides[3], const long long k_out_strides[3],
+                   const long long position_strides[2], void* stream);
+
+/*
+ * The boundary between two blocks: the residual update with its gate, and the modulated norm the next block starts with.
+ *
+ *     fhat = f,  or with LINFUSION_FLAG_NORM_POST  norm(f) * w_post
+ *     y    = residual_scale * x + gate * fhat
+ *     h    = norm(y) * w_pre * (1 + scale) + shift              (of the unrounded y)
+ *
+ * norm: over a token's C channels, (t - mean) / sqrt(mean((t - mean)^2) + norm_eps); with LINFUSION_FLAG_NORM_RMS
+ * t / sqrt(mean(t^2) + norm_eps).
+ *
+ *   x, f, y, h      [B, N, C] views, strides[i] of them in this order (strides NULL: all contiguous); C a multiple of 8 up to
+ *                   8192.  f NULL: no block output (the first norm of a model: y = residual_scale * x).  y or h may be NULL
+ *                   (not both): not written.  y == x with the same strides works in place; no other overlap.
+ *   gate, scale, shift  fp32 modulation rows, row b at b * mod_stride (a multiple of 4; 0: one row for the batch); each may
+ *                   be NULL (1, 0, 0).
+ *   w_pre, w_post   fp32 [C] or NULL (1).
+ */
+int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, const float* scale, const float* shift,
+                            const float* w_pre, const float* w_post, void* y, void* h, int B, long long N, int C,
+                            int dtype, float residual_scale, float norm_eps, unsigned flags, const int* lengths,
+                            const long long strides[4][2], long long mod_stride, void* stream);
+
+/*
+ * Its gradients, given dy (gradient that reaches y past the next block) and dh; either may be NULL (0).  x, f and the
+ * vectors are the forward call's; y and the statistics are formed again.  strides: x, f, dy, dh, dx, df.
+ * Every output may be NULL (not all).  dx == dy with the same strides works in place; no other overlap.
+ * dgate, dscale, dshift: fp32 rows with dmod_stride between them; with mod_stride 0 one row each, summed over the
+ * batch.  dw_pre, dw_post: fp32 [C].  The workspace is needed only for these vectors (else NULL).
+ */
+int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, const float* scale, const float* w_pre,
+                            const float* w_post, const void* dy, const void* dh, void* dx, void* df, float* dgate,
+                            float* dscale, float* dshift, float* dw_pre, float* dw_post, int B, long long N, int C,
+                            int dtype, float residual_scale, float norm_eps, unsigned flags, const int* lengths,
+                            const long long strides[6][2], long long mod_stride, long long dmod_stride,
+                            void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C);
+
+/*
+ * The gated delta rule: a causal linear attention whose d_k x d_v state S forgets by a gate and corrects what it holds for a
+ * key instead of adding to it.  Per (batch, head), token after token:
+ *
+ *     S' = e^g_t S;   u_t = beta_t (v_t - S'^T k_t);   S = S' + k_t u_t^T;   out_t = scale S^T q_t
+ *
+ *   q, k            [B, H_k, N, d_k] views, v, out: [B, H, N, d_v] views; H a multiple of H_k, value head h reads query and key
+ *                   head h / (H / H_k).  d_k a multiple of 8 up to 160, d_v up to 256; B * H <= 65535, N < 2^30.
+ *   g, beta         fp32 views [B, H, N] that share gate_strides {batch, head, token}: log decays (<= 0; -infinity forgets
+ *                   everything) and corrections (0: the token leaves the state as it is apart from its decay).  The recurrence
+ *                   is stable for keys of length at most sqrt(2 / beta), unit length usually.
+ *   state_in        fp32 [B, H, d_k, d_v], 16-byte aligned, or NULL (zeros).  state_out: the state behind the last token, or
+ *                   NULL; may be state_in itself.
+ *   saved           NULL, or DEVICE memory of linfusion_delta_saved_bytes that keeps what linfusion_delta_bwd needs again.
+ *   flags           0.
+ *   workspace       DEVICE scratch of linfusion_delta_workspace_bytes, 16-byte aligned; not used when `saved` is given.
+ * No output may overlap another buffer, apart from state_out == state_in.
+ */
+int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                        const float* state_in, void* out, float* state_out, const int* lengths, void* saved,
+                        size_t saved_bytes, int B, int H, int H_k, long long N, int d_k, int d_v, int dtype, float scale,
+                        unsigned flags, const long long q_strides[3], const long long k_strides[3],
+                        const long long v_strides[3], const long long out_strides[3], const long long gate_strides[3],
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_delta_workspace_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype);
+size_t linfusion_delta_saved_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype);
+
+/*
+ * Its gradients, given dout and dstate_out (gradient of state_out; NULL: 0).  dq, dk: [B, H_k, N, d_k] views, the sum over
+ * the value heads that share them; dv [B, H, N, d_v]; dg, dbeta: fp32 [B, H, N] views that share dgate_strides; dstate_in:
+ * fp32 [B, H, d_k, d_v] or NULL, may be dstate_out itself.  `saved`: what the forward call with the same arguments left,
+ * or NULL: formed again.  With `saved`, linfusion_delta_saved_bytes less than linfusion_delta_bwd_workspace_bytes suffice.
+ */
+int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                        const float* state_in, const void* dout, const float* dstate_out, const void* saved,
+                        size_t saved_bytes, void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dstate_in,
+                        const int* lengths, int B, int H, int H_k, long long N, int d_k, int d_v, int dtype, float scale,
+                        unsigned flags, const long long q_strides[3], const long long k_strides[3],
+                        const long long v_strides[3], const long long gate_strides[3], const long long dout_strides[3],
+                        const long long dq_strides[3], const long long dk_strides[3], const long long dv_strides[3],
+                        const long long dgate_strides[3], void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_delta_bwd_workspace_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype);
+
+/*
+ * The gated delta rule for one new token of every batch row: q, k [B, H_k, d_k], v, out [B, H, d_v], g, beta [B, H], with
+ * element strides {batch, head} (NULL: contiguous).  state_out may be state_in itself.  One kernel, no workspace.
+ */
+int linfusion_delta_step(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                         const float* state_in, float* state_out, void* out, int B, int H, int H_k, int d_k, int d_v,
+                         int dtype, float scale, unsigned flags, const long long q_strides[2],
+                         const long long k_strides[2], const long long v_strides[2], const long long out_strides[2],
+                         const long long gate_strides[2], void* stream);
 
 /* Frees the library-owned scratch buffers (synchronises).  Optional; safe to call twice. */
 void linfusion_release(void);

@@ -12,3 +12,9 @@ from .binding import (  # noqa: F401
     linfusion_attn_fwd_f32, linfusion_attn_fwd_profile, linfusion_attn_fwd_static, linfusion_attn_static_scratch_bytes, linfusion_init, linfusion_attn_fwd_strided, linfusion_attn_last_error, linfusion_attn_plan, linfusion_attn_apply_kernel, linfusion_attn_state, linfusion_attn_workspace_bytes, linfusion_attn_workspace_state_offset,
     linfusion_hbm_probe, linfusion_launch_probe, linfusion_release, linfusion_set_tuning, linfusion_status_string, linfusion_version,
 )
+from .block import (  # noqa: F401
+    FLAG_NORM_POST, FLAG_NORM_RMS, FLAG_ROPE_INVERSE, FLAG_ROPE_NEIGHBOURS, linfusion_delta_bwd,
+    linfusion_delta_bwd_workspace_bytes, linfusion_delta_fwd, linfusion_delta_saved_bytes, linfusion_delta_step,
+    linfusion_delta_workspace_bytes, linfusion_gate_norm_bwd, linfusion_gate_norm_bwd_workspace_bytes,
+    linfusion_gate_norm_fwd, linfusion_rope,
+)

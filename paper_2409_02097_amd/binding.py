@@ -107,6 +107,8 @@ def library() -> ctypes.CDLL:
     lib.linfusion_attn_apply_kernel.restype = ctypes.c_char_p
     lib.linfusion_attn_plan.argtypes = [i32, i32, i64, i32, i32, u32, ctypes.POINTER(ctypes.c_int * 4)]
     lib.linfusion_attn_plan.restype = i32
+    from . import block
+    block.declare(lib)
     _lib = lib
     return lib
 

@@ -1,0 +1,185 @@
+// Rotary positions with several axes: an axis owns a section of a head's channels, in pairs, and turns pair i of its c
+// channels by  theta = pos * scale * base^(-2 i / c):
+//
+//     (x1, x2) -> (x1 cos theta - x2 sin theta, x2 cos theta + x1 sin theta)
+//
+// Turning by -theta is the inverse and the gradient.  Bound: HBM, each value read once and written once.  The angles depend
+// on the token and the pair, not on the head: a workgroup takes a few tokens of one batch row through all heads of q and k
+// and computes each sine and cosine once.  theta is formed in turns, in fp64: a position of 10^5 leaves an fp32 product
+// no more than 3 correct digits of the angle, and the fraction of the fp64 product is exact to 2^-36.
+#pragma once
+#include "lf_vec8.hpp"
+
+namespace lf {
+
+constexpr int kRopeAxes = 4;
+constexpr int kRopePairs = 128;   // d <= 256
+
+struct RopeSide {
+  const void* x;
+  void* y;
+  long long xb, xh, xn, yb, yh, yn;   // element strides {batch, head, token}
+  int H;
+  int by_token;                       // heads of a token are the nearer neighbours in memory
+};
+
+struct RopeArgs {
+  RopeSide side[2];
+  const int* positions;
+  long long pos_batch, pos_axis;
+  const int* lengths;
+  long long N;
+  int d, pairs, axes, tokens;         // tokens: per workgroup
+  int first[kRopeAxes + 1];           // first channel of each section; behind the last one channels have no position
+  unsigned inverse;
+  double rate[kRopePairs];            // turns per unit of position
+};
+
+// cos and sin of `turns` of a full turn.  The hardware's own (argument in turns; absolute error near 2^-20) for the 16-bit
+// types, whose results are rounded to 2^-9 or 2^-12; the library's for fp32.
+template <typename T> LF_DEV f32x2 turn_of(double turns) {
+  const float r = (float)(turns - __builtin_rint(turns));
+  if constexpr (Stored<T>::kBytes == 4) {
+    float s, c;
+    sincospif(2.0f * r, &s, &c);
+    return f32x2{c, s};
+  } else {
+    return f32x2{__builtin_amdgcn_cosf(r), __builtin_amdgcn_sinf(r)};
+  }
+}
+
+inline __host__ __device__ size_t rope_table_bytes(int tokens, int pairs) { return ((size_t)tokens * pairs * 8 + 15) & ~(size_t)15; }
+
+// MODE 0: neighbouring channels are paired (pair = channel / 2).  1: a section's first half with its second half, all
+// halves whole vectors of 8 channels; 2: the same, halves of any size.
+// A wave takes 64 / (d / 8) whole rows at a time, a lane 8 channels; the halves change places through LDS that only the
+// wave itself uses, after its loads and before its stores, so a call may work in place.
+template <typename T, int MODE>
+__global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kVec = 8 * Stored<T>::kBytes;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int b = blockIdx.y;
+  const long long n_end = tokens_of(a.lengths, b, a.N);
+  const long long n0 = (long long)blockIdx.x * a.tokens;
+  if (n0 >= n_end) return;
+  const int tokens = n_end - n0 < a.tokens ? (int)(n_end - n0) : a.tokens;
+  f32x2* table = reinterpret_cast<f32x2*>(smem);                       // [tokens][pairs]
+  unsigned char* stage = smem + rope_table_bytes(a.tokens, a.pairs) + (size_t)wave * 64 * kVec;
+  for (int i = tid; i < tokens * a.pairs; i += 256) {
+    const int t = i / a.pairs, p = i - t * a.pairs;
+    int axis = 0;
+#pragma unroll
+    for (int s = 1; s < kRopeAxes; ++s)
+      if (s < a.axes && 2 * p >= a.first[s]) axis = s;
+    const int pos = a.positions[b * a.pos_batch + axis * a.pos_axis + n0 + t];
+    f32x2 cs = turn_of<T>((double)pos * a.rate[p]);
+    if (a.inverse) cs[1] = -cs[1];
+    table[i] = cs;
+  }
+  __syncthreads();
+  const int chunks = a.d >> 3, per = 64 / chunks;      // vectors per row, rows per wave and step
+  const int own = lane / chunks, c0 = (lane - own * chunks) * 8;
+  // where this lane's 8 channels stand: the pair of the first, the partner's channel, and the sign of its part
+  int pair = c0 >> 1, partner = 0;
+  float sign = 1.0f;
+  const bool turned = c0 < a.first[a.axes];
+  if constexpr (MODE == 1) {
+    int s0 = 0, s1 = a.first[1];
+#pragma unroll
+    for (int s = 1; s < kRopeAxes; ++s)
+      if (s < a.axes && c0 >= a.first[s]) { s0 = a.first[s]; s1 = a.first[s + 1]; }
+    const int half = (s1 - s0) >> 1, o = c0 - s0;
+    const bool upper = o >= half;
+    pair = (s0 >> 1) + (upper ? o - half : o);
+    partner = upper ? c0 - half : c0 + half;
+    sign = upper ? 1.0f : -1.0f;
+  }
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    const RopeSide& side = a.side[which];
+    if (!side.x) continue;
+    const int rows = tokens * side.H, step = 4 * per;
+    for (int r0 = wave * per; r0 < rows; r0 += step) {
+      const int r = r0 + own;
+      const bool on = own < per && r < rows;
+      int t, h;
+      if (side.by_token) { t = (int)((unsigned)r / (unsigned)side.H); h = r - t * side.H; }
+      else { h = (int)((unsigned)r / (unsigned)tokens); t = r - h * tokens; }
+      float x[8], y[8];
+      Raw8<T> raw;
+      if (on) {
+        raw = load8_raw<T>(at<T>(side.x, b * side.xb + h * side.xh + (n0 + t) * side.xn + c0));
+        widen8<T>(raw, x);
+        if constexpr (MODE != 0) {
+          unsigned char* p = stage + lane * kVec;
+          *reinterpret_cast<u32x4*>(p) = raw.w;
+          if constexpr (Stored<T>::kBytes == 4) *reinterpret_cast<u32x4*>(p + 16) = raw.w2;
+        }
+      }
+      if constexpr (MODE != 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (LDS that only this wave uses)
+      if (on) {
+        const f32x2* cs = table + t * a.pairs;
+        if constexpr (MODE == 0) {
+          if (turned) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (pair + j < a.pairs) {
+                const f32x2 e = cs[pair + j];
+                y[2 * j] = x[2 * j] * e[0] - x[2 * j + 1] * e[1];
+                y[2 * j + 1] = x[2 * j + 1] * e[0] + x[2 * j] * e[1];
+              } else {
+                y[2 * j] = x[2 * j];
+                y[2 * j + 1] = x[2 * j + 1];
+              }
+            }
+          }
+        } else if constexpr (MODE == 1) {
+          if (turned) {
+            float z[8];
+            load8<T>(stage + (lane + (partner - c0) / 8) * kVec, z);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const f32x2 e = cs[pair + j];
+              y[j] = x[j] * e[0] + sign * (z[j] * e[1]);
+            }
+          }
+        } else if (turned) {
+          const unsigned char* row = stage + own * chunks * kVec;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int c = c0 + j;
+            y[j] = x[j];
+            if (c >= a.first[a.axes]) continue;
+            int s0 = 0, s1 = a.first[1];
+#pragma unroll
+            for (int s = 1; s < kRopeAxes; ++s)
+              if (s < a.axes && c >= a.first[s]) { s0 = a.first[s]; s1 = a.first[s + 1]; }
+            const int half = (s1 - s0) >> 1, o = c - s0;
+            const bool upper = o >= half;
+            const f32x2 e = cs[(s0 >> 1) + (upper ? o - half : o)];
+            const int other = upper ? c - half : c + half;
+            float z;
+            if constexpr (Stored<T>::kBytes == 4) {
+              z = *reinterpret_cast<const float*>(row + other * 4);
+            } else {
+              float dummy;
+              unpack2<T>(*reinterpret_cast<const uint16_t*>(row + other * 2), z, dummy);
+            }
+            y[j] = x[j] * e[0] + (upper ? z * e[1] : -(z * e[1]));
+          }
+        }
+        unsigned char* to = at<T>(side.y, b * side.yb + h * side.yh + (n0 + t) * side.yn + c0);
+        if (turned) {
+          store8<T>(to, y);
+        } else {   // channels without a position keep their bits
+          *reinterpret_cast<u32x4*>(to) = raw.w;
+          if constexpr (Stored<T>::kBytes == 4) *reinterpret_cast<u32x4*>(to + 16) = raw.w2;
+        }
+      }
+      if constexpr (MODE != 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+}
+
+}  // namespace lf

@@ -1,0 +1,338 @@
+// The gated delta rule (lf_delta.hpp, lf_delta_bwd.hpp, lf_delta_step.hpp): checks, workspace layout, launches.
+#include "../../include/linfusion.h"
+
+#include <stdint.h>
+
+#include <cmath>
+#include <initializer_list>
+
+#include "lf_delta.hpp"
+#include "lf_delta_bwd.hpp"
+#include "lf_delta_step.hpp"
+#include "lf_host_api.hpp"
+
+namespace {
+
+using lfh::overlaps;
+
+constexpr int kMaxKey = 160, kMaxValue = 256;
+
+size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct Sizes {
+  long long nc, heads;   // chunks of N tokens; B * H
+  int dkb, dvb;
+  size_t esz;
+  size_t t, w, u, s, decay, du, ds;   // bytes
+  size_t saved() const { return t + w + u + s + decay; }
+  size_t forward() const { return w + u + s + decay; }
+  size_t backward() const { return du + ds; }
+};
+
+int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Sizes* z) {
+  if (B <= 0 || H <= 0 || H_k <= 0 || N <= 0 || dk <= 0 || dv <= 0) return LINFUSION_ERR_INVALID;
+  if ((long long)B * H > 65535 || H % H_k || N >= 1LL << 30) return LINFUSION_ERR_INVALID;
+  if (dtype != LINFUSION_DTYPE_F32 && dtype != LINFUSION_DTYPE_F16 && dtype != LINFUSION_DTYPE_BF16)
+    return LINFUSION_ERR_UNSUPPORTED;
+  if (dk % 8 || dv % 8 || dk > kMaxKey || dv > kMaxValue) return LINFUSION_ERR_UNSUPPORTED;
+  z->nc = (N + lf::kDeltaChunk - 1) / lf::kDeltaChunk;
+  z->heads = (long long)B * H;
+  z->dkb = (dk + 15) / 16;
+  z->dvb = (dv + 15) / 16;
+  z->esz = dtype == LINFUSION_DTYPE_F32 ? 4 : 2;
+  const size_t chunks = (size_t)z->heads * (size_t)z->nc;
+  z->t = up(chunks * 4096 * 4);
+  z->w = up(chunks * z->dkb * 1024 * 4);
+  z->u = up(chunks * z->dvb * 1024 * 4);
+  z->s = up((chunks + (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
+  z->decay = up(chunks * lf::kDecayRows * 4);
+  z->du = z->u;
+  z->ds = up(chunks * z->dvb * z->dkb * 256 * 4);
+  return LINFUSION_OK;
+}
+
+struct Range { const void* p; size_t n; bool written; const void* same; };   // `same`: the one range it may coincide with
+
+bool clash(const Range* r, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = i + 1; j < n; ++j) {
+      if (!r[i].p || !r[j].p || !(r[i].written || r[j].written)) continue;
+      if (!overlaps(r[i].p, r[i].n, r[j].p, r[j].n)) continue;
+      if (r[i].p == r[j].p && r[i].n == r[j].n && (r[i].same == r[j].p && r[i].same)) continue;
+      return true;
+    }
+  return false;
+}
+
+// rows of `d` channels of the tensors' type
+int check_rows(const void* p, const long long* given, int B, int H, long long N, int d, size_t esz, bool written,
+               lf::DeltaView* v, size_t* bytes) {
+  long long s[3] = {H * N * d, N * d, d};
+  const long long extent[3] = {B, H, N};
+  for (int i = 0; i < 3; ++i)
+    if (extent[i] == 1) s[i] = 0;   // (never used, whatever it says)
+    else if (given) s[i] = given[i];
+  if ((uintptr_t)p & 15) return LINFUSION_ERR_MISALIGNED;
+  const int rc = lfh::check_strides(s, B, H, N, d, esz, written);
+  if (rc != LINFUSION_OK) return rc;
+  *v = lf::DeltaView{s[0], s[1], s[2]};
+  *bytes = lfh::span_bytes(s, B, H, N, d, esz);
+  return LINFUSION_OK;
+}
+
+// one fp32 value per token and head, at any strides: judged as rows of four at four times the strides
+int check_scalars(std::initializer_list<const void*> ps, const long long* given, int B, int H, long long N, bool written,
+                  lf::DeltaView* v, size_t* bytes) {
+  long long s[3] = {H * N, N, 1};
+  const long long extent[3] = {B, H, N};
+  for (int i = 0; i < 3; ++i)
+    if (extent[i] == 1) s[i] = 0;
+    else if (given) s[i] = given[i];
+  for (const void* p : ps)
+    if ((uintptr_t)p & 3) return LINFUSION_ERR_MISALIGNED;
+  for (int i = 0; i < 3; ++i)
+    if (s[i] < 0 || s[i] >= 1LL << 44) return LINFUSION_ERR_INVALID;
+  const long long wide[3] = {4 * s[0], 4 * s[1], 4 * s[2]};
+  const int rc = lfh::check_strides(wide, B, H, N, 4, 4, written);
+  if (rc != LINFUSION_OK) return rc;
+  *v = lf::DeltaView{s[0], s[1], s[2]};
+  *bytes = (size_t)((B - 1) * s[0] + (H - 1) * s[1] + (N - 1) * s[2] + 1) * 4;
+  return LINFUSION_OK;
+}
+
+float* take(unsigned char*& p, size_t n) {
+  float* r = reinterpret_cast<float*>(p);
+  p += n;
+  return r;
+}
+
+void place_saved(lf::DeltaArgs* a, const Sizes& z, void* at, bool with_t) {
+  unsigned char* p = static_cast<unsigned char*>(at);
+  a->t = with_t ? take(p, z.t) : nullptr;
+  a->w = take(p, z.w);
+  a->u = take(p, z.u);
+  a->s = take(p, z.s);
+  a->decay = take(p, z.decay);
+}
+
+template <typename T, int BLOCKS> void launch_scan(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  lf::delta_scan<T, BLOCKS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+}
+template <typename T, int BLOCKS> void launch_back_scan(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  lf::delta_back_scan<T, BLOCKS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+}
+
+// T, W, U, the states and the decays of all chunks
+template <typename T> int run_states(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  const int lds = lf::delta_prepare_lds(a.dkb, a.dvb);
+  if (!lfh::allow_lds(lf::delta_prepare<T>, lds)) return LINFUSION_ERR_HIP;
+  lf::delta_prepare<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+  if (a.dkb <= 4) launch_scan<T, 1>(a, BH, st);
+  else if (a.dkb <= 8) launch_scan<T, 2>(a, BH, st);
+  else launch_scan<T, 3>(a, BH, st);
+  return LINFUSION_OK;
+}
+
+template <typename T> int run_fwd(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  const int lds = lf::delta_out_lds(a.dkb);
+  if (!lfh::allow_lds(lf::delta_out<T>, lds)) return LINFUSION_ERR_HIP;
+  const int rc = run_states<T>(a, BH, st);
+  if (rc != LINFUSION_OK) return rc;
+  lf::delta_out<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+  return LINFUSION_OK;
+}
+
+template <typename T, int KB> int launch_gradients(const lf::DeltaArgs& a, int B, hipStream_t st) {
+  const int lds = lf::delta_gradients_lds(a.dkb);
+  auto kernel = lf::delta_gradients<T, KB>;
+  if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
+  kernel<<<dim3(a.nc, B * a.Hk), dim3(256), lds, st>>>(a);
+  return LINFUSION_OK;
+}
+
+template <typename T> int run_bwd(const lf::DeltaArgs& a, int B, bool states, hipStream_t st) {
+  const int BH = B * a.H, lds = lf::delta_back_outputs_lds(a.dkb, a.dvb);
+  if (!lfh::allow_lds(lf::delta_back_outputs<T>, lds)) return LINFUSION_ERR_HIP;
+  if (states) {
+    const int rc = run_states<T>(a, BH, st);
+    if (rc != LINFUSION_OK) return rc;
+  }
+  lf::delta_back_outputs<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+  if (a.dkb <= 4) launch_back_scan<T, 1>(a, BH, st);
+  else if (a.dkb <= 8) launch_back_scan<T, 2>(a, BH, st);
+  else launch_back_scan<T, 3>(a, BH, st);
+  if (a.dkb <= 4) return launch_gradients<T, 4>(a, B, st);
+  if (a.dkb <= 8) return launch_gradients<T, 8>(a, B, st);
+  return launch_gradients<T, 10>(a, B, st);
+}
+
+template <typename T, int ROWS> void launch_step(const lf::DeltaStepArgs& a, int BH, hipStream_t st) {
+  lf::delta_step<T, ROWS><<<dim3((a.dv + lf::kStepCols - 1) / lf::kStepCols, BH), dim3(256), 0, st>>>(a);
+}
+template <typename T> void run_step(const lf::DeltaStepArgs& a, int BH, hipStream_t st) {
+  if (a.dk <= 32) launch_step<T, 1>(a, BH, st);
+  else if (a.dk <= 64) launch_step<T, 2>(a, BH, st);
+  else if (a.dk <= 96) launch_step<T, 3>(a, BH, st);
+  else if (a.dk <= 128) launch_step<T, 4>(a, BH, st);
+  else launch_step<T, 5>(a, BH, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t linfusion_delta_workspace_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype) {
+  Sizes z;
+  return make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z) == LINFUSION_OK ? z.forward() : 0;
+}
+
+size_t linfusion_delta_saved_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype) {
+  Sizes z;
+  return make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z) == LINFUSION_OK ? z.saved() : 0;
+}
+
+size_t linfusion_delta_bwd_workspace_bytes(int B, int H, int H_k, long long N, int d_k, int d_v, int dtype) {
+  Sizes z;
+  return make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z) == LINFUSION_OK ? z.saved() + z.backward() : 0;
+}
+
+int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                        const float* state_in, void* out, float* state_out, const int* lengths, void* saved,
+                        size_t saved_bytes, int B, int H, int H_k, long long N, int d_k, int d_v, int dtype, float scale,
+                        unsigned flags, const long long q_strides[3], const long long k_strides[3],
+                        const long long v_strides[3], const long long out_strides[3], const long long gate_strides[3],
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !g || !beta || !out) return LINFUSION_ERR_INVALID;
+  if (flags || !std::isfinite(scale)) return LINFUSION_ERR_INVALID;
+  Sizes z;
+  int rc = make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z);
+  if (rc != LINFUSION_OK) return rc;
+  lf::DeltaArgs a{};
+  size_t nq, nk, nv, no, ng;
+  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &nq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &nk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &nv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(out, out_strides, B, H, N, d_v, z.esz, true, &a.vo, &no)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars({g, beta}, gate_strides, B, H, N, false, &a.vg, &ng)) != LINFUSION_OK) return rc;
+  if (((uintptr_t)state_in | (uintptr_t)state_out | (uintptr_t)saved) & 15) return LINFUSION_ERR_MISALIGNED;
+  if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
+  if (saved && saved_bytes < z.saved()) return LINFUSION_ERR_WORKSPACE;
+  if (!saved) {
+    if (!workspace || workspace_bytes < z.forward()) return LINFUSION_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15) return LINFUSION_ERR_MISALIGNED;
+  }
+  const size_t ns = (size_t)z.heads * d_k * d_v * 4;
+  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
+                          {beta, ng, false, nullptr}, {lengths, (size_t)B * 4, false, nullptr},
+                          {state_in, ns, false, state_out}, {state_out, ns, true, state_in}, {out, no, true, nullptr},
+                          saved ? Range{saved, z.saved(), true, nullptr} : Range{workspace, z.forward(), true, nullptr}};
+  if (clash(ranges, 10)) return LINFUSION_ERR_OVERLAP;
+  if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
+  a.state_in = state_in; a.out = out; a.state_out = state_out; a.lengths = lengths;
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.scale = scale;
+  place_saved(&a, z, saved ? saved : workspace, saved != nullptr);
+  const hipStream_t st = (hipStream_t)stream;
+  const int BH = (int)z.heads;
+  rc = dtype == LINFUSION_DTYPE_F16   ? run_fwd<lf::F16>(a, BH, st)
+       : dtype == LINFUSION_DTYPE_BF16 ? run_fwd<lf::BF16>(a, BH, st)
+                                       : run_fwd<lf::F32>(a, BH, st);
+  if (rc != LINFUSION_OK) return rc;
+  return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
+}
+
+int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                        const float* state_in, const void* dout, const float* dstate_out, const void* saved,
+                        size_t saved_bytes, void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dstate_in,
+                        const int* lengths, int B, int H, int H_k, long long N, int d_k, int d_v, int dtype, float scale,
+                        unsigned flags, const long long q_strides[3], const long long k_strides[3],
+                        const long long v_strides[3], const long long gate_strides[3], const long long dout_strides[3],
+                        const long long dq_strides[3], const long long dk_strides[3], const long long dv_strides[3],
+                        const long long dgate_strides[3], void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !g || !beta || !dout || !dq || !dk || !dv || !dg || !dbeta) return LINFUSION_ERR_INVALID;
+  if (flags || !std::isfinite(scale)) return LINFUSION_ERR_INVALID;
+  Sizes z;
+  int rc = make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z);
+  if (rc != LINFUSION_OK) return rc;
+  lf::DeltaArgs a{};
+  size_t nq, nk, nv, ng, ndo, ndq, ndk, ndv, ndg;
+  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &nq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &nk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &nv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dout, dout_strides, B, H, N, d_v, z.esz, false, &a.vdo, &ndo)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dq, dq_strides, B, H_k, N, d_k, z.esz, true, &a.vdq, &ndq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dk, dk_strides, B, H_k, N, d_k, z.esz, true, &a.vdk, &ndk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dv, dv_strides, B, H, N, d_v, z.esz, true, &a.vdv, &ndv)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars({g, beta}, gate_strides, B, H, N, false, &a.vg, &ng)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars({dg, dbeta}, dgate_strides, B, H, N, true, &a.vdg, &ndg)) != LINFUSION_OK) return rc;
+  if (((uintptr_t)state_in | (uintptr_t)dstate_out | (uintptr_t)dstate_in | (uintptr_t)saved) & 15)
+    return LINFUSION_ERR_MISALIGNED;
+  if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
+  if (saved && saved_bytes < z.saved()) return LINFUSION_ERR_WORKSPACE;
+  const size_t need = z.backward() + (saved ? 0 : z.saved());
+  if (!workspace || workspace_bytes < need) return LINFUSION_ERR_WORKSPACE;
+  if ((uintptr_t)workspace & 15) return LINFUSION_ERR_MISALIGNED;
+  const size_t ns = (size_t)z.heads * d_k * d_v * 4;
+  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
+                          {beta, ng, false, nullptr}, {lengths, (size_t)B * 4, false, nullptr}, {state_in, ns, false, nullptr},
+                          {dout, ndo, false, nullptr}, {saved, z.saved(), false, nullptr},
+                          {dstate_out, ns, false, dstate_in}, {dstate_in, ns, true, dstate_out}, {dq, ndq, true, nullptr},
+                          {dk, ndk, true, nullptr}, {dv, ndv, true, nullptr}, {dg, ndg, true, nullptr},
+                          {dbeta, ndg, true, nullptr}, {workspace, need, true, nullptr}};
+  if (clash(ranges, 17)) return LINFUSION_ERR_OVERLAP;
+  if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
+  a.state_in = state_in; a.lengths = lengths; a.dout = dout; a.dstate_out = dstate_out;
+  a.dq = dq; a.dk_out = dk; a.dv_out = dv; a.dg = dg; a.dbeta = dbeta; a.dstate_in = dstate_in;
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.scale = scale;
+  unsigned char* p = static_cast<unsigned char*>(workspace);
+  a.du = take(p, z.du);
+  a.ds = take(p, z.ds);
+  place_saved(&a, z, saved ? const_cast<void*>(saved) : p, true);
+  const hipStream_t st = (hipStream_t)stream;
+  rc = dtype == LINFUSION_DTYPE_F16   ? run_bwd<lf::F16>(a, B, !saved, st)
+       : dtype == LINFUSION_DTYPE_BF16 ? run_bwd<lf::BF16>(a, B, !saved, st)
+                                       : run_bwd<lf::F32>(a, B, !saved, st);
+  if (rc != LINFUSION_OK) return rc;
+  return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
+}
+
+int linfusion_delta_step(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                         const float* state_in, float* state_out, void* out, int B, int H, int H_k, int d_k, int d_v,
+                         int dtype, float scale, unsigned flags, const long long q_strides[2],
+                         const long long k_strides[2], const long long v_strides[2], const long long out_strides[2],
+                         const long long gate_strides[2], void* stream) {
+  if (!q || !k || !v || !g || !beta || !state_out || !out) return LINFUSION_ERR_INVALID;
+  if (flags || !std::isfinite(scale)) return LINFUSION_ERR_INVALID;
+  Sizes z;
+  int rc = make_sizes(B, H, H_k, 1, d_k, d_v, dtype, &z);
+  if (rc != LINFUSION_OK) return rc;
+  lf::DeltaView vq, vk, vv, vo, vg;
+  size_t nq, nk, nv, no, ng;
+  struct Three { long long s[3]; };
+  auto three = [](const long long* s, int heads, int d) {
+    return s ? Three{{s[0], s[1], 0}} : Three{{(long long)heads * d, d, 0}};
+  };
+  if ((rc = check_rows(q, three(q_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vq, &nq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, three(k_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vk, &nk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, three(v_strides, H, d_v).s, B, H, 1, d_v, z.esz, false, &vv, &nv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(out, three(out_strides, H, d_v).s, B, H, 1, d_v, z.esz, true, &vo, &no)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars({g, beta}, three(gate_strides, H, 1).s, B, H, 1, false, &vg, &ng)) != LINFUSION_OK) return rc;
+  if (((uintptr_t)state_in | (uintptr_t)state_out) & 15) return LINFUSION_ERR_MISALIGNED;
+  const size_t ns = (size_t)z.heads * d_k * d_v * 4;
+  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
+                          {beta, ng, false, nullptr}, {state_in, ns, false, state_out}, {state_out, ns, true, state_in},
+                          {out, no, true, nullptr}};
+  if (clash(ranges, 8)) return LINFUSION_ERR_OVERLAP;
+  if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
+  const lf::DeltaStepArgs a{q, k, v, g, beta, state_in, out, state_out, vq.b, vq.h, vk.b, vk.h, vv.b, vv.h,
+                            vg.b, vg.h, vo.b, vo.h, H, H_k, d_k, d_v, scale};
+  const hipStream_t st = (hipStream_t)stream;
+  const int BH = (int)z.heads;
+  if (dtype == LINFUSION_DTYPE_F16) run_step<lf::F16>(a, BH, st);
+  else if (dtype == LINFUSION_DTYPE_BF16) run_step<lf::BF16>(a, BH, st);
+  else run_step<lf::F32>(a, BH, st);
+  return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
+}
+
+}  // extern "C"

@@ -14,10 +14,14 @@
 // (delta_out).  gamma and its differences are fp64: behind a token that forgets nearly everything the differences of an
 // fp32 sum have lost the small decays that follow it.  Everything that reaches the state or an fp32 result is fp32 accurate.
 //
-// Layout of what passes between the kernels, fp32: blocks of 16 channels, [channels / 16][rows][16], so that every matrix
-// operand is a contiguous kilobyte.
+// Products run on the 16-bit matrix instruction with operands as sums of bf16 terms (lf_terms.hpp): three where a state or
+// an fp32 result depends on them, two where a 16-bit output does.  What passes between the kernels is stored as its reader
+// takes it, a contiguous kilobyte for each operand or accumulator of a wave:
+//     w    T (beta e^gamma K) as operand: [4 row blocks][d_k / 32][3 terms][64 lanes][8 steps]
+//     kt   K^T as operand: [d_k / 16][2][terms][64][8], once per query and key head
+//     u    U0, then U, and s the state before each chunk and behind the last, as fp32 accumulators: [d_v / 16][row blocks][64][4]
 #pragma once
-#include "lf_vec8.hpp"
+#include "lf_terms.hpp"
 
 namespace lf {
 
@@ -34,10 +38,11 @@ struct DeltaArgs {
   float* state_out;
   const int* lengths;
   DeltaView vq, vk, vv, vg, vo;
-  float *t, *w, *u, *s, *decay;   // per chunk: [64][64], [dkb][64][16], [dvb][64][16], [dvb][16 dkb][16] (one more per head), [4][64]
+  uint16_t *w, *kt, *wt, *tt;     // operands; wt = W^T, tt = (T beta)^T: for the backward pass, else null
+  float *u, *s, *decay;           // accumulators; per chunk [4][64]
   long long N;
   int H, Hk, nc;                  // chunks of N tokens
-  int dk, dv, dkb, dvb;           // channels, and blocks of 16 of them
+  int dk, dv, dkb, dvb, dks;      // channels, blocks of 16 of them, and of 32
   float scale;
   // backward
   const void* dout;
@@ -45,6 +50,7 @@ struct DeltaArgs {
   void *dq, *dk_out, *dv_out;
   float *dg, *dbeta, *dstate_in;
   DeltaView vdo, vdq, vdk, vdv, vdg;
+  uint16_t* kn;                   // K as operand
   float *du, *ds;                 // as u; as s (the gradient of a chunk's last state)
 };
 
@@ -86,33 +92,21 @@ LF_DEV f32x4 rows_near(const float* p, int ld) {
   return f32x4{r[0], r[ld], r[2 * ld], r[3 * ld]};
 }
 
-template <typename T> LF_DEV float load1(const void* p, long long i) {
+// Four neighbouring channels.
+template <typename T> LF_DEV f32x4 load4(const unsigned char* p) {
   if constexpr (Stored<T>::kBytes == 4) {
-    return static_cast<const float*>(p)[i];
+    return *reinterpret_cast<const f32x4*>(p);
   } else {
-    float x, y;
-    unpack2<T>(static_cast<const uint16_t*>(p)[i], x, y);
-    return x;
+    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+    float a, b, c, d;
+    unpack2<T>(w[0], a, b);
+    unpack2<T>(w[1], c, d);
+    return f32x4{a, b, c, d};
   }
 }
-template <typename T> LF_DEV void store1(void* p, long long i, float v) {
-  if constexpr (Stored<T>::kBytes == 4) static_cast<float*>(p)[i] = v;
-  else static_cast<uint16_t*>(p)[i] = (uint16_t)pack2<T>(v, 0.0f);
-}
-
-// A chunk's rows of one head in LDS as fp32, `ld` apart, zeros behind the last token and channel.
-template <typename T>
-LF_DEV void stage_rows(float* to, int ld, const void* x, const DeltaView& v, int b, int h, long long n0, int valid, int d,
-                       int blocks) {
-  const int vecs = blocks * 2;
-  for (int i = threadIdx.x; i < kDeltaChunk * vecs; i += blockDim.x) {
-    const int t = (unsigned)i / (unsigned)vecs, c = (i - t * vecs) * 8;
-    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (t < valid && c < d) load8<T>(at<T>(x, b * v.b + h * v.h + (n0 + t) * v.n + c), y);
-    float* p = to + t * ld + c;
-    *reinterpret_cast<f32x4*>(p) = f32x4{y[0], y[1], y[2], y[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{y[4], y[5], y[6], y[7]};
-  }
+template <typename T> LF_DEV void store4(unsigned char* p, const f32x4& v) {
+  if constexpr (Stored<T>::kBytes == 4) *reinterpret_cast<f32x4*>(p) = v;
+  else *reinterpret_cast<u32x2*>(p) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
 }
 
 // gamma of the 64 tokens, by the first wave; a decay of -infinity counts as -10^4, which is none left
@@ -131,26 +125,51 @@ LF_DEV double chunk_gamma(const DeltaArgs& a, const DeltaAt& w) {
 
 LF_DEV float decay_between(const double* gamma, int i, int j) { return expf((float)(gamma[i] - gamma[j])); }
 
-constexpr int kLdT = 68;   // leading dimension of a 64 x 64 matrix in LDS: both operand forms are free of bank conflicts
+constexpr int kLdT = 68;   // leading dimension of a 64 x 64 fp32 matrix in LDS: both operand forms are free of bank conflicts
+constexpr int kLdP = 72;   // of a plane of one
+constexpr int kLdU = 20;   // of planes of 16 value channels per token
 
-// ---- T, W, U0 of every chunk ----------------------------------------------------------------------------------------------
-inline int delta_prepare_lds(int dkb, int dvb) {
-  const int wide = dkb > dvb ? dkb : dvb;
-  return 64 * (16 * wide + 4) * 4 + 2 * 64 * kLdT * 4 + 64 * 8 + kDecayRows * 4 + 64 * 4;
+LF_DEV int plane_ld(int steps) { return 32 * steps + 8; }
+inline int plane_bytes(int rows, int steps) { return rows * (32 * steps + 8) * 2; }
+
+constexpr int kFrag = 512;   // elements of one term of an operand
+
+// An accumulator block as terms of an operand in global memory: its lane holds steps 4 g .. + 3 (g = lane / 16) of row (or
+// column) lane % 16 of the 16 steps that are the `upper` half or not of the operand's 32.
+template <int N> LF_DEV void store_operand(uint16_t* frag, bool upper, const f32x4& v) {
+  const int l = threadIdx.x & 63, g = l >> 4;
+  split4_lds<N>(frag + ((l & 15) + 16 * ((upper ? 2 : 0) + (g >> 1))) * 8 + (g & 1) * 4, kFrag, v);
+}
+template <int N> LF_DEV void store_frag(uint16_t* frag, const Terms<N>& t) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(frag + i * kFrag + (threadIdx.x & 63) * 8) = t.t[i];
+}
+template <int N> LF_DEV void load_frag(const uint16_t* frag, Terms<N>& t) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) t.t[i] = *reinterpret_cast<const u32x4*>(frag + i * kFrag + (threadIdx.x & 63) * 8);
+}
+
+// ---- the operands and U0 of every chunk -----------------------------------------------------------------------------------
+template <typename T> inline int delta_prepare_lds(int dks, int dvs) {
+  const int wide = dks > dvs ? dks : dvs;
+  return TermsOf<T>::kStored * plane_bytes(64, wide) + 64 * kLdT * 4 + 3 * 64 * kLdP * 2 + 64 * 8 + kDecayRows * 4 + 64 * 4;
 }
 
 template <typename T> __global__ __launch_bounds__(256) void delta_prepare(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NI = TermsOf<T>::kStored;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int wide = a.dkb > a.dvb ? a.dkb : a.dvb, ld = 16 * wide + 4;
-  float* x = reinterpret_cast<float*>(smem);
-  float* ma = x + 64 * ld;
-  float* mt = ma + 64 * kLdT;
-  double* gamma = reinterpret_cast<double*>(mt + 64 * kLdT);
+  const int dvs = (a.dvb + 1) / 2, ld = plane_ld(a.dks), ldv = plane_ld(dvs), plane = 64 * ld;
+  const int most = ld > ldv ? ld : ldv;
+  float* mt = reinterpret_cast<float*>(smem);
+  uint16_t* tp = reinterpret_cast<uint16_t*>(mt + 64 * kLdT);   // A, then T times a factor per column, as terms
+  float* ma = reinterpret_cast<float*>(tp);
+  uint16_t* x = tp + 3 * 64 * kLdP;                             // the keys, then the values
+  double* gamma = reinterpret_cast<double*>(x + NI * 64 * most);
   float* decay = reinterpret_cast<float*>(gamma + 64);
-  float* both = decay + kDecayRows;   // beta e^gamma
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4;
+  float* both = decay + kDecayRows;                             // beta e^gamma
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g8 = (lane >> 4) * 8, row4 = (lane >> 4) * 4;
   const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
   if (wave == 0) {
     const double y = chunk_gamma(a, w), last = __shfl(y, 63, 64);
@@ -166,15 +185,27 @@ template <typename T> __global__ __launch_bounds__(256) void delta_prepare(Delta
     decay[kDecayLeft + lane] = left;
     both[lane] = beta * since;
   }
-  stage_rows<T>(x, ld, a.k, a.vk, w.b, w.hk, w.n0, w.valid, a.dk, a.dkb);
+  stage_terms<T>(x, ld, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, a.dks);
   for (int i = tid; i < 64 * kLdT; i += 256) mt[i] = 0.0f;
   __syncthreads();
-  if (tid < kDecayRows) a.decay[c * kDecayRows + tid] = decay[tid];
+  a.decay[c * kDecayRows + tid] = decay[tid];
+  if (w.h % (a.H / a.Hk) == 0) {
+    uint16_t* kt = a.kt + ((long long)(w.b * a.Hk + w.hk) * a.nc + blockIdx.x) * a.dkb * 2 * NI * kFrag;
+    for (int i = wave; i < a.dkb * 2; i += 4) {
+      Terms<NI> f;
+      terms_across<NI>(x + 32 * (i & 1) * ld + 16 * (i >> 1), plane, ld, f);
+      store_frag<NI>(kt + i * NI * kFrag, f);
+    }
+  }
   // A, rows 16 wave .. + 15
   for (int nt = 0; nt <= wave; ++nt) {
     f32x4 acc = {0, 0, 0, 0};
-    for (int kb = 0; kb < a.dkb; ++kb)
-      acc = mfma_block(steps_near(x + 16 * wave * ld + 16 * kb, ld), steps_near(x + 16 * nt * ld + 16 * kb, ld), acc);
+    for (int ks = 0; ks < a.dks; ++ks) {
+      Terms<NI> fi, fj;
+      terms_near<NI>(x + (16 * wave + col) * ld + 32 * ks + g8, plane, fi);
+      terms_near<NI>(x + (16 * nt + col) * ld + 32 * ks + g8, plane, fj);
+      acc = mul_terms<3>(fi, fj, acc);
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * wave + row4 + r, j = 16 * nt + col;
@@ -182,7 +213,7 @@ template <typename T> __global__ __launch_bounds__(256) void delta_prepare(Delta
     }
   }
   __syncthreads();
-  // the blocks on the diagonal, a column per lane, by substitution
+  // T: the blocks on the diagonal, a column per lane, by substitution
   if (lane < 16) {
     const float* m = ma + 16 * wave * kLdT + 16 * wave;
     float t[16];
@@ -196,123 +227,182 @@ template <typename T> __global__ __launch_bounds__(256) void delta_prepare(Delta
     }
   }
   __syncthreads();
-  // the blocks below it: T_ij = -T_ii sum_l A_il T_lj, by their distance from the diagonal
+  // the blocks below it: T_ij = -T_ii sum_l A_il T_lj, by their distance from the diagonal; the inner sum waits in T_ij's place
   for (int far = 1; far < 4; ++far) {
     const int i = wave + far, j = wave;
-    float* tij = mt + 16 * i * kLdT + 16 * j;
     if (i < 4) {
+      float* tij = mt + 16 * i * kLdT + 16 * j;
       f32x4 acc = {0, 0, 0, 0};
       for (int l = j; l < i; ++l)
         acc = mfma_block(steps_near(ma + 16 * i * kLdT + 16 * l, kLdT), rows_near(mt + 16 * l * kLdT + 16 * j, kLdT), acc);
 #pragma unroll
       for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdT + col] = acc[r];
-    }
-    __syncthreads();
-    f32x4 acc = {0, 0, 0, 0};
-    if (i < 4) acc = mfma_block(steps_near(mt + 16 * i * kLdT + 16 * i, kLdT), rows_near(tij, kLdT), acc);
-    __syncthreads();
-    if (i < 4) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (only this wave uses the block until the barrier)
+      acc = mfma_block(steps_near(mt + 16 * i * kLdT + 16 * i, kLdT), rows_near(tij, kLdT), f32x4{0, 0, 0, 0});
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
       for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdT + col] = -acc[r];
     }
     __syncthreads();
   }
-  if (a.t) {
-    for (int i = tid; i < 64 * 16; i += 256) {
-      const int r = i >> 4, v = (i & 15) * 4;
-      *reinterpret_cast<f32x4*>(a.t + c * 4096 + r * 64 + v) = *reinterpret_cast<const f32x4*>(mt + r * kLdT + v);
-    }
-  }
-  // W, then U0 where the keys were
-  auto times = [&](const float* scale, float* to, int blocks) {
-    for (int nb = 0; nb < blocks; ++nb) {
-      f32x4 acc = {0, 0, 0, 0};
-      for (int kb = 0; kb <= wave; ++kb) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(scale + 16 * kb + row4);
-        acc = mfma_block(steps_near(mt + 16 * wave * kLdT + 16 * kb, kLdT) * s, rows_near(x + 16 * kb * ld + 16 * nb, ld), acc);
-      }
+  auto scaled = [&](const float* by) {   // T with a factor per column, as terms
+    for (int i = tid; i < 64 * 8; i += 256) {
+      const int r = i >> 3, v = (i & 7) * 8;
+      float y[8];
+      load8_f32(mt + r * kLdT + v, y);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[((long long)nb * 64 + 16 * wave + row4 + r) * 16 + col] = acc[r];
+      for (int e = 0; e < 8; ++e) y[e] *= by[v + e];
+      Terms<3> t;
+      split8(y, t);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(tp + p * 64 * kLdP + r * kLdP + v) = t.t[p];
     }
   };
-  times(both, a.w + c * a.dkb * 1024, a.dkb);
+  scaled(both);
   __syncthreads();
-  stage_rows<T>(x, ld, a.v, a.vv, w.b, w.h, w.n0, w.valid, a.dv, a.dvb);
+  // T's rows 16 wave .. + 15 have nothing behind column 16 wave + 15
+  const int steps = wave < 2 ? 1 : 2;
+  Terms<3> ft[2];
+  auto rows_of_t = [&]() {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      if (ks < steps) terms_near<3>(tp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, ft[ks]);
+  };
+  rows_of_t();
+  uint16_t* mw = a.w + (c * 4 + wave) * a.dks * 3 * kFrag;
+  for (int cb = 0; cb < 2 * a.dks; ++cb) {
+    f32x4 acc = {0, 0, 0, 0}, act = {0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if (ks >= steps) continue;
+      Terms<NI> key;
+      terms_across<NI>(x + 32 * ks * ld + 16 * cb, plane, ld, key);
+      acc = mul_terms<3>(key, ft[ks], acc);
+      if (a.wt) act = mul_terms<3>(ft[ks], key, act);
+    }
+    store_operand<3>(mw + (cb >> 1) * 3 * kFrag, cb & 1, acc);
+    if (a.wt && cb < a.dkb) store_operand<3>(a.wt + ((c * a.dkb + cb) * 2 + (wave >> 1)) * 3 * kFrag, wave & 1, act);
+  }
   __syncthreads();
-  times(decay + kDecayBeta, a.u + c * a.dvb * 1024, a.dvb);
+  scaled(decay + kDecayBeta);
+  stage_terms<T>(x, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);
+  __syncthreads();
+  rows_of_t();
+  for (int vb = 0; vb < a.dvb; ++vb) {
+    f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if (ks >= steps) continue;
+      Terms<NI> val;
+      terms_across<NI>(x + 32 * ks * ldv + 16 * vb, 64 * ldv, ldv, val);
+      acc = mul_terms<3>(val, ft[ks], acc);
+    }
+    *reinterpret_cast<f32x4*>(a.u + (((c * a.dvb + vb) * 4 + wave) * 64 + lane) * 4) = acc;
+  }
+  if (a.tt) {
+    for (int ks = 0; ks < 2; ++ks) {
+      Terms<3> f;
+      terms_across<3>(tp + 32 * ks * kLdP + 16 * wave, 64 * kLdP, kLdP, f);
+      store_frag<3>(a.tt + ((c * 4 + wave) * 2 + ks) * 3 * kFrag, f);
+    }
+  }
 }
 
 // ---- the scan ---------------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 value channels of one head through all chunks; its four waves hold the state's row blocks
-// wave, wave + 4, ... as accumulators.
-constexpr int kLdS = 20;
+// wave, wave + 4, ... as accumulators and compute 16 tokens of U each.  Bound: the chain from one chunk's state to the next
+// (two products, two passes through LDS); everything it reads from memory is requested a chunk ahead.
+template <int NI, int KS> struct ScanIn {
+  static constexpr int kBlocks = (2 * KS + 3) / 4;
+  Terms<3> w[KS];
+  Terms<NI> kt[kBlocks][2];
+  f32x4 u0;
+  float write, whole;
+};
 
-template <typename T, int BLOCKS> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
-  __shared__ __align__(16) float sl[16 * 4 * BLOCKS * kLdS];
-  __shared__ __align__(16) float ul[64 * kLdS];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4;
+template <int NI, int KS> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
+  constexpr int kBlocks = ScanIn<NI, KS>::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * kLd;
+  __shared__ __align__(16) uint16_t sp[3 * kPlane];
+  __shared__ __align__(16) uint16_t up[3 * 64 * kLdU];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   const int slice = blockIdx.x, bh = blockIdx.y, ch = slice * 16 + col;
   const DeltaAt first(a, bh, 0);
-  const long long tokens = tokens_of(a.lengths, first.b, a.N);
-  const int chunks = (int)((tokens + 63) / 64);
-  f32x4 s[BLOCKS];
+  const int chunks = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
+  f32x4 s[kBlocks];
 #pragma unroll
-  for (int t = 0; t < BLOCKS; ++t)
+  for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * (wave + 4 * t) + row4 + r;
       s[t][r] = a.state_in && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
     }
-  for (int i = 0;; ++i) {
-    float* keep = a.s + (((long long)bh * (a.nc + 1) + i) * a.dvb + slice) * a.dkb * 256;
+  for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
+  __syncthreads();
+  const long long c0 = (long long)bh * a.nc;
+  const long long k0 = (long long)(first.b * a.Hk + first.hk) * a.nc;
+  auto request = [&](ScanIn<NI, KS>& n, int i) {
+    const uint16_t* mw = a.w + ((c0 + i) * 4 + wave) * a.dks * 3 * kFrag;
 #pragma unroll
-    for (int t = 0; t < BLOCKS; ++t) {
+    for (int ks = 0; ks < KS; ++ks) load_frag<3>(mw + ks * 3 * kFrag, n.w[ks]);
+    const uint16_t* kt = a.kt + (k0 + i) * a.dkb * 2 * NI * kFrag;
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+        if (wave + 4 * t < a.dkb) load_frag<NI>(kt + ((wave + 4 * t) * 2 + ks) * NI * kFrag, n.kt[t][ks]);
+    n.u0 = *reinterpret_cast<const f32x4*>(a.u + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4);
+    const float* decay = a.decay + (c0 + i) * kDecayRows;
+    n.write = decay[kDecayWrite + 16 * wave + col];
+    n.whole = decay[kDecaySince + 63];
+  };
+  auto keep = [&](int i) {
+    float* to = a.s + (((long long)bh * (a.nc + 1) + i) * a.dvb + slice) * a.dkb * 256;
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t)
+      if (wave + 4 * t < a.dkb) *reinterpret_cast<f32x4*>(to + (wave + 4 * t) * 256 + lane * 4) = s[t];
+  };
+  auto chunk = [&](ScanIn<NI, KS>& in, ScanIn<NI, KS>& next, int i) {
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t)
+      if (wave + 4 * t < a.dkb) split4_lds<3>(sp + col * kLd + 16 * (wave + 4 * t) + row4, kPlane, s[t]);
+    if (i + 1 < chunks) request(next, i + 1);
+    keep(i);
+    lds_barrier();
+    f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      Terms<3> fs;
+      terms_near<3>(sp + col * kLd + 32 * ks + g8, kPlane, fs);
+      if (ks & 1) acc2 = mul_terms<3>(fs, in.w[ks], acc2);
+      else acc = mul_terms<3>(fs, in.w[ks], acc);
+    }
+    const f32x4 u = in.u0 - (acc + acc2);
+    *reinterpret_cast<f32x4*>(a.u + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4) = u;
+    split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, u * in.write);
+    lds_barrier();
+    Terms<3> fu[2];
+    terms_across<3>(up, 64 * kLdU, kLdU, fu[0]);
+    terms_across<3>(up + 32 * kLdU, 64 * kLdU, kLdU, fu[1]);
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) {
       if (wave + 4 * t >= a.dkb) continue;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave + 4 * t) + row4 + r;
-        sl[row * kLdS + col] = s[t][r];
-        keep[row * 16 + col] = s[t][r];
-      }
+      s[t] *= in.whole;
+      s[t] = mul_terms<3>(in.kt[t][0], fu[0], s[t]);
+      s[t] = mul_terms<3>(in.kt[t][1], fu[1], s[t]);
     }
-    if (i == chunks) break;
-    __syncthreads();
-    const DeltaAt w(a, bh, i);
-    const long long c = (long long)bh * a.nc + i;
-    const float* decay = a.decay + c * kDecayRows;
-    const float* mw = a.w + c * a.dkb * 1024 + 16 * wave * 16;
-    float* mu = a.u + (c * a.dvb + slice) * 1024;
-    f32x4 acc = {0, 0, 0, 0};
-    for (int kb = 0; kb < a.dkb; ++kb)
-      acc = mfma_block(steps_near(mw + kb * 1024, 16), rows_near(sl + 16 * kb * kLdS, kLdS), acc);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = 16 * wave + row4 + r;
-      const float u = mu[row * 16 + col] - acc[r];
-      mu[row * 16 + col] = u;
-      ul[row * kLdS + col] = u * decay[kDecayWrite + row];
-    }
-    __syncthreads();
-    const float whole = decay[kDecaySince + 63];
-#pragma unroll
-    for (int t = 0; t < BLOCKS; ++t) {
-      if (wave + 4 * t >= a.dkb) continue;
-      s[t] *= whole;
-      const int kc = 16 * (wave + 4 * t) + col;
-      for (int kb = 0; kb < 4; ++kb) {
-        f32x4 key = {0, 0, 0, 0};
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int n = 16 * kb + row4 + r;
-          if (n < w.valid && kc < a.dk) key[r] = load1<T>(a.k, w.b * a.vk.b + w.hk * a.vk.h + (w.n0 + n) * a.vk.n + kc);
-        }
-        s[t] = mfma_block(key, rows_near(ul + 16 * kb * kLdS, kLdS), s[t]);
-      }
-    }
+  };
+  ScanIn<NI, KS> x, y;
+  if (chunks > 0) request(x, 0);
+  int i = 0;
+  for (; i + 1 < chunks; i += 2) {
+    chunk(x, y, i);
+    chunk(y, x, i + 1);
   }
+  if (i < chunks) chunk(x, y, i);
+  keep(chunks);
   if (a.state_out) {
 #pragma unroll
-    for (int t = 0; t < BLOCKS; ++t)
+    for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * (wave + 4 * t) + row4 + r;
@@ -321,62 +411,100 @@ template <typename T, int BLOCKS> __global__ __launch_bounds__(256) void delta_s
   }
 }
 
-// P_ij = q_i.k_j D_ij for j <= i, into `mp`; FORWARD: 0 where beta_j is 0 (the u_j that is kept is not)
-template <bool FORWARD>
-LF_DEV void chunk_scores(const DeltaArgs& a, const float* q, const float* k, int ld, const double* gamma,
-                         const float* beta, float* mp) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, row4 = (lane >> 4) * 4;
-  for (int nt = 0; nt < 4; ++nt) {
-    f32x4 acc = {0, 0, 0, 0};
-    if (nt <= wave)
-      for (int kb = 0; kb < a.dkb; ++kb)
-        acc = mfma_block(steps_near(q + 16 * wave * ld + 16 * kb, ld), steps_near(k + 16 * nt * ld + 16 * kb, ld), acc);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = 16 * wave + row4 + r, j = 16 * nt + col;
-      const bool on = j <= i && !(FORWARD && beta[j] == kDeltaTinyBeta);
-      mp[i * kLdT + j] = on ? acc[r] * decay_between(gamma, i, j) : 0.0f;
-    }
-  }
+// ---- the outputs --------------------------------------------------------------------------------------------------------------
+// Formed transposed, so that a lane has four neighbouring channels of a token: O^T = e^gamma S0^T Q^T + U^T P^T.
+constexpr int kOutBlocks = 4;   // of 16 value channels at a time
+
+template <typename T> inline int delta_out_lds(int dks) {
+  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut;
+  const int rows = 2 * NI * plane_bytes(64, dks);
+  const int later = kOutBlocks * NO * (plane_bytes(16, dks) + 64 * kLdU * 2);
+  return NO * 64 * kLdP * 2 + (rows > later ? rows : later) + 64 * 8 + kDecayRows * 4;
 }
 
-// ---- the outputs --------------------------------------------------------------------------------------------------------------
-inline int delta_out_lds(int dkb) { return 2 * 64 * (16 * dkb + 4) * 4 + 64 * kLdT * 4 + 64 * 8 + kDecayRows * 4; }
-
-template <typename T> __global__ __launch_bounds__(256) void delta_out(DeltaArgs a) {
+template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut, kLd = 32 * KS + 8, kSPlane = 16 * kLd, kUPlane = 64 * kLdU;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int ld = 16 * a.dkb + 4;
-  float* q = reinterpret_cast<float*>(smem);
-  float* k = q + 64 * ld;
-  float* mp = k + 64 * ld;
-  double* gamma = reinterpret_cast<double*>(mp + 64 * kLdT);
+  double* gamma = reinterpret_cast<double*>(smem);
   float* decay = reinterpret_cast<float*>(gamma + 64);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4;
+  uint16_t* pp = reinterpret_cast<uint16_t*>(decay + kDecayRows);
+  uint16_t* q = pp + NO * 64 * kLdP;
+  uint16_t* k = q + NI * 64 * kLd;
+  uint16_t* sp = q;                                     // where q and k were
+  uint16_t* up = sp + kOutBlocks * NO * kSPlane;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
   if (wave == 0) gamma[lane] = chunk_gamma(a, w);
   decay[tid] = a.decay[c * kDecayRows + tid];
-  stage_rows<T>(q, ld, a.q, a.vq, w.b, w.hk, w.n0, w.valid, a.dk, a.dkb);
-  stage_rows<T>(k, ld, a.k, a.vk, w.b, w.hk, w.n0, w.valid, a.dk, a.dkb);
+  stage_terms<T>(q, kLd, a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk, KS);
+  stage_terms<T>(k, kLd, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, KS);
   __syncthreads();
-  chunk_scores<true>(a, q, k, ld, gamma, decay + kDecayBeta, mp);
-  __syncthreads();
-  for (int sl = 0; sl < a.dvb; ++sl) {
-    const float* s0 = a.s + (((long long)blockIdx.y * (a.nc + 1) + blockIdx.x) * a.dvb + sl) * a.dkb * 256;
-    const float* u = a.u + (c * a.dvb + sl) * 1024;
+  Terms<NI> fq[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) terms_near<NI>(q + (16 * wave + col) * kLd + 32 * ks + g8, 64 * kLd, fq[ks]);
+  // P, four neighbouring columns j of row i at a time; 0 where beta_j is 0 (the u_j that is kept is not)
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt) {
     f32x4 acc = {0, 0, 0, 0};
-    for (int kb = 0; kb < a.dkb; ++kb)
-      acc = mfma_block(steps_near(q + 16 * wave * ld + 16 * kb, ld), rows_near(s0 + 256 * kb, 16), acc);
+    if (jt <= wave) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] *= decay[kDecaySince + 16 * wave + row4 + r];
-    for (int kb = 0; kb <= wave; ++kb)
-      acc = mfma_block(steps_near(mp + 16 * wave * kLdT + 16 * kb, kLdT), rows_near(u + 256 * kb, 16), acc);
-    const int ch = 16 * sl + col;
+      for (int ks = 0; ks < KS; ++ks) {
+        Terms<NI> fk;
+        terms_near<NI>(k + (16 * jt + col) * kLd + 32 * ks + g8, 64 * kLd, fk);
+        acc = mul_terms<NO>(fk, fq[ks], acc);
+      }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = 16 * wave + row4 + r;
-      if (n < w.valid && ch < a.dv) store1<T>(a.out, w.b * a.vo.b + w.h * a.vo.h + (w.n0 + n) * a.vo.n + ch, acc[r] * a.scale);
+      for (int r = 0; r < 4; ++r) {
+        const int i = 16 * wave + col, j = 16 * jt + row4 + r;
+        const bool on = j <= i && decay[kDecayBeta + j] != kDeltaTinyBeta;
+        acc[r] = on ? acc[r] * decay_between(gamma, i, j) : 0.0f;
+      }
+    }
+    split4_lds<NO>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, acc);
+  }
+  __syncthreads();
+  Terms<NO> fp[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) terms_near<NO>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
+  const float since = decay[kDecaySince + 16 * wave + col];
+  const int n = 16 * wave + col;
+  // (the half block behind dkb of the last 32 channels: the queries there are 0, the state's planes are too)
+  for (int i = tid; i < kOutBlocks * NO * kSPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
+  for (int vb0 = 0; vb0 < a.dvb; vb0 += kOutBlocks) {
+    const int blocks = a.dvb - vb0 < kOutBlocks ? a.dvb - vb0 : kOutBlocks;
+    __syncthreads();
+    const float* s0 = a.s + (((long long)blockIdx.y * (a.nc + 1) + blockIdx.x) * a.dvb + vb0) * a.dkb * 256;
+    for (int i = wave; i < blocks * a.dkb; i += 4) {
+      const int vb = (unsigned)i / (unsigned)a.dkb, kb = i - vb * a.dkb;
+      split4_lds<NO>(sp + vb * NO * kSPlane + col * kLd + 16 * kb + row4, kSPlane,
+                     *reinterpret_cast<const f32x4*>(s0 + (long long)i * 256 + lane * 4));
+    }
+    const float* mu = a.u + (c * a.dvb + vb0) * 1024;
+    for (int i = wave; i < blocks * 4; i += 4)
+      split4_lds<NO>(up + (i >> 2) * NO * kUPlane + (16 * (i & 3) + col) * kLdU + row4, kUPlane,
+                     *reinterpret_cast<const f32x4*>(mu + i * 256 + lane * 4));
+    __syncthreads();
+    for (int vb = 0; vb < blocks; ++vb) {
+      f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Terms<NO> fs;
+        terms_near<NO>(sp + vb * NO * kSPlane + col * kLd + 32 * ks + g8, kSPlane, fs);
+        acc = mul_terms<NO>(fs, fq[ks], acc);
+      }
+      acc *= since;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        if (2 * ks > wave) continue;
+        Terms<NO> fu;
+        terms_across<NO>(up + vb * NO * kUPlane + 32 * ks * kLdU, kUPlane, kLdU, fu);
+        acc = mul_terms<NO>(fu, fp[ks], acc);
+      }
+      const int ch = 16 * (vb0 + vb) + row4;
+      if (n < w.valid && ch < a.dv)
+        store4<T>(at<T>(a.out, w.b * a.vo.b + w.h * a.vo.h + (w.n0 + n) * a.vo.n + ch), acc * a.scale);
     }
   }
 }

@@ -21,12 +21,12 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct Sizes {
   long long nc, heads;   // chunks of N tokens; B * H
-  int dkb, dvb;
+  int dkb, dvb, dks;
   size_t esz;
-  size_t t, w, u, s, decay, du, ds;   // bytes
-  size_t saved() const { return t + w + u + s + decay; }
-  size_t forward() const { return w + u + s + decay; }
-  size_t backward() const { return du + ds; }
+  size_t w, kt, u, s, decay, wt, tt, kn, du, ds;   // bytes
+  size_t forward() const { return w + kt + u + s + decay; }
+  size_t saved() const { return forward() + wt + tt; }
+  size_t backward() const { return kn + du + ds; }
 };
 
 int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Sizes* z) {
@@ -40,9 +40,14 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->dkb = (dk + 15) / 16;
   z->dvb = (dv + 15) / 16;
   z->esz = dtype == LINFUSION_DTYPE_F32 ? 4 : 2;
-  const size_t chunks = (size_t)z->heads * (size_t)z->nc;
-  z->t = up(chunks * 4096 * 4);
-  z->w = up(chunks * z->dkb * 1024 * 4);
+  z->dks = (dk + 31) / 32;
+  const size_t chunks = (size_t)z->heads * (size_t)z->nc, key_chunks = (size_t)B * H_k * (size_t)z->nc;
+  const size_t terms = dtype == LINFUSION_DTYPE_F32 ? 3 : (dtype == LINFUSION_DTYPE_F16 ? 2 : 1), frag = lf::kFrag * 2;
+  z->w = up(chunks * 4 * z->dks * 3 * frag);
+  z->wt = up(chunks * z->dkb * 2 * 3 * frag);
+  z->tt = up(chunks * 4 * 2 * 3 * frag);
+  z->kt = up(key_chunks * z->dkb * 2 * terms * frag);
+  z->kn = up(key_chunks * 4 * z->dks * terms * frag);
   z->u = up(chunks * z->dvb * 1024 * 4);
   z->s = up((chunks + (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
   z->decay = up(chunks * lf::kDecayRows * 4);
@@ -100,70 +105,84 @@ int check_scalars(std::initializer_list<const void*> ps, const long long* given,
   return LINFUSION_OK;
 }
 
-float* take(unsigned char*& p, size_t n) {
-  float* r = reinterpret_cast<float*>(p);
+template <typename P> void take(P*& to, unsigned char*& p, size_t n) {
+  to = reinterpret_cast<P*>(p);
   p += n;
-  return r;
 }
 
-void place_saved(lf::DeltaArgs* a, const Sizes& z, void* at, bool with_t) {
+void place_forward(lf::DeltaArgs* a, const Sizes& z, void* at, bool for_backward) {
   unsigned char* p = static_cast<unsigned char*>(at);
-  a->t = with_t ? take(p, z.t) : nullptr;
-  a->w = take(p, z.w);
-  a->u = take(p, z.u);
-  a->s = take(p, z.s);
-  a->decay = take(p, z.decay);
+  take(a->w, p, z.w);
+  take(a->kt, p, z.kt);
+  take(a->u, p, z.u);
+  take(a->s, p, z.s);
+  take(a->decay, p, z.decay);
+  a->wt = a->tt = nullptr;
+  if (!for_backward) return;
+  take(a->wt, p, z.wt);
+  take(a->tt, p, z.tt);
 }
 
-template <typename T, int BLOCKS> void launch_scan(const lf::DeltaArgs& a, int BH, hipStream_t st) {
-  lf::delta_scan<T, BLOCKS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
-}
-template <typename T, int BLOCKS> void launch_back_scan(const lf::DeltaArgs& a, int BH, hipStream_t st) {
-  lf::delta_back_scan<T, BLOCKS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
-}
+#define LF_FOR_STEPS(X)                                                                           \
+  switch (a.dks) {                                                                                \
+    case 1: X(1) break;                                                                           \
+    case 2: X(2) break;                                                                           \
+    case 3: X(3) break;                                                                           \
+    case 4: X(4) break;                                                                           \
+    default: X(5) break;                                                                          \
+  }
 
-// T, W, U, the states and the decays of all chunks
+// operands, U, the states and the decays of all chunks
 template <typename T> int run_states(const lf::DeltaArgs& a, int BH, hipStream_t st) {
-  const int lds = lf::delta_prepare_lds(a.dkb, a.dvb);
+  constexpr int NI = lf::TermsOf<T>::kStored;
+  const int lds = lf::delta_prepare_lds<T>(a.dks, (a.dvb + 1) / 2);
   if (!lfh::allow_lds(lf::delta_prepare<T>, lds)) return LINFUSION_ERR_HIP;
   lf::delta_prepare<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
-  if (a.dkb <= 4) launch_scan<T, 1>(a, BH, st);
-  else if (a.dkb <= 8) launch_scan<T, 2>(a, BH, st);
-  else launch_scan<T, 3>(a, BH, st);
+#define X(KS) lf::delta_scan<NI, KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+  LF_FOR_STEPS(X)
+#undef X
+  return LINFUSION_OK;
+}
+
+template <typename T, int KS> int launch_out(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  const int lds = lf::delta_out_lds<T>(KS);
+  auto kernel = lf::delta_out<T, KS>;
+  if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
+  kernel<<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
   return LINFUSION_OK;
 }
 
 template <typename T> int run_fwd(const lf::DeltaArgs& a, int BH, hipStream_t st) {
-  const int lds = lf::delta_out_lds(a.dkb);
-  if (!lfh::allow_lds(lf::delta_out<T>, lds)) return LINFUSION_ERR_HIP;
-  const int rc = run_states<T>(a, BH, st);
+  int rc = run_states<T>(a, BH, st);
   if (rc != LINFUSION_OK) return rc;
-  lf::delta_out<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
-  return LINFUSION_OK;
+#define X(KS) rc = launch_out<T, KS>(a, BH, st);
+  LF_FOR_STEPS(X)
+#undef X
+  return rc;
 }
 
-template <typename T, int KB> int launch_gradients(const lf::DeltaArgs& a, int B, hipStream_t st) {
-  const int lds = lf::delta_gradients_lds(a.dkb);
-  auto kernel = lf::delta_gradients<T, KB>;
+template <typename T, int KS, bool SHARED> int launch_gradients(const lf::DeltaArgs& a, int B, hipStream_t st) {
+  const int lds = lf::delta_gradients_lds<T>(KS);
+  auto kernel = lf::delta_gradients<T, KS, SHARED>;
   if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
   kernel<<<dim3(a.nc, B * a.Hk), dim3(256), lds, st>>>(a);
   return LINFUSION_OK;
 }
 
 template <typename T> int run_bwd(const lf::DeltaArgs& a, int B, bool states, hipStream_t st) {
-  const int BH = B * a.H, lds = lf::delta_back_outputs_lds(a.dkb, a.dvb);
-  if (!lfh::allow_lds(lf::delta_back_outputs<T>, lds)) return LINFUSION_ERR_HIP;
-  if (states) {
-    const int rc = run_states<T>(a, BH, st);
-    if (rc != LINFUSION_OK) return rc;
-  }
-  lf::delta_back_outputs<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
-  if (a.dkb <= 4) launch_back_scan<T, 1>(a, BH, st);
-  else if (a.dkb <= 8) launch_back_scan<T, 2>(a, BH, st);
-  else launch_back_scan<T, 3>(a, BH, st);
-  if (a.dkb <= 4) return launch_gradients<T, 4>(a, B, st);
-  if (a.dkb <= 8) return launch_gradients<T, 8>(a, B, st);
-  return launch_gradients<T, 10>(a, B, st);
+  constexpr int NI = lf::TermsOf<T>::kStored;
+  const int BH = B * a.H, lds = lf::delta_back_prepare_lds<T>(a.dks, (a.dvb + 1) / 2);
+  if (!lfh::allow_lds(lf::delta_back_prepare<T>, lds)) return LINFUSION_ERR_HIP;
+  int rc = LINFUSION_OK;
+  if (states && (rc = run_states<T>(a, BH, st)) != LINFUSION_OK) return rc;
+  lf::delta_back_prepare<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+#define X(KS) lf::delta_back_scan<NI, KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+  LF_FOR_STEPS(X)
+#undef X
+#define X(KS) rc = a.H == a.Hk ? launch_gradients<T, KS, false>(a, B, st) : launch_gradients<T, KS, true>(a, B, st);
+  LF_FOR_STEPS(X)
+#undef X
+  return rc;
 }
 
 template <typename T, int ROWS> void launch_step(const lf::DeltaStepArgs& a, int BH, hipStream_t st) {
@@ -230,8 +249,8 @@ int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.out = out; a.state_out = state_out; a.lengths = lengths;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.scale = scale;
-  place_saved(&a, z, saved ? saved : workspace, saved != nullptr);
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
+  place_forward(&a, z, saved ? saved : workspace, saved != nullptr);
   const hipStream_t st = (hipStream_t)stream;
   const int BH = (int)z.heads;
   rc = dtype == LINFUSION_DTYPE_F16   ? run_fwd<lf::F16>(a, BH, st)
@@ -284,11 +303,12 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.lengths = lengths; a.dout = dout; a.dstate_out = dstate_out;
   a.dq = dq; a.dk_out = dk; a.dv_out = dv; a.dg = dg; a.dbeta = dbeta; a.dstate_in = dstate_in;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.scale = scale;
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
   unsigned char* p = static_cast<unsigned char*>(workspace);
-  a.du = take(p, z.du);
-  a.ds = take(p, z.ds);
-  place_saved(&a, z, saved ? const_cast<void*>(saved) : p, true);
+  take(a.kn, p, z.kn);
+  take(a.du, p, z.du);
+  take(a.ds, p, z.ds);
+  place_forward(&a, z, saved ? const_cast<void*>(saved) : p, true);
   const hipStream_t st = (hipStream_t)stream;
   rc = dtype == LINFUSION_DTYPE_F16   ? run_bwd<lf::F16>(a, B, !saved, st)
        : dtype == LINFUSION_DTYPE_BF16 ? run_bwd<lf::BF16>(a, B, !saved, st)

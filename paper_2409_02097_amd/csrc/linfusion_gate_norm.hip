@@ -146,7 +146,6 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
   const bool rms = (flags & LINFUSION_FLAG_NORM_RMS) != 0, post = (flags & LINFUSION_FLAG_NORM_POST) != 0;
   if ((post || gate) && !f) return LINFUSION_ERR_INVALID;
   if (w_post && !post) return LINFUSION_ERR_INVALID;
-  if (!h && (scale || shift || w_pre)) return LINFUSION_ERR_INVALID;
   if (!(norm_eps > 0.0f) || std::isinf(norm_eps) || !std::isfinite(residual_scale)) return LINFUSION_ERR_INVALID;
   const size_t esz = dtype == LINFUSION_DTYPE_F32 ? 4 : 2;
   View vx, vf, vy, vh;

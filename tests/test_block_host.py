@@ -1,0 +1,177 @@
+"""Refusals of the operators around the mixer, which need no GPU: every bad argument is an error code before anything is
+enqueued, and a good call ends at the missing device (-6)."""
+import ctypes
+
+import pytest
+
+import paper_2409_02097_amd as lf
+
+
+def _device_present():
+    import torch
+    return torch.cuda.is_available()
+
+
+# made-up device addresses: only where no kernel could be launched on them
+pytestmark = pytest.mark.skipif(_device_present(), reason="passes made-up device addresses")
+
+M = 1 << 24
+OK = -6   # all checks passed, no device
+i64x3 = lambda *v: (ctypes.c_longlong * 3)(*v)
+
+
+def rope(**kw):
+    a = dict(q=M, k=2 * M, qo=3 * M, ko=4 * M, pos=5 * M, axes=2, channels=(16, 16), bases=(1e4, 1e4), scales=None, B=2, H=4, Hk=2,
+             N=100, d=40, dtype=2, flags=0, lengths=None, sq=None, sk=None, sqo=None, sko=None, sp=None) | kw
+    arr = lambda t, v: None if v is None else (t * len(v))(*v)
+    s3 = lambda v: None if v is None else i64x3(*v)
+    return lf.library().linfusion_rope(a["q"], a["k"], a["qo"], a["ko"], a["pos"], a["axes"], arr(ctypes.c_int, a["channels"]),
+                                       arr(ctypes.c_double, a["bases"]), arr(ctypes.c_double, a["scales"]), a["B"], a["H"], a["Hk"],
+                                       a["N"], a["d"], a["dtype"], a["flags"], a["lengths"], s3(a["sq"]), s3(a["sk"]), s3(a["sqo"]),
+                                       s3(a["sko"]), None if a["sp"] is None else (ctypes.c_longlong * 2)(*a["sp"]), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(k=None, ko=None, Hk=0), OK), (dict(qo=M, ko=2 * M), OK), (dict(flags=3), OK), (dict(lengths=6 * M), OK),
+    (dict(q=None), -1), (dict(ko=None), -1), (dict(pos=None), -1), (dict(channels=None), -1), (dict(bases=None), -1),
+    (dict(B=0), -1), (dict(N=0), -1), (dict(H=-1), -1), (dict(Hk=0), -1), (dict(B=70000), -1), (dict(N=1 << 50), -1), (dict(flags=4), -1),
+    (dict(channels=(16, 15)), -1), (dict(channels=(32, 16)), -1), (dict(channels=(0, 16)), -1), (dict(bases=(1e4, 0.0)), -1),
+    (dict(bases=(float("nan"), 1.0)), -1), (dict(scales=(1.0, float("inf"))), -1),
+    (dict(dtype=3), -2), (dict(d=44), -2), (dict(d=264), -2), (dict(axes=0), -2), (dict(axes=5, channels=(8,) * 5, bases=(1.0,) * 5), -2),
+    (dict(q=M + 8), -3), (dict(qo=3 * M + 2), -3), (dict(pos=5 * M + 2), -3), (dict(sq=(16000, 4001, 40)), -3), (dict(sq=(-16000, 4000, 40)), -1),
+    (dict(qo=M + 16), -7), (dict(qo=2 * M), -7), (dict(ko=3 * M), -7), (dict(qo=5 * M - 1024), -7), (dict(lengths=3 * M), -7),
+    (dict(sqo=(16000, 0, 160)), -7), (dict(qo=M, sqo=(16000, 40, 160)), -7),
+    # queries and keys as columns of one [B, N, 6 heads, 40] buffer, each in place; then keys that begin inside the queries
+    (dict(k=M + 320, qo=M, ko=M + 320, sq=(24000, 40, 240), sqo=(24000, 40, 240), sk=(24000, 40, 240), sko=(24000, 40, 240)), OK),
+    (dict(k=M + 240, qo=M, ko=M + 240, sq=(24000, 40, 240), sqo=(24000, 40, 240), sk=(24000, 40, 240), sko=(24000, 40, 240)), -7),
+    (dict(sp=(-1, 100)), -1),
+], ids=str)
+def test_rope(kw, status):
+    assert rope(**kw) == status
+
+
+def norm_fwd(**kw):
+    a = dict(x=M, f=2 * M, gate=3 * M, scale=4 * M, shift=5 * M, wpre=None, wpost=None, y=8 * M, h=9 * M, B=2, N=50, C=320, dtype=2, rs=1.0,
+             eps=1e-6, flags=0, lengths=None, strides=None, mod=320) | kw
+    st = None if a["strides"] is None else (ctypes.c_longlong * 8)(*a["strides"])
+    return lf.library().linfusion_gate_norm_fwd(a["x"], a["f"], a["gate"], a["scale"], a["shift"], a["wpre"], a["wpost"], a["y"], a["h"], a["B"],
+                                                a["N"], a["C"], a["dtype"], a["rs"], a["eps"], a["flags"], a["lengths"], st, a["mod"], None)
+
+
+D = (16000, 320)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(y=None), OK), (dict(h=None), OK), (dict(y=M), OK), (dict(f=None, gate=None), OK), (dict(mod=0), OK), (dict(flags=3, wpost=6 * M), OK),
+    (dict(strides=D * 4), OK), (dict(strides=(64000, 1280) + D * 3), OK),
+    (dict(x=None), -1), (dict(y=None, h=None), -1), (dict(f=None), -1), (dict(f=None, gate=None, flags=2), -1), (dict(wpost=6 * M), -1),
+    (dict(B=0), -1), (dict(N=-1), -1), (dict(eps=0.0), -1), (dict(eps=float("inf")), -1), (dict(rs=float("nan")), -1), (dict(flags=8), -1),
+    (dict(mod=-4), -1), (dict(mod=160), -1), (dict(N=1 << 45), -1),
+    (dict(C=324), -2), (dict(C=8200), -2), (dict(dtype=7), -2),
+    (dict(x=M + 8), -3), (dict(gate=3 * M + 4), -3), (dict(mod=322), -3), (dict(strides=(16000, 321) + D * 3), -3), (dict(lengths=6 * M + 2), -3),
+    (dict(h=8 * M), -7), (dict(h=M), -7), (dict(y=2 * M), -7), (dict(y=M + 640), -7), (dict(h=3 * M), -7), (dict(strides=D * 3 + (16000, 160)), -7),
+    (dict(y=M, strides=(64000, 1280) + D * 3), -7), (dict(lengths=8 * M), -7),
+], ids=str)
+def test_gate_norm_forward(kw, status):
+    assert norm_fwd(**kw) == status
+
+
+WS = lf.linfusion_gate_norm_bwd_workspace_bytes(2, 50, 320)
+
+
+def norm_bwd(**kw):
+    a = dict(x=M, f=2 * M, gate=3 * M, scale=4 * M, wpre=None, wpost=None, dy=5 * M, dh=6 * M, dx=7 * M, df=8 * M, dgate=9 * M, dscale=10 * M,
+             dshift=11 * M, dwpre=None, dwpost=None, B=2, N=50, C=320, dtype=2, rs=1.0, eps=1e-6, flags=0, lengths=None, mod=320, dmod=320,
+             ws=20 * M, n=WS) | kw
+    return lf.library().linfusion_gate_norm_bwd(*(a[n] for n in ("x", "f", "gate", "scale", "wpre", "wpost", "dy", "dh", "dx", "df", "dgate", "dscale",
+                                                                 "dshift", "dwpre", "dwpost", "B", "N", "C", "dtype", "rs", "eps", "flags", "lengths")),
+                                                None, a["mod"], a["dmod"], a["ws"], a["n"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(dy=None), OK), (dict(dh=None), OK), (dict(dx=5 * M), OK), (dict(dgate=None, dscale=None, dshift=None, ws=None, n=0), OK),
+    (dict(mod=0, dmod=0), OK), (dict(dscale=9 * M + 1280, dshift=9 * M + 2560, dmod=1920), OK), (dict(flags=2, dwpost=12 * M, dwpre=13 * M), OK),
+    (dict(f=None, gate=None, df=None, dgate=None), OK),
+    (dict(x=None), -1), (dict(dy=None, dh=None), -1), (dict(dx=None, df=None, dgate=None, dscale=None, dshift=None), -1), (dict(f=None), -1),
+    (dict(dwpost=12 * M), -1), (dict(dmod=160), -1), (dict(ws=None), -4), (dict(n=WS - 1), -4), (dict(ws=20 * M + 4), -3), (dict(C=12), -2),
+    (dict(dx=M), -7), (dict(df=5 * M), -7), (dict(dx=8 * M), -7), (dict(dgate=3 * M), -7), (dict(dscale=9 * M), -7),
+    (dict(dscale=9 * M + 640, dmod=1920), -7), (dict(dmod=0), -7), (dict(ws=7 * M), -7), (dict(dshift=20 * M), -7),
+], ids=str)
+def test_gate_norm_backward(kw, status):
+    assert norm_bwd(**kw) == status
+
+
+SIZES = dict(B=2, H=4, Hk=2, N=100, dk=40, dv=64, dtype=2)
+
+
+def sizes(**kw):
+    return [(SIZES | kw)[n] for n in ("B", "H", "Hk", "N", "dk", "dv", "dtype")]
+
+
+def delta_fwd(**kw):
+    a = dict(q=M, k=2 * M, v=3 * M, g=4 * M, beta=5 * M, s0=6 * M, out=7 * M, s1=8 * M, lengths=None, saved=None, nsaved=0, scale=1.0, flags=0,
+             sq=None, sk=None, sv=None, so=None, sg=None, ws=20 * M, n=lf.linfusion_delta_workspace_bytes(*sizes())) | SIZES | kw
+    s3 = lambda v: None if v is None else i64x3(*v)
+    return lf.library().linfusion_delta_fwd(*(a[n] for n in ("q", "k", "v", "g", "beta", "s0", "out", "s1", "lengths", "saved", "nsaved", "B", "H", "Hk",
+                                                             "N", "dk", "dv", "dtype", "scale", "flags")),
+                                            *(s3(a[n]) for n in ("sq", "sk", "sv", "so", "sg")), a["ws"], a["n"], None)
+
+
+SAVED = lf.linfusion_delta_saved_bytes(*sizes())
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(s0=None), OK), (dict(s1=None), OK), (dict(s1=6 * M), OK), (dict(saved=30 * M, nsaved=SAVED, ws=None, n=0), OK),
+    (dict(sg=(400, 1, 4)), OK), (dict(sq=(0, 0, 40)), OK), (dict(g=4 * M + 4), OK), (dict(beta=4 * M + 4, sg=(800, 2, 8)), OK),
+    (dict(q=None), -1), (dict(beta=None), -1), (dict(out=None), -1), (dict(flags=1), -1), (dict(scale=float("nan")), -1), (dict(Hk=3), -1),
+    (dict(N=0), -1), (dict(N=1 << 30), -1), (dict(B=40000), -1), (dict(Hk=0), -1), (dict(sg=(400, -1, 4)), -1),
+    (dict(dk=20), -2), (dict(dk=168), -2), (dict(dv=264), -2), (dict(dtype=5), -2),
+    (dict(q=M + 8), -3), (dict(s0=6 * M + 4), -3), (dict(g=4 * M + 2), -3), (dict(ws=20 * M + 8), -3), (dict(sq=(8004, 4000, 40)), -3),
+    (dict(n=lf.linfusion_delta_workspace_bytes(*sizes()) - 1), -4), (dict(ws=None), -4), (dict(saved=30 * M, nsaved=SAVED - 1), -4),
+    (dict(out=3 * M), -7), (dict(s1=6 * M + 64), -7), (dict(s1=M), -7), (dict(out=20 * M), -7), (dict(so=(25600, 0, 64)), -7), (dict(s1=7 * M), -7),
+    (dict(lengths=7 * M), -7),
+], ids=str)
+def test_delta_forward(kw, status):
+    assert delta_fwd(**kw) == status
+
+
+def delta_bwd(**kw):
+    a = dict(q=M, k=2 * M, v=3 * M, g=4 * M, beta=5 * M, s0=6 * M, dout=7 * M, ds1=8 * M, saved=None, nsaved=0, dq=9 * M, dk_=10 * M, dv_=11 * M, dg=12 * M,
+             dbeta=13 * M, ds0=14 * M, lengths=None, scale=1.0, flags=0, sdg=None, ws=20 * M, n=lf.linfusion_delta_bwd_workspace_bytes(*sizes())) | SIZES | kw
+    return lf.library().linfusion_delta_bwd(*(a[n] for n in ("q", "k", "v", "g", "beta", "s0", "dout", "ds1", "saved", "nsaved", "dq", "dk_", "dv_", "dg",
+                                                             "dbeta", "ds0", "lengths", "B", "H", "Hk", "N", "dk", "dv", "dtype", "scale", "flags")),
+                                            *[None] * 8, None if a["sdg"] is None else i64x3(*a["sdg"]), a["ws"], a["n"], None)
+
+
+LESS = lf.linfusion_delta_bwd_workspace_bytes(*sizes()) - SAVED
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(s0=None, ds1=None, ds0=None), OK), (dict(ds0=8 * M), OK), (dict(saved=30 * M, nsaved=SAVED, n=LESS), OK), (dict(sdg=(400, 1, 4)), OK),
+    (dict(dout=None), -1), (dict(dg=None), -1), (dict(flags=2), -1), (dict(dk=12), -2), (dict(dq=9 * M + 2), -3), (dict(ds1=8 * M + 4), -3),
+    (dict(n=LESS), -4), (dict(saved=30 * M, nsaved=SAVED, n=LESS - 1), -4), (dict(saved=30 * M, nsaved=0), -4), (dict(ws=None), -4),
+    (dict(dq=10 * M), -7), (dict(dv_=3 * M), -7), (dict(dbeta=12 * M), -7), (dict(ds0=6 * M), -7), (dict(sdg=(400, 0, 4)), -7), (dict(saved=20 * M, nsaved=SAVED), -7),
+], ids=str)
+def test_delta_backward(kw, status):
+    assert delta_bwd(**kw) == status
+
+
+def delta_step(**kw):
+    a = dict(q=M, k=2 * M, v=3 * M, g=4 * M, beta=5 * M, s0=6 * M, s1=7 * M, out=8 * M, scale=1.0, flags=0, sq=None) | SIZES | kw
+    return lf.library().linfusion_delta_step(*(a[n] for n in ("q", "k", "v", "g", "beta", "s0", "s1", "out", "B", "H", "Hk", "dk", "dv", "dtype", "scale",
+                                                              "flags")), None if a["sq"] is None else (ctypes.c_longlong * 2)(*a["sq"]), *[None] * 5)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({}, OK), (dict(s0=None), OK), (dict(s1=6 * M), OK), (dict(s1=None), -1), (dict(v=None), -1), (dict(flags=1), -1), (dict(Hk=3), -1), (dict(B=0), -1),
+    (dict(dk=164), -2), (dict(v=3 * M + 8), -3), (dict(sq=(81, 40)), -3), (dict(out=6 * M), -7), (dict(s1=6 * M + 16), -7), (dict(s1=8 * M), -7),
+], ids=str)
+def test_delta_step(kw, status):
+    assert delta_step(**kw) == status
+
+
+def test_sizes_of_refused_calls_are_zero():
+    for bad in (dict(B=0), dict(dk=12), dict(Hk=3), dict(N=1 << 31), dict(dtype=9)):
+        for f in (lf.linfusion_delta_workspace_bytes, lf.linfusion_delta_saved_bytes, lf.linfusion_delta_bwd_workspace_bytes):
+            assert f(*sizes(**bad)) == 0
+    assert lf.linfusion_gate_norm_bwd_workspace_bytes(2, 50, 12) == 0

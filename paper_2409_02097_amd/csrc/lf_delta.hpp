@@ -41,7 +41,9 @@ struct DeltaArgs {
   uint16_t *w, *kt, *wt, *tt;     // operands; wt = W^T, tt = (T beta)^T: for the backward pass, else null
   float *u, *s, *decay;           // accumulators; per chunk [4][64]
   long long N;
-  int H, Hk, nc;                  // chunks of N tokens
+  int H, Hk, heads, nc;           // B * H; chunks of N tokens
+  int runs, run;                  // runs that the chunks are parted into, and how many make one
+  float *parts, *joined;          // per run: what delta_scan<PARTIAL> leaves, and the state it starts from
   int dk, dv, dkb, dvb, dks;      // channels, blocks of 16 of them, and of 32
   float scale;
   // backward
@@ -125,8 +127,7 @@ LF_DEV double chunk_gamma(const DeltaArgs& a, const DeltaAt& w) {
 
 LF_DEV float decay_between(const double* gamma, int i, int j) { return expf((float)(gamma[i] - gamma[j])); }
 
-constexpr int kLdT = 68;   // leading dimension of a 64 x 64 fp32 matrix in LDS: both operand forms are free of bank conflicts
-constexpr int kLdP = 72;   // of a plane of one
+constexpr int kLdP = 72;   // leading dimension in LDS of a 64 x 64 plane
 constexpr int kLdU = 20;   // of planes of 16 value channels per token
 
 LF_DEV int plane_ld(int steps) { return 32 * steps + 8; }
@@ -150,27 +151,35 @@ template <int N> LF_DEV void load_frag(const uint16_t* frag, Terms<N>& t) {
 }
 
 // ---- the operands and U0 of every chunk -----------------------------------------------------------------------------------
+// A lower triangular matrix of 64 rows in LDS as its ten 16 x 16 blocks on and below the diagonal (fp32, 20 floats a row: both operand
+// forms are free of bank conflicts): 13 KB, so that four workgroups of heads up to 64 fit a CU's LDS beside their keys.  What
+// bounds the kernel is its chain of dependent small steps, so workgroups per CU are what counts.
+constexpr int kLdB = 20, kBlock = 16 * kLdB;
+LF_DEV int block_at(int i, int j) { return (i * (i + 1) / 2 + j) * kBlock; }
+
 template <typename T> inline int delta_prepare_lds(int dks, int dvs) {
-  const int wide = dks > dvs ? dks : dvs;
-  return TermsOf<T>::kStored * plane_bytes(64, wide) + 64 * kLdT * 4 + 3 * 64 * kLdP * 2 + 64 * 8 + kDecayRows * 4 + 64 * 4;
+  constexpr int N = TermsOf<T>::kStored;
+  const int values = N * plane_bytes(64, dvs), solve = 10 * kBlock * 4;
+  return N * plane_bytes(64, dks) + solve + (values > solve ? values : solve) + 64 * 8 + kDecayRows * 4 + 64 * 4;
 }
 
-template <typename T> __global__ __launch_bounds__(256) void delta_prepare(DeltaArgs a) {
+template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepare(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int NI = TermsOf<T>::kStored;
+  constexpr int NI = TermsOf<T>::kStored, kLd = 32 * KS + 8, kPlane = 64 * kLd;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int dvs = (a.dvb + 1) / 2, ld = plane_ld(a.dks), ldv = plane_ld(dvs), plane = 64 * ld;
-  const int most = ld > ldv ? ld : ldv;
-  float* mt = reinterpret_cast<float*>(smem);
-  uint16_t* tp = reinterpret_cast<uint16_t*>(mt + 64 * kLdT);   // A, then T times a factor per column, as terms
-  float* ma = reinterpret_cast<float*>(tp);
-  uint16_t* x = tp + 3 * 64 * kLdP;                             // the keys, then the values
-  double* gamma = reinterpret_cast<double*>(x + NI * 64 * most);
+  const int dvs = (a.dvb + 1) / 2, ldv = plane_ld(dvs);
+  double* gamma = reinterpret_cast<double*>(smem);
   float* decay = reinterpret_cast<float*>(gamma + 64);
   float* both = decay + kDecayRows;                             // beta e^gamma
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g8 = (lane >> 4) * 8, row4 = (lane >> 4) * 4;
+  float* mt = both + 64;                                        // T
+  uint16_t* x = reinterpret_cast<uint16_t*>(mt + 10 * kBlock);  // the keys
+  uint16_t* v = x + NI * kPlane;                                // A, then the values
+  float* ma = reinterpret_cast<float*>(v);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int g8 = (lane >> 4) * 8, row4 = (lane >> 4) * 4;
   const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
+  stage_terms<T>(x, kLd, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, KS);
   if (wave == 0) {
     const double y = chunk_gamma(a, w), last = __shfl(y, 63, 64);
     float beta = 0.0f;
@@ -185,45 +194,61 @@ template <typename T> __global__ __launch_bounds__(256) void delta_prepare(Delta
     decay[kDecayLeft + lane] = left;
     both[lane] = beta * since;
   }
-  stage_terms<T>(x, ld, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, a.dks);
-  for (int i = tid; i < 64 * kLdT; i += 256) mt[i] = 0.0f;
   __syncthreads();
   a.decay[c * kDecayRows + tid] = decay[tid];
   if (w.h % (a.H / a.Hk) == 0) {
     uint16_t* kt = a.kt + ((long long)(w.b * a.Hk + w.hk) * a.nc + blockIdx.x) * a.dkb * 2 * NI * kFrag;
     for (int i = wave; i < a.dkb * 2; i += 4) {
       Terms<NI> f;
-      terms_across<NI>(x + 32 * (i & 1) * ld + 16 * (i >> 1), plane, ld, f);
+      terms_across<NI>(x + 32 * (i & 1) * kLd + 16 * (i >> 1), kPlane, kLd, f);
       store_frag<NI>(kt + i * NI * kFrag, f);
     }
   }
   // A, rows 16 wave .. + 15
-  for (int nt = 0; nt <= wave; ++nt) {
-    f32x4 acc = {0, 0, 0, 0};
-    for (int ks = 0; ks < a.dks; ++ks) {
-      Terms<NI> fi, fj;
-      terms_near<NI>(x + (16 * wave + col) * ld + 32 * ks + g8, plane, fi);
-      terms_near<NI>(x + (16 * nt + col) * ld + 32 * ks + g8, plane, fj);
-      acc = mul_terms<3>(fi, fj, acc);
-    }
+  {
+    Terms<NI> fi[KS];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = 16 * wave + row4 + r, j = 16 * nt + col;
-      ma[i * kLdT + j] = i > j ? decay[kDecayBeta + i] * acc[r] * decay_between(gamma, i, j) : 0.0f;
+    for (int ks = 0; ks < KS; ++ks) terms_near<NI>(x + (16 * wave + col) * kLd + 32 * ks + g8, kPlane, fi[ks]);
+    for (int nt = 0; nt <= wave; ++nt) {
+      f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Terms<NI> fj;
+        terms_near<NI>(x + (16 * nt + col) * kLd + 32 * ks + g8, kPlane, fj);
+        acc = mul_terms<3>(fi[ks], fj, acc);
+      }
+      float* to = ma + block_at(wave, nt);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = 16 * wave + row4 + r, j = 16 * nt + col;
+        to[(row4 + r) * kLdB + col] = i > j ? decay[kDecayBeta + i] * acc[r] * decay_between(gamma, i, j) : 0.0f;
+      }
     }
   }
-  __syncthreads();
-  // T: the blocks on the diagonal, a column per lane, by substitution
-  if (lane < 16) {
-    const float* m = ma + 16 * wave * kLdT + 16 * wave;
+  // T: the blocks on the diagonal, a column per lane, by substitution (each wave its own: no barrier)
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  {
+    const float* m = ma + block_at(wave, wave);
     float t[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float s = i == lane ? 1.0f : 0.0f;
+      float s0 = i == col ? 1.0f : 0.0f, s1 = 0.0f;
 #pragma unroll
-      for (int l = 0; l < i; ++l) s = __builtin_fmaf(-m[i * kLdT + l], t[l], s);
-      t[i] = s;
-      mt[(16 * wave + i) * kLdT + 16 * wave + lane] = s;
+      for (int q = 0; q * 4 < i; ++q) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(m + i * kLdB + 4 * q);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+          if (4 * q + l >= i) continue;
+          if (l & 1) s1 = __builtin_fmaf(-e[l], t[4 * q + l], s1);
+          else s0 = __builtin_fmaf(-e[l], t[4 * q + l], s0);
+        }
+      }
+      t[i] = s0 + s1;
+    }
+    if (lane < 16) {
+      float* to = mt + block_at(wave, wave);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[i * kLdB + lane] = t[i];
     }
   }
   __syncthreads();
@@ -231,142 +256,172 @@ template <typename T> __global__ __launch_bounds__(256) void delta_prepare(Delta
   for (int far = 1; far < 4; ++far) {
     const int i = wave + far, j = wave;
     if (i < 4) {
-      float* tij = mt + 16 * i * kLdT + 16 * j;
+      float* tij = mt + block_at(i, j);
       f32x4 acc = {0, 0, 0, 0};
       for (int l = j; l < i; ++l)
-        acc = mfma_block(steps_near(ma + 16 * i * kLdT + 16 * l, kLdT), rows_near(mt + 16 * l * kLdT + 16 * j, kLdT), acc);
+        acc = mfma_block(steps_near(ma + block_at(i, l), kLdB), rows_near(mt + block_at(l, j), kLdB), acc);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdT + col] = acc[r];
+      for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdB + col] = acc[r];
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (only this wave uses the block until the barrier)
-      acc = mfma_block(steps_near(mt + 16 * i * kLdT + 16 * i, kLdT), rows_near(tij, kLdT), f32x4{0, 0, 0, 0});
+      acc = mfma_block(steps_near(mt + block_at(i, i), kLdB), rows_near(tij, kLdB), f32x4{0, 0, 0, 0});
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdT + col] = -acc[r];
+      for (int r = 0; r < 4; ++r) tij[(row4 + r) * kLdB + col] = -acc[r];
     }
     __syncthreads();
   }
-  auto scaled = [&](const float* by) {   // T with a factor per column, as terms
-    for (int i = tid; i < 64 * 8; i += 256) {
-      const int r = i >> 3, v = (i & 7) * 8;
-      float y[8];
-      load8_f32(mt + r * kLdT + v, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] *= by[v + e];
-      Terms<3> t;
-      split8(y, t);
-#pragma unroll
-      for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(tp + p * 64 * kLdP + r * kLdP + v) = t.t[p];
-    }
-  };
-  scaled(both);
-  __syncthreads();
-  // T's rows 16 wave .. + 15 have nothing behind column 16 wave + 15
+  stage_terms<T>(v, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);   // (A is read)
+  // T's rows 16 wave .. + 15 as an operand with a factor per column; nothing behind column 16 wave + 15
   const int steps = wave < 2 ? 1 : 2;
-  Terms<3> ft[2];
-  auto rows_of_t = [&]() {
+  auto rows_of_t = [&](const float* by, int ks, Terms<3>& f) {
+    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int j = 32 * ks + g8, jb = j >> 4;
+    if (jb <= wave) {
+      load8_f32(mt + block_at(wave, jb) + col * kLdB + (j & 15), y);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      if (ks < steps) terms_near<3>(tp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, ft[ks]);
+      for (int e = 0; e < 8; ++e) y[e] *= by[j + e];
+    }
+    split8(y, f);
   };
-  rows_of_t();
-  uint16_t* mw = a.w + (c * 4 + wave) * a.dks * 3 * kFrag;
-  for (int cb = 0; cb < 2 * a.dks; ++cb) {
+  Terms<3> ft[2];
+  rows_of_t(both, 0, ft[0]);
+  if (steps > 1) rows_of_t(both, 1, ft[1]);
+  uint16_t* mw = a.w + (c * 4 + wave) * KS * 3 * kFrag;
+#pragma unroll
+  for (int cb = 0; cb < 2 * KS; ++cb) {
     f32x4 acc = {0, 0, 0, 0}, act = {0, 0, 0, 0};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       if (ks >= steps) continue;
       Terms<NI> key;
-      terms_across<NI>(x + 32 * ks * ld + 16 * cb, plane, ld, key);
+      terms_across<NI>(x + 32 * ks * kLd + 16 * cb, kPlane, kLd, key);
       acc = mul_terms<3>(key, ft[ks], acc);
       if (a.wt) act = mul_terms<3>(ft[ks], key, act);
     }
     store_operand<3>(mw + (cb >> 1) * 3 * kFrag, cb & 1, acc);
     if (a.wt && cb < a.dkb) store_operand<3>(a.wt + ((c * a.dkb + cb) * 2 + (wave >> 1)) * 3 * kFrag, wave & 1, act);
   }
+  rows_of_t(decay + kDecayBeta, 0, ft[0]);
+  if (steps > 1) rows_of_t(decay + kDecayBeta, 1, ft[1]);
   __syncthreads();
-  scaled(decay + kDecayBeta);
-  stage_terms<T>(x, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);
-  __syncthreads();
-  rows_of_t();
   for (int vb = 0; vb < a.dvb; ++vb) {
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       if (ks >= steps) continue;
       Terms<NI> val;
-      terms_across<NI>(x + 32 * ks * ldv + 16 * vb, 64 * ldv, ldv, val);
+      terms_across<NI>(v + 32 * ks * ldv + 16 * vb, 64 * ldv, ldv, val);
       acc = mul_terms<3>(val, ft[ks], acc);
     }
     *reinterpret_cast<f32x4*>(a.u + (((c * a.dvb + vb) * 4 + wave) * 64 + lane) * 4) = acc;
   }
-  if (a.tt) {
-    for (int ks = 0; ks < 2; ++ks) {
+  if (a.tt) {   // (T beta)^T's rows j of this wave: nothing before column i = j
+    const float by = decay[kDecayBeta + 16 * wave + col];
+    for (int ks = wave >> 1; ks < 2; ++ks) {
+      float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      const int i = 32 * ks + g8, ib = i >> 4;
+      if (ib >= wave) {
+        const float* p = mt + block_at(ib, wave) + (i & 15) * kLdB + col;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = p[e * kLdB] * by;
+      }
       Terms<3> f;
-      terms_across<3>(tp + 32 * ks * kLdP + 16 * wave, 64 * kLdP, kLdP, f);
+      split8(y, f);
       store_frag<3>(a.tt + ((c * 4 + wave) * 2 + ks) * 3 * kFrag, f);
     }
   }
 }
 
 // ---- the scan ---------------------------------------------------------------------------------------------------------------
-// A workgroup takes 16 value channels of one head through all chunks; its four waves hold the state's row blocks
+// A workgroup takes 16 value channels of one head through a run of chunks; its four waves hold the state's row blocks
 // wave, wave + 4, ... as accumulators and compute 16 tokens of U each.  Bound: the chain from one chunk's state to the next
-// (two products, two passes through LDS); everything it reads from memory is requested a chunk ahead.
+// (two products, two passes through LDS); what it reads is requested two chunks ahead where registers allow it, one else:
+// a chunk takes 0.45 us, a request up to 0.9.
+//
+// With fewer workgroups than the device has room for, a head's chunks are parted into runs.  A run turns the state it starts
+// from into M S + R with a d_k x d_k matrix M of its own: a first pass (PARTIAL) takes zeros and the columns of the identity
+// through every run at once, delta_join takes the state through the runs, and the second pass starts each from its state.
 template <int NI, int KS> struct ScanIn {
   static constexpr int kBlocks = (2 * KS + 3) / 4;
+  static constexpr int kDepth = 12 * KS + 8 * NI * kBlocks <= 110 ? 3 : 2;
   Terms<3> w[KS];
   Terms<NI> kt[kBlocks][2];
   f32x4 u0;
   float write, whole;
 };
 
-template <int NI, int KS> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
-  constexpr int kBlocks = ScanIn<NI, KS>::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * kLd;
+// The slices of a head on one XCD, whose L2 they share: workgroups are dealt to the eight XCDs in turn.
+LF_DEV void slice_of_head(unsigned i, int slices, int heads, int& slice, int& bh) {
+  const unsigned group = i / (8u * slices), r = i - group * 8u * slices;
+  const unsigned here = heads - 8 * group < 8 ? heads - 8 * group : 8;
+  slice = r / here;
+  bh = 8 * group + (r - slice * here);
+}
+
+template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
+  using In = ScanIn<NI, KS>;
+  constexpr int kBlocks = In::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * kLd;
   __shared__ __align__(16) uint16_t sp[3 * kPlane];
   __shared__ __align__(16) uint16_t up[3 * 64 * kLdU];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
-  const int slice = blockIdx.x, bh = blockIdx.y, ch = slice * 16 + col;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  int slice, bh;
+  slice_of_head(blockIdx.x, PARTIAL ? a.dvb + a.dkb : a.dvb, a.heads, slice, bh);
+  const int ch = slice * 16 + col, run = blockIdx.y;
+  const bool unit = PARTIAL && slice >= a.dvb;   // columns of the identity, and no values
   const DeltaAt first(a, bh, 0);
-  const int chunks = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
+  const int all = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
+  const int begin = run * a.run, end = begin + a.run < all ? begin + a.run : all;
+  if (!PARTIAL && run > 0 && begin >= all) return;
+  // A wave without a block of its own does the last one's work again, to the same bits: with every load and store of a chunk
+  // unconditional, the compiler can wait for exactly those that it needs.
+  int blk[kBlocks];
+#pragma unroll
+  for (int t = 0; t < kBlocks; ++t) blk[t] = wave + 4 * t < a.dkb ? wave + 4 * t : a.dkb - 1;
   f32x4 s[kBlocks];
 #pragma unroll
-  for (int t = 0; t < kBlocks; ++t)
+  for (int t = 0; t < kBlocks; ++t) {
+    if (!PARTIAL && run > 0) {
+      s[t] = *reinterpret_cast<const f32x4*>(a.joined + ((((long long)bh * a.runs + run) * a.dvb + slice) * a.dkb + blk[t]) * 256 + lane * 4);
+      continue;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = 16 * (wave + 4 * t) + row4 + r;
-      s[t][r] = a.state_in && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
+      const int row = 16 * blk[t] + row4 + r;
+      if (unit) s[t][r] = row == (slice - a.dvb) * 16 + col ? 1.0f : 0.0f;
+      else s[t][r] = a.state_in && run == 0 && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
     }
+  }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
   const long long c0 = (long long)bh * a.nc;
   const long long k0 = (long long)(first.b * a.Hk + first.hk) * a.nc;
-  auto request = [&](ScanIn<NI, KS>& n, int i) {
-    const uint16_t* mw = a.w + ((c0 + i) * 4 + wave) * a.dks * 3 * kFrag;
+  const long long u_at = ((unit ? 0 : slice) * 4 + wave) * 256 + lane * 4;
+  auto request = [&](In& n, int i) {
+    i = i < end ? i : end - 1;
+    const uint16_t* mw = a.w + ((c0 + i) * 4 + wave) * KS * 3 * kFrag;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<3>(mw + ks * 3 * kFrag, n.w[ks]);
     const uint16_t* kt = a.kt + (k0 + i) * a.dkb * 2 * NI * kFrag;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-        if (wave + 4 * t < a.dkb) load_frag<NI>(kt + ((wave + 4 * t) * 2 + ks) * NI * kFrag, n.kt[t][ks]);
-    n.u0 = *reinterpret_cast<const f32x4*>(a.u + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4);
+      for (int ks = 0; ks < 2; ++ks) load_frag<NI>(kt + (blk[t] * 2 + ks) * NI * kFrag, n.kt[t][ks]);
+    n.u0 = *reinterpret_cast<const f32x4*>(a.u + (c0 + i) * a.dvb * 1024 + u_at);
     const float* decay = a.decay + (c0 + i) * kDecayRows;
     n.write = decay[kDecayWrite + 16 * wave + col];
     n.whole = decay[kDecaySince + 63];
   };
-  auto keep = [&](int i) {
-    float* to = a.s + (((long long)bh * (a.nc + 1) + i) * a.dvb + slice) * a.dkb * 256;
+  auto keep = [&](float* to) {
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-      if (wave + 4 * t < a.dkb) *reinterpret_cast<f32x4*>(to + (wave + 4 * t) * 256 + lane * 4) = s[t];
+    for (int t = 0; t < kBlocks; ++t) *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
   };
-  auto chunk = [&](ScanIn<NI, KS>& in, ScanIn<NI, KS>& next, int i) {
+  auto state_at = [&](int i) { return a.s + (((long long)bh * (a.nc + 1) + i) * a.dvb + slice) * a.dkb * 256; };
+  auto chunk = [&](In& in, In& next, int i) {
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-      if (wave + 4 * t < a.dkb) split4_lds<3>(sp + col * kLd + 16 * (wave + 4 * t) + row4, kPlane, s[t]);
-    if (i + 1 < chunks) request(next, i + 1);
-    keep(i);
+    for (int t = 0; t < kBlocks; ++t) split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
+    request(next, i + In::kDepth - 1);
+    if constexpr (!PARTIAL) keep(state_at(i));
     lds_barrier();
     f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
 #pragma unroll
@@ -376,8 +431,10 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_scan(Delt
       if (ks & 1) acc2 = mul_terms<3>(fs, in.w[ks], acc2);
       else acc = mul_terms<3>(fs, in.w[ks], acc);
     }
-    const f32x4 u = in.u0 - (acc + acc2);
-    *reinterpret_cast<f32x4*>(a.u + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4) = u;
+    f32x4 u0 = in.u0;
+    if (unit) u0 = f32x4{0, 0, 0, 0};
+    const f32x4 u = u0 - (acc + acc2);
+    if constexpr (!PARTIAL) *reinterpret_cast<f32x4*>(a.u + (c0 + i) * a.dvb * 1024 + u_at) = u;
     split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, u * in.write);
     lds_barrier();
     Terms<3> fu[2];
@@ -385,29 +442,83 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_scan(Delt
     terms_across<3>(up + 32 * kLdU, 64 * kLdU, kLdU, fu[1]);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      if (wave + 4 * t >= a.dkb) continue;
       s[t] *= in.whole;
       s[t] = mul_terms<3>(in.kt[t][0], fu[0], s[t]);
       s[t] = mul_terms<3>(in.kt[t][1], fu[1], s[t]);
     }
   };
-  ScanIn<NI, KS> x, y;
-  if (chunks > 0) request(x, 0);
-  int i = 0;
-  for (; i + 1 < chunks; i += 2) {
-    chunk(x, y, i);
-    chunk(y, x, i + 1);
-  }
-  if (i < chunks) chunk(x, y, i);
-  keep(chunks);
-  if (a.state_out) {
-#pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave + 4 * t) + row4 + r;
-        if (row < a.dk && ch < a.dv) a.state_out[((long long)bh * a.dk + row) * a.dv + ch] = s[t][r];
+  if (begin < end) {
+    In x, y;
+    request(x, begin);
+    if constexpr (In::kDepth == 3) {
+      In z;
+      request(y, begin + 1);
+      int i = begin;
+      for (; i + 2 < end; i += 3) {
+        chunk(x, z, i);
+        chunk(y, x, i + 1);
+        chunk(z, y, i + 2);
       }
+      if (i < end) chunk(x, z, i);
+      if (i + 1 < end) chunk(y, x, i + 1);
+    } else {
+      int i = begin;
+      for (; i + 1 < end; i += 2) {
+        chunk(x, y, i);
+        chunk(y, x, i + 1);
+      }
+      if (i < end) chunk(x, y, i);
+    }
+  }
+  if constexpr (PARTIAL) {
+    keep(a.parts + (((long long)bh * a.runs + run) * (a.dvb + a.dkb) + slice) * a.dkb * 256);
+  } else if (end == all) {
+    keep(state_at(all));
+    if (a.state_out) {
+#pragma unroll
+      for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * blk[t] + row4 + r;
+          if (row < a.dk && ch < a.dv) a.state_out[((long long)bh * a.dk + row) * a.dv + ch] = s[t][r];
+        }
+    }
+  }
+}
+
+// The state that each run starts from, 16 value channels of one head: the first run's end, then M S + R run by run.  M's column k
+// is a partial state's column k: the operand gathers its four steps from four lanes' accumulators.
+template <int KS> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a) {
+  constexpr int kBlocks = (2 * KS + 3) / 4;
+  __shared__ __align__(16) float sl[32 * KS * kLdB];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int row4 = (lane >> 4) * 4, slice = blockIdx.x, bh = blockIdx.y, slices = a.dvb + a.dkb;
+  f32x4 s[kBlocks];
+  for (int run = 0; run + 1 < a.runs; ++run) {
+    const float* part = a.parts + ((long long)bh * a.runs + run) * slices * a.dkb * 256;
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) {
+      const int mb = wave + 4 * t;
+      if (mb >= a.dkb) continue;
+      f32x4 acc = *reinterpret_cast<const f32x4*>(part + (slice * a.dkb + mb) * 256 + lane * 4);
+      if (run > 0) {
+        for (int kb = 0; kb < a.dkb; ++kb) {
+          const float* m = part + ((a.dvb + kb) * a.dkb + mb) * 256 + (row4 + 16 * (col >> 2)) * 4 + (col & 3);
+          acc = mfma_block(f32x4{m[0], m[4], m[8], m[12]}, rows_near(sl + 16 * kb * kLdB, kLdB), acc);
+        }
+      }
+      s[t] = acc;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) {
+      const int mb = wave + 4 * t;
+      if (mb >= a.dkb) continue;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sl[(16 * mb + row4 + r) * kLdB + col] = s[t][r];
+      *reinterpret_cast<f32x4*>(a.joined + ((((long long)bh * a.runs + run + 1) * a.dvb + slice) * a.dkb + mb) * 256 + lane * 4) = s[t];
+    }
+    __syncthreads();
   }
 }
 
@@ -417,34 +528,51 @@ constexpr int kOutBlocks = 4;   // of 16 value channels at a time
 
 template <typename T> inline int delta_out_lds(int dks) {
   constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut;
-  const int rows = 2 * NI * plane_bytes(64, dks);
+  const int rows = 2 * NI * plane_bytes(64, dks) + NO * 64 * kLdP * 2;
   const int later = kOutBlocks * NO * (plane_bytes(16, dks) + 64 * kLdU * 2);
-  return NO * 64 * kLdP * 2 + (rows > later ? rows : later) + 64 * 8 + kDecayRows * 4;
+  return (rows > later ? rows : later) + 64 * 8 + 2 * 64 * 4;
 }
 
 template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut, kLd = 32 * KS + 8, kSPlane = 16 * kLd, kUPlane = 64 * kLdU;
+  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut, KB = 2 * KS, kLd = 32 * KS + 8;
+  constexpr int kSPlane = 16 * kLd, kUPlane = 64 * kLdU;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
   double* gamma = reinterpret_cast<double*>(smem);
-  float* decay = reinterpret_cast<float*>(gamma + 64);
-  uint16_t* pp = reinterpret_cast<uint16_t*>(decay + kDecayRows);
-  uint16_t* q = pp + NO * 64 * kLdP;
+  float* decay = reinterpret_cast<float*>(gamma + 64);   // e^gamma, beta
+  uint16_t* q = reinterpret_cast<uint16_t*>(decay + 128);
   uint16_t* k = q + NI * 64 * kLd;
-  uint16_t* sp = q;                                     // where q and k were
+  uint16_t* pp = k + NI * 64 * kLd;
+  uint16_t* sp = q;                                      // later, where all of these were
   uint16_t* up = sp + kOutBlocks * NO * kSPlane;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
-  if (wave == 0) gamma[lane] = chunk_gamma(a, w);
-  decay[tid] = a.decay[c * kDecayRows + tid];
   stage_terms<T>(q, kLd, a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk, KS);
   stage_terms<T>(k, kLd, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, KS);
+  if (wave == 0) gamma[lane] = chunk_gamma(a, w);
+  if (tid < 64) decay[tid] = a.decay[c * kDecayRows + kDecaySince + tid];
+  else if (tid < 128) decay[tid] = a.decay[c * kDecayRows + kDecayBeta + tid - 64];
+  // the first blocks of U and of the state, requested now, put down when there is room
+  f32x4 s_in[KB], u_in[kOutBlocks];
+  int vb0 = 0, blocks = a.dvb < kOutBlocks ? a.dvb : kOutBlocks;
+  auto request = [&]() {   // wave w: block w of the state (all of its rows), 16 tokens of every block of U
+    const float* s0 = a.s + (((long long)blockIdx.y * (a.nc + 1) + blockIdx.x) * a.dvb + vb0) * a.dkb * 256;
+    const float* mu = a.u + (c * a.dvb + vb0) * 1024;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      if (wave < blocks && kb < a.dkb) s_in[kb] = *reinterpret_cast<const f32x4*>(s0 + (wave * a.dkb + kb) * 256 + lane * 4);
+#pragma unroll
+    for (int i = 0; i < kOutBlocks; ++i)
+      if (i < blocks) u_in[i] = *reinterpret_cast<const f32x4*>(mu + (i * 4 + wave) * 256 + lane * 4);
+  };
+  request();
   __syncthreads();
   Terms<NI> fq[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) terms_near<NI>(q + (16 * wave + col) * kLd + 32 * ks + g8, 64 * kLd, fq[ks]);
-  // P, four neighbouring columns j of row i at a time; 0 where beta_j is 0 (the u_j that is kept is not)
+  // P's rows of this wave, four neighbouring columns j of row i at a time; 0 where beta_j is 0 (the u_j that is kept is not)
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt) {
     f32x4 acc = {0, 0, 0, 0};
@@ -458,35 +586,34 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = 16 * wave + col, j = 16 * jt + row4 + r;
-        const bool on = j <= i && decay[kDecayBeta + j] != kDeltaTinyBeta;
+        const bool on = j <= i && decay[64 + j] != kDeltaTinyBeta;
         acc[r] = on ? acc[r] * decay_between(gamma, i, j) : 0.0f;
       }
     }
     split4_lds<NO>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, acc);
   }
-  __syncthreads();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (rows that only this wave writes and reads)
   Terms<NO> fp[2];
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) terms_near<NO>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
-  const float since = decay[kDecaySince + 16 * wave + col];
+  const float since = decay[16 * wave + col];
   const int n = 16 * wave + col;
-  // (the half block behind dkb of the last 32 channels: the queries there are 0, the state's planes are too)
-  for (int i = tid; i < kOutBlocks * NO * kSPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
-  for (int vb0 = 0; vb0 < a.dvb; vb0 += kOutBlocks) {
-    const int blocks = a.dvb - vb0 < kOutBlocks ? a.dvb - vb0 : kOutBlocks;
+  for (;;) {
     __syncthreads();
-    const float* s0 = a.s + (((long long)blockIdx.y * (a.nc + 1) + blockIdx.x) * a.dvb + vb0) * a.dkb * 256;
-    for (int i = wave; i < blocks * a.dkb; i += 4) {
-      const int vb = (unsigned)i / (unsigned)a.dkb, kb = i - vb * a.dkb;
-      split4_lds<NO>(sp + vb * NO * kSPlane + col * kLd + 16 * kb + row4, kSPlane,
-                     *reinterpret_cast<const f32x4*>(s0 + (long long)i * 256 + lane * 4));
+    if (wave < blocks) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)   // (zeros in the half block behind d_k: the queries' zeros times what is there)
+        split4_lds<NO>(sp + wave * NO * kSPlane + col * kLd + 16 * kb + row4, kSPlane, kb < a.dkb ? s_in[kb] : f32x4{0, 0, 0, 0});
     }
-    const float* mu = a.u + (c * a.dvb + vb0) * 1024;
-    for (int i = wave; i < blocks * 4; i += 4)
-      split4_lds<NO>(up + (i >> 2) * NO * kUPlane + (16 * (i & 3) + col) * kLdU + row4, kUPlane,
-                     *reinterpret_cast<const f32x4*>(mu + i * 256 + lane * 4));
+#pragma unroll
+    for (int i = 0; i < kOutBlocks; ++i)
+      if (i < blocks) split4_lds<NO>(up + i * NO * kUPlane + n * kLdU + row4, kUPlane, u_in[i]);
+    const int here = blocks, at_block = vb0;
+    vb0 += kOutBlocks;
+    blocks = a.dvb - vb0 < kOutBlocks ? a.dvb - vb0 : kOutBlocks;
+    if (vb0 < a.dvb) request();
     __syncthreads();
-    for (int vb = 0; vb < blocks; ++vb) {
+    for (int vb = 0; vb < here; ++vb) {
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -502,10 +629,11 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
         terms_across<NO>(up + vb * NO * kUPlane + 32 * ks * kLdU, kUPlane, kLdU, fu);
         acc = mul_terms<NO>(fu, fp[ks], acc);
       }
-      const int ch = 16 * (vb0 + vb) + row4;
+      const int ch = 16 * (at_block + vb) + row4;
       if (n < w.valid && ch < a.dv)
         store4<T>(at<T>(a.out, w.b * a.vo.b + w.h * a.vo.h + (w.n0 + n) * a.vo.n + ch), acc * a.scale);
     }
+    if (vb0 >= a.dvb) break;
   }
 }
 

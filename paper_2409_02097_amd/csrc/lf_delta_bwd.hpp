@@ -13,7 +13,8 @@
 // chunks at once (delta_back_prepare), a scan runs from the last chunk to the first (delta_back_scan), and the rest follows
 // for all chunks at once (delta_gradients), where the value heads that share a query and key head are summed in their order.
 //     kn   K as operand: [4 token blocks][d_k / 32][terms][64][8], once per query and key head
-//     du   P^T dO, then dU, as u;   ds   (e^gamma Q)^T dO, then dS1, as s
+//     du   P^T dO, then dU, as u;   ds   as s, two places more per head: (e^gamma Q)^T dO of chunk c at c, dS1 two places on,
+//          which every wave of the scan has behind it when dS1 is written
 #pragma once
 #include "lf_delta.hpp"
 
@@ -118,7 +119,7 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
       f32x4 z = {0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) z = mul_terms<3>(fq[t][ks], fo[ks], z);
-      *reinterpret_cast<f32x4*>(a.ds + ((c * a.dvb + vb) * a.dkb + wave + 4 * t) * 256 + lane * 4) = z;
+      *reinterpret_cast<f32x4*>(a.ds + (((c + 2 * w.bh) * a.dvb + vb) * a.dkb + wave + 4 * t) * 256 + lane * 4) = z;
     }
   }
 }
@@ -136,16 +137,20 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
   constexpr int kBlocks = BackScanIn<NI, KS>::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * kLd;
   __shared__ __align__(16) uint16_t sp[3 * kPlane];
   __shared__ __align__(16) uint16_t up[3 * 64 * kLdU];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   const int slice = blockIdx.x, bh = blockIdx.y, ch = slice * 16 + col;
   const DeltaAt first(a, bh, 0);
   const int chunks = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
+  int blk[kBlocks];   // (as in delta_scan)
+#pragma unroll
+  for (int t = 0; t < kBlocks; ++t) blk[t] = wave + 4 * t < a.dkb ? wave + 4 * t : a.dkb - 1;
   f32x4 s[kBlocks];
 #pragma unroll
   for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = 16 * (wave + 4 * t) + row4 + r;
+      const int row = 16 * blk[t] + row4 + r;
       s[t][r] = a.dstate_out && row < a.dk && ch < a.dv ? a.dstate_out[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
     }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
@@ -157,13 +162,12 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<NI>(kn + ks * NI * kFrag, n.kn[ks]);
     const uint16_t* wt = a.wt + (c0 + i) * a.dkb * 2 * 3 * kFrag;
-    const float* z = a.ds + ((c0 + i) * a.dvb + slice) * a.dkb * 256;
+    const float* z = a.ds + ((c0 + 2 * bh + i) * a.dvb + slice) * a.dkb * 256;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      if (wave + 4 * t >= a.dkb) continue;
-      n.z[t] = *reinterpret_cast<const f32x4*>(z + (wave + 4 * t) * 256 + lane * 4);
+      n.z[t] = *reinterpret_cast<const f32x4*>(z + blk[t] * 256 + lane * 4);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) load_frag<3>(wt + ((wave + 4 * t) * 2 + ks) * 3 * kFrag, n.wt[t][ks]);
+      for (int ks = 0; ks < 2; ++ks) load_frag<3>(wt + (blk[t] * 2 + ks) * 3 * kFrag, n.wt[t][ks]);
     }
     n.du = *reinterpret_cast<const f32x4*>(a.du + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4);
     const float* decay = a.decay + (c0 + i) * kDecayRows;
@@ -173,12 +177,12 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
   auto chunk = [&](BackScanIn<NI, KS>& in, BackScanIn<NI, KS>& next, int i) {
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
-      if (wave + 4 * t < a.dkb) split4_lds<3>(sp + col * kLd + 16 * (wave + 4 * t) + row4, kPlane, s[t]);
-    if (i > 0) request(next, i - 1);
-    float* to = a.ds + ((c0 + i) * a.dvb + slice) * a.dkb * 256;
+      split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
+    request(next, i > 0 ? i - 1 : 0);
+    float* to = a.ds + ((c0 + 2 * bh + i + 2) * a.dvb + slice) * a.dkb * 256;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
-      if (wave + 4 * t < a.dkb) *reinterpret_cast<f32x4*>(to + (wave + 4 * t) * 256 + lane * 4) = s[t];
+      *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
     lds_barrier();
     f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
 #pragma unroll
@@ -197,7 +201,6 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
     terms_across<3>(up + 32 * kLdU, 64 * kLdU, kLdU, fu[1]);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      if (wave + 4 * t >= a.dkb) continue;
       s[t] = s[t] * in.whole + in.z[t];
       s[t] = mul_terms<3>(in.wt[t][0], fu[0], s[t]);
       s[t] = mul_terms<3>(in.wt[t][1], fu[1], s[t]);
@@ -216,7 +219,7 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = 16 * (wave + 4 * t) + row4 + r;
+        const int row = 16 * blk[t] + row4 + r;
         if (row < a.dk && ch < a.dv) a.dstate_in[((long long)bh * a.dk + row) * a.dv + ch] = s[t][r];
       }
   }
@@ -304,7 +307,7 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(256) voi
         if (vb + e < a.dvb) {
           const float* s0 = a.s + (((long long)w.bh * (a.nc + 1) + blockIdx.x) * a.dvb + vb + e) * a.dkb * 256 + lane * 4;
           const float* s1 = s0 + (long long)a.dvb * a.dkb * 256;
-          const float* ds = a.ds + (c * a.dvb + vb + e) * a.dkb * 256 + lane * 4;
+          const float* ds = a.ds + ((c + 2 * w.bh + 2) * a.dvb + vb + e) * a.dkb * 256 + lane * 4;
           for (int kb = wave; kb < a.dkb; kb += 4) {
             const f32x4 d1 = *reinterpret_cast<const f32x4*>(ds + kb * 256), t1 = *reinterpret_cast<const f32x4*>(s1 + kb * 256);
             split4_lds<3>(ps + (16 * e + col) * kLd + 16 * kb + row4, kSPlane, *reinterpret_cast<const f32x4*>(s0 + kb * 256));

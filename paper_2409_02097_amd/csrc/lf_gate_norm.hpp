@@ -41,7 +41,7 @@ struct GateNormBwdArgs {
 // Sums `v` over the threads of a token: LANES lanes of a wave, or the whole workgroup of four waves (LANES = 256) through
 // LDS.  `slot` alternates, so that a second sum needs no barrier behind the first one's reads.
 template <int LANES> LF_DEV float token_sum(float v, float* lds, int slot) {
-  v = lanes_sum<LANES>(v);
+  v = lanes_sum<64>(v);
   if constexpr (LANES == 256) {
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) lds[slot * 4 + wave] = v;
@@ -52,8 +52,8 @@ template <int LANES> LF_DEV float token_sum(float v, float* lds, int slot) {
 }
 
 template <int LANES> LF_DEV void token_sum2(float& a, float& b, float* lds, int slot) {
-  a = lanes_sum<LANES>(a);
-  b = lanes_sum<LANES>(b);
+  a = lanes_sum<64>(a);
+  b = lanes_sum<64>(b);
   if constexpr (LANES == 256) {
     const int wave = threadIdx.x >> 6;
     float* p = lds + 8 + slot * 8;   // (behind the single sums' slots, which other waves may still be reading)

@@ -67,10 +67,30 @@ template <typename T> LF_DEV void store8_stream(unsigned char* p, const float (&
 
 LF_DEV void load8_f32(const float* p, float (&x)[8]) { load8<F32>(reinterpret_cast<const unsigned char*>(p), x); }
 
-// Sum over the LANES neighbouring lanes ; every one of them gets it.
+// Sum over the LANES neighbouring lanes (16 or 64); every one of them gets it.  Without LDS: exchanges inside a row of 16 lanes
+// as modifiers of the additions, rows and halves by the swapping moves (a step through the LDS crossbar takes 60 cycles or more, and
+// the row-wise operators wait for four to eight of these sums per token).
+template <int CTRL> LF_DEV float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// v plus the other row's (LANES = 16: rows 0 and 1, 2 and 3) or the other half's.  (The two copies are kept apart: with one value
+// as both operands this compiler takes both results for the first.)
+template <int LANES> LF_DEV float swap_add(float v) {
+  unsigned a = __builtin_bit_cast(unsigned, v), b = a;
+  asm("" : "+v"(b));
+  const auto r = LANES == 16 ? __builtin_amdgcn_permlane16_swap(a, b, false, false) : __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
 template <int LANES> LF_DEV float lanes_sum(float v) {
-#pragma unroll
-  for (int m = LANES < 64 ? LANES / 2 : 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+  static_assert(LANES == 16 || LANES == 64, "a row or a wave");
+  v = dpp_add<0xB1>(v);    // lanes 1 apart
+  v = dpp_add<0x4E>(v);    // 2 apart
+  v = dpp_add<0x141>(v);   // the other half of 8
+  v = dpp_add<0x140>(v);   // of 16
+  if constexpr (LANES == 64) {
+    v = swap_add<16>(v);
+    v = swap_add<32>(v);
+  }
   return v;
 }
 

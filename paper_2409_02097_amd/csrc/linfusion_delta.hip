@@ -21,10 +21,10 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct Sizes {
   long long nc, heads;   // chunks of N tokens; B * H
-  int dkb, dvb, dks;
+  int dkb, dvb, dks, runs, run;
   size_t esz;
-  size_t w, kt, u, s, decay, wt, tt, kn, du, ds;   // bytes
-  size_t forward() const { return w + kt + u + s + decay; }
+  size_t parts, joined, w, kt, u, s, decay, wt, tt, kn, du, ds;   // bytes
+  size_t forward() const { return w + kt + u + s + decay + parts + joined; }
   size_t saved() const { return forward() + wt + tt; }
   size_t backward() const { return kn + du + ds; }
 };
@@ -51,8 +51,20 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->u = up(chunks * z->dvb * 1024 * 4);
   z->s = up((chunks + (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
   z->decay = up(chunks * lf::kDecayRows * 4);
+  // Runs: as many as fill the device twice over with workgroups of the second pass, of 16 chunks at least; each costs delta_join
+  // a step of a few us, and the first pass does (d_k + d_v) / d_v times the work of the second.
+  const long long scans = z->heads * z->dvb;
+  long long runs = 2LL * lfh::num_cu() / scans;
+  if (runs > z->nc / 16) runs = z->nc / 16;
+  if (runs > 32) runs = 32;
+  if (runs < 3) runs = 1;
+  z->run = (int)((z->nc + runs - 1) / runs);
+  z->runs = (int)((z->nc + z->run - 1) / z->run);
+  const size_t blocks = z->runs > 1 ? (size_t)z->heads * z->runs * z->dkb * 1024 : 0;
+  z->parts = up(blocks * (z->dvb + z->dkb));
+  z->joined = up(blocks * z->dvb);
   z->du = z->u;
-  z->ds = up(chunks * z->dvb * z->dkb * 256 * 4);
+  z->ds = up((chunks + 2 * (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
   return LINFUSION_OK;
 }
 
@@ -117,6 +129,8 @@ void place_forward(lf::DeltaArgs* a, const Sizes& z, void* at, bool for_backward
   take(a->u, p, z.u);
   take(a->s, p, z.s);
   take(a->decay, p, z.decay);
+  take(a->parts, p, z.parts);
+  take(a->joined, p, z.joined);
   a->wt = a->tt = nullptr;
   if (!for_backward) return;
   take(a->wt, p, z.wt);
@@ -132,16 +146,27 @@ void place_forward(lf::DeltaArgs* a, const Sizes& z, void* at, bool for_backward
     default: X(5) break;                                                                          \
   }
 
+template <typename T, int KS> int launch_states(const lf::DeltaArgs& a, int BH, hipStream_t st) {
+  constexpr int NI = lf::TermsOf<T>::kStored;
+  const int lds = lf::delta_prepare_lds<T>(KS, (a.dvb + 1) / 2);
+  auto prepare = lf::delta_prepare<T, KS>;
+  if (!lfh::allow_lds(prepare, lds)) return LINFUSION_ERR_HIP;
+  prepare<<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+  if (a.runs > 1) {
+    lf::delta_scan<NI, KS, true><<<dim3((a.dvb + a.dkb) * BH, a.runs - 1), dim3(256), 0, st>>>(a);
+    lf::delta_join<KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+  }
+  lf::delta_scan<NI, KS, false><<<dim3(a.dvb * BH, a.runs), dim3(256), 0, st>>>(a);
+  return LINFUSION_OK;
+}
+
 // operands, U, the states and the decays of all chunks
 template <typename T> int run_states(const lf::DeltaArgs& a, int BH, hipStream_t st) {
-  constexpr int NI = lf::TermsOf<T>::kStored;
-  const int lds = lf::delta_prepare_lds<T>(a.dks, (a.dvb + 1) / 2);
-  if (!lfh::allow_lds(lf::delta_prepare<T>, lds)) return LINFUSION_ERR_HIP;
-  lf::delta_prepare<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
-#define X(KS) lf::delta_scan<NI, KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
+  int rc = LINFUSION_OK;
+#define X(KS) rc = launch_states<T, KS>(a, BH, st);
   LF_FOR_STEPS(X)
 #undef X
-  return LINFUSION_OK;
+  return rc;
 }
 
 template <typename T, int KS> int launch_out(const lf::DeltaArgs& a, int BH, hipStream_t st) {
@@ -249,7 +274,7 @@ int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.out = out; a.state_out = state_out; a.lengths = lengths;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.heads = (int)z.heads; a.runs = z.runs; a.run = z.run; a.scale = scale;
   place_forward(&a, z, saved ? saved : workspace, saved != nullptr);
   const hipStream_t st = (hipStream_t)stream;
   const int BH = (int)z.heads;
@@ -303,7 +328,7 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.lengths = lengths; a.dout = dout; a.dstate_out = dstate_out;
   a.dq = dq; a.dk_out = dk; a.dv_out = dv; a.dg = dg; a.dbeta = dbeta; a.dstate_in = dstate_in;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
+  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.heads = (int)z.heads; a.runs = z.runs; a.run = z.run; a.scale = scale;
   unsigned char* p = static_cast<unsigned char*>(workspace);
   take(a.kn, p, z.kn);
   take(a.du, p, z.du);

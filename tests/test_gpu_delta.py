@@ -329,3 +329,18 @@ def test_refusals_on_the_device():
     with pytest.raises(lf.LinFusionError) as e:
         lf.linfusion_delta_fwd(g["q"], g["k"], g["v"], g["g"], g["beta"], g["v"], workspace=ws)
     assert e.value.status == -7
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [("bf16", 40, 24), ("f32", 16, 16), ("f16", 72, 40)])
+def test_long_sequences_of_few_heads_in_runs(dtype, dk, dv):
+    """Chunks parted into runs, whole and not, rows that end inside each of them; gradients behind such a forward call."""
+    N, lengths = 64 * 70 + 5, [64 * 70 + 5, 64 * 33, 1100, 0]
+    c = make(4, 1, 1, N, dk, dv, dtype, seed=51, lengths=lengths)
+    g = on_gpu(c)
+    out, last, saved = forward(c, g, saved=True)
+    d = backward(c, g, saved)
+    for b, n in enumerate(lengths):
+        for t in (out, *(d[m] for m in ("q", "k", "v", "g", "beta"))):
+            t[b, :, n:] = 0.0
+    check_forward(c, out, last)
+    check_backward(c, d)

@@ -16,10 +16,13 @@
 //
 // Products run on the 16-bit matrix instruction with operands as sums of bf16 terms (lf_terms.hpp): three where a state or
 // an fp32 result depends on them, two where a 16-bit output does.  What passes between the kernels is stored as its reader
-// takes it, a contiguous kilobyte for each operand or accumulator of a wave:
-//     w    T (beta e^gamma K) as operand: [4 row blocks][d_k / 32][3 terms][64 lanes][8 steps]
-//     kt   K^T as operand: [d_k / 16][2][terms][64][8], once per query and key head
-//     u    U0, then U, and s the state before each chunk and behind the last, as fp32 accumulators: [d_v / 16][row blocks][64][4]
+// takes it, a contiguous kilobyte for each operand or accumulator of a wave, all of a chunk and head in one record (a workgroup
+// then touches a page or two of the workspace, not one per array):
+//     w      T (beta e^gamma K) as operand: [4 row blocks][d_k / 32][3 terms][64 lanes][8 steps]
+//     kt     K^T as operand: [d_k / 16][2][terms][64][8], in the record of the first value head that has the key head
+//     u      U0, then U, and s the state before the chunk, as fp32 accumulators: [d_v / 16][row blocks][64][4]
+//     decay  what follows from g and beta per token
+//     wt     W^T as operand, [d_k / 16][2][3][64][8], and tt (T beta)^T, six operands of 64 x 8 fp32: for the backward pass
 #pragma once
 #include "lf_terms.hpp"
 
@@ -38,8 +41,10 @@ struct DeltaArgs {
   float* state_out;
   const int* lengths;
   DeltaView vq, vk, vv, vg, vo;
-  uint16_t *w, *kt, *wt, *tt;     // operands; wt = W^T, tt = (T beta)^T: for the backward pass, else null
-  float *u, *s, *decay;           // accumulators; per chunk [4][64]
+  unsigned char *record, *record_b;   // of the forward pass, of the backward pass
+  unsigned size, size_b;              // bytes of one
+  unsigned at_kt, at_u, at_s, at_decay, at_wt, at_tt, at_kn, at_ds;   // bytes into it; w, and du in the other, come first
+  int for_backward;
   long long N;
   int H, Hk, heads, nc;           // B * H; chunks of N tokens
   int runs, run;                  // runs that the chunks are parted into, and how many make one
@@ -52,13 +57,16 @@ struct DeltaArgs {
   void *dq, *dk_out, *dv_out;
   float *dg, *dbeta, *dstate_in;
   DeltaView vdo, vdq, vdk, vdv, vdg;
-  uint16_t* kn;                   // K as operand
-  float *du, *ds;                 // as u; as s (the gradient of a chunk's last state)
+
+  LF_DEV unsigned char* rec(int bh, int chunk) const { return record + ((long long)bh * nc + chunk) * size; }
+  LF_DEV unsigned char* rec_b(int bh, int chunk) const { return record_b + ((long long)bh * (nc + 2) + chunk) * size_b; }
 };
+template <typename P> LF_DEV P* part(unsigned char* record, unsigned at) { return reinterpret_cast<P*>(record + at); }
 
 // rows of `decay`: e^gamma; e^(gamma_63 - gamma), 0 where beta is 0 (such a token leaves the state alone); beta, never 0 (u / beta
 // is needed where beta is 0 too, for its gradient); e^(gamma_63 - gamma) everywhere
 constexpr int kDecaySince = 0, kDecayWrite = 64, kDecayBeta = 128, kDecayLeft = 192, kDecayRows = 256;
+constexpr int kDecayBytes = kDecayRows * 4 + 64 * 8;   // and gamma, as powers of two, in fp64
 
 struct DeltaAt {
   int b, h, hk, bh;
@@ -111,7 +119,7 @@ template <typename T> LF_DEV void store4(unsigned char* p, const f32x4& v) {
   else *reinterpret_cast<u32x2*>(p) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
 }
 
-// gamma of the 64 tokens, by the first wave; a decay of -infinity counts as -10^4, which is none left
+// gamma of the 64 tokens, by one wave, as a power of two; a decay of -infinity counts as -10^4, which is none left
 LF_DEV double chunk_gamma(const DeltaArgs& a, const DeltaAt& w) {
   const int t = threadIdx.x & 63;
   float g = 0.0f;
@@ -122,10 +130,12 @@ LF_DEV double chunk_gamma(const DeltaArgs& a, const DeltaAt& w) {
     const double y = __shfl_up(x, m, 64);
     if (t >= m) x += y;
   }
-  return x;
+  return x * 1.4426950408889634074;
 }
 
-LF_DEV float decay_between(const double* gamma, int i, int j) { return expf((float)(gamma[i] - gamma[j])); }
+// 2^x of an fp64 power: the rounding of x to fp32 is off by 2^-24 of x, which matters the less the smaller the result
+LF_DEV float power(double x) { return __builtin_amdgcn_exp2f((float)x); }
+LF_DEV float decay_between(const double* gamma, int i, int j) { return power(gamma[i] - gamma[j]); }
 
 constexpr int kLdP = 72;   // leading dimension in LDS of a 64 x 64 plane
 constexpr int kLdU = 20;   // of planes of 16 value channels per token
@@ -178,26 +188,29 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
   float* ma = reinterpret_cast<float*>(v);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int g8 = (lane >> 4) * 8, row4 = (lane >> 4) * 4;
-  const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
-  stage_terms<T>(x, kLd, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, KS);
+  unsigned char* rec = a.rec(w.bh, blockIdx.x);
+  Rows<T, KS, 256> keys;
+  keys.request(a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk);
   if (wave == 0) {
     const double y = chunk_gamma(a, w), last = __shfl(y, 63, 64);
     float beta = 0.0f;
     if (lane < w.valid) beta = a.beta[w.b * a.vg.b + w.h * a.vg.h + (w.n0 + lane) * a.vg.n];
     const bool none = fabsf(beta) < kDeltaTinyBeta;
     if (none) beta = kDeltaTinyBeta;
-    const float since = expf((float)y), left = expf((float)(last - y));
+    const float since = power(y), left = power(last - y);
     gamma[lane] = y;
+    part<double>(rec, a.at_decay + kDecayRows * 4)[lane] = y;
     decay[kDecaySince + lane] = since;
     decay[kDecayWrite + lane] = none ? 0.0f : left;
     decay[kDecayBeta + lane] = beta;
     decay[kDecayLeft + lane] = left;
     both[lane] = beta * since;
   }
+  keys.put(x, kLd);
   __syncthreads();
-  a.decay[c * kDecayRows + tid] = decay[tid];
+  part<float>(rec, a.at_decay)[tid] = decay[tid];
   if (w.h % (a.H / a.Hk) == 0) {
-    uint16_t* kt = a.kt + ((long long)(w.b * a.Hk + w.hk) * a.nc + blockIdx.x) * a.dkb * 2 * NI * kFrag;
+    uint16_t* kt = part<uint16_t>(rec, a.at_kt);
     for (int i = wave; i < a.dkb * 2; i += 4) {
       Terms<NI> f;
       terms_across<NI>(x + 32 * (i & 1) * kLd + 16 * (i >> 1), kPlane, kLd, f);
@@ -270,7 +283,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
     }
     __syncthreads();
   }
-  stage_terms<T>(v, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);   // (A is read)
+  stage_terms<T, 256>(v, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);   // (A is read)
   // T's rows 16 wave .. + 15 as an operand with a factor per column; nothing behind column 16 wave + 15
   const int steps = wave < 2 ? 1 : 2;
   auto rows_of_t = [&](const float* by, int ks, Terms<3>& f) {
@@ -286,7 +299,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
   Terms<3> ft[2];
   rows_of_t(both, 0, ft[0]);
   if (steps > 1) rows_of_t(both, 1, ft[1]);
-  uint16_t* mw = a.w + (c * 4 + wave) * KS * 3 * kFrag;
+  uint16_t* mw = part<uint16_t>(rec, 0) + wave * KS * 3 * kFrag;
 #pragma unroll
   for (int cb = 0; cb < 2 * KS; ++cb) {
     f32x4 acc = {0, 0, 0, 0}, act = {0, 0, 0, 0};
@@ -296,10 +309,11 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
       Terms<NI> key;
       terms_across<NI>(x + 32 * ks * kLd + 16 * cb, kPlane, kLd, key);
       acc = mul_terms<3>(key, ft[ks], acc);
-      if (a.wt) act = mul_terms<3>(ft[ks], key, act);
+      if (a.for_backward) act = mul_terms<3>(ft[ks], key, act);
     }
     store_operand<3>(mw + (cb >> 1) * 3 * kFrag, cb & 1, acc);
-    if (a.wt && cb < a.dkb) store_operand<3>(a.wt + ((c * a.dkb + cb) * 2 + (wave >> 1)) * 3 * kFrag, wave & 1, act);
+    if (a.for_backward && cb < a.dkb)
+      store_operand<3>(part<uint16_t>(rec, a.at_wt) + (cb * 2 + (wave >> 1)) * 3 * kFrag, wave & 1, act);
   }
   rows_of_t(decay + kDecayBeta, 0, ft[0]);
   if (steps > 1) rows_of_t(decay + kDecayBeta, 1, ft[1]);
@@ -313,9 +327,9 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
       terms_across<NI>(v + 32 * ks * ldv + 16 * vb, 64 * ldv, ldv, val);
       acc = mul_terms<3>(val, ft[ks], acc);
     }
-    *reinterpret_cast<f32x4*>(a.u + (((c * a.dvb + vb) * 4 + wave) * 64 + lane) * 4) = acc;
+    *reinterpret_cast<f32x4*>(part<float>(rec, a.at_u) + ((vb * 4 + wave) * 64 + lane) * 4) = acc;
   }
-  if (a.tt) {   // (T beta)^T's rows j of this wave: nothing before column i = j
+  if (a.for_backward) {   // (T beta)^T's rows j of this wave: nothing before column i = j, so six operands of the eight, in fp32
     const float by = decay[kDecayBeta + 16 * wave + col];
     for (int ks = wave >> 1; ks < 2; ++ks) {
       float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -325,9 +339,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = p[e * kLdB] * by;
       }
-      Terms<3> f;
-      split8(y, f);
-      store_frag<3>(a.tt + ((c * 4 + wave) * 2 + ks) * 3 * kFrag, f);
+      store8<F32>(rec + a.at_tt + ((wave < 2 ? 2 * wave + ks : 2 + wave) * 64 + lane) * 32, y);
     }
   }
 }
@@ -394,21 +406,21 @@ template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void d
   }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
-  const long long c0 = (long long)bh * a.nc;
-  const long long k0 = (long long)(first.b * a.Hk + first.hk) * a.nc;
-  const long long u_at = ((unit ? 0 : slice) * 4 + wave) * 256 + lane * 4;
+  const int key_head = bh - first.h + first.hk * (a.H / a.Hk);   // whose records have K^T
+  const int u_at = ((unit ? 0 : slice) * 4 + wave) * 256 + lane * 4;
   auto request = [&](In& n, int i) {
     i = i < end ? i : end - 1;
-    const uint16_t* mw = a.w + ((c0 + i) * 4 + wave) * KS * 3 * kFrag;
+    unsigned char* rec = a.rec(bh, i);
+    const uint16_t* mw = part<uint16_t>(rec, 0) + wave * KS * 3 * kFrag;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<3>(mw + ks * 3 * kFrag, n.w[ks]);
-    const uint16_t* kt = a.kt + (k0 + i) * a.dkb * 2 * NI * kFrag;
+    const uint16_t* kt = part<uint16_t>(a.rec(key_head, i), a.at_kt);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) load_frag<NI>(kt + (blk[t] * 2 + ks) * NI * kFrag, n.kt[t][ks]);
-    n.u0 = *reinterpret_cast<const f32x4*>(a.u + (c0 + i) * a.dvb * 1024 + u_at);
-    const float* decay = a.decay + (c0 + i) * kDecayRows;
+    n.u0 = *reinterpret_cast<const f32x4*>(part<float>(rec, a.at_u) + u_at);
+    const float* decay = part<float>(rec, a.at_decay);
     n.write = decay[kDecayWrite + 16 * wave + col];
     n.whole = decay[kDecaySince + 63];
   };
@@ -416,12 +428,11 @@ template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void d
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
   };
-  auto state_at = [&](int i) { return a.s + (((long long)bh * (a.nc + 1) + i) * a.dvb + slice) * a.dkb * 256; };
   auto chunk = [&](In& in, In& next, int i) {
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
     request(next, i + In::kDepth - 1);
-    if constexpr (!PARTIAL) keep(state_at(i));
+    if constexpr (!PARTIAL) keep(part<float>(a.rec(bh, i), a.at_s) + slice * a.dkb * 256);
     lds_barrier();
     f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
 #pragma unroll
@@ -434,7 +445,7 @@ template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void d
     f32x4 u0 = in.u0;
     if (unit) u0 = f32x4{0, 0, 0, 0};
     const f32x4 u = u0 - (acc + acc2);
-    if constexpr (!PARTIAL) *reinterpret_cast<f32x4*>(a.u + (c0 + i) * a.dvb * 1024 + u_at) = u;
+    if constexpr (!PARTIAL) *reinterpret_cast<f32x4*>(part<float>(a.rec(bh, i), a.at_u) + u_at) = u;
     split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, u * in.write);
     lds_barrier();
     Terms<3> fu[2];
@@ -473,7 +484,6 @@ template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void d
   if constexpr (PARTIAL) {
     keep(a.parts + (((long long)bh * a.runs + run) * (a.dvb + a.dkb) + slice) * a.dkb * 256);
   } else if (end == all) {
-    keep(state_at(all));
     if (a.state_out) {
 #pragma unroll
       for (int t = 0; t < kBlocks; ++t)
@@ -548,18 +558,21 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
   uint16_t* up = sp + kOutBlocks * NO * kSPlane;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
-  const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
-  stage_terms<T>(q, kLd, a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk, KS);
-  stage_terms<T>(k, kLd, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, KS);
-  if (wave == 0) gamma[lane] = chunk_gamma(a, w);
-  if (tid < 64) decay[tid] = a.decay[c * kDecayRows + kDecaySince + tid];
-  else if (tid < 128) decay[tid] = a.decay[c * kDecayRows + kDecayBeta + tid - 64];
+  unsigned char* rec = a.rec(w.bh, blockIdx.x);
+  Rows<T, KS, 256> queries, keys;
+  queries.request(a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk);
+  keys.request(a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk);
+  if (wave == 0) {
+    gamma[lane] = part<double>(rec, a.at_decay + kDecayRows * 4)[lane];
+    decay[lane] = part<float>(rec, a.at_decay)[kDecaySince + lane];
+    decay[64 + lane] = part<float>(rec, a.at_decay)[kDecayBeta + lane];
+  }
   // the first blocks of U and of the state, requested now, put down when there is room
   f32x4 s_in[KB], u_in[kOutBlocks];
   int vb0 = 0, blocks = a.dvb < kOutBlocks ? a.dvb : kOutBlocks;
   auto request = [&]() {   // wave w: block w of the state (all of its rows), 16 tokens of every block of U
-    const float* s0 = a.s + (((long long)blockIdx.y * (a.nc + 1) + blockIdx.x) * a.dvb + vb0) * a.dkb * 256;
-    const float* mu = a.u + (c * a.dvb + vb0) * 1024;
+    const float* s0 = part<float>(rec, a.at_s) + vb0 * a.dkb * 256;
+    const float* mu = part<float>(rec, a.at_u) + vb0 * 1024;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
       if (wave < blocks && kb < a.dkb) s_in[kb] = *reinterpret_cast<const f32x4*>(s0 + (wave * a.dkb + kb) * 256 + lane * 4);
@@ -568,6 +581,8 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
       if (i < blocks) u_in[i] = *reinterpret_cast<const f32x4*>(mu + (i * 4 + wave) * 256 + lane * 4);
   };
   request();
+  queries.put(q, kLd);
+  keys.put(k, kLd);
   __syncthreads();
   Terms<NI> fq[KS];
 #pragma unroll

@@ -12,9 +12,10 @@
 // and the values by its inverse.  Only dU and dS0 depend on the chunk behind: P^T dO and (e^gamma Q)^T dO are formed for all
 // chunks at once (delta_back_prepare), a scan runs from the last chunk to the first (delta_back_scan), and the rest follows
 // for all chunks at once (delta_gradients), where the value heads that share a query and key head are summed in their order.
-//     kn   K as operand: [4 token blocks][d_k / 32][terms][64][8], once per query and key head
-//     du   P^T dO, then dU, as u;   ds   as s, two places more per head: (e^gamma Q)^T dO of chunk c at c, dS1 two places on,
-//          which every wave of the scan has behind it when dS1 is written
+// The backward pass has records of its own, two more than chunks per head:
+//     du   P^T dO, then dU, as u
+//     kn   K as operand: [4 token blocks][d_k / 32][terms][64][8], in the record of the first value head that has the key head
+//     ds   as s: (e^gamma Q)^T dO of chunk c in record c, dS1 two records on, which every wave of the scan has behind it by then
 #pragma once
 #include "lf_delta.hpp"
 
@@ -27,28 +28,35 @@ template <typename T> inline int delta_back_prepare_lds(int dks, int dvs) {
   return 64 * 8 + 64 * 4 + 3 * 64 * kLdP * 2 + (2 * keys > out ? 2 * keys : out);
 }
 
-template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(DeltaArgs a) {
+template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_prepare(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int NI = TermsOf<T>::kStored;
+  constexpr int NI = TermsOf<T>::kStored, ld = 32 * KS + 8, plane = 64 * ld, kOwn = (2 * KS + 3) / 4;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int dvs = (a.dvb + 1) / 2, ld = plane_ld(a.dks), ldo = plane_ld(dvs), plane = 64 * ld;
+  const int dvs = (a.dvb + 1) / 2, ldo = plane_ld(dvs);
   double* gamma = reinterpret_cast<double*>(smem);
   float* since = reinterpret_cast<float*>(gamma + 64);
   uint16_t* pp = reinterpret_cast<uint16_t*>(since + 64);
   uint16_t* q = pp + 3 * 64 * kLdP;
   uint16_t* k = q + NI * plane;
   uint16_t* o = q;                      // where q and k were
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
-  const long long c = (long long)blockIdx.y * a.nc + blockIdx.x;
-  if (wave == 0) gamma[lane] = chunk_gamma(a, w);
-  if (tid < 64) since[tid] = a.decay[c * kDecayRows + kDecaySince + tid];
-  stage_terms<T>(q, ld, a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk, a.dks);
-  stage_terms<T>(k, ld, a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk, a.dks);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
+  const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  unsigned char *rec = a.rec(w.bh, blockIdx.x), *rec_b = a.rec_b(w.bh, blockIdx.x);
+  Rows<T, KS, 256> queries, keys;
+  queries.request(a.q, w.b * a.vq.b + w.hk * a.vq.h + w.n0 * a.vq.n, a.vq.n, w.valid, a.dk);
+  keys.request(a.k, w.b * a.vk.b + w.hk * a.vk.h + w.n0 * a.vk.n, a.vk.n, w.valid, a.dk);
+  if (wave == 0) {
+    gamma[lane] = part<double>(rec, a.at_decay + kDecayRows * 4)[lane];
+    since[lane] = part<float>(rec, a.at_decay)[kDecaySince + lane];
+  }
+  queries.put(q, ld);
+  keys.put(k, ld);
   __syncthreads();
   if (w.h % (a.H / a.Hk) == 0) {
-    uint16_t* kn = a.kn + (((long long)(w.b * a.Hk + w.hk) * a.nc + blockIdx.x) * 4 + wave) * a.dks * NI * kFrag;
-    for (int ks = 0; ks < a.dks; ++ks) {
+    uint16_t* kn = part<uint16_t>(rec_b, a.at_kn) + wave * KS * NI * kFrag;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
       Terms<NI> f;
       terms_near<NI>(k + (16 * wave + col) * ld + 32 * ks + g8, plane, f);
       store_frag<NI>(kn + ks * NI * kFrag, f);
@@ -58,7 +66,8 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
   for (int it = 0; it < 4; ++it) {
     f32x4 acc = {0, 0, 0, 0};
     if (it >= wave) {
-      for (int ks = 0; ks < a.dks; ++ks) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
         Terms<NI> fq, fk;
         terms_near<NI>(q + (16 * it + col) * ld + 32 * ks + g8, plane, fq);
         terms_near<NI>(k + (16 * wave + col) * ld + 32 * ks + g8, plane, fk);
@@ -74,9 +83,9 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
   }
   // (e^gamma Q)^T as operands of this wave's channel blocks, before the queries make room: scaled, then split again
   __syncthreads();
-  Terms<3> fq[3][2];   // channel blocks wave, wave + 4, wave + 8
+  Terms<3> fq[kOwn][2];   // channel blocks wave, wave + 4, ...
 #pragma unroll
-  for (int t = 0; t < 3; ++t)
+  for (int t = 0; t < kOwn; ++t)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       if (wave + 4 * t >= a.dkb) continue;
@@ -100,7 +109,7 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
       split8(y, fq[t][ks]);
     }
   __syncthreads();
-  stage_terms<T>(o, ldo, a.dout, w.b * a.vdo.b + w.h * a.vdo.h + w.n0 * a.vdo.n, a.vdo.n, w.valid, a.dv, dvs);
+  stage_terms<T, 256>(o, ldo, a.dout, w.b * a.vdo.b + w.h * a.vdo.h + w.n0 * a.vdo.n, a.vdo.n, w.valid, a.dv, dvs);
   Terms<3> fp[2];      // P^T's rows j of this wave
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) terms_near<3>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
@@ -112,14 +121,14 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
     f32x4 acc = {0, 0, 0, 0};   // rows: value channels, columns: tokens j
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) acc = mul_terms<3>(fo[ks], fp[ks], acc);
-    *reinterpret_cast<f32x4*>(a.du + (((c * a.dvb + vb) * 4 + wave) * 64 + lane) * 4) = acc * a.scale;
+    *reinterpret_cast<f32x4*>(part<float>(rec_b, 0) + ((vb * 4 + wave) * 64 + lane) * 4) = acc * a.scale;
 #pragma unroll
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < kOwn; ++t) {
       if (wave + 4 * t >= a.dkb) continue;
       f32x4 z = {0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) z = mul_terms<3>(fq[t][ks], fo[ks], z);
-      *reinterpret_cast<f32x4*>(a.ds + (((c + 2 * w.bh) * a.dvb + vb) * a.dkb + wave + 4 * t) * 256 + lane * 4) = z;
+      *reinterpret_cast<f32x4*>(part<float>(rec_b, a.at_ds) + (vb * a.dkb + wave + 4 * t) * 256 + lane * 4) = z;
     }
   }
 }
@@ -127,6 +136,7 @@ template <typename T> __global__ __launch_bounds__(256) void delta_back_prepare(
 // ---- the scan backwards ----------------------------------------------------------------------------------------------------------
 template <int NI, int KS> struct BackScanIn {
   static constexpr int kBlocks = (2 * KS + 3) / 4;
+  static constexpr int kDepth = 4 * NI * KS + 28 * kBlocks <= 110 ? 3 : 2;   // (as ScanIn's)
   Terms<NI> kn[KS];
   Terms<3> wt[kBlocks][2];
   f32x4 du, z[kBlocks];
@@ -139,7 +149,9 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
   __shared__ __align__(16) uint16_t up[3 * 64 * kLdU];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
-  const int slice = blockIdx.x, bh = blockIdx.y, ch = slice * 16 + col;
+  int slice, bh;
+  slice_of_head(blockIdx.x, a.dvb, a.heads, slice, bh);
+  const int ch = slice * 16 + col;
   const DeltaAt first(a, bh, 0);
   const int chunks = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
   int blk[kBlocks];   // (as in delta_scan)
@@ -155,22 +167,24 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
     }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
-  const long long c0 = (long long)bh * a.nc;
-  const long long k0 = (long long)(first.b * a.Hk + first.hk) * a.nc;
+  const int key_head = bh - first.h + first.hk * (a.H / a.Hk);
+  const int u_at = (slice * 4 + wave) * 256 + lane * 4;
   auto request = [&](BackScanIn<NI, KS>& n, int i) {
-    const uint16_t* kn = a.kn + ((k0 + i) * 4 + wave) * a.dks * NI * kFrag;
+    i = i < 0 ? 0 : i;
+    unsigned char *rec = a.rec(bh, i), *rec_b = a.rec_b(bh, i);
+    const uint16_t* kn = part<uint16_t>(a.rec_b(key_head, i), a.at_kn) + wave * KS * NI * kFrag;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<NI>(kn + ks * NI * kFrag, n.kn[ks]);
-    const uint16_t* wt = a.wt + (c0 + i) * a.dkb * 2 * 3 * kFrag;
-    const float* z = a.ds + ((c0 + 2 * bh + i) * a.dvb + slice) * a.dkb * 256;
+    const uint16_t* wt = part<uint16_t>(rec, a.at_wt);
+    const float* z = part<float>(rec_b, a.at_ds) + slice * a.dkb * 256;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
       n.z[t] = *reinterpret_cast<const f32x4*>(z + blk[t] * 256 + lane * 4);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) load_frag<3>(wt + (blk[t] * 2 + ks) * 3 * kFrag, n.wt[t][ks]);
     }
-    n.du = *reinterpret_cast<const f32x4*>(a.du + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4);
-    const float* decay = a.decay + (c0 + i) * kDecayRows;
+    n.du = *reinterpret_cast<const f32x4*>(part<float>(rec_b, 0) + u_at);
+    const float* decay = part<float>(rec, a.at_decay);
     n.left = decay[kDecayLeft + 16 * wave + col];
     n.whole = decay[kDecaySince + 63];
   };
@@ -178,8 +192,8 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
       split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
-    request(next, i > 0 ? i - 1 : 0);
-    float* to = a.ds + ((c0 + 2 * bh + i + 2) * a.dvb + slice) * a.dkb * 256;
+    request(next, i + 1 - BackScanIn<NI, KS>::kDepth);
+    float* to = part<float>(a.rec_b(bh, i + 2), a.at_ds) + slice * a.dkb * 256;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
       *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
@@ -193,7 +207,7 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
       else acc = mul_terms<3>(fs, in.kn[ks], acc);
     }
     const f32x4 u = in.du + (acc + acc2) * in.left;
-    *reinterpret_cast<f32x4*>(a.du + ((((c0 + i) * a.dvb + slice) * 4 + wave) * 64 + lane) * 4) = u;
+    *reinterpret_cast<f32x4*>(part<float>(a.rec_b(bh, i), 0) + u_at) = u;
     split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, -u);
     lds_barrier();
     Terms<3> fu[2];
@@ -206,14 +220,28 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
       s[t] = mul_terms<3>(in.wt[t][1], fu[1], s[t]);
     }
   };
-  BackScanIn<NI, KS> x, y;
-  int i = chunks - 1;
-  if (chunks > 0) request(x, i);
-  for (; i > 0; i -= 2) {
-    chunk(x, y, i);
-    chunk(y, x, i - 1);
+  if (chunks > 0) {
+    BackScanIn<NI, KS> x, y;
+    int i = chunks - 1;
+    request(x, i);
+    if constexpr (BackScanIn<NI, KS>::kDepth == 3) {
+      BackScanIn<NI, KS> z;
+      request(y, i - 1);
+      for (; i > 1; i -= 3) {
+        chunk(x, z, i);
+        chunk(y, x, i - 1);
+        chunk(z, y, i - 2);
+      }
+      if (i >= 0) chunk(x, z, i);
+      if (i >= 1) chunk(y, x, i - 1);
+    } else {
+      for (; i > 0; i -= 2) {
+        chunk(x, y, i);
+        chunk(y, x, i - 1);
+      }
+      if (i == 0) chunk(x, y, 0);
+    }
   }
-  if (i == 0) chunk(x, y, 0);
   if (a.dstate_in) {
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
@@ -226,260 +254,297 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
 }
 
 // ---- the gradients ------------------------------------------------------------------------------------------------------------
-// Formed transposed (rows: channels, columns: tokens), a wave per 16 tokens.  32 value channels at a time pass through LDS:
-// dU (then dV in its place), dO, U as [token][channel], S0 and dS1 as [channel][key channel].
+// Formed transposed (rows: channels, columns: tokens).  Eight waves: wave w takes tokens 16 (w % 4) .. + 15 and one half of the
+// channels.  32 value channels at a time pass through LDS: dU (then dV in its place), dO, U as [token][channel], S0 and dS1 as
+// [channel][key channel]; what comes next is requested a round ahead, keys and queries at the start.
 constexpr int kLdV = 40;
 
 template <typename T> inline int delta_gradients_lds(int dks) {
   constexpr int NI = TermsOf<T>::kStored;
-  const int first = 3 * 3 * 64 * kLdV * 2 + 2 * 3 * plane_bytes(32, dks);
+  const int first = (3 + NI + 3) * 64 * kLdV * 2 + 2 * 3 * plane_bytes(32, dks);
   const int second = 2 * 3 * 64 * kLdP * 2 + NI * plane_bytes(64, dks);
-  return (first > second ? first : second) + 64 * 8 + kDecayRows * 4 + 16;
+  return (first > second ? first : second) + 64 * 8 + kDecayRows * 4 + 8 * 4 + 2 * 64 * 8 + 2 * 64 * 4;
 }
 
 // sum over the four lanes of a wave that share l % 16
-LF_DEV float groups_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
+LF_DEV float groups_sum(float v) { return swap_add<32>(swap_add<16>(v)); }
 
-template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(256) void delta_gradients(DeltaArgs a) {
+template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) void delta_gradients(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int NI = TermsOf<T>::kStored, KB = 2 * KS, kLd = 32 * KS + 8, kVPlane = 64 * kLdV, kSPlane = 32 * kLd;
+  constexpr int NI = TermsOf<T>::kStored, kLd = 32 * KS + 8, kVPlane = 64 * kLdV, kSPlane = 32 * kLd, kPPlane = 64 * kLdP;
+  constexpr int kOwn = (2 * KS + 3) / 4;
   const int b = (unsigned)blockIdx.y / (unsigned)a.Hk, hk = blockIdx.y - b * a.Hk, group = SHARED ? a.H / a.Hk : 1;
   double* gamma = reinterpret_cast<double*>(smem);
-  float* decay = reinterpret_cast<float*>(gamma + 64);
-  float* inner = decay + kDecayRows;
-  uint16_t* pv = reinterpret_cast<uint16_t*>(inner + 4);   // dU, then dV
-  uint16_t* po = pv + 3 * kVPlane;
-  uint16_t* pu = po + 3 * kVPlane;
-  uint16_t* ps = pu + 3 * kVPlane;
+  double* dg64 = gamma + 64;                               // [2][64]
+  float* decay = reinterpret_cast<float*>(dg64 + 128);
+  float* db32 = decay + kDecayRows;                        // [2][64]
+  float* inner = db32 + 128;                               // [8]
+  uint16_t* pv = reinterpret_cast<uint16_t*>(inner + 8);   // dU, then dV
+  uint16_t* pu = pv + 3 * kVPlane;
+  uint16_t* po = pu + 3 * kVPlane;
+  uint16_t* ps = po + NI * kVPlane;
   uint16_t* pd = ps + 3 * kSPlane;
   uint16_t* pm = pv;                                       // later: dO U^T * D, M, and the keys, then the queries
-  uint16_t* pn = pm + 3 * 64 * kLdP;
-  uint16_t* x = pn + 3 * 64 * kLdP;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
+  uint16_t* pn = pm + 3 * kPPlane;
+  uint16_t* x = pn + 3 * kPPlane;
+  const int tid = threadIdx.x, wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 & 3, half = wave8 >> 2;
+  const int lane = tid & 63, col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   const int n = 16 * wave + col;                           // this lane's token
   const DeltaAt any(a, b * a.H + hk * group, blockIdx.x);
   if (any.valid == 0) return;
   const bool on = n < any.valid;
-  f32x4 sum_q[SHARED ? KB : 1], sum_k[SHARED ? KB : 1];
+  Rows<T, KS, 512> keys, queries;
+  auto channels_of = [&](const uint16_t* rows, int ch) {   // four channels of this lane's token, from their terms
+    f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = NI - 1; k >= 0; --k) {
+      const u32x2 e = *reinterpret_cast<const u32x2*>(rows + k * 64 * kLd + n * kLd + ch);
+      float e0, e1, e2, e3;
+      unpack2<BF16>(e[0], e0, e1);
+      unpack2<BF16>(e[1], e2, e3);
+      y += f32x4{e0, e1, e2, e3};
+    }
+    return y;
+  };
+  f32x4 sum_q[SHARED ? KS : 1], sum_k[SHARED ? KS : 1];
   if constexpr (SHARED) {
 #pragma unroll
-    for (int i = 0; i < KB; ++i) sum_q[i] = sum_k[i] = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < KS; ++i) sum_q[i] = sum_k[i] = f32x4{0, 0, 0, 0};
   }
   for (int member = 0; member < group; ++member) {
     const DeltaAt w(a, b * a.H + hk * group + member, blockIdx.x);
-    const long long c = (long long)w.bh * a.nc + blockIdx.x;
-    __syncthreads();
-    if (wave == 0) gamma[lane] = chunk_gamma(a, w);
-    decay[tid] = a.decay[c * kDecayRows + tid];
-    f32x4 dq[KB], dk[KB], dw[KB], mo[4], mv[4];
-#pragma unroll
-    for (int i = 0; i < KB; ++i) dq[i] = dk[i] = dw[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mo[i] = mv[i] = f32x4{0, 0, 0, 0};
-    Terms<3> ft[2];   // (T beta)^T's rows of this wave: nothing before them
+    unsigned char *rec = a.rec(w.bh, blockIdx.x), *rec_b = a.rec_b(w.bh, blockIdx.x);
+    const float* ds = part<float>(a.rec_b(w.bh, blockIdx.x + 2), a.at_ds);
+    // requested in the order in which they are waited for: (T beta)^T's rows of this wave (nothing before them), decays, ...
+    Raw8<F32> tt[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
-      if (2 * ks + 1 >= wave) load_frag<3>(a.tt + ((c * 4 + wave) * 2 + ks) * 3 * kFrag, ft[ks]);
-    float dbeta = 0.0f, ss = 0.0f;
-    double vdv = 0.0;
-    for (int i = tid; i < 2 * 3 * kSPlane / 8; i += 256) reinterpret_cast<u32x4*>(ps)[i] = u32x4{0, 0, 0, 0};
-    for (int vb = 0; vb < a.dvb; vb += 2) {
-      __syncthreads();   // the planes of the channels before are read; the zeros are there
-      f32x4 u[2];
+      if (2 * ks + 1 >= wave) tt[ks] = load8_raw<F32>(rec + a.at_tt + ((wave < 2 ? 2 * wave + ks : 2 + wave) * 64 + lane) * 32);
+    double gamma_in = 0.0;
+    float decay_in = 0.0f;
+    if (tid < kDecayRows) decay_in = part<float>(rec, a.at_decay)[tid];
+    else if (wave8 == 4) gamma_in = part<double>(rec, a.at_decay + kDecayRows * 4)[lane];
+    // ... 16 value channels of this wave's tokens, and row blocks wave, wave + 4, ... of S0 and dS1: block vb + half
+    f32x4 du, u, o, v, s0[kOwn], d1[kOwn];
+    auto request = [&](int vb) {
+      const f32x4 none = {0, 0, 0, 0};
+      const int ch = 16 * vb + row4;
+      du = u = o = v = none;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int ch = 16 * (vb + e) + row4;
-        f32x4 du = {0, 0, 0, 0}, o = {0, 0, 0, 0};
-        u[e] = f32x4{0, 0, 0, 0};
-        if (vb + e < a.dvb) {
-          const long long at4 = (((c * a.dvb + vb + e) * 4 + wave) * 64 + lane) * 4;
-          du = *reinterpret_cast<const f32x4*>(a.du + at4);
-          u[e] = *reinterpret_cast<const f32x4*>(a.u + at4);
-          if (on && ch < a.dv) o = load4<T>(at<T>(a.dout, w.b * a.vdo.b + w.h * a.vdo.h + (w.n0 + n) * a.vdo.n + ch)) * a.scale;
-        }
-        const bool none = decay[kDecayBeta + n] == kDeltaTinyBeta;
-        split4_lds<3>(pv + n * kLdV + 16 * e + row4, kVPlane, du);
-        split4_lds<3>(po + n * kLdV + 16 * e + row4, kVPlane, o);
-        split4_lds<3>(pu + n * kLdV + 16 * e + row4, kVPlane, none ? f32x4{0, 0, 0, 0} : u[e]);
-        if (vb + e < a.dvb) {
-          const float* s0 = a.s + (((long long)w.bh * (a.nc + 1) + blockIdx.x) * a.dvb + vb + e) * a.dkb * 256 + lane * 4;
-          const float* s1 = s0 + (long long)a.dvb * a.dkb * 256;
-          const float* ds = a.ds + ((c + 2 * w.bh + 2) * a.dvb + vb + e) * a.dkb * 256 + lane * 4;
-          for (int kb = wave; kb < a.dkb; kb += 4) {
-            const f32x4 d1 = *reinterpret_cast<const f32x4*>(ds + kb * 256), t1 = *reinterpret_cast<const f32x4*>(s1 + kb * 256);
-            split4_lds<3>(ps + (16 * e + col) * kLd + 16 * kb + row4, kSPlane, *reinterpret_cast<const f32x4*>(s0 + kb * 256));
-            split4_lds<3>(pd + (16 * e + col) * kLd + 16 * kb + row4, kSPlane, d1);
-            ss += (d1[0] * t1[0] + d1[1] * t1[1]) + (d1[2] * t1[2] + d1[3] * t1[3]);
-          }
-        } else {   // an odd last block: zeros where the one before it was
-          for (int kb = wave; kb < a.dkb; kb += 4) {
-            split4_lds<3>(ps + (16 * e + col) * kLd + 16 * kb + row4, kSPlane, f32x4{0, 0, 0, 0});
-            split4_lds<3>(pd + (16 * e + col) * kLd + 16 * kb + row4, kSPlane, f32x4{0, 0, 0, 0});
-          }
-        }
-      }
-      __syncthreads();
-      f32x4 dv[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          if (2 * ks + 1 < wave) continue;
-          Terms<3> f;
-          terms_across<3>(pv + 32 * ks * kLdV + 16 * e, kVPlane, kLdV, f);
-          acc = mul_terms<3>(f, ft[ks], acc);
-        }
-        const int ch = 16 * (vb + e) + row4;
-        const float beta = decay[kDecayBeta + n];
-        const f32x4 per = acc * (1.0f / beta) * (u[e] * (1.0f / beta));
-        dbeta += (per[0] + per[1]) + (per[2] + per[3]);
-        dv[e] = beta == kDeltaTinyBeta ? f32x4{0, 0, 0, 0} : acc;
-        if (on && ch < a.dv) {
-          const f32x4 v = load4<T>(at<T>(a.v, w.b * a.vv.b + w.h * a.vv.h + (w.n0 + n) * a.vv.n + ch));
-          vdv += (double)(v[0] * dv[e][0] + v[1] * dv[e][1]) + (double)(v[2] * dv[e][2] + v[3] * dv[e][3]);
-          store4<T>(at<T>(a.dv_out, w.b * a.vdv.b + w.h * a.vdv.h + (w.n0 + n) * a.vdv.n + ch), dv[e]);
-        }
-      }
-      __syncthreads();   // dU is read
-#pragma unroll
-      for (int e = 0; e < 2; ++e) split4_lds<3>(pv + n * kLdV + 16 * e + row4, kVPlane, dv[e]);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (its own rows are all a wave reads of dV)
-      Terms<3> fo, fv, fu;
-      terms_near<3>(po + n * kLdV + g8, kVPlane, fo);
-      terms_near<3>(pv + n * kLdV + g8, kVPlane, fv);
-      terms_near<3>(pu + n * kLdV + g8, kVPlane, fu);
-#pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        if (jt > wave) continue;
-        Terms<3> fj;
-        terms_near<3>(pu + (16 * jt + col) * kLdV + g8, kVPlane, fj);
-        mo[jt] = mul_terms<3>(fj, fo, mo[jt]);
-        mv[jt] = mul_terms<3>(fj, fv, mv[jt]);
+      for (int t = 0; t < kOwn; ++t) s0[t] = d1[t] = none;
+      if (vb >= a.dvb) return;
+      const int at4 = ((vb * 4 + wave) * 64 + lane) * 4;
+      du = *reinterpret_cast<const f32x4*>(part<float>(rec_b, 0) + at4);
+      u = *reinterpret_cast<const f32x4*>(part<float>(rec, a.at_u) + at4);
+      if (on && ch < a.dv) {
+        o = load4<T>(at<T>(a.dout, w.b * a.vdo.b + w.h * a.vdo.h + (w.n0 + n) * a.vdo.n + ch));
+        v = load4<T>(at<T>(a.v, w.b * a.vv.b + w.h * a.vv.h + (w.n0 + n) * a.vv.n + ch));
       }
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
+      for (int t = 0; t < kOwn; ++t) {
+        const int kb = wave + 4 * t;
         if (kb >= a.dkb) continue;
-        Terms<3> f0, f1;
-        terms_across<3>(ps + 16 * kb, kSPlane, kLd, f0);
-        terms_across<3>(pd + 16 * kb, kSPlane, kLd, f1);
-        dq[kb] = mul_terms<3>(f0, fo, dq[kb]);
-        dk[kb] = mul_terms<3>(f0, fv, dk[kb]);
-        dw[kb] = mul_terms<3>(f1, fu, dw[kb]);
+        s0[t] = *reinterpret_cast<const f32x4*>(part<float>(rec, a.at_s) + (vb * a.dkb + kb) * 256 + lane * 4);
+        d1[t] = *reinterpret_cast<const f32x4*>(ds + (vb * a.dkb + kb) * 256 + lane * 4);
       }
+    };
+    request(half);
+    // and keys and queries at the end
+    if (member == 0) {
+      keys.request(a.k, b * a.vk.b + hk * a.vk.h + any.n0 * a.vk.n, a.vk.n, any.valid, a.dk);
+      queries.request(a.q, b * a.vq.b + hk * a.vq.h + any.n0 * a.vq.n, a.vq.n, any.valid, a.dk);
     }
-    __syncthreads();
-    const float since = decay[kDecaySince + n], write = decay[kDecayWrite + n];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      dq[kb] *= since;
-      dk[kb] = dw[kb] * write - dk[kb] * since;
-    }
-#pragma unroll
-    for (int jt = 0; jt < 4; ++jt) {
-      f32x4 e = mo[jt], m = mv[jt];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = 16 * jt + row4 + r;
-        const float d = j <= n ? decay_between(gamma, n, j) : 0.0f;
-        e[r] = j <= n ? e[r] * d : 0.0f;
-        m[r] = j < n ? -m[r] * d : 0.0f;
-      }
-      split4_lds<3>(pm + n * kLdP + 16 * jt + row4, 64 * kLdP, e);
-      split4_lds<3>(pn + n * kLdP + 16 * jt + row4, 64 * kLdP, m);
-    }
-    stage_terms<T>(x, kLd, a.k, b * a.vk.b + hk * a.vk.h + any.n0 * a.vk.n, a.vk.n, any.valid, a.dk, KS);
-    ss = lanes_sum<64>(ss);
-    if (lane == 0) inner[wave] = ss;
-    dbeta = groups_sum(dbeta);
-    __syncthreads();
-    Terms<3> fe[2], fm[2], em[2];
+    Terms<3> ft[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      terms_near<3>(pm + n * kLdP + 32 * ks + g8, 64 * kLdP, fe[ks]);
-      terms_near<3>(pn + n * kLdP + 32 * ks + g8, 64 * kLdP, fm[ks]);
-      terms_across<3>(pn + 32 * ks * kLdP + 16 * wave, 64 * kLdP, kLdP, em[ks]);
+      if (2 * ks + 1 < wave) continue;
+      float y[8];
+      widen8<F32>(tt[ks], y);
+      split8(y, ft[ks]);
     }
+    __syncthreads();   // (the member before has been read)
+    if (tid < kDecayRows) decay[tid] = decay_in;
+    else if (wave8 == 4) gamma[lane] = gamma_in;
+    f32x4 dq[KS], dk[KS], dw[KS], mx[4];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      if (kb >= a.dkb) continue;
+    for (int i = 0; i < KS; ++i) dq[i] = dk[i] = dw[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        Terms<NI> f;
-        terms_across<NI>(x + 32 * ks * kLd + 16 * kb, 64 * kLd, kLd, f);
-        if (2 * ks <= wave) {
-          dq[kb] = mul_terms<3>(f, fe[ks], dq[kb]);
-          dk[kb] = mul_terms<3>(f, fm[ks], dk[kb]);
-        }
-        if (2 * ks + 1 >= wave) dk[kb] = mul_terms<3>(f, em[ks], dk[kb]);
+    for (int i = 0; i < 4; ++i) mx[i] = f32x4{0, 0, 0, 0};
+    float dbeta = 0.0f, ss = 0.0f;
+    double vdv = 0.0;
+    __syncthreads();
+    const float beta = decay[kDecayBeta + n], per_beta = 1.0f / beta;
+    const bool none = beta == kDeltaTinyBeta;
+    for (int vb = 0; vb < a.dvb; vb += 2) {
+      const int ch = 16 * (vb + half) + row4;
+      split4_lds<3>(pv + n * kLdV + 16 * half + row4, kVPlane, du);
+      split4_lds<3>(pu + n * kLdV + 16 * half + row4, kVPlane, none ? f32x4{0, 0, 0, 0} : u);
+      split4_lds<NI>(po + n * kLdV + 16 * half + row4, kVPlane, o);
+#pragma unroll
+      for (int t = 0; t < kOwn; ++t) {
+        const int kb = wave + 4 * t;
+        if (kb >= 2 * KS) continue;   // (zeros behind d_k too)
+        split4_lds<3>(ps + (16 * half + col) * kLd + 16 * kb + row4, kSPlane, s0[t]);
+        split4_lds<3>(pd + (16 * half + col) * kLd + 16 * kb + row4, kSPlane, d1[t]);
+        ss += (d1[t][0] * s0[t][0] + d1[t][1] * s0[t][1]) + (d1[t][2] * s0[t][2] + d1[t][3] * s0[t][3]);
       }
-    }
-    __syncthreads();
-    stage_terms<T>(x, kLd, a.q, b * a.vq.b + hk * a.vq.h + any.n0 * a.vq.n, a.vq.n, any.valid, a.dk, KS);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) terms_across<3>(pm + 32 * ks * kLdP + 16 * wave, 64 * kLdP, kLdP, fe[ks]);
-    __syncthreads();
-    double qdq = 0.0;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      if (kb >= a.dkb) continue;
+      const f32x4 u_now = u, v_now = v;
+      if (vb + 2 < a.dvb) request(vb + 2 + half);
+      lds_barrier();
+      f32x4 dv = {0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         if (2 * ks + 1 < wave) continue;
+        Terms<3> f;
+        terms_across<3>(pv + 32 * ks * kLdV + 16 * half, kVPlane, kLdV, f);
+        dv = mul_terms<3>(f, ft[ks], dv);
+      }
+      const f32x4 per = (dv * per_beta) * (u_now * per_beta);
+      dbeta += (per[0] + per[1]) + (per[2] + per[3]);
+      if (none) dv = f32x4{0, 0, 0, 0};
+      if (on && ch < a.dv) {
+        vdv += (double)(v_now[0] * dv[0] + v_now[1] * dv[1]) + (double)(v_now[2] * dv[2] + v_now[3] * dv[3]);
+        store4<T>(at<T>(a.dv_out, w.b * a.vdv.b + w.h * a.vdv.h + (w.n0 + n) * a.vdv.n + ch), dv);
+      }
+      lds_barrier();   // dU is read
+      split4_lds<3>(pv + n * kLdV + 16 * half + row4, kVPlane, dv);
+      lds_barrier();
+      Terms<3> fv, fu;
+      Terms<NI> fo;
+      terms_near<3>(pv + n * kLdV + g8, kVPlane, fv);
+      terms_near<3>(pu + n * kLdV + g8, kVPlane, fu);
+      terms_near<NI>(po + n * kLdV + g8, kVPlane, fo);
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        if (jt > wave) continue;
+        __builtin_amdgcn_sched_barrier(0);   // (one operand at a time: two workgroups per CU have 128 registers a lane)
+        Terms<3> fj;
+        terms_near<3>(pu + (16 * jt + col) * kLdV + g8, kVPlane, fj);
+        if (half == 0) mx[jt] = mul_terms<3>(fj, fo, mx[jt]);
+        else mx[jt] = mul_terms<3>(fj, fv, mx[jt]);
+      }
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int kb = 2 * i + half;
+        __builtin_amdgcn_sched_barrier(0);
+        Terms<3> f;
+        terms_across<3>(ps + 16 * kb, kSPlane, kLd, f);
+        dq[i] = mul_terms<3>(f, fo, dq[i]);
+        dk[i] = mul_terms<3>(f, fv, dk[i]);
+        terms_across<3>(pd + 16 * kb, kSPlane, kLd, f);
+        dw[i] = mul_terms<3>(f, fu, dw[i]);
+      }
+      lds_barrier();   // the planes are read
+    }
+    const float since = decay[kDecaySince + n], write = decay[kDecayWrite + n];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      dq[i] *= since * a.scale;
+      dw[i] *= write;
+      dk[i] = dw[i] - dk[i] * since;
+    }
+    // half 0: scale dO U^T * D;  half 1: M
+    uint16_t* mine = half ? pn : pm;
+    const float factor = half ? -1.0f : a.scale;
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 e = mx[jt];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = 16 * jt + row4 + r;
+        e[r] = j + half <= n ? e[r] * factor * decay_between(gamma, n, j) : 0.0f;
+      }
+      split4_lds<3>(mine + n * kLdP + 16 * jt + row4, kPPlane, e);
+    }
+    keys.put(x, kLd);
+    dbeta = groups_sum(dbeta);
+    if (lane < 16) db32[half * 64 + n] = dbeta;
+    lds_barrier();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      __builtin_amdgcn_sched_barrier(0);
+      Terms<3> fe, fm, em;
+      terms_near<3>(pm + n * kLdP + 32 * ks + g8, kPPlane, fe);
+      terms_near<3>(pn + n * kLdP + 32 * ks + g8, kPPlane, fm);
+      terms_across<3>(pn + 32 * ks * kLdP + 16 * wave, kPPlane, kLdP, em);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
         Terms<NI> f;
-        terms_across<NI>(x + 32 * ks * kLd + 16 * kb, 64 * kLd, kLd, f);
-        dk[kb] = mul_terms<3>(f, fe[ks], dk[kb]);
-      }
-      const int ch = 16 * kb + row4;
-      if (on && ch < a.dk) {
-        const f32x4 q = load4<T>(at<T>(a.q, b * a.vq.b + hk * a.vq.h + (any.n0 + n) * a.vq.n + ch));
-        qdq += (double)(q[0] * dq[kb][0] + q[1] * dq[kb][1]) + (double)(q[2] * dq[kb][2] + q[3] * dq[kb][3]);
-      }
-      if constexpr (SHARED) {
-        sum_q[kb] += dq[kb];
-        sum_k[kb] += dk[kb];
+        terms_across<NI>(x + 32 * ks * kLd + 16 * (2 * i + half), 64 * kLd, kLd, f);
+        if (2 * ks <= wave) {
+          dq[i] = mul_terms<3>(f, fe, dq[i]);
+          dk[i] = mul_terms<3>(f, fm, dk[i]);
+        }
+        if (2 * ks + 1 >= wave) dk[i] = mul_terms<3>(f, em, dk[i]);
       }
     }
-    double both = qdq - vdv;
+    // <dS1, S1> = e^gamma_63 <dS1, S0> + sum of k.(e^(gamma_63 - gamma) dS1 u) over the tokens
+    ss *= decay[kDecaySince + 63];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const f32x4 k = channels_of(x, 16 * (2 * i + half) + row4);
+      ss += (k[0] * dw[i][0] + k[1] * dw[i][1]) + (k[2] * dw[i][2] + k[3] * dw[i][3]);
+    }
+    ss = lanes_sum<64>(ss);
+    if (lane == 0) inner[wave8] = ss;
+    lds_barrier();
+    queries.put(x, kLd);
+    lds_barrier();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if (2 * ks + 1 < wave) continue;
+      __builtin_amdgcn_sched_barrier(0);
+      Terms<3> fe;
+      terms_across<3>(pm + 32 * ks * kLdP + 16 * wave, kPPlane, kLdP, fe);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        Terms<NI> f;
+        terms_across<NI>(x + 32 * ks * kLd + 16 * (2 * i + half), 64 * kLd, kLd, f);
+        dk[i] = mul_terms<3>(f, fe, dk[i]);
+      }
+    }
+    double both = -vdv;   // q.dq - v.dv, the queries from their planes
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int ch = 16 * (2 * i + half) + row4;
+      const f32x4 q = channels_of(x, ch);
+      both += (double)(q[0] * dq[i][0] + q[1] * dq[i][1]) + (double)(q[2] * dq[i][2] + q[3] * dq[i][3]);
+      if constexpr (SHARED) {
+        sum_q[i] += dq[i];
+        sum_k[i] += dk[i];
+      } else if (on && ch < a.dk) {
+        store4<T>(at<T>(a.dq, b * a.vdq.b + hk * a.vdq.h + (any.n0 + n) * a.vdq.n + ch), dq[i]);
+        store4<T>(at<T>(a.dk_out, b * a.vdk.b + hk * a.vdk.h + (any.n0 + n) * a.vdk.n + ch), dk[i]);
+      }
+    }
     both += __shfl_xor(both, 16, 64);
     both += __shfl_xor(both, 32, 64);
-    double* dg64 = reinterpret_cast<double*>(pm);   // (the planes there are read)
+    if (lane < 16) dg64[half * 64 + n] = both;
     __syncthreads();
-    if (lane < 16) {
-      dg64[n] = both;
-      if (on) a.dbeta[w.b * a.vdg.b + w.h * a.vdg.h + (w.n0 + n) * a.vdg.n] = dbeta;
-    }
-    __syncthreads();
-    if (wave == 0) {
-      double y = dg64[lane];
+    if (wave8 == 0) {
+      double y = dg64[lane] + dg64[64 + lane];
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
         const double z = __shfl_down(y, m, 64);
         if (lane + m < 64) y += z;
       }
-      y += ((double)inner[0] + inner[1]) + ((double)inner[2] + inner[3]);
-      if (lane < w.valid) a.dg[w.b * a.vdg.b + w.h * a.vdg.h + (w.n0 + lane) * a.vdg.n] = (float)y;
-    }
-    if constexpr (!SHARED) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const int ch = 16 * kb + row4;
-        if (!on || ch >= a.dk) continue;
-        store4<T>(at<T>(a.dq, b * a.vdq.b + hk * a.vdq.h + (any.n0 + n) * a.vdq.n + ch), dq[kb]);
-        store4<T>(at<T>(a.dk_out, b * a.vdk.b + hk * a.vdk.h + (any.n0 + n) * a.vdk.n + ch), dk[kb]);
+      for (int i = 0; i < 8; ++i) y += (double)inner[i];
+      if (lane < w.valid) {
+        const long long to = w.b * a.vdg.b + w.h * a.vdg.h + (w.n0 + lane) * a.vdg.n;
+        a.dg[to] = (float)y;
+        a.dbeta[to] = db32[lane] + db32[64 + lane];
       }
     }
   }
   if constexpr (SHARED) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int ch = 16 * kb + row4;
+    for (int i = 0; i < KS; ++i) {
+      const int ch = 16 * (2 * i + half) + row4;
       if (!on || ch >= a.dk) continue;
-      store4<T>(at<T>(a.dq, b * a.vdq.b + hk * a.vdq.h + (any.n0 + n) * a.vdq.n + ch), sum_q[kb]);
-      store4<T>(at<T>(a.dk_out, b * a.vdk.b + hk * a.vdk.h + (any.n0 + n) * a.vdk.n + ch), sum_k[kb]);
+      store4<T>(at<T>(a.dq, b * a.vdq.b + hk * a.vdq.h + (any.n0 + n) * a.vdq.n + ch), sum_q[i]);
+      store4<T>(at<T>(a.dk_out, b * a.vdk.b + hk * a.vdk.h + (any.n0 + n) * a.vdk.n + ch), sum_k[i]);
     }
   }
 }

@@ -88,20 +88,59 @@ template <int LEVEL, int NA, int NB> LF_DEV f32x4 mul_terms(const Terms<NA>& a, 
   return c;
 }
 
-// A chunk's rows of one head as term planes in LDS ([64][ld] each), zeros behind the last token and channel; `steps` blocks of
-// 32 channels.
-template <typename T>
+// A chunk's rows of one head, 8 channels a vector: requested first, put down as term planes in LDS later ([64][ld] each, zeros
+// behind the last token and channel; `steps` blocks of 32 channels).  Requests of several tensors are in flight together.
+template <typename T, int STEPS, int THREADS> struct Rows {
+  static constexpr int kVecs = (64 * 4 * STEPS + THREADS - 1) / THREADS;
+  Raw8<T> raw[kVecs];
+  LF_DEV void request(const void* x, long long base, long long row, int valid, int d) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int e = threadIdx.x + THREADS * i, t = e / (4 * STEPS), c = (e - t * 4 * STEPS) * 8;
+      raw[i].w = u32x4{0, 0, 0, 0};
+      if constexpr (Stored<T>::kBytes == 4) raw[i].w2 = u32x4{0, 0, 0, 0};
+      if (t < valid && c < d) raw[i] = load8_raw<T>(at<T>(x, base + t * row + c));
+    }
+  }
+  LF_DEV void put(uint16_t* to, int ld) const {
+    constexpr int N = TermsOf<T>::kStored;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int e = threadIdx.x + THREADS * i, t = e / (4 * STEPS), c = (e - t * 4 * STEPS) * 8;
+      Terms<N> y;
+      terms_of<T>(raw[i], y);
+      if (e < 64 * 4 * STEPS) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) *reinterpret_cast<u32x4*>(to + k * 64 * ld + t * ld + c) = y.t[k];
+      }
+    }
+  }
+};
+// The same in one go for a number of steps known at run time, four vectors in flight.
+template <typename T, int THREADS>
 LF_DEV void stage_terms(uint16_t* to, int ld, const void* x, long long base, long long row, int valid, int d, int steps) {
   constexpr int N = TermsOf<T>::kStored;
   const int vecs = steps * 4;
-  for (int i = threadIdx.x; i < 64 * vecs; i += blockDim.x) {
-    const int t = (unsigned)i / (unsigned)vecs, c = (i - t * vecs) * 8;
-    Terms<N> y;
+  for (int i0 = threadIdx.x; i0 < 64 * vecs; i0 += 4 * THREADS) {
+    Raw8<T> raw[4];
+    int t[4], c[4];
 #pragma unroll
-    for (int k = 0; k < N; ++k) y.t[k] = u32x4{0, 0, 0, 0};
-    if (t < valid && c < d) terms_of<T>(load8_raw<T>(at<T>(x, base + t * row + c)), y);
+    for (int i = 0; i < 4; ++i) {
+      const int e = i0 + THREADS * i;
+      t[i] = (unsigned)e / (unsigned)vecs;
+      c[i] = (e - t[i] * vecs) * 8;
+      raw[i].w = u32x4{0, 0, 0, 0};
+      if constexpr (Stored<T>::kBytes == 4) raw[i].w2 = u32x4{0, 0, 0, 0};
+      if (t[i] < valid && c[i] < d) raw[i] = load8_raw<T>(at<T>(x, base + t[i] * row + c[i]));
+    }
 #pragma unroll
-    for (int k = 0; k < N; ++k) *reinterpret_cast<u32x4*>(to + k * 64 * ld + t * ld + c) = y.t[k];
+    for (int i = 0; i < 4; ++i) {
+      if (t[i] >= 64) continue;
+      Terms<N> y;
+      terms_of<T>(raw[i], y);
+#pragma unroll
+      for (int k = 0; k < N; ++k) *reinterpret_cast<u32x4*>(to + k * 64 * ld + t[i] * ld + c[i]) = y.t[k];
+    }
   }
 }
 

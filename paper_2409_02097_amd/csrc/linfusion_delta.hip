@@ -23,10 +23,12 @@ struct Sizes {
   long long nc, heads;   // chunks of N tokens; B * H
   int dkb, dvb, dks, runs, run;
   size_t esz;
-  size_t parts, joined, w, kt, u, s, decay, wt, tt, kn, du, ds;   // bytes
-  size_t forward() const { return w + kt + u + s + decay + parts + joined; }
-  size_t saved() const { return forward() + wt + tt; }
-  size_t backward() const { return kn + du + ds; }
+  size_t at_kt, at_u, at_s, at_decay, at_wt, at_tt, at_kn, at_ds;   // bytes into a record
+  size_t record, record_saved, record_b;                            // bytes of one
+  size_t parts, joined;
+  size_t forward() const { return (size_t)heads * nc * record + parts + joined; }
+  size_t saved() const { return (size_t)heads * nc * record_saved + parts + joined; }
+  size_t backward() const { return (size_t)heads * (nc + 2) * record_b; }
 };
 
 int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Sizes* z) {
@@ -41,16 +43,19 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->dvb = (dv + 15) / 16;
   z->esz = dtype == LINFUSION_DTYPE_F32 ? 4 : 2;
   z->dks = (dk + 31) / 32;
-  const size_t chunks = (size_t)z->heads * (size_t)z->nc, key_chunks = (size_t)B * H_k * (size_t)z->nc;
   const size_t terms = dtype == LINFUSION_DTYPE_F32 ? 3 : (dtype == LINFUSION_DTYPE_F16 ? 2 : 1), frag = lf::kFrag * 2;
-  z->w = up(chunks * 4 * z->dks * 3 * frag);
-  z->wt = up(chunks * z->dkb * 2 * 3 * frag);
-  z->tt = up(chunks * 4 * 2 * 3 * frag);
-  z->kt = up(key_chunks * z->dkb * 2 * terms * frag);
-  z->kn = up(key_chunks * 4 * z->dks * terms * frag);
-  z->u = up(chunks * z->dvb * 1024 * 4);
-  z->s = up((chunks + (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
-  z->decay = up(chunks * lf::kDecayRows * 4);
+  const size_t u = (size_t)z->dvb * 4096, state = (size_t)z->dvb * z->dkb * 1024;
+  z->at_kt = 4 * z->dks * 3 * frag;
+  z->at_u = z->at_kt + z->dkb * 2 * terms * frag;
+  z->at_s = z->at_u + u;
+  z->at_decay = z->at_s + state;
+  z->record = up(z->at_decay + lf::kDecayBytes);
+  z->at_wt = z->record;
+  z->at_tt = z->at_wt + z->dkb * 2 * 3 * frag;
+  z->record_saved = up(z->at_tt + 6 * lf::kFrag * 4);
+  z->at_kn = u;
+  z->at_ds = z->at_kn + 4 * z->dks * terms * frag;
+  z->record_b = up(z->at_ds + state);
   // Runs: as many as fill the device twice over with workgroups of the second pass, of 16 chunks at least; each costs delta_join
   // a step of a few us, and the first pass does (d_k + d_v) / d_v times the work of the second.
   const long long scans = z->heads * z->dvb;
@@ -63,8 +68,6 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   const size_t blocks = z->runs > 1 ? (size_t)z->heads * z->runs * z->dkb * 1024 : 0;
   z->parts = up(blocks * (z->dvb + z->dkb));
   z->joined = up(blocks * z->dvb);
-  z->du = z->u;
-  z->ds = up((chunks + 2 * (size_t)z->heads) * z->dvb * z->dkb * 256 * 4);
   return LINFUSION_OK;
 }
 
@@ -117,24 +120,25 @@ int check_scalars(std::initializer_list<const void*> ps, const long long* given,
   return LINFUSION_OK;
 }
 
-template <typename P> void take(P*& to, unsigned char*& p, size_t n) {
-  to = reinterpret_cast<P*>(p);
-  p += n;
+void place_forward(lf::DeltaArgs* a, const Sizes& z, void* at, bool for_backward) {
+  a->record = static_cast<unsigned char*>(at);
+  a->size = (unsigned)(for_backward ? z.record_saved : z.record);
+  a->for_backward = for_backward;
+  a->at_kt = (unsigned)z.at_kt;
+  a->at_u = (unsigned)z.at_u;
+  a->at_s = (unsigned)z.at_s;
+  a->at_decay = (unsigned)z.at_decay;
+  a->at_wt = (unsigned)z.at_wt;
+  a->at_tt = (unsigned)z.at_tt;
+  a->parts = reinterpret_cast<float*>(a->record + (size_t)z.heads * z.nc * a->size);
+  a->joined = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(a->parts) + z.parts);
 }
 
-void place_forward(lf::DeltaArgs* a, const Sizes& z, void* at, bool for_backward) {
-  unsigned char* p = static_cast<unsigned char*>(at);
-  take(a->w, p, z.w);
-  take(a->kt, p, z.kt);
-  take(a->u, p, z.u);
-  take(a->s, p, z.s);
-  take(a->decay, p, z.decay);
-  take(a->parts, p, z.parts);
-  take(a->joined, p, z.joined);
-  a->wt = a->tt = nullptr;
-  if (!for_backward) return;
-  take(a->wt, p, z.wt);
-  take(a->tt, p, z.tt);
+void place_backward(lf::DeltaArgs* a, const Sizes& z, void* at) {
+  a->record_b = static_cast<unsigned char*>(at);
+  a->size_b = (unsigned)z.record_b;
+  a->at_kn = (unsigned)z.at_kn;
+  a->at_ds = (unsigned)z.at_ds;
 }
 
 #define LF_FOR_STEPS(X)                                                                           \
@@ -190,21 +194,24 @@ template <typename T, int KS, bool SHARED> int launch_gradients(const lf::DeltaA
   const int lds = lf::delta_gradients_lds<T>(KS);
   auto kernel = lf::delta_gradients<T, KS, SHARED>;
   if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
-  kernel<<<dim3(a.nc, B * a.Hk), dim3(256), lds, st>>>(a);
+  kernel<<<dim3(a.nc, B * a.Hk), dim3(512), lds, st>>>(a);
   return LINFUSION_OK;
 }
 
-template <typename T> int run_bwd(const lf::DeltaArgs& a, int B, bool states, hipStream_t st) {
+template <typename T, int KS> int launch_bwd(const lf::DeltaArgs& a, int B, hipStream_t st) {
   constexpr int NI = lf::TermsOf<T>::kStored;
-  const int BH = B * a.H, lds = lf::delta_back_prepare_lds<T>(a.dks, (a.dvb + 1) / 2);
-  if (!lfh::allow_lds(lf::delta_back_prepare<T>, lds)) return LINFUSION_ERR_HIP;
+  const int BH = B * a.H, lds = lf::delta_back_prepare_lds<T>(KS, (a.dvb + 1) / 2);
+  auto prepare = lf::delta_back_prepare<T, KS>;
+  if (!lfh::allow_lds(prepare, lds)) return LINFUSION_ERR_HIP;
+  prepare<<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
+  lf::delta_back_scan<NI, KS><<<dim3(a.dvb * BH), dim3(256), 0, st>>>(a);
+  return a.H == a.Hk ? launch_gradients<T, KS, false>(a, B, st) : launch_gradients<T, KS, true>(a, B, st);
+}
+
+template <typename T> int run_bwd(const lf::DeltaArgs& a, int B, bool states, hipStream_t st) {
   int rc = LINFUSION_OK;
-  if (states && (rc = run_states<T>(a, BH, st)) != LINFUSION_OK) return rc;
-  lf::delta_back_prepare<T><<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
-#define X(KS) lf::delta_back_scan<NI, KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
-  LF_FOR_STEPS(X)
-#undef X
-#define X(KS) rc = a.H == a.Hk ? launch_gradients<T, KS, false>(a, B, st) : launch_gradients<T, KS, true>(a, B, st);
+  if (states && (rc = run_states<T>(a, B * a.H, st)) != LINFUSION_OK) return rc;
+#define X(KS) rc = launch_bwd<T, KS>(a, B, st);
   LF_FOR_STEPS(X)
 #undef X
   return rc;
@@ -329,11 +336,8 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   a.state_in = state_in; a.lengths = lengths; a.dout = dout; a.dstate_out = dstate_out;
   a.dq = dq; a.dk_out = dk; a.dv_out = dv; a.dg = dg; a.dbeta = dbeta; a.dstate_in = dstate_in;
   a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.heads = (int)z.heads; a.runs = z.runs; a.run = z.run; a.scale = scale;
-  unsigned char* p = static_cast<unsigned char*>(workspace);
-  take(a.kn, p, z.kn);
-  take(a.du, p, z.du);
-  take(a.ds, p, z.ds);
-  place_forward(&a, z, saved ? const_cast<void*>(saved) : p, true);
+  place_backward(&a, z, workspace);
+  place_forward(&a, z, saved ? const_cast<void*>(saved) : static_cast<unsigned char*>(workspace) + z.backward(), true);
   const hipStream_t st = (hipStream_t)stream;
   rc = dtype == LINFUSION_DTYPE_F16   ? run_bwd<lf::F16>(a, B, !saved, st)
        : dtype == LINFUSION_DTYPE_BF16 ? run_bwd<lf::BF16>(a, B, !saved, st)

@@ -345,20 +345,21 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
 }
 
 // ---- the scan ---------------------------------------------------------------------------------------------------------------
-// A workgroup takes 16 value channels of one head through a run of chunks; its four waves hold the state's row blocks
-// wave, wave + 4, ... as accumulators and compute 16 tokens of U each.  Bound: the chain from one chunk's state to the next
-// (two products, two passes through LDS); what it reads is requested two chunks ahead where registers allow it, one else:
-// a chunk takes 0.45 us, a request up to 0.9.
+// A workgroup takes 16 COLS value channels of one head through a run of chunks; its four waves hold the state's row blocks
+// wave, wave + 4, ... as accumulators and compute 16 tokens of U each.  Bound: with few workgroups the chain from one chunk's
+// state to the next (two products, two passes through LDS; what it reads is requested two chunks ahead where registers
+// allow it), with many the operands' way from the L2, which every slice of a head reads anew: hence 32 channels where there
+// are enough of them.
 //
 // With fewer workgroups than the device has room for, a head's chunks are parted into runs.  A run turns the state it starts
 // from into M S + R with a d_k x d_k matrix M of its own: a first pass (PARTIAL) takes zeros and the columns of the identity
 // through every run at once, delta_join takes the state through the runs, and the second pass starts each from its state.
-template <int NI, int KS> struct ScanIn {
+template <int NI, int KS, int COLS> struct ScanIn {
   static constexpr int kBlocks = (2 * KS + 3) / 4;
-  static constexpr int kDepth = 12 * KS + 8 * NI * kBlocks <= 110 ? 3 : 2;
+  static constexpr int kDepth = 12 * KS + 8 * NI * kBlocks + 4 * COLS <= 114 ? 3 : 2;
   Terms<3> w[KS];
   Terms<NI> kt[kBlocks][2];
-  f32x4 u0;
+  f32x4 u0[COLS];
   float write, whole;
 };
 
@@ -370,129 +371,171 @@ LF_DEV void slice_of_head(unsigned i, int slices, int heads, int& slice, int& bh
   bh = 8 * group + (r - slice * here);
 }
 
-template <int NI, int KS, bool PARTIAL> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
-  using In = ScanIn<NI, KS>;
-  constexpr int kBlocks = In::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * kLd;
+template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(256) void delta_scan(DeltaArgs a) {
+  using In = ScanIn<NI, KS, COLS>;
+  constexpr int kBlocks = In::kBlocks, kLd = 32 * KS + 8, kPlane = 16 * COLS * kLd, kLdU = 16 * COLS + 4, kUPlane = 64 * kLdU;
   __shared__ __align__(16) uint16_t sp[3 * kPlane];
-  __shared__ __align__(16) uint16_t up[3 * 64 * kLdU];
+  __shared__ __align__(16) uint16_t up[3 * kUPlane];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
-  int slice, bh;
-  slice_of_head(blockIdx.x, PARTIAL ? a.dvb + a.dkb : a.dvb, a.heads, slice, bh);
-  const int ch = slice * 16 + col, run = blockIdx.y;
-  const bool unit = PARTIAL && slice >= a.dvb;   // columns of the identity, and no values
+  const int slices = PARTIAL ? a.dvb + a.dkb : a.dvb, run = blockIdx.y;
+  int group, bh;
+  slice_of_head(blockIdx.x, (slices + COLS - 1) / COLS, a.heads, group, bh);
   const DeltaAt first(a, bh, 0);
   const int all = (int)((tokens_of(a.lengths, first.b, a.N) + 63) / 64);
   const int begin = run * a.run, end = begin + a.run < all ? begin + a.run : all;
   if (!PARTIAL && run > 0 && begin >= all) return;
-  // A wave without a block of its own does the last one's work again, to the same bits: with every load and store of a chunk
-  // unconditional, the compiler can wait for exactly those that it needs.
-  int blk[kBlocks];
+  // A wave without a block of its own does the last one's work again, to the same bits, and so does a last odd slice: with
+  // every load and store of a chunk unconditional, the compiler can wait for exactly those that it needs.
+  int blk[kBlocks], slice[COLS];
+  bool unit[COLS];   // columns of the identity, and no values
 #pragma unroll
   for (int t = 0; t < kBlocks; ++t) blk[t] = wave + 4 * t < a.dkb ? wave + 4 * t : a.dkb - 1;
-  f32x4 s[kBlocks];
 #pragma unroll
-  for (int t = 0; t < kBlocks; ++t) {
-    if (!PARTIAL && run > 0) {
-      s[t] = *reinterpret_cast<const f32x4*>(a.joined + ((((long long)bh * a.runs + run) * a.dvb + slice) * a.dkb + blk[t]) * 256 + lane * 4);
-      continue;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = 16 * blk[t] + row4 + r;
-      if (unit) s[t][r] = row == (slice - a.dvb) * 16 + col ? 1.0f : 0.0f;
-      else s[t][r] = a.state_in && run == 0 && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
-    }
+  for (int e = 0; e < COLS; ++e) {
+    slice[e] = COLS * group + e < slices ? COLS * group + e : slices - 1;
+    unit[e] = PARTIAL && slice[e] >= a.dvb;
   }
+  f32x4 s[COLS][kBlocks];
+#pragma unroll
+  for (int e = 0; e < COLS; ++e)
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) {
+      if (!PARTIAL && run > 0) {
+        s[e][t] = *reinterpret_cast<const f32x4*>(a.joined + ((((long long)bh * a.runs + run) * a.dvb + slice[e]) * a.dkb + blk[t]) * 256 + lane * 4);
+        continue;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * blk[t] + row4 + r, ch = slice[e] * 16 + col;
+        if (unit[e]) s[e][t][r] = row == (slice[e] - a.dvb) * 16 + col ? 1.0f : 0.0f;
+        else s[e][t][r] = a.state_in && run == 0 && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
+      }
+    }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
   const int key_head = bh - first.h + first.hk * (a.H / a.Hk);   // whose records have K^T
-  const int u_at = ((unit ? 0 : slice) * 4 + wave) * 256 + lane * 4;
-  auto request = [&](In& n, int i) {
-    i = i < end ? i : end - 1;
-    unsigned char* rec = a.rec(bh, i);
-    const uint16_t* mw = part<uint16_t>(rec, 0) + wave * KS * 3 * kFrag;
+  int u_at[COLS];
+#pragma unroll
+  for (int e = 0; e < COLS; ++e) u_at[e] = ((unit[e] ? 0 : slice[e]) * 4 + wave) * 256 + lane * 4;
+  // An address that differs by lane as far as the compiler can see: uniform loads would go through the scalar cache, whose
+  // counter the barriers wait for, and its misses with it.
+  int zero = 0;
+  asm volatile("" : "+v"(zero));
+  const unsigned char* ahead = a.rec(bh, begin);            // the record requested next
+  const unsigned char* ahead_key = a.rec(key_head, begin);
+  int requested = begin;
+  auto request = [&](In& n) {
+    const uint16_t* mw = reinterpret_cast<const uint16_t*>(ahead) + wave * KS * 3 * kFrag;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<3>(mw + ks * 3 * kFrag, n.w[ks]);
-    const uint16_t* kt = part<uint16_t>(a.rec(key_head, i), a.at_kt);
+    const uint16_t* kt = reinterpret_cast<const uint16_t*>(ahead_key + a.at_kt);
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) load_frag<NI>(kt + (blk[t] * 2 + ks) * NI * kFrag, n.kt[t][ks]);
-    n.u0 = *reinterpret_cast<const f32x4*>(part<float>(rec, a.at_u) + u_at);
-    const float* decay = part<float>(rec, a.at_decay);
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) n.u0[e] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(ahead + a.at_u) + u_at[e]);
+    const float* decay = reinterpret_cast<const float*>(ahead + a.at_decay);
     n.write = decay[kDecayWrite + 16 * wave + col];
-    n.whole = decay[kDecaySince + 63];
+    n.whole = decay[kDecaySince + 63 + zero];
+    const unsigned step = ++requested < end ? a.size : 0;   // (the last one again behind the end)
+    ahead += step;
+    ahead_key += step;
   };
-  auto keep = [&](float* to) {
+  unsigned char* here = a.rec(bh, begin);
+  auto keep = [&](float* to) {   // `to`: the first slice
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t) *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
+    for (int e = 0; e < COLS; ++e)
+#pragma unroll
+      for (int t = 0; t < kBlocks; ++t) *reinterpret_cast<f32x4*>(to + (slice[e] * a.dkb + blk[t]) * 256 + lane * 4) = s[e][t];
   };
-  auto chunk = [&](In& in, In& next, int i) {
+  auto chunk = [&](In& in, In& next) {
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t) split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
-    request(next, i + In::kDepth - 1);
-    if constexpr (!PARTIAL) keep(part<float>(a.rec(bh, i), a.at_s) + slice * a.dkb * 256);
+    for (int e = 0; e < COLS; ++e)
+#pragma unroll
+      for (int t = 0; t < kBlocks; ++t) split4_lds<3>(sp + (16 * e + col) * kLd + 16 * blk[t] + row4, kPlane, s[e][t]);
     lds_barrier();
-    f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
+    f32x4 acc[COLS], acc2[COLS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      Terms<3> fs;
-      terms_near<3>(sp + col * kLd + 32 * ks + g8, kPlane, fs);
-      if (ks & 1) acc2 = mul_terms<3>(fs, in.w[ks], acc2);
-      else acc = mul_terms<3>(fs, in.w[ks], acc);
+    for (int e = 0; e < COLS; ++e) acc[e] = acc2[e] = f32x4{0, 0, 0, 0};
+    Terms<3> first_fs;
+    terms_near<3>(sp + col * kLd + g8, kPlane, first_fs);
+    __builtin_amdgcn_sched_barrier(0);
+    request(next);                                           // while the planes are on their way
+    if constexpr (!PARTIAL) keep(reinterpret_cast<float*>(here + a.at_s));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) {
+        Terms<3> fs;
+        if (ks == 0 && e == 0) fs = first_fs;
+        else terms_near<3>(sp + (16 * e + col) * kLd + 32 * ks + g8, kPlane, fs);
+        if (COLS == 1 && (ks & 1)) acc2[e] = mul_terms<3>(fs, in.w[ks], acc2[e]);
+        else acc[e] = mul_terms<3>(fs, in.w[ks], acc[e]);
+      }
+    f32x4 u[COLS];
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) {
+      f32x4 u0 = in.u0[e];
+      if (unit[e]) u0 = f32x4{0, 0, 0, 0};
+      u[e] = u0 - (acc[e] + acc2[e]);
+      split4_lds<3>(up + (16 * wave + col) * kLdU + 16 * e + row4, kUPlane, u[e] * in.write);
     }
-    f32x4 u0 = in.u0;
-    if (unit) u0 = f32x4{0, 0, 0, 0};
-    const f32x4 u = u0 - (acc + acc2);
-    if constexpr (!PARTIAL) *reinterpret_cast<f32x4*>(part<float>(a.rec(bh, i), a.at_u) + u_at) = u;
-    split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, u * in.write);
     lds_barrier();
-    Terms<3> fu[2];
-    terms_across<3>(up, 64 * kLdU, kLdU, fu[0]);
-    terms_across<3>(up + 32 * kLdU, 64 * kLdU, kLdU, fu[1]);
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t) {
-      s[t] *= in.whole;
-      s[t] = mul_terms<3>(in.kt[t][0], fu[0], s[t]);
-      s[t] = mul_terms<3>(in.kt[t][1], fu[1], s[t]);
+    for (int e = 0; e < COLS; ++e) {
+      Terms<3> fu[2];
+      terms_across<3>(up + 16 * e, kUPlane, kLdU, fu[0]);
+      terms_across<3>(up + 32 * kLdU + 16 * e, kUPlane, kLdU, fu[1]);
+      if constexpr (!PARTIAL) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(here + a.at_u) + u_at[e]) = u[e];
+#pragma unroll
+      for (int t = 0; t < kBlocks; ++t) {
+        f32x4 more = {0, 0, 0, 0};
+        s[e][t] *= in.whole;
+        s[e][t] = mul_terms<3>(in.kt[t][0], fu[0], s[e][t]);
+        more = mul_terms<3>(in.kt[t][1], fu[1], more);
+        s[e][t] += more;
+      }
     }
+    here += a.size;
   };
   if (begin < end) {
     In x, y;
-    request(x, begin);
+    request(x);
     if constexpr (In::kDepth == 3) {
       In z;
-      request(y, begin + 1);
+      request(y);
       int i = begin;
       for (; i + 2 < end; i += 3) {
-        chunk(x, z, i);
-        chunk(y, x, i + 1);
-        chunk(z, y, i + 2);
+        chunk(x, z);
+        chunk(y, x);
+        chunk(z, y);
       }
-      if (i < end) chunk(x, z, i);
-      if (i + 1 < end) chunk(y, x, i + 1);
+      if (i < end) chunk(x, z);
+      if (i + 1 < end) chunk(y, x);
     } else {
       int i = begin;
       for (; i + 1 < end; i += 2) {
-        chunk(x, y, i);
-        chunk(y, x, i + 1);
+        chunk(x, y);
+        chunk(y, x);
       }
-      if (i < end) chunk(x, y, i);
+      if (i < end) chunk(x, y);
     }
   }
   if constexpr (PARTIAL) {
-    keep(a.parts + (((long long)bh * a.runs + run) * (a.dvb + a.dkb) + slice) * a.dkb * 256);
-  } else if (end == all) {
-    if (a.state_out) {
+    keep(a.parts + ((long long)bh * a.runs + run) * (a.dvb + a.dkb) * a.dkb * 256);
+  } else if (end == all && a.state_out) {
+#pragma unroll
+    for (int e = 0; e < COLS; ++e)
 #pragma unroll
       for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = 16 * blk[t] + row4 + r;
-          if (row < a.dk && ch < a.dv) a.state_out[((long long)bh * a.dk + row) * a.dv + ch] = s[t][r];
+          const int row = 16 * blk[t] + row4 + r, ch = slice[e] * 16 + col;
+          if (row < a.dk && ch < a.dv) a.state_out[((long long)bh * a.dk + row) * a.dv + ch] = s[e][t][r];
         }
-    }
   }
 }
 

@@ -169,77 +169,92 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
   __syncthreads();
   const int key_head = bh - first.h + first.hk * (a.H / a.Hk);
   const int u_at = (slice * 4 + wave) * 256 + lane * 4;
-  auto request = [&](BackScanIn<NI, KS>& n, int i) {
-    i = i < 0 ? 0 : i;
-    unsigned char *rec = a.rec(bh, i), *rec_b = a.rec_b(bh, i);
-    const uint16_t* kn = part<uint16_t>(a.rec_b(key_head, i), a.at_kn) + wave * KS * NI * kFrag;
+  int zero = 0;   // (as in delta_scan)
+  asm volatile("" : "+v"(zero));
+  const int last = chunks > 0 ? chunks - 1 : 0;
+  const unsigned char *ahead = a.rec(bh, last), *ahead_b = a.rec_b(bh, last), *ahead_key = a.rec_b(key_head, last);
+  int requested = last;
+  auto request = [&](BackScanIn<NI, KS>& n) {
+    const uint16_t* kn = reinterpret_cast<const uint16_t*>(ahead_key + a.at_kn) + wave * KS * NI * kFrag;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) load_frag<NI>(kn + ks * NI * kFrag, n.kn[ks]);
-    const uint16_t* wt = part<uint16_t>(rec, a.at_wt);
-    const float* z = part<float>(rec_b, a.at_ds) + slice * a.dkb * 256;
+    const uint16_t* wt = reinterpret_cast<const uint16_t*>(ahead + a.at_wt);
+    const float* z = reinterpret_cast<const float*>(ahead_b + a.at_ds) + slice * a.dkb * 256;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
       n.z[t] = *reinterpret_cast<const f32x4*>(z + blk[t] * 256 + lane * 4);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) load_frag<3>(wt + (blk[t] * 2 + ks) * 3 * kFrag, n.wt[t][ks]);
     }
-    n.du = *reinterpret_cast<const f32x4*>(part<float>(rec_b, 0) + u_at);
-    const float* decay = part<float>(rec, a.at_decay);
+    n.du = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(ahead_b) + u_at);
+    const float* decay = reinterpret_cast<const float*>(ahead + a.at_decay);
     n.left = decay[kDecayLeft + 16 * wave + col];
-    n.whole = decay[kDecaySince + 63];
+    n.whole = decay[kDecaySince + 63 + zero];
+    if (requested-- > 0) {   // (the first one again before the beginning)
+      ahead -= a.size;
+      ahead_b -= a.size_b;
+      ahead_key -= a.size_b;
+    }
   };
-  auto chunk = [&](BackScanIn<NI, KS>& in, BackScanIn<NI, KS>& next, int i) {
+  unsigned char* here = a.rec_b(bh, last);
+  auto chunk = [&](BackScanIn<NI, KS>& in, BackScanIn<NI, KS>& next) {
 #pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-      split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
-    request(next, i + 1 - BackScanIn<NI, KS>::kDepth);
-    float* to = part<float>(a.rec_b(bh, i + 2), a.at_ds) + slice * a.dkb * 256;
-#pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-      *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
+    for (int t = 0; t < kBlocks; ++t) split4_lds<3>(sp + col * kLd + 16 * blk[t] + row4, kPlane, s[t]);
     lds_barrier();
     f32x4 acc = {0, 0, 0, 0}, acc2 = {0, 0, 0, 0};
+    Terms<3> first_fs;
+    terms_near<3>(sp + col * kLd + g8, kPlane, first_fs);
+    __builtin_amdgcn_sched_barrier(0);
+    request(next);
+    float* to = reinterpret_cast<float*>(here + 2 * (size_t)a.size_b + a.at_ds) + slice * a.dkb * 256;
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) *reinterpret_cast<f32x4*>(to + blk[t] * 256 + lane * 4) = s[t];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       Terms<3> fs;
-      terms_near<3>(sp + col * kLd + 32 * ks + g8, kPlane, fs);
+      if (ks == 0) fs = first_fs;
+      else terms_near<3>(sp + col * kLd + 32 * ks + g8, kPlane, fs);
       if (ks & 1) acc2 = mul_terms<3>(fs, in.kn[ks], acc2);
       else acc = mul_terms<3>(fs, in.kn[ks], acc);
     }
     const f32x4 u = in.du + (acc + acc2) * in.left;
-    *reinterpret_cast<f32x4*>(part<float>(a.rec_b(bh, i), 0) + u_at) = u;
     split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, -u);
     lds_barrier();
     Terms<3> fu[2];
     terms_across<3>(up, 64 * kLdU, kLdU, fu[0]);
     terms_across<3>(up + 32 * kLdU, 64 * kLdU, kLdU, fu[1]);
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(here) + u_at) = u;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      s[t] = s[t] * in.whole + in.z[t];
+      f32x4 more = in.z[t];
+      s[t] *= in.whole;
       s[t] = mul_terms<3>(in.wt[t][0], fu[0], s[t]);
-      s[t] = mul_terms<3>(in.wt[t][1], fu[1], s[t]);
+      more = mul_terms<3>(in.wt[t][1], fu[1], more);
+      s[t] += more;
     }
+    here -= a.size_b;
   };
   if (chunks > 0) {
     BackScanIn<NI, KS> x, y;
     int i = chunks - 1;
-    request(x, i);
+    request(x);
     if constexpr (BackScanIn<NI, KS>::kDepth == 3) {
       BackScanIn<NI, KS> z;
-      request(y, i - 1);
+      request(y);
       for (; i > 1; i -= 3) {
-        chunk(x, z, i);
-        chunk(y, x, i - 1);
-        chunk(z, y, i - 2);
+        chunk(x, z);
+        chunk(y, x);
+        chunk(z, y);
       }
-      if (i >= 0) chunk(x, z, i);
-      if (i >= 1) chunk(y, x, i - 1);
+      if (i >= 0) chunk(x, z);
+      if (i >= 1) chunk(y, x);
     } else {
       for (; i > 0; i -= 2) {
-        chunk(x, y, i);
-        chunk(y, x, i - 1);
+        chunk(x, y);
+        chunk(y, x);
       }
-      if (i == 0) chunk(x, y, 0);
+      if (i == 0) chunk(x, y);
     }
   }
   if (a.dstate_in) {

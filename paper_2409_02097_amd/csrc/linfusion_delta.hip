@@ -58,8 +58,8 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->record_b = up(z->at_ds + state);
   // Runs: as many as fill the device twice over with workgroups of the second pass, of 16 chunks at least; each costs delta_join
   // a step of a few us, and the first pass does (d_k + d_v) / d_v times the work of the second.
-  const long long scans = z->heads * z->dvb;
-  long long runs = 2LL * lfh::num_cu() / scans;
+  const long long scans = z->heads * ((z->dvb + 1) / 2);
+  long long runs = lfh::env_int("LINFUSION_DELTA_RUNS", 1) > 1 ? lfh::env_int("LINFUSION_DELTA_RUNS", 1) : lfh::num_cu() / scans;
   if (runs > z->nc / 16) runs = z->nc / 16;
   if (runs > 32) runs = 32;
   if (runs < 3) runs = 1;
@@ -150,6 +150,15 @@ void place_backward(lf::DeltaArgs* a, const Sizes& z, void* at) {
     default: X(5) break;                                                                          \
   }
 
+// 32 value channels a workgroup where that still gives three quarters of the CUs one
+template <int NI, int KS, bool PARTIAL> void launch_scan(const lf::DeltaArgs& a, int slices, int runs, hipStream_t st) {
+  const int pairs = (slices + 1) / 2;
+  if (slices > 1 && 4LL * pairs * a.heads * runs >= 3LL * lfh::num_cu())
+    lf::delta_scan<NI, KS, 2, PARTIAL><<<dim3(pairs * a.heads, runs), dim3(256), 0, st>>>(a);
+  else
+    lf::delta_scan<NI, KS, 1, PARTIAL><<<dim3(slices * a.heads, runs), dim3(256), 0, st>>>(a);
+}
+
 template <typename T, int KS> int launch_states(const lf::DeltaArgs& a, int BH, hipStream_t st) {
   constexpr int NI = lf::TermsOf<T>::kStored;
   const int lds = lf::delta_prepare_lds<T>(KS, (a.dvb + 1) / 2);
@@ -157,10 +166,10 @@ template <typename T, int KS> int launch_states(const lf::DeltaArgs& a, int BH, 
   if (!lfh::allow_lds(prepare, lds)) return LINFUSION_ERR_HIP;
   prepare<<<dim3(a.nc, BH), dim3(256), lds, st>>>(a);
   if (a.runs > 1) {
-    lf::delta_scan<NI, KS, true><<<dim3((a.dvb + a.dkb) * BH, a.runs - 1), dim3(256), 0, st>>>(a);
+    launch_scan<NI, KS, true>(a, a.dvb + a.dkb, a.runs - 1, st);
     lf::delta_join<KS><<<dim3(a.dvb, BH), dim3(256), 0, st>>>(a);
   }
-  lf::delta_scan<NI, KS, false><<<dim3(a.dvb * BH, a.runs), dim3(256), 0, st>>>(a);
+  launch_scan<NI, KS, false>(a, a.dvb, a.runs, st);
   return LINFUSION_OK;
 }
 

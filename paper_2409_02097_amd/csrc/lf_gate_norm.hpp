@@ -140,16 +140,26 @@ __global__ __launch_bounds__(256) void gate_norm_fwd(GateNormArgs a) {
   }
   const float inv_c = 1.0f / (float)a.C;
   int slot = 0;
+  Raw8<T> next_x[VPT], next_f[VPT];   // the token after this one is on its way meanwhile
+  auto request = [&](long long m) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      next_x[i] = none8<T>();
+      next_f[i] = none8<T>();
+      if (!on[i] || m >= stop) continue;
+      next_x[i] = load8_raw<T>(at<T>(a.x, b * a.vx.batch + m * a.vx.token + c[i]));
+      if (a.f) next_f[i] = load8_raw<T>(at<T>(a.f, b * a.vf.batch + m * a.vf.token + c[i]));
+    }
+  };
+  request(n);
   for (; n < stop; n += 256 / LANES) {
     float y[VPT][8], f[VPT][8];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[i][j] = f[i][j] = 0.0f;
-      if (!on[i]) continue;
-      load8<T>(at<T>(a.x, b * a.vx.batch + n * a.vx.token + c[i]), y[i]);
-      if (a.f) load8<T>(at<T>(a.f, b * a.vf.batch + n * a.vf.token + c[i]), f[i]);
+      widen8<T>(next_x[i], y[i]);
+      widen8<T>(next_f[i], f[i]);
     }
+    request(n + 256 / LANES);
     if constexpr (POST) {
       normalise<LANES, VPT, RMS>(f, on, inv_c, a.eps, lds, slot);
 #pragma unroll
@@ -171,7 +181,7 @@ __global__ __launch_bounds__(256) void gate_norm_fwd(GateNormArgs a) {
     if (a.y) {
 #pragma unroll
       for (int i = 0; i < VPT; ++i)
-        if (on[i]) store8<T>(at<T>(a.y, b * a.vy.batch + n * a.vy.token + c[i]), y[i]);
+        if (on[i]) store8_stream<T>(at<T>(a.y, b * a.vy.batch + n * a.vy.token + c[i]), y[i]);
     }
     if (a.h) {
       normalise<LANES, VPT, RMS>(y, on, inv_c, a.eps, lds, slot);
@@ -180,7 +190,7 @@ __global__ __launch_bounds__(256) void gate_norm_fwd(GateNormArgs a) {
         if (!on[i]) continue;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[i][j] = __builtin_fmaf(y[i][j], mul[i][j], add[i][j]);
-        store8<T>(at<T>(a.h, b * a.vh.batch + n * a.vh.token + c[i]), y[i]);
+        store8_stream<T>(at<T>(a.h, b * a.vh.batch + n * a.vh.token + c[i]), y[i]);
       }
     }
   }
@@ -241,17 +251,29 @@ __global__ __launch_bounds__(256) void gate_norm_bwd(GateNormBwdArgs a) {
   }
   const float inv_c = 1.0f / (float)a.C;
   int slot = 0, slot2 = 0;
-  for (long long n = first; n < stop; n += 256 / LANES) {
-    float y[VPT][8], f[VPT][8], d[VPT][8];
+  Raw8<T> next_x[VPT], next_f[VPT], next_h[VPT], next_y[VPT];
+  auto request = [&](long long m) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[i][j] = f[i][j] = d[i][j] = 0.0f;
-      if (!on[i]) continue;
-      load8<T>(at<T>(a.x, b * a.vx.batch + n * a.vx.token + c[i]), y[i]);
-      if (a.f) load8<T>(at<T>(a.f, b * a.vf.batch + n * a.vf.token + c[i]), f[i]);
-      if (a.dh) load8<T>(at<T>(a.dh, b * a.vdh.batch + n * a.vdh.token + c[i]), d[i]);
+      next_x[i] = next_f[i] = next_h[i] = next_y[i] = none8<T>();
+      if (!on[i] || m >= stop) continue;
+      next_x[i] = load8_raw<T>(at<T>(a.x, b * a.vx.batch + m * a.vx.token + c[i]));
+      if (a.f) next_f[i] = load8_raw<T>(at<T>(a.f, b * a.vf.batch + m * a.vf.token + c[i]));
+      if (a.dh) next_h[i] = load8_raw<T>(at<T>(a.dh, b * a.vdh.batch + m * a.vdh.token + c[i]));
+      if (a.dy) next_y[i] = load8_raw<T>(at<T>(a.dy, b * a.vdy.batch + m * a.vdy.token + c[i]));
     }
+  };
+  request(first);
+  for (long long n = first; n < stop; n += 256 / LANES) {
+    float y[VPT][8], f[VPT][8], d[VPT][8], up[VPT][8];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      widen8<T>(next_x[i], y[i]);
+      widen8<T>(next_f[i], f[i]);
+      widen8<T>(next_h[i], d[i]);
+      widen8<T>(next_y[i], up[i]);
+    }
+    request(n + 256 / LANES);
     float rate_f = 1.0f;
     if constexpr (POST) rate_f = normalise<LANES, VPT, RMS>(f, on, inv_c, a.eps, lds, slot);
 #pragma unroll
@@ -285,16 +307,10 @@ __global__ __launch_bounds__(256) void gate_norm_bwd(GateNormBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[i][j] = (d[i][j] - s1 - y[i][j] * s2) * rate;
     }
-    if (a.dy) {
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        if (!on[i]) continue;
-        float g[8];
-        load8<T>(at<T>(a.dy, b * a.vdy.batch + n * a.vdy.token + c[i]), g);
+    for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[i][j] += g[j];
-      }
-    }
+      for (int j = 0; j < 8; ++j) d[i][j] += up[i][j];
     // d is dY now; y is free
     if (a.dx) {
 #pragma unroll
@@ -303,7 +319,7 @@ __global__ __launch_bounds__(256) void gate_norm_bwd(GateNormBwdArgs a) {
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] = a.residual_scale * d[i][j];
-        store8<T>(at<T>(a.dx, b * a.vdx.batch + n * a.vdx.token + c[i]), g);
+        store8_stream<T>(at<T>(a.dx, b * a.vdx.batch + n * a.vdx.token + c[i]), g);
       }
     }
     float s1 = 0.0f, s2 = 0.0f;
@@ -335,7 +351,7 @@ __global__ __launch_bounds__(256) void gate_norm_bwd(GateNormBwdArgs a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) d[i][j] = (d[i][j] - s1 - f[i][j] * s2) * rate_f;
         }
-        store8<T>(at<T>(a.df, b * a.vdf.batch + n * a.vdf.token + c[i]), d[i]);
+        store8_stream<T>(at<T>(a.df, b * a.vdf.batch + n * a.vdf.token + c[i]), d[i]);
       }
     }
   }
@@ -368,64 +384,74 @@ __global__ __launch_bounds__(256) void gate_norm_bwd(GateNormBwdArgs a) {
   }
 }
 
-// [B][wgs][3][C] partial sums -> [B][3][C]: 64 elements per workgroup, each of its four waves a quarter of the partials in
-// their order, the quarters in theirs.
-__global__ __launch_bounds__(256) void gate_norm_sums(const float* partials, float* out, int wgs, int n3c) {
-  __shared__ float part[4][64];
-  const int e = blockIdx.x * 64 + (threadIdx.x & 63), quarter = threadIdx.x >> 6;
-  const float* p = partials + (long long)blockIdx.y * wgs * n3c;
-  const int per = (wgs + 3) / 4, from = quarter * per, to = from + per < wgs ? from + per : wgs;
-  float s = 0.0f;
-  if (e < n3c) {
-    int w = from;
-    for (; w + 4 <= to; w += 4) {
-      const float v0 = p[(long long)w * n3c + e], v1 = p[(long long)(w + 1) * n3c + e];
-      const float v2 = p[(long long)(w + 2) * n3c + e], v3 = p[(long long)(w + 3) * n3c + e];
-      s += v0; s += v1; s += v2; s += v3;
-    }
-    for (; w < to; ++w) s += p[(long long)w * n3c + e];
-  }
-  part[quarter][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (quarter == 0 && e < n3c)
-    out[(long long)blockIdx.y * n3c + e] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
-}
-
 struct GateNormVectors {
-  const float* sums;   // [B][3][C]: A, Bs, G
+  const float* partials;   // [B][wgs][3][C]
+  float* sums;             // [B][3][C]: A, Bs, G
   const float *gate, *scale, *w_pre, *w_post;
   float *dgate, *dscale, *dshift, *dw_pre, *dw_post;
   long long mod_stride, dmod_stride;
-  int B, C;
-  bool shared;         // one modulation row for the whole batch: its gradient is the sum over the batch
+  int B, C, wgs;
+  bool shared;             // one modulation row for the whole batch: its gradient is the sum over the batch
 };
 
 // The vectors' gradients: dshift = A, dscale = Bs w_pre, dgate = G w_post per modulation row;
-// dw_pre = sum_b Bs (1 + scale), dw_post = sum_b G gate.  One thread per channel, batch rows in their order.
+// dw_pre = sum_b Bs (1 + scale), dw_post = sum_b G gate.
+// First the workgroups' partial sums: 64 elements per workgroup, each of its sixteen waves a sixteenth of the partials in their
+// order, the sixteenths in theirs (with four waves a sum over 2048 partials of one batch row took 30 us).  Where every modulation row has its own gradient that ends here; for the sums over the batch
+// the totals are left for gate_norm_vectors.
+__global__ __launch_bounds__(1024) void gate_norm_sums(GateNormVectors a) {
+  constexpr int kWaves = 16;
+  __shared__ float part[kWaves][64];
+  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, which = blockIdx.y, b = blockIdx.z;
+  const int per = (a.wgs + kWaves - 1) / kWaves, from = share * per, to = from + per < a.wgs ? from + per : a.wgs;
+  const long long step = 3LL * a.C;
+  float s = 0.0f;
+  if (c < a.C) {
+    const float* p = a.partials + ((long long)b * a.wgs + from) * step + (long long)which * a.C + c;
+    int w = from;
+    for (; w + 8 <= to; w += 8, p += 8 * step) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p[i * step];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    for (; w < to; ++w, p += step) s += *p;
+  }
+  part[share][lane] = s;
+  __syncthreads();
+  if (share != 0 || c >= a.C) return;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) s += part[i][lane];
+  if (a.sums) a.sums[((long long)b * 3 + which) * a.C + c] = s;
+  if (a.shared) return;
+  const long long o = b * a.dmod_stride + c;
+  if (which == 0 && a.dshift) a.dshift[o] = s;
+  if (which == 1 && a.dscale) a.dscale[o] = s * (a.w_pre ? a.w_pre[c] : 1.0f);
+  if (which == 2 && a.dgate) a.dgate[o] = s * (a.w_post ? a.w_post[c] : 1.0f);
+}
+
+// The sums over the batch, one thread per channel, batch rows in their order.
 __global__ __launch_bounds__(64) void gate_norm_vectors(GateNormVectors a) {
   const int c = blockIdx.x * 64 + threadIdx.x;
   if (c >= a.C) return;
-  const float wp = a.w_pre ? a.w_pre[c] : 1.0f, wo = a.w_post ? a.w_post[c] : 1.0f;
   float ta = 0.0f, tb = 0.0f, tg = 0.0f, pre = 0.0f, post = 0.0f;
+#pragma unroll 4
   for (int b = 0; b < a.B; ++b) {
     const float* s = a.sums + (long long)b * 3 * a.C + c;
     const float va = s[0], vb = s[a.C], vg = s[2 * a.C];
     const long long m = b * a.mod_stride + c;
-    if (a.dw_pre) pre = __builtin_fmaf(vb, a.scale ? 1.0f + a.scale[m] : 1.0f, pre);
-    if (a.dw_post) post = __builtin_fmaf(vg, a.gate ? a.gate[m] : 1.0f, post);
-    if (a.shared) {
-      ta += va; tb += vb; tg += vg;
-    } else {
-      const long long o = b * a.dmod_stride + c;
-      if (a.dshift) a.dshift[o] = va;
-      if (a.dscale) a.dscale[o] = vb * wp;
-      if (a.dgate) a.dgate[o] = vg * wo;
-    }
+    pre = __builtin_fmaf(vb, a.scale ? 1.0f + a.scale[m] : 1.0f, pre);
+    post = __builtin_fmaf(vg, a.gate ? a.gate[m] : 1.0f, post);
+    ta += va;
+    tb += vb;
+    tg += vg;
   }
   if (a.shared) {
     if (a.dshift) a.dshift[c] = ta;
-    if (a.dscale) a.dscale[c] = tb * wp;
-    if (a.dgate) a.dgate[c] = tg * wo;
+    if (a.dscale) a.dscale[c] = tb * (a.w_pre ? a.w_pre[c] : 1.0f);
+    if (a.dgate) a.dgate[c] = tg * (a.w_post ? a.w_post[c] : 1.0f);
   }
   if (a.dw_pre) a.dw_pre[c] = pre;
   if (a.dw_post) a.dw_post[c] = post;

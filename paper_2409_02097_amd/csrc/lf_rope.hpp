@@ -51,13 +51,13 @@ template <typename T> LF_DEV f32x2 turn_of(double turns) {
 inline __host__ __device__ size_t rope_table_bytes(int tokens, int pairs) { return ((size_t)tokens * pairs * 8 + 15) & ~(size_t)15; }
 
 // MODE 0: neighbouring channels are paired (pair = channel / 2).  1: a section's first half with its second half, all
-// halves whole vectors of 8 channels; 2: the same, halves of any size.
-// A wave takes 64 / (d / 8) whole rows at a time, a lane 8 channels; the halves change places through LDS that only the
+// halves whole 16-byte pieces; 2: the same, halves of any size.
+// A wave takes whole rows, a lane 16 bytes of one, kRows of them in flight; the halves change places through LDS that only the
 // wave itself uses, after its loads and before its stores, so a call may work in place.
 template <typename T, int MODE>
 __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int kVec = 8 * Stored<T>::kBytes;
+  constexpr int E = 16 / Stored<T>::kBytes, kRows = 2;   // channels a lane; groups of rows in flight
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int b = blockIdx.y;
   const long long n_end = tokens_of(a.lengths, b, a.N);
@@ -65,9 +65,9 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
   if (n0 >= n_end) return;
   const int tokens = n_end - n0 < a.tokens ? (int)(n_end - n0) : a.tokens;
   f32x2* table = reinterpret_cast<f32x2*>(smem);                       // [tokens][pairs]
-  unsigned char* stage = smem + rope_table_bytes(a.tokens, a.pairs) + (size_t)wave * 64 * kVec;
+  unsigned char* stage = smem + rope_table_bytes(a.tokens, a.pairs) + (size_t)wave * kRows * 1024;
   for (int i = tid; i < tokens * a.pairs; i += 256) {
-    const int t = i / a.pairs, p = i - t * a.pairs;
+    const int t = (unsigned)i / (unsigned)a.pairs, p = i - t * a.pairs;
     int axis = 0;
 #pragma unroll
     for (int s = 1; s < kRopeAxes; ++s)
@@ -78,9 +78,9 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
     table[i] = cs;
   }
   __syncthreads();
-  const int chunks = a.d >> 3, per = 64 / chunks;      // vectors per row, rows per wave and step
-  const int own = lane / chunks, c0 = (lane - own * chunks) * 8;
-  // where this lane's 8 channels stand: the pair of the first, the partner's channel, and the sign of its part
+  const int chunks = a.d / E, per = 64 / chunks;       // pieces per row, rows per wave and step
+  const int own = lane / chunks, c0 = (lane - own * chunks) * E;
+  // where this lane's channels stand: the pair of the first, the partner's channel, and the sign of its part
   int pair = c0 >> 1, partner = 0;
   float sign = 1.0f;
   const bool turned = c0 < a.first[a.axes];
@@ -95,35 +95,48 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
     partner = upper ? c0 - half : c0 + half;
     sign = upper ? 1.0f : -1.0f;
   }
+  auto widen = [](const u32x4& w, float (&x)[E]) {
+    if constexpr (E == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __builtin_bit_cast(f32x4, w)[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) unpack2<T>(w[j], x[2 * j], x[2 * j + 1]);
+    }
+  };
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
     const RopeSide& side = a.side[which];
     if (!side.x) continue;
     const int rows = tokens * side.H, step = 4 * per;
-    for (int r0 = wave * per; r0 < rows; r0 += step) {
-      const int r = r0 + own;
-      const bool on = own < per && r < rows;
-      int t, h;
-      if (side.by_token) { t = (int)((unsigned)r / (unsigned)side.H); h = r - t * side.H; }
-      else { h = (int)((unsigned)r / (unsigned)tokens); t = r - h * tokens; }
-      float x[8], y[8];
-      Raw8<T> raw;
-      if (on) {
-        raw = load8_raw<T>(at<T>(side.x, b * side.xb + h * side.xh + (n0 + t) * side.xn + c0));
-        widen8<T>(raw, x);
-        if constexpr (MODE != 0) {
-          unsigned char* p = stage + lane * kVec;
-          *reinterpret_cast<u32x4*>(p) = raw.w;
-          if constexpr (Stored<T>::kBytes == 4) *reinterpret_cast<u32x4*>(p + 16) = raw.w2;
-        }
+    for (int r0 = wave * per; r0 < rows; r0 += kRows * step) {
+      u32x4 raw[kRows];
+      int t[kRows], h[kRows];
+      bool on[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const int r = r0 + k * step + own;
+        on[k] = own < per && r < rows;
+        if (side.by_token) { t[k] = (int)((unsigned)r / (unsigned)side.H); h[k] = r - t[k] * side.H; }
+        else { h[k] = (int)((unsigned)r / (unsigned)tokens); t[k] = r - h[k] * tokens; }
+        if (on[k]) raw[k] = *reinterpret_cast<const u32x4*>(at<T>(side.x, b * side.xb + h[k] * side.xh + (n0 + t[k]) * side.xn + c0));
       }
-      if constexpr (MODE != 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (LDS that only this wave uses)
-      if (on) {
-        const f32x2* cs = table + t * a.pairs;
+      if constexpr (MODE != 0) {
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+          if (on[k]) *reinterpret_cast<u32x4*>(stage + (k * 64 + lane) * 16) = raw[k];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (LDS that only this wave uses)
+      }
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        if (!on[k]) continue;
+        const f32x2* cs = table + t[k] * a.pairs;
+        float x[E], y[E];
+        widen(raw[k], x);
         if constexpr (MODE == 0) {
           if (turned) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < E / 2; ++j) {
               if (pair + j < a.pairs) {
                 const f32x2 e = cs[pair + j];
                 y[2 * j] = x[2 * j] * e[0] - x[2 * j + 1] * e[1];
@@ -136,18 +149,18 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
           }
         } else if constexpr (MODE == 1) {
           if (turned) {
-            float z[8];
-            load8<T>(stage + (lane + (partner - c0) / 8) * kVec, z);
+            float z[E];
+            widen(*reinterpret_cast<const u32x4*>(stage + (k * 64 + lane + (partner - c0) / E) * 16), z);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < E; ++j) {
               const f32x2 e = cs[pair + j];
               y[j] = x[j] * e[0] + sign * (z[j] * e[1]);
             }
           }
         } else if (turned) {
-          const unsigned char* row = stage + own * chunks * kVec;
+          const unsigned char* row = stage + (k * 64 + own * chunks) * 16;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < E; ++j) {
             const int c = c0 + j;
             y[j] = x[j];
             if (c >= a.first[a.axes]) continue;
@@ -160,7 +173,7 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
             const f32x2 e = cs[(s0 >> 1) + (upper ? o - half : o)];
             const int other = upper ? c - half : c + half;
             float z;
-            if constexpr (Stored<T>::kBytes == 4) {
+            if constexpr (E == 4) {
               z = *reinterpret_cast<const float*>(row + other * 4);
             } else {
               float dummy;
@@ -169,13 +182,12 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
             y[j] = x[j] * e[0] + (upper ? z * e[1] : -(z * e[1]));
           }
         }
-        unsigned char* to = at<T>(side.y, b * side.yb + h * side.yh + (n0 + t) * side.yn + c0);
+        u32x4 out = raw[k];   // channels without a position keep their bits
         if (turned) {
-          store8<T>(to, y);
-        } else {   // channels without a position keep their bits
-          *reinterpret_cast<u32x4*>(to) = raw.w;
-          if constexpr (Stored<T>::kBytes == 4) *reinterpret_cast<u32x4*>(to + 16) = raw.w2;
+          if constexpr (E == 4) out = __builtin_bit_cast(u32x4, f32x4{y[0], y[1], y[2], y[3]});
+          else out = u32x4{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
         }
+        st_stream(reinterpret_cast<u32x4*>(at<T>(side.y, b * side.yb + h[k] * side.yh + (n0 + t[k]) * side.yn + c0)), out);
       }
       if constexpr (MODE != 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }

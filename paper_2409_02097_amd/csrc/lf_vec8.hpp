@@ -28,6 +28,13 @@ template <typename T> LF_DEV Raw8<T> load8_raw(const unsigned char* p) {
   return r;
 }
 
+template <typename T> LF_DEV Raw8<T> none8() {
+  Raw8<T> r;
+  r.w = u32x4{0, 0, 0, 0};
+  if constexpr (Stored<T>::kBytes == 4) r.w2 = u32x4{0, 0, 0, 0};
+  return r;
+}
+
 template <typename T> LF_DEV void widen8(const Raw8<T>& r, float (&x)[8]) {
   if constexpr (Stored<T>::kBytes == 4) {
     const f32x4 a = __builtin_bit_cast(f32x4, r.w), b = __builtin_bit_cast(f32x4, r.w2);

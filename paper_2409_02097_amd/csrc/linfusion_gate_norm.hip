@@ -66,17 +66,21 @@ int check_vectors(int B, int C, long long stride, std::initializer_list<const vo
 
 size_t mod_bytes(int B, int C, long long stride) { return ((size_t)(B - 1) * (size_t)stride + (size_t)C) * 4; }
 
-// Threads per token and tokens per workgroup.  A wave per token where its registers hold it and there are tokens for
-// every wave of the device; a workgroup per token for wide tokens and for few.
+// Threads per token and tokens per workgroup.  A wave per token where its registers hold it (`most_wave` vectors of 8 channels a
+// lane) and there are tokens for every wave of the device; a workgroup per token for wide tokens and for few.  Workgroups per CU:
+// many short ones where a token takes a workgroup, whose start (the modulation of its channels) is small against four tokens or
+// more; fewer where it takes a wave, and in the backward pass, where each leaves partial sums.
 struct Shape { int lanes, vpt, rows, wgs; };
-Shape shape_of(long long tokens, long long N, int C, int most_wave, int wgs_per_cu) {
+Shape shape_of(long long tokens, long long N, int C, int most_wave, int per_cu_wave, int per_cu_whole) {
   Shape s;
   const int vecs = C / 8;
   const long long cus = lfh::num_cu();
   s.lanes = (vecs <= 64 * most_wave && (tokens >= 16 * cus || vecs <= 64)) ? 64 : 256;
   s.vpt = (vecs + s.lanes - 1) / s.lanes;
   const int per = 256 / s.lanes;
-  long long rows = (tokens + cus * wgs_per_cu - 1) / (cus * wgs_per_cu);
+  const long long want = cus * (s.lanes == 64 ? per_cu_wave : per_cu_whole);
+  long long rows = (tokens + want - 1) / want;
+  if (per_cu_whole > 16 && rows < 4 && tokens > 4 * cus) rows = 4;
   rows = (rows + per - 1) / per * per;
   if (rows > N) rows = (N + per - 1) / per * per;
   if (rows > 1 << 20) rows = 1 << 20;
@@ -85,9 +89,9 @@ Shape shape_of(long long tokens, long long N, int C, int most_wave, int wgs_per_
   return s;
 }
 
-constexpr int kFwdWave = 3, kBwdWave = 2;
-Shape fwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, kFwdWave, 8); }
-Shape bwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, kBwdWave, 4); }
+
+Shape fwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, 3, 16, 64); }
+Shape bwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, 2, C <= 512 ? 8 : 4, 2); }
 
 template <typename T, int LANES, int VPT, bool RMS, bool POST>
 int launch_fwd(const lf::GateNormArgs& a, int B, const Shape& s, hipStream_t st) {
@@ -268,10 +272,11 @@ int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, con
                                        : run_bwd<lf::F32>(a, B, s, rms, post, st);
   if (rc != LINFUSION_OK) return rc;
   if (sums) {
-    lf::gate_norm_sums<<<dim3((3 * C + 63) / 64, B), dim3(256), 0, st>>>(partials, total, s.wgs, 3 * C);
-    const lf::GateNormVectors v{total, gate, scale, w_pre, w_post, dgate, dscale, dshift, dw_pre, dw_post,
-                                mod_stride, dmod_stride, B, C, shared};
-    lf::gate_norm_vectors<<<dim3((C + 63) / 64), dim3(64), 0, st>>>(v);
+    const bool over_batch = shared || dw_pre || dw_post;
+    const lf::GateNormVectors v{partials, over_batch ? total : nullptr, gate, scale, w_pre, w_post, dgate, dscale, dshift, dw_pre, dw_post,
+                                mod_stride, dmod_stride, B, C, s.wgs, shared};
+    lf::gate_norm_sums<<<dim3((C + 63) / 64, 3, B), dim3(1024), 0, st>>>(v);
+    if (over_batch) lf::gate_norm_vectors<<<dim3((C + 63) / 64), dim3(64), 0, st>>>(v);
   }
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }

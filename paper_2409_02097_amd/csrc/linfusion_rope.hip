@@ -52,7 +52,7 @@ bool side_by_side(const void* p, const long long sp[3], int Hp, const void* r, c
 }
 
 template <typename T, int MODE> int launch(const lf::RopeArgs& a, int B, unsigned wgs, hipStream_t st) {
-  const int lds = (int)lf::rope_table_bytes(a.tokens, a.pairs) + (MODE != 0 ? 256 * 8 * lf::Stored<T>::kBytes : 0);
+  const int lds = (int)lf::rope_table_bytes(a.tokens, a.pairs) + (MODE != 0 ? 4 * 2 * 1024 : 0);
   auto kernel = lf::rope_rows<T, MODE>;
   if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
   kernel<<<dim3(wgs, B), dim3(256), lds, st>>>(a);
@@ -95,7 +95,7 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
     double rate = scale / 6.283185307179586476925287;
     for (int p = 0; p < c / 2; ++p, rate *= step) a.rate[at / 2 + p] = rate;
     at += c;
-    whole = whole && c % 16 == 0;   // (then every section begins at a multiple of 8 too)
+    whole = whole && c % (dtype == LINFUSION_DTYPE_F32 ? 8 : 16) == 0;   // (then sections begin and halves end at whole 16 bytes)
   }
   for (int i = axes; i <= lf::kRopeAxes; ++i) a.first[i] = at;
   const size_t esz = dtype == LINFUSION_DTYPE_F32 ? 4 : 2;
@@ -136,10 +136,12 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
   a.pairs = at / 2;
   a.axes = axes;
   a.inverse = (flags & LINFUSION_FLAG_ROPE_INVERSE) != 0;
-  // Tokens per workgroup: so many that the angles are a small part of its work and every CU still has several workgroups
+  // Tokens per workgroup: 16 KB of rows, so that the angles are a small part of its work, while every CU has several workgroups
+  // (us per call, 8 / 16 / 32 / 64 KB: bf16 81120 x 2 x 16 x 128 252 / 227 / 233 / 236, fp32 2 x 36503 x 2 x 8 x 40 60 / 57 / 60 / 66)
   const long long heads = H + (k ? H_k : 0), all = (long long)B * N;
   int tokens = 1;
-  while (tokens < 64 && all / (2 * tokens) >= 4LL * lfh::num_cu() && tokens * heads * d < 32768 && 2 * tokens * a.pairs * 8 <= 32768)
+  while (tokens < 64 && all / (2 * tokens) >= 4LL * lfh::num_cu() && tokens * heads * d * (long long)esz < 16384 &&
+         2 * tokens * a.pairs * 8 <= 32768)
     tokens *= 2;
   a.tokens = tokens;
   const long long wgs = (N + tokens - 1) / tokens;

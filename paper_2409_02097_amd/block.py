@@ -82,16 +82,28 @@ def _current_device() -> int:
 
 
 def _rows(name, t, shape, head):
-    """A view of the call's type with contiguous channels."""
+    """The host array of strides of a view of the call's type with contiguous channels."""
     if t.shape != shape or t.dtype is not head[1] or t.get_device() != head[0]:
         raise ValueError(f"{name} must be a {list(shape)} tensor of the call's type and device")
-    if t.stride(-1) != 1 and shape[-1] > 1:
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the channels of a token must be contiguous")
+    return _longs(strides)
 
 
 def _scalars(name, t, shape, head):
     if t.shape != shape or t.dtype is not _types[0] or t.get_device() != head[0]:
         raise ValueError(f"{name} must be an fp32 {list(shape)} tensor on the call's device")
+
+
+def _scalars2(name, t, name2, t2, shape, head):
+    """Two fp32 views that share their strides, whose host array this is."""
+    _scalars(name, t, shape, head)
+    _scalars(name2, t2, shape, head)
+    strides = t.stride()
+    if strides != t2.stride():
+        raise ValueError(f"{name} and {name2} must share their strides")
+    return _longs(strides)
 
 
 def _vector(name, t, shape, head):
@@ -147,10 +159,6 @@ def _doubles(values):
     return (ctypes.c_double * len(values))(*values)
 
 
-def _strides(t):
-    return None if t is None else _longs(t.stride())
-
-
 def linfusion_rope(q, k, q_out, k_out, positions, channels, bases, scales=None, flags: int = 0, lengths=None, stream=None,
                    check: bool = True) -> int:
     """q_out, k_out <- q, k with rotary positions.  q, q_out: [B, H, N, d] views; k, k_out: [B, H_k, N, d] views or None.
@@ -161,12 +169,11 @@ def linfusion_rope(q, k, q_out, k_out, positions, channels, bases, scales=None, 
         raise ValueError("q: [B, H, N, d]; k and k_out come together")
     B, H, N, d = shape = q.shape
     Hk = 0
-    _rows("q", q, shape, head)
-    _rows("q_out", q_out, shape, head)
+    sq, sqo, sk, sko = _rows("q", q, shape, head), _rows("q_out", q_out, shape, head), None, None
     if k is not None:
         Hk = k.shape[1] if k.dim() == 4 else -1
-        _rows("k", k, (B, Hk, N, d), head)
-        _rows("k_out", k_out, (B, Hk, N, d), head)
+        sk = _rows("k", k, (B, Hk, N, d), head)
+        sko = _rows("k_out", k_out, k.shape, head)
     axes = len(channels)
     if len(bases) != axes or (scales is not None and len(scales) != axes):
         raise ValueError("channels, bases and scales have one value per axis")
@@ -179,14 +186,16 @@ def linfusion_rope(q, k, q_out, k_out, positions, channels, bases, scales=None, 
     rc = binding.library().linfusion_rope(
         q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), positions.data_ptr(), axes, _ints(tuple(channels)),
         _doubles(tuple(bases)), None if scales is None else _doubles(tuple(scales)), B, H, Hk, N, d, _dtype_code(q), flags,
-        _ptr(lengths), _strides(q), _strides(k), _strides(q_out), _strides(k_out), _longs(places), _stream_ptr(stream))
+        _ptr(lengths), sq, sk, sqo, sko, _longs(places), _stream_ptr(stream))
     return _done(rc, "linfusion_rope", check)
 
 
+def _plain(t, shape, head) -> bool:
+    return t is None or (t.shape == shape and t.dtype is head[1] and t.is_contiguous() and t.get_device() == head[0])
+
+
 def _strides2(*tensors):
-    """{batch, token} strides of [B, N, C] views, one after the other; None where all are contiguous."""
-    if all(t is None or t.is_contiguous() for t in tensors):
-        return None
+    """{batch, token} strides of [B, N, C] views, one after the other."""
     flat = ()
     for t in tensors:
         flat += (0, 0) if t is None else t.stride()[:2]
@@ -202,17 +211,19 @@ def linfusion_gate_norm_fwd(x, f, gate, scale, shift, y, h, w_pre=None, w_post=N
     if x.dim() != 3:
         raise ValueError("x: [B, N, C]")
     B, N, C = shape = x.shape
-    _rows("x", x, shape, head)
-    for name, t in (("f", f), ("y", y), ("h", h)):
-        if t is not None:
-            _rows(name, t, shape, head)
+    strides = None
+    if not (_plain(x, shape, head) and _plain(f, shape, head) and _plain(y, shape, head) and _plain(h, shape, head)):
+        for name, t in (("x", x), ("f", f), ("y", y), ("h", h)):
+            if t is not None:
+                _rows(name, t, shape, head)
+        strides = _strides2(x, f, y, h)
     stride = _modulation(("gate", "scale", "shift"), (gate, scale, shift), B, C, head) or 0
     _vector("w_pre", w_pre, (C,), head)
     _vector("w_post", w_post, (C,), head)
     _lengths(lengths, B, head)
     rc = binding.library().linfusion_gate_norm_fwd(
         x.data_ptr(), _ptr(f), _ptr(gate), _ptr(scale), _ptr(shift), _ptr(w_pre), _ptr(w_post), _ptr(y), _ptr(h), B, N, C,
-        _dtype_code(x), residual_scale, norm_eps, flags, _ptr(lengths), _strides2(x, f, y, h), stride,
+        _dtype_code(x), residual_scale, norm_eps, flags, _ptr(lengths), strides, stride,
         _stream_ptr(stream))
     return _done(rc, "linfusion_gate_norm_fwd", check)
 
@@ -231,10 +242,13 @@ def linfusion_gate_norm_bwd(x, f, gate, scale, dy, dh, dx=None, df=None, dgate=N
     if x.dim() != 3:
         raise ValueError("x: [B, N, C]")
     B, N, C = shape = x.shape
-    _rows("x", x, shape, head)
-    for name, t in (("f", f), ("dy", dy), ("dh", dh), ("dx", dx), ("df", df)):
-        if t is not None:
-            _rows(name, t, shape, head)
+    rows = (x, f, dy, dh, dx, df)
+    strides = None
+    if not all([_plain(t, shape, head) for t in rows]):
+        for name, t in zip(("x", "f", "dy", "dh", "dx", "df"), rows):
+            if t is not None:
+                _rows(name, t, shape, head)
+        strides = _strides2(*rows)
     stride = _modulation(("gate", "scale"), (gate, scale), B, C, head)
     dstride = _modulation(("dgate", "dscale", "dshift"), (dgate, dscale, dshift), B, C, head)
     if stride is None:
@@ -248,7 +262,7 @@ def linfusion_gate_norm_bwd(x, f, gate, scale, dy, dh, dx=None, df=None, dgate=N
     rc = binding.library().linfusion_gate_norm_bwd(
         x.data_ptr(), _ptr(f), _ptr(gate), _ptr(scale), _ptr(w_pre), _ptr(w_post), _ptr(dy), _ptr(dh), _ptr(dx), _ptr(df),
         _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dw_pre), _ptr(dw_post), B, N, C, _dtype_code(x), residual_scale,
-        norm_eps, flags, _ptr(lengths), _strides2(x, f, dy, dh, dx, df), stride or 0, dstride or 0, _ptr(workspace), _size(workspace),
+        norm_eps, flags, _ptr(lengths), strides, stride or 0, dstride or 0, _ptr(workspace), _size(workspace),
         _stream_ptr(stream))
     return _done(rc, "linfusion_gate_norm_bwd", check)
 
@@ -271,14 +285,9 @@ def _delta_tensors(q, k, v, g, beta):
         raise ValueError("q, k: [B, H_k, N, d_k]; v: [B, H, N, d_v]")
     B, Hk, N, dk = q.shape
     H, dv = v.shape[1], v.shape[3]
-    _rows("q", q, (B, Hk, N, dk), head)
-    _rows("k", k, (B, Hk, N, dk), head)
-    _rows("v", v, (B, H, N, dv), head)
-    _scalars("g", g, (B, H, N), head)
-    _scalars("beta", beta, (B, H, N), head)
-    if g.stride() != beta.stride():
-        raise ValueError("g and beta must share their strides")
-    return head, B, H, Hk, N, dk, dv
+    key = q.shape
+    strides = _rows("q", q, key, head), _rows("k", k, key, head), _rows("v", v, (B, H, N, dv), head), _scalars2("g", g, "beta", beta, (B, H, N), head)
+    return head, strides, B, H, Hk, N, dk, dv
 
 
 def linfusion_delta_fwd(q, k, v, g, beta, out, scale: float = 1.0, state_in=None, state_out=None, lengths=None, saved=None,
@@ -287,8 +296,8 @@ def linfusion_delta_fwd(q, k, v, g, beta, out, scale: float = 1.0, state_in=None
     decays) and beta: fp32 [B, H, N] views with one set of strides, states: contiguous fp32 [B, H, d_k, d_v].  `saved`:
     memory of linfusion_delta_saved_bytes(...) for linfusion_delta_bwd, else `workspace` of
     linfusion_delta_workspace_bytes(...)."""
-    head, B, H, Hk, N, dk, dv = _delta_tensors(q, k, v, g, beta)
-    _rows("out", out, (B, H, N, dv), head)
+    head, (sq, sk, sv, sg), B, H, Hk, N, dk, dv = _delta_tensors(q, k, v, g, beta)
+    so = _rows("out", out, v.shape, head)
     _vector("state_in", state_in, (B, H, dk, dv), head)
     _vector("state_out", state_out, (B, H, dk, dv), head)
     _lengths(lengths, B, head)
@@ -297,8 +306,7 @@ def linfusion_delta_fwd(q, k, v, g, beta, out, scale: float = 1.0, state_in=None
     rc = binding.library().linfusion_delta_fwd(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _ptr(state_in), out.data_ptr(),
         _ptr(state_out), _ptr(lengths), _ptr(saved), _size(saved), B, H, Hk, N, dk, dv, _dtype_code(q), scale, 0,
-        _strides(q), _strides(k), _strides(v), _strides(out), _strides(g), _ptr(workspace), _size(workspace),
-        _stream_ptr(stream))
+        sq, sk, sv, so, sg, _ptr(workspace), _size(workspace), _stream_ptr(stream))
     return _done(rc, "linfusion_delta_fwd", check)
 
 
@@ -306,15 +314,10 @@ def linfusion_delta_bwd(q, k, v, g, beta, dout, dq, dk, dv, dg, dbeta, scale: fl
                         dstate_in=None, lengths=None, saved=None, workspace=None, stream=None, check: bool = True) -> int:
     """The gradients of linfusion_delta_fwd, given those of out and (or None) state_out.  dg and dbeta: fp32 [B, H, N] views with
     one set of strides.  `saved`: what the forward call with the same arguments left there; None forms it again."""
-    head, B, H, Hk, N, d_k, d_v = _delta_tensors(q, k, v, g, beta)
-    _rows("dout", dout, (B, H, N, d_v), head)
-    _rows("dq", dq, (B, Hk, N, d_k), head)
-    _rows("dk", dk, (B, Hk, N, d_k), head)
-    _rows("dv", dv, (B, H, N, d_v), head)
-    _scalars("dg", dg, (B, H, N), head)
-    _scalars("dbeta", dbeta, (B, H, N), head)
-    if dg.stride() != dbeta.stride():
-        raise ValueError("dg and dbeta must share their strides")
+    head, (sq, sk, sv, sg), B, H, Hk, N, d_k, d_v = _delta_tensors(q, k, v, g, beta)
+    sdo = _rows("dout", dout, v.shape, head)
+    sdq, sdk, sdv = _rows("dq", dq, q.shape, head), _rows("dk", dk, q.shape, head), _rows("dv", dv, v.shape, head)
+    sdg = _scalars2("dg", dg, "dbeta", dbeta, (B, H, N), head)
     for name, t in (("state_in", state_in), ("dstate_out", dstate_out), ("dstate_in", dstate_in)):
         _vector(name, t, (B, H, d_k, d_v), head)
     _lengths(lengths, B, head)
@@ -323,9 +326,8 @@ def linfusion_delta_bwd(q, k, v, g, beta, dout, dq, dk, dv, dg, dbeta, scale: fl
     rc = binding.library().linfusion_delta_bwd(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _ptr(state_in), dout.data_ptr(),
         _ptr(dstate_out), _ptr(saved), _size(saved), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dg.data_ptr(),
-        dbeta.data_ptr(), _ptr(dstate_in), _ptr(lengths), B, H, Hk, N, d_k, d_v, _dtype_code(q), scale, 0, _strides(q),
-        _strides(k), _strides(v), _strides(g), _strides(dout), _strides(dq), _strides(dk), _strides(dv),
-        _strides(dg), _ptr(workspace), _size(workspace), _stream_ptr(stream))
+        dbeta.data_ptr(), _ptr(dstate_in), _ptr(lengths), B, H, Hk, N, d_k, d_v, _dtype_code(q), scale, 0, sq, sk, sv, sg, sdo,
+        sdq, sdk, sdv, sdg, _ptr(workspace), _size(workspace), _stream_ptr(stream))
     return _done(rc, "linfusion_delta_bwd", check)
 
 
@@ -338,18 +340,12 @@ def linfusion_delta_step(q, k, v, g, beta, state_in, state_out, out, scale: floa
         raise ValueError("q, k: [B, H_k, d_k]; v: [B, H, d_v]")
     B, Hk, dk = q.shape
     H, dv = v.shape[1:]
-    _rows("q", q, (B, Hk, dk), head)
-    _rows("k", k, (B, Hk, dk), head)
-    _rows("v", v, (B, H, dv), head)
-    _rows("out", out, (B, H, dv), head)
-    _scalars("g", g, (B, H), head)
-    _scalars("beta", beta, (B, H), head)
-    if g.stride() != beta.stride():
-        raise ValueError("g and beta must share their strides")
-    _vector("state_in", state_in, (B, H, dk, dv), head)
-    _vector("state_out", state_out, (B, H, dk, dv), head)
+    key, val, state = q.shape, v.shape, (B, H, dk, dv)
+    sq, sk, sv, so = _rows("q", q, key, head), _rows("k", k, key, head), _rows("v", v, val, head), _rows("out", out, val, head)
+    sg = _scalars2("g", g, "beta", beta, (B, H), head)
+    _vector("state_in", state_in, state, head)
+    _vector("state_out", state_out, state, head)
     rc = binding.library().linfusion_delta_step(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _ptr(state_in), _ptr(state_out),
-        out.data_ptr(), B, H, Hk, dk, dv, _dtype_code(q), scale, 0, _strides(q), _strides(k), _strides(v), _strides(out), _strides(g),
-        _stream_ptr(stream))
+        out.data_ptr(), B, H, Hk, dk, dv, _dtype_code(q), scale, 0, sq, sk, sv, so, sg, _stream_ptr(stream))
     return _done(rc, "linfusion_delta_step", check)

@@ -167,9 +167,13 @@ template <int N> LF_DEV void load_frag(const uint16_t* frag, Terms<N>& t) {
 constexpr int kLdB = 20, kBlock = 16 * kLdB;
 LF_DEV int block_at(int i, int j) { return (i * (i + 1) / 2 + j) * kBlock; }
 
+// Blocks of 32 value channels that pass through LDS at a time: all where a value is one term, two else (fp32 heads of 64 keys and 128
+// values: 68 KB, two workgroups per CU, where all of them make it 95 KB and one).
+template <typename T> LF_DEV_HOST int value_steps(int dvs) { return TermsOf<T>::kStored == 1 || dvs < 2 ? dvs : 2; }
+
 template <typename T> inline int delta_prepare_lds(int dks, int dvs) {
   constexpr int N = TermsOf<T>::kStored;
-  const int values = N * plane_bytes(64, dvs), solve = 10 * kBlock * 4;
+  const int values = N * plane_bytes(64, value_steps<T>(dvs)), solve = 10 * kBlock * 4;
   return N * plane_bytes(64, dks) + solve + (values > solve ? values : solve) + 64 * 8 + kDecayRows * 4 + 64 * 4;
 }
 
@@ -178,7 +182,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
   constexpr int NI = TermsOf<T>::kStored, kLd = 32 * KS + 8, kPlane = 64 * kLd;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int dvs = (a.dvb + 1) / 2, ldv = plane_ld(dvs);
+  const int dvs = (a.dvb + 1) / 2, group = value_steps<T>(dvs), ldv = plane_ld(group);
   double* gamma = reinterpret_cast<double*>(smem);
   float* decay = reinterpret_cast<float*>(gamma + 64);
   float* both = decay + kDecayRows;                             // beta e^gamma
@@ -283,7 +287,10 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
     }
     __syncthreads();
   }
-  stage_terms<T, 256>(v, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n, a.vv.n, w.valid, a.dv, dvs);   // (A is read)
+  auto put_values = [&](int step) {   // (A is read)
+    stage_terms<T, 256>(v, ldv, a.v, w.b * a.vv.b + w.h * a.vv.h + w.n0 * a.vv.n + 32 * step, a.vv.n, w.valid, a.dv - 32 * step, group);
+  };
+  put_values(0);
   // T's rows 16 wave .. + 15 as an operand with a factor per column; nothing behind column 16 wave + 15
   const int steps = wave < 2 ? 1 : 2;
   auto rows_of_t = [&](const float* by, int ks, Terms<3>& f) {
@@ -319,12 +326,18 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
   if (steps > 1) rows_of_t(decay + kDecayBeta, 1, ft[1]);
   __syncthreads();
   for (int vb = 0; vb < a.dvb; ++vb) {
+    const int at_vb = vb % (2 * group);
+    if (vb > 0 && at_vb == 0) {
+      __syncthreads();
+      put_values(vb / 2);
+      __syncthreads();
+    }
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       if (ks >= steps) continue;
       Terms<NI> val;
-      terms_across<NI>(v + 32 * ks * ldv + 16 * vb, 64 * ldv, ldv, val);
+      terms_across<NI>(v + 32 * ks * ldv + 16 * at_vb, 64 * ldv, ldv, val);
       acc = mul_terms<3>(val, ft[ks], acc);
     }
     *reinterpret_cast<f32x4*>(part<float>(rec, a.at_u) + ((vb * 4 + wave) * 64 + lane) * 4) = acc;
@@ -581,7 +594,7 @@ constexpr int kOutBlocks = 4;   // of 16 value channels at a time
 
 template <typename T> inline int delta_out_lds(int dks) {
   constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut;
-  const int rows = 2 * NI * plane_bytes(64, dks) + NO * 64 * kLdP * 2;
+  const int keys = NI * plane_bytes(64, dks), scores = NO * 64 * kLdP * 2, rows = keys + (keys > scores ? keys : scores);
   const int later = kOutBlocks * NO * (plane_bytes(16, dks) + 64 * kLdU * 2);
   return (rows > later ? rows : later) + 64 * 8 + 2 * 64 * 4;
 }
@@ -596,7 +609,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
   float* decay = reinterpret_cast<float*>(gamma + 64);   // e^gamma, beta
   uint16_t* q = reinterpret_cast<uint16_t*>(decay + 128);
   uint16_t* k = q + NI * 64 * kLd;
-  uint16_t* pp = k + NI * 64 * kLd;
+  uint16_t* pp = k;                                      // where the keys were
   uint16_t* sp = q;                                      // later, where all of these were
   uint16_t* up = sp + kOutBlocks * NO * kSPlane;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
@@ -631,6 +644,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) terms_near<NI>(q + (16 * wave + col) * kLd + 32 * ks + g8, 64 * kLd, fq[ks]);
   // P's rows of this wave, four neighbouring columns j of row i at a time; 0 where beta_j is 0 (the u_j that is kept is not)
+  f32x4 scores[4];
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt) {
     f32x4 acc = {0, 0, 0, 0};
@@ -648,8 +662,11 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
         acc[r] = on ? acc[r] * decay_between(gamma, i, j) : 0.0f;
       }
     }
-    split4_lds<NO>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, acc);
+    scores[jt] = acc;
   }
+  __syncthreads();   // the keys are read
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt) split4_lds<NO>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, scores[jt]);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (rows that only this wave writes and reads)
   Terms<NO> fp[2];
 #pragma unroll

@@ -24,8 +24,8 @@ namespace lf {
 // ---- what does not depend on the chunk behind ---------------------------------------------------------------------------------
 template <typename T> inline int delta_back_prepare_lds(int dks, int dvs) {
   constexpr int NI = TermsOf<T>::kStored;
-  const int keys = NI * plane_bytes(64, dks), out = NI * plane_bytes(64, dvs);
-  return 64 * 8 + 64 * 4 + 3 * 64 * kLdP * 2 + (2 * keys > out ? 2 * keys : out);
+  const int keys = NI * plane_bytes(64, dks), out = NI * plane_bytes(64, value_steps<T>(dvs)), scores = 3 * 64 * kLdP * 2;
+  return 64 * 8 + 64 * 4 + (keys > out ? keys : out) + (keys > scores ? keys : scores);
 }
 
 template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_prepare(DeltaArgs a) {
@@ -33,13 +33,13 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
   constexpr int NI = TermsOf<T>::kStored, ld = 32 * KS + 8, plane = 64 * ld, kOwn = (2 * KS + 3) / 4;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
-  const int dvs = (a.dvb + 1) / 2, ldo = plane_ld(dvs);
+  const int dvs = (a.dvb + 1) / 2, group = value_steps<T>(dvs), ldo = plane_ld(group);
   double* gamma = reinterpret_cast<double*>(smem);
   float* since = reinterpret_cast<float*>(gamma + 64);
-  uint16_t* pp = reinterpret_cast<uint16_t*>(since + 64);
-  uint16_t* q = pp + 3 * 64 * kLdP;
-  uint16_t* k = q + NI * plane;
-  uint16_t* o = q;                      // where q and k were
+  uint16_t* q = reinterpret_cast<uint16_t*>(since + 64);
+  uint16_t* o = q;                      // where the queries were
+  uint16_t* k = q + NI * (ld > ldo ? plane : 64 * ldo);
+  uint16_t* pp = k;                     // where the keys were
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   unsigned char *rec = a.rec(w.bh, blockIdx.x), *rec_b = a.rec_b(w.bh, blockIdx.x);
@@ -63,6 +63,8 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
     }
   }
   // P transposed, [j][i]: four neighbouring rows i of column j at a time; rows i of tile `it`, columns of this wave's
+  f32x4 scores[4];
+#pragma unroll
   for (int it = 0; it < 4; ++it) {
     f32x4 acc = {0, 0, 0, 0};
     if (it >= wave) {
@@ -79,10 +81,9 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
         acc[r] = j <= i ? acc[r] * decay_between(gamma, i, j) : 0.0f;
       }
     }
-    split4_lds<3>(pp + (16 * wave + col) * kLdP + 16 * it + row4, 64 * kLdP, acc);
+    scores[it] = acc;
   }
   // (e^gamma Q)^T as operands of this wave's channel blocks, before the queries make room: scaled, then split again
-  __syncthreads();
   Terms<3> fq[kOwn][2];   // channel blocks wave, wave + 4, ...
 #pragma unroll
   for (int t = 0; t < kOwn; ++t)
@@ -108,16 +109,27 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
       }
       split8(y, fq[t][ks]);
     }
+  __syncthreads();   // queries and keys are read
+#pragma unroll
+  for (int it = 0; it < 4; ++it) split4_lds<3>(pp + (16 * wave + col) * kLdP + 16 * it + row4, 64 * kLdP, scores[it]);
+  auto put_gradients = [&](int step) {
+    stage_terms<T, 256>(o, ldo, a.dout, w.b * a.vdo.b + w.h * a.vdo.h + w.n0 * a.vdo.n + 32 * step, a.vdo.n, w.valid, a.dv - 32 * step, group);
+  };
+  put_gradients(0);
   __syncthreads();
-  stage_terms<T, 256>(o, ldo, a.dout, w.b * a.vdo.b + w.h * a.vdo.h + w.n0 * a.vdo.n, a.vdo.n, w.valid, a.dv, dvs);
   Terms<3> fp[2];      // P^T's rows j of this wave
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) terms_near<3>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
-  __syncthreads();
   for (int vb = 0; vb < a.dvb; ++vb) {
+    const int at_vb = vb % (2 * group);
+    if (vb > 0 && at_vb == 0) {
+      __syncthreads();
+      put_gradients(vb / 2);
+      __syncthreads();
+    }
     Terms<NI> fo[2];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) terms_across<NI>(o + 32 * ks * ldo + 16 * vb, 64 * ldo, ldo, fo[ks]);
+    for (int ks = 0; ks < 2; ++ks) terms_across<NI>(o + 32 * ks * ldo + 16 * at_vb, 64 * ldo, ldo, fo[ks]);
     f32x4 acc = {0, 0, 0, 0};   // rows: value channels, columns: tokens j
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) acc = mul_terms<3>(fo[ks], fp[ks], acc);

@@ -5,6 +5,8 @@
 
 namespace lf {
 
+#define LF_DEV_HOST __host__ __device__ __forceinline__
+
 struct F32 {};   // tag: IEEE binary32 storage
 
 template <typename T> struct Stored { static constexpr int kBytes = 2; };

@@ -56,10 +56,10 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->at_kn = u;
   z->at_ds = z->at_kn + 4 * z->dks * terms * frag;
   z->record_b = up(z->at_ds + state);
-  // Runs: as many as fill the device twice over with workgroups of the second pass, of 16 chunks at least; each costs delta_join
-  // a step of a few us, and the first pass does (d_k + d_v) / d_v times the work of the second.
+  // Runs: as many as give every CU a workgroup of the second pass, of 16 chunks at least; each costs delta_join a step
+  // of 1.6 us, and the first pass does (d_k + d_v) / d_v times the work of the second.
   const long long scans = z->heads * ((z->dvb + 1) / 2);
-  long long runs = lfh::env_int("LINFUSION_DELTA_RUNS", 1) > 1 ? lfh::env_int("LINFUSION_DELTA_RUNS", 1) : lfh::num_cu() / scans;
+  long long runs = lfh::num_cu() / scans;
   if (runs > z->nc / 16) runs = z->nc / 16;
   if (runs > 32) runs = 32;
   if (runs < 3) runs = 1;

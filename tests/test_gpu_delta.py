@@ -344,3 +344,57 @@ def test_long_sequences_of_few_heads_in_runs(dtype, dk, dv):
             t[b, :, n:] = 0.0
     check_forward(c, out, last)
     check_backward(c, d)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_heads(dtype):
+    """Enough heads for 32 value channels a workgroup, an odd number of 16s among them."""
+    c = make(16, 8, 8, 70, 16, 40, dtype, seed=61)
+    g = on_gpu(c)
+    out, last, saved = forward(c, g, saved=True)
+    check_forward(c, out, last)
+    check_backward(c, backward(c, g, saved))
+
+
+def test_runs_of_many_heads():
+    """Runs whose first pass takes 32 channels a workgroup too."""
+    B, H, N, d = 1, 8, 64 * 220 - 7, 32
+    c = make(B, H, H, N, d, d, "bf16", seed=62)
+    g = on_gpu(c)
+    out, last, _ = forward(c, g)
+    ref = np.zeros((B, H, N, d))
+    s = np.array(c["state"])
+    for t in range(N):   # (all heads at once; the states of all tokens would be a gigabyte)
+        key, qry = c["k"][:, :, t], c["q"][:, :, t]
+        s *= np.exp(c["g"][:, :, t])[..., None, None]
+        u = c["beta"][:, :, t, None] * (c["v"][:, :, t] - np.matmul(key[:, :, None], s)[:, :, 0])
+        s += key[..., None] * u[:, :, None]
+        ref[:, :, t] = c["scale"] * np.matmul(qry[:, :, None], s)[:, :, 0]
+    check(out, ref, "bf16", chain(c), "out")
+    check(last, s, "f32", chain(c), "state")
+
+
+def test_two_graphs_that_share_a_workspace_and_a_stream_of_their_own():
+    cases = [make(2, 4, 2, 130, 40, 56, "bf16", seed=71), make(2, 4, 2, 130, 40, 56, "bf16", seed=72)]
+    gs = [on_gpu(c) for c in cases]
+    want = [forward(c, g) for c, g in zip(cases, gs)]
+    ws = torch.empty(lf.linfusion_delta_workspace_bytes(2, 4, 2, 130, 40, 56, CODE["bf16"]), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty_like(w[0]) for w in want]
+    call = lambda i, **kw: lf.linfusion_delta_fwd(*(gs[i][n] for n in ("q", "k", "v", "g", "beta")), outs[i], scale=cases[i]["scale"],
+                                                  state_in=gs[i]["state"], workspace=ws, **kw)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    call(0, stream=side)          # named, not current
+    side.synchronize()
+    assert torch.equal(outs[0], want[0][0])
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            call(i)
+    for _ in range(3):
+        for i in (0, 1, 1, 0):
+            outs[i].fill_(float("nan"))
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i][0])

@@ -414,8 +414,9 @@ template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(2
   for (int e = 0; e < COLS; ++e)
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      if (!PARTIAL && run > 0) {
-        s[e][t] = *reinterpret_cast<const f32x4*>(a.joined + ((((long long)bh * a.runs + run) * a.dvb + slice[e]) * a.dkb + blk[t]) * 256 + lane * 4);
+      float* joined = a.joined + ((((long long)bh * a.runs + run) * a.dvb + slice[e]) * a.dkb + blk[t]) * 256 + lane * 4;
+      if (!PARTIAL && a.runs > 1) {
+        s[e][t] = *reinterpret_cast<const f32x4*>(joined);
         continue;
       }
 #pragma unroll
@@ -424,6 +425,8 @@ template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(2
         if (unit[e]) s[e][t][r] = row == (slice[e] - a.dvb) * 16 + col ? 1.0f : 0.0f;
         else s[e][t][r] = a.state_in && run == 0 && row < a.dk && ch < a.dv ? a.state_in[((long long)bh * a.dk + row) * a.dv + ch] : 0.0f;
       }
+      // (the second pass takes the first run's from here too: another run of it may have written over `state_in` by then)
+      if (PARTIAL && run == 0 && !unit[e]) *reinterpret_cast<f32x4*>(joined) = s[e][t];
     }
   for (int i = tid; i < 3 * kPlane / 8; i += 256) reinterpret_cast<u32x4*>(sp)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();

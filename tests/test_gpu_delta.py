@@ -398,3 +398,15 @@ def test_two_graphs_that_share_a_workspace_and_a_stream_of_their_own():
             graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(outs[i], want[i][0])
+
+
+def test_runs_with_the_state_in_place():
+    """Rows that end in the first run, just behind it and in the last one: whichever run writes the state, the first has read it."""
+    N, lengths = 64 * 70, [64 * 70, 64 * 18 + 1, 64 * 17, 64 * 16, 64, 1, 0, 64 * 40]
+    c = make(8, 1, 1, N, 32, 48, "bf16", seed=81, lengths=lengths)
+    g = on_gpu(c)
+    out, last, mem = forward(c, g)
+    again, state = torch.zeros_like(out), g["state"].clone()
+    lf.linfusion_delta_fwd(*(g[n] for n in ("q", "k", "v", "g", "beta")), again, scale=c["scale"], state_in=state, state_out=state,
+                           lengths=g["lengths"], workspace=mem)
+    assert torch.equal(again, out) and torch.equal(state, last)

@@ -102,12 +102,15 @@ LF_DEV f32x4 rows_near(const float* p, int ld) {
   return f32x4{r[0], r[ld], r[2 * ld], r[3 * ld]};
 }
 
-// Four neighbouring channels.
-template <typename T> LF_DEV f32x4 load4(const unsigned char* p) {
+// Four neighbouring channels, as they are stored and widened.
+template <typename T> struct Raw4Of { using type = u32x2; };
+template <> struct Raw4Of<F32> { using type = f32x4; };
+template <typename T> using Raw4 = typename Raw4Of<T>::type;
+template <typename T> LF_DEV Raw4<T> load4_raw(const unsigned char* p) { return *reinterpret_cast<const Raw4<T>*>(p); }
+template <typename T> LF_DEV f32x4 widen4(const Raw4<T>& w) {
   if constexpr (Stored<T>::kBytes == 4) {
-    return *reinterpret_cast<const f32x4*>(p);
+    return w;
   } else {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
     float a, b, c, d;
     unpack2<T>(w[0], a, b);
     unpack2<T>(w[1], c, d);

@@ -283,7 +283,7 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
 // ---- the gradients ------------------------------------------------------------------------------------------------------------
 // Formed transposed (rows: channels, columns: tokens).  Eight waves: wave w takes tokens 16 (w % 4) .. + 15 and one half of the
 // channels.  32 value channels at a time pass through LDS: dU (then dV in its place), dO, U as [token][channel], S0 and dS1 as
-// [channel][key channel]; what comes next is requested a round ahead, keys and queries at the start.
+// [channel][key channel]; what comes next is requested a round ahead, keys and queries behind the last one.
 constexpr int kLdV = 40;
 
 template <typename T> inline int delta_gradients_lds(int dks) {
@@ -296,7 +296,21 @@ template <typename T> inline int delta_gradients_lds(int dks) {
 // sum over the four lanes of a wave that share l % 16
 LF_DEV float groups_sum(float v) { return swap_add<32>(swap_add<16>(v)); }
 
-template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) void delta_gradients(DeltaArgs a) {
+// The same value, as far as the compiler can see another: what follows from it is computed where it is used and not kept in
+// registers through a loop.
+template <typename X> LF_DEV X again(X x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Two workgroups per CU, which leaves 128 registers a lane, where the planes are small enough and no sums over heads are held: a
+// workgroup is a chain of barriers.  4096 tokens of 96 heads of 40 channels, bf16: 281 us against 344 with one workgroup
+// and 203 registers; with the sums (2 rows, 16 value heads, 4 key heads, 64 channels) 148 against 122, the rest in scratch memory.
+template <typename T, int KS, bool SHARED> constexpr int gradients_waves() {   // per SIMD
+  return !SHARED && KS <= 2 && TermsOf<T>::kStored < 3 ? 4 : 2;
+}
+
+template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gradients_waves<T, KS, SHARED>())) void delta_gradients(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NI = TermsOf<T>::kStored, kLd = 32 * KS + 8, kVPlane = 64 * kLdV, kSPlane = 32 * kLd, kPPlane = 64 * kLdP;
   constexpr int kOwn = (2 * KS + 3) / 4;
@@ -342,21 +356,20 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
     const DeltaAt w(a, b * a.H + hk * group + member, blockIdx.x);
     unsigned char *rec = a.rec(w.bh, blockIdx.x), *rec_b = a.rec_b(w.bh, blockIdx.x);
     const float* ds = part<float>(a.rec_b(w.bh, blockIdx.x + 2), a.at_ds);
-    // requested in the order in which they are waited for: (T beta)^T's rows of this wave (nothing before them), decays, ...
-    Raw8<F32> tt[2];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      if (2 * ks + 1 >= wave) tt[ks] = load8_raw<F32>(rec + a.at_tt + ((wave < 2 ? 2 * wave + ks : 2 + wave) * 64 + lane) * 32);
+    // requested in the order in which they are waited for: the decays, ...
     double gamma_in = 0.0;
     float decay_in = 0.0f;
     if (tid < kDecayRows) decay_in = part<float>(rec, a.at_decay)[tid];
     else if (wave8 == 4) gamma_in = part<double>(rec, a.at_decay + kDecayRows * 4)[lane];
     // ... 16 value channels of this wave's tokens, and row blocks wave, wave + 4, ... of S0 and dS1: block vb + half
-    f32x4 du, u, o, v, s0[kOwn], d1[kOwn];
+    f32x4 du, u, s0[kOwn], d1[kOwn];
+    Raw4<T> o, v;
     auto request = [&](int vb) {
       const f32x4 none = {0, 0, 0, 0};
+      const int lane = again(tid & 63), row4 = (lane >> 4) * 4, n = 16 * wave + (lane & 15);
       const int ch = 16 * vb + row4;
-      du = u = o = v = none;
+      du = u = none;
+      o = v = Raw4<T>{};
 #pragma unroll
       for (int t = 0; t < kOwn; ++t) s0[t] = d1[t] = none;
       if (vb >= a.dvb) return;
@@ -364,8 +377,8 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
       du = *reinterpret_cast<const f32x4*>(part<float>(rec_b, 0) + at4);
       u = *reinterpret_cast<const f32x4*>(part<float>(rec, a.at_u) + at4);
       if (on && ch < a.dv) {
-        o = load4<T>(at<T>(a.dout, w.b * a.vdo.b + w.h * a.vdo.h + (w.n0 + n) * a.vdo.n + ch));
-        v = load4<T>(at<T>(a.v, w.b * a.vv.b + w.h * a.vv.h + (w.n0 + n) * a.vv.n + ch));
+        o = load4_raw<T>(at<T>(a.dout, w.b * a.vdo.b + w.h * a.vdo.h + (w.n0 + n) * a.vdo.n + ch));
+        v = load4_raw<T>(at<T>(a.v, w.b * a.vv.b + w.h * a.vv.h + (w.n0 + n) * a.vv.n + ch));
       }
 #pragma unroll
       for (int t = 0; t < kOwn; ++t) {
@@ -376,19 +389,6 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
       }
     };
     request(half);
-    // and keys and queries at the end
-    if (member == 0) {
-      keys.request(a.k, b * a.vk.b + hk * a.vk.h + any.n0 * a.vk.n, a.vk.n, any.valid, a.dk);
-      queries.request(a.q, b * a.vq.b + hk * a.vq.h + any.n0 * a.vq.n, a.vq.n, any.valid, a.dk);
-    }
-    Terms<3> ft[2];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      if (2 * ks + 1 < wave) continue;
-      float y[8];
-      widen8<F32>(tt[ks], y);
-      split8(y, ft[ks]);
-    }
     __syncthreads();   // (the member before has been read)
     if (tid < kDecayRows) decay[tid] = decay_in;
     else if (wave8 == 4) gamma[lane] = gamma_in;
@@ -403,10 +403,12 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
     const float beta = decay[kDecayBeta + n], per_beta = 1.0f / beta;
     const bool none = beta == kDeltaTinyBeta;
     for (int vb = 0; vb < a.dvb; vb += 2) {
+      const int lane = again(tid & 63), col = lane & 15, row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8, n = 16 * wave + col;
+      const bool on = n < any.valid;
       const int ch = 16 * (vb + half) + row4;
       split4_lds<3>(pv + n * kLdV + 16 * half + row4, kVPlane, du);
       split4_lds<3>(pu + n * kLdV + 16 * half + row4, kVPlane, none ? f32x4{0, 0, 0, 0} : u);
-      split4_lds<NI>(po + n * kLdV + 16 * half + row4, kVPlane, o);
+      split4_lds<NI>(po + n * kLdV + 16 * half + row4, kVPlane, widen4<T>(o));
 #pragma unroll
       for (int t = 0; t < kOwn; ++t) {
         const int kb = wave + 4 * t;
@@ -415,26 +417,38 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
         split4_lds<3>(pd + (16 * half + col) * kLd + 16 * kb + row4, kSPlane, d1[t]);
         ss += (d1[t][0] * s0[t][0] + d1[t][1] * s0[t][1]) + (d1[t][2] * s0[t][2] + d1[t][3] * s0[t][3]);
       }
-      const f32x4 u_now = u, v_now = v;
-      if (vb + 2 < a.dvb) request(vb + 2 + half);
+      // (T beta)^T's rows of this wave, nothing before them
+      auto tt_at = [&](int ks) { return load8_raw<F32>(rec + a.at_tt + ((wave < 2 ? 2 * wave + ks : 2 + wave) * 64 + lane) * 32); };
+      Raw8<F32> tt[2];
+      tt[0] = tt_at(0);   // (waves without one: the other again)
+      tt[1] = tt_at(1);
+      const f32x4 u_now = u;
+      const Raw4<T> v_raw = v;
       lds_barrier();
       f32x4 dv = {0, 0, 0, 0};
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        if (2 * ks + 1 < wave) continue;
-        Terms<3> f;
+      for (int ks = 1; ks >= 0; --ks) {
+        if (ks == 0 && wave > 1) continue;
+        Terms<3> f, ft;
+        float y[8];
+        widen8<F32>(tt[ks], y);
+        split8(y, ft);
         terms_across<3>(pv + 32 * ks * kLdV + 16 * half, kVPlane, kLdV, f);
-        dv = mul_terms<3>(f, ft[ks], dv);
+        dv = mul_terms<3>(f, ft, dv);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const f32x4 per = (dv * per_beta) * (u_now * per_beta);
+      const float by = again(per_beta);
+      const f32x4 per = (dv * by) * (u_now * by);
       dbeta += (per[0] + per[1]) + (per[2] + per[3]);
       if (none) dv = f32x4{0, 0, 0, 0};
       if (on && ch < a.dv) {
+        const f32x4 v_now = widen4<T>(v_raw);
         vdv += (double)(v_now[0] * dv[0] + v_now[1] * dv[1]) + (double)(v_now[2] * dv[2] + v_now[3] * dv[3]);
         store4<T>(at<T>(a.dv_out, w.b * a.vdv.b + w.h * a.vdv.h + (w.n0 + n) * a.vdv.n + ch), dv);
       }
       lds_barrier();   // dU is read
       split4_lds<3>(pv + n * kLdV + 16 * half + row4, kVPlane, dv);
+      if (vb + 2 < a.dvb) request(vb + 2 + half);
       lds_barrier();
       Terms<3> fv, fu;
       Terms<NI> fo;
@@ -463,6 +477,8 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512) voi
       }
       lds_barrier();   // the planes are read
     }
+    keys.request(a.k, b * a.vk.b + hk * a.vk.h + any.n0 * a.vk.n, a.vk.n, any.valid, a.dk);
+    queries.request(a.q, b * a.vq.b + hk * a.vq.h + any.n0 * a.vq.n, a.vq.n, any.valid, a.dk);
     const float since = decay[kDecaySince + n], write = decay[kDecayWrite + n];
 #pragma unroll
     for (int i = 0; i < KS; ++i) {

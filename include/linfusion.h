@@ -447,7 +447,7 @@ int linfusion_attn_state(const void* k, const void* v, float* state_out,
  *   q, q_out        [B, H, N, d] views; k, k_out: [B, H_k, N, d] views, or both NULL.  q_out == q (k_out == k) with the same
  *                   strides works in place; else an output must not overlap an input.  Views whose spans interleave
  *                   (columns of one projection) are accepted where their rows lie side by side in each token.
- *   d               multiple of 8 up to 256.  axes: 1 .. 4.  channels, bases, scales: HOST arrays of `axes` values;
+ *   N               < 2^28.  d: multiple of 8 up to 256.  axes: 1 .. 4.  channels, bases, scales: HOST arrays of `axes` values;
  *                   channels even, positive, in all at most d; bases > 0; scales NULL = 1.
  *   positions       DEVICE int32, element {b, a, n} at b * position_strides[0] + a * position_strides[1] + n; NULL strides:
  *                   {0, N}, one [axes, N] table for the whole batch.
@@ -514,6 +514,7 @@ size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C);
  *   saved           NULL, or DEVICE memory of linfusion_delta_saved_bytes that keeps what linfusion_delta_bwd needs again.
  *   flags           0.
  *   workspace       DEVICE scratch of linfusion_delta_workspace_bytes, 16-byte aligned; not used when `saved` is given.
+ * Tokens are taken in chunks of 64: an infinity or NaN in one may reach every output of its chunk, and reaches those behind.
  * No output may overlap another buffer, apart from state_out == state_in.
  */
 int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float* g, const float* beta,

@@ -164,6 +164,9 @@ template <int N> LF_DEV void load_frag(const uint16_t* frag, Terms<N>& t) {
 }
 
 // ---- the operands and U0 of every chunk -----------------------------------------------------------------------------------
+// 10 heads of 64 channels, 65536 tokens, bf16: 139 to 176 us for 25 MB read and 500 MB of records written (3 to 3.6 TB/s); 96 heads of
+// 40, 4096 tokens, with what the backward pass needs: 120 us, 450 MB (3.8 TB/s).
+//
 // A lower triangular matrix of 64 rows in LDS as its ten 16 x 16 blocks on and below the diagonal (fp32, 20 floats a row: both operand
 // forms are free of bank conflicts): 13 KB, so that four workgroups of heads up to 64 fit a CU's LDS beside their keys.  What
 // bounds the kernel is its chain of dependent small steps, so workgroups per CU are what counts.
@@ -171,7 +174,7 @@ constexpr int kLdB = 20, kBlock = 16 * kLdB;
 LF_DEV int block_at(int i, int j) { return (i * (i + 1) / 2 + j) * kBlock; }
 
 // Blocks of 32 value channels that pass through LDS at a time: all where a value is one term, two else (fp32 heads of 64 keys and 128
-// values: 68 KB, two workgroups per CU, where all of them make it 95 KB and one).
+// values: 68 KB, two workgroups per CU, 18.8 us for 3 x 8 heads of 1000 tokens; all of them make it 95 KB, one, and 28.5 us).
 template <typename T> LF_DEV_HOST int value_steps(int dvs) { return TermsOf<T>::kStored == 1 || dvs < 2 ? dvs : 2; }
 
 template <typename T> inline int delta_prepare_lds(int dks, int dvs) {
@@ -365,13 +368,16 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
 // wave, wave + 4, ... as accumulators and compute 16 tokens of U each.  Bound: with few workgroups the chain from one chunk's
 // state to the next (two products, two passes through LDS; what it reads is requested two chunks ahead where registers
 // allow it), with many the operands' way from the L2, which every slice of a head reads anew: hence 32 channels where there
-// are enough of them.
+// are enough of them.  10 heads of 64 channels, 65536 tokens, bf16, in 12 runs: 184 us, 2.1 us a chunk (the first pass 196 us with two
+// workgroups on most CUs); 96 heads of 40, 4096 tokens: 113 us, 1.8 us a chunk.  64 channels a workgroup were slower.
 //
 // With fewer workgroups than the device has room for, a head's chunks are parted into runs.  A run turns the state it starts
 // from into M S + R with a d_k x d_k matrix M of its own: a first pass (PARTIAL) takes zeros and the columns of the identity
 // through every run at once, delta_join takes the state through the runs, and the second pass starts each from its state.
 template <int NI, int KS, int COLS> struct ScanIn {
   static constexpr int kBlocks = (2 * KS + 3) / 4;
+  // chunks in flight and in work: three where the registers hold them (the first pass over 65536 tokens of 10 heads of 64, bf16: 185 us
+  // against 193 with two; the others are the same)
   static constexpr int kDepth = 12 * KS + 8 * NI * kBlocks + 4 * COLS <= 114 ? 3 : 2;
   Terms<3> w[KS];
   Terms<NI> kt[kBlocks][2];
@@ -558,44 +564,90 @@ template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(2
   }
 }
 
-// The state that each run starts from, 16 value channels of one head: the first run's end, then M S + R run by run.  M's column k
-// is a partial state's column k: the operand gathers its four steps from four lanes' accumulators.
+// The state that each run starts from, 16 value channels of one head: the first run's end, then M S + R run by run, in fp32 products.
+// M's column k is a partial state's column k: the operand gathers its four steps from four lanes' accumulators.  A chain too, so what
+// later runs need is requested ahead: 0.75 us a run for states of 64 x 64 (1.6 without), 3 for 128 x 128.
+template <int KS> struct JoinIn {
+  static constexpr int kBlocks = (2 * KS + 3) / 4, kDepth = KS <= 2 ? 4 : 2;
+  f32x4 r[kBlocks], m[kBlocks][2 * KS];
+};
+
 template <int KS> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a) {
-  constexpr int kBlocks = (2 * KS + 3) / 4;
+  using In = JoinIn<KS>;
+  constexpr int kBlocks = In::kBlocks;
   __shared__ __align__(16) float sl[32 * KS * kLdB];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
-  const int row4 = (lane >> 4) * 4, slice = blockIdx.x, bh = blockIdx.y, slices = a.dvb + a.dkb;
-  f32x4 s[kBlocks];
-  for (int run = 0; run + 1 < a.runs; ++run) {
-    const float* part = a.parts + ((long long)bh * a.runs + run) * slices * a.dkb * 256;
+  const int row4 = (lane >> 4) * 4, slice = blockIdx.x, bh = blockIdx.y, slices = a.dvb + a.dkb, last = a.runs - 2;
+  int blk[kBlocks];   // (as in delta_scan)
+#pragma unroll
+  for (int t = 0; t < kBlocks; ++t) blk[t] = wave + 4 * t < a.dkb ? wave + 4 * t : a.dkb - 1;
+  const int step = slices * a.dkb * 256;
+  const float* ahead = a.parts + (long long)bh * a.runs * step;
+  int requested = 0;
+  auto request = [&](In& n) {
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      const int mb = wave + 4 * t;
-      if (mb >= a.dkb) continue;
-      f32x4 acc = *reinterpret_cast<const f32x4*>(part + (slice * a.dkb + mb) * 256 + lane * 4);
-      if (run > 0) {
-        for (int kb = 0; kb < a.dkb; ++kb) {
-          const float* m = part + ((a.dvb + kb) * a.dkb + mb) * 256 + (row4 + 16 * (col >> 2)) * 4 + (col & 3);
-          acc = mfma_block(f32x4{m[0], m[4], m[8], m[12]}, rows_near(sl + 16 * kb * kLdB, kLdB), acc);
-        }
+      n.r[t] = *reinterpret_cast<const f32x4*>(ahead + (slice * a.dkb + blk[t]) * 256 + lane * 4);
+#pragma unroll
+      for (int kb = 0; kb < 2 * KS; ++kb) {
+        const int k = kb < a.dkb ? kb : a.dkb - 1;
+        const float* m = ahead + ((a.dvb + k) * a.dkb + blk[t]) * 256 + (row4 + 16 * (col >> 2)) * 4 + (col & 3);
+        n.m[t][kb] = f32x4{m[0], m[4], m[8], m[12]};
       }
-      s[t] = acc;
     }
-    __syncthreads();
+    ahead += requested++ < last ? step : 0;   // (the last one again behind the end)
+  };
+  float* to = a.joined + (((long long)bh * a.runs + 1) * a.dvb + slice) * a.dkb * 256 + lane * 4;
+  auto join = [&](int run, const In& in, In& next) {
+    request(next);
+    f32x4 s[kBlocks];
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
-      const int mb = wave + 4 * t;
-      if (mb >= a.dkb) continue;
+      s[t] = in.r[t];
+      if (run == 0) continue;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sl[(16 * mb + row4 + r) * kLdB + col] = s[t][r];
-      *reinterpret_cast<f32x4*>(a.joined + ((((long long)bh * a.runs + run + 1) * a.dvb + slice) * a.dkb + mb) * 256 + lane * 4) = s[t];
+      for (int kb = 0; kb < 2 * KS; ++kb)
+        if (kb < a.dkb) s[t] = mfma_block(in.m[t][kb], rows_near(sl + 16 * kb * kLdB, kLdB), s[t]);
     }
-    __syncthreads();
+    lds_barrier();
+#pragma unroll
+    for (int t = 0; t < kBlocks; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sl[(16 * blk[t] + row4 + r) * kLdB + col] = s[t][r];
+      *reinterpret_cast<f32x4*>(to + blk[t] * 256) = s[t];
+    }
+    to += a.dvb * a.dkb * 256;
+    lds_barrier();
+  };
+  In x, y;
+  request(x);
+  if constexpr (In::kDepth == 4) {
+    In z, w;
+    request(y);
+    request(z);
+    int run = 0;
+    for (; run + 3 <= last; run += 4) {
+      join(run, x, w);
+      join(run + 1, y, x);
+      join(run + 2, z, y);
+      join(run + 3, w, z);
+    }
+    if (run <= last) join(run, x, w);
+    if (run + 1 <= last) join(run + 1, y, x);
+    if (run + 2 <= last) join(run + 2, z, y);
+  } else {
+    int run = 0;
+    for (; run + 1 <= last; run += 2) {
+      join(run, x, y);
+      join(run + 1, y, x);
+    }
+    if (run <= last) join(run, x, y);
   }
 }
 
 // ---- the outputs --------------------------------------------------------------------------------------------------------------
 // Formed transposed, so that a lane has four neighbouring channels of a token: O^T = e^gamma S0^T Q^T + U^T P^T.
+// Bound: what it reads, U and the state in fp32.  10 heads of 64 channels, 65536 tokens, bf16: 133 us for 470 MB (3.5 TB/s).
 constexpr int kOutBlocks = 4;   // of 16 value channels at a time
 
 template <typename T> inline int delta_out_lds(int dks) {

@@ -1,6 +1,7 @@
 // The gated delta rule for one new token: S' = e^g S, u = beta (v - S'^T k), S = S' + k u^T, o = scale S^T q.
 // Bound: HBM, the state in and out once.  A workgroup holds 32 value channels of one head's state in registers (a thread 4 of
 // them in every 32nd row), so that S0^T k and S0^T q come from one pass: o = scale (e^g S0^T q + (q.k) u).
+// 64 rows of 16 heads of 128 x 128: 24.2 us for 135 MB (5.6 TB/s); one row of 8 heads of 64 x 64: 4.0 us, a launch's latency.
 #pragma once
 #include "lf_vec8.hpp"
 

@@ -5,7 +5,9 @@
 //     h    = norm(y) * w_pre * (1 + scale) + shift                     (norm before the next block, of the unrounded y)
 //
 // norm(t) = (t - mean) / sqrt(mean((t - mean)^2) + eps) over a token's C channels, or t / sqrt(mean(t^2) + eps).
-// Every token is read once and written once; sums and statistics are fp32, the variance from the deviations.
+// Every token is read once and written once; sums and statistics are fp32, the variance from the deviations.  Bound: HBM.
+// bf16, forward: 81120 tokens of 2048 channels 240 us for 1.33 GB (5.5 TB/s); 12 x 4096 of 320: 21 us for 126 MB (6.0 TB/s), backward
+// 36 us for 189 MB (5.3 TB/s) and 4.8 us for the vectors' sums; fp16, 2 x 256 of 1280: 4.3 us.
 #pragma once
 #include "lf_vec8.hpp"
 
@@ -397,8 +399,8 @@ struct GateNormVectors {
 // The vectors' gradients: dshift = A, dscale = Bs w_pre, dgate = G w_post per modulation row;
 // dw_pre = sum_b Bs (1 + scale), dw_post = sum_b G gate.
 // First the workgroups' partial sums: 64 elements per workgroup, each of its sixteen waves a sixteenth of the partials in their
-// order, the sixteenths in theirs (with four waves a sum over 2048 partials of one batch row took 30 us).  Where every modulation row has its own gradient that ends here; for the sums over the batch
-// the totals are left for gate_norm_vectors.
+// order, the sixteenths in theirs (with four waves a sum over 2048 partials of one batch row took 30 us).  Where every
+// modulation row has its own gradient that ends here; for the sums over the batch the totals are left for gate_norm_vectors.
 __global__ __launch_bounds__(1024) void gate_norm_sums(GateNormVectors a) {
   constexpr int kWaves = 16;
   __shared__ float part[kWaves][64];

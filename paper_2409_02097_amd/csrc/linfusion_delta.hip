@@ -56,13 +56,15 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   z->at_kn = u;
   z->at_ds = z->at_kn + 4 * z->dks * terms * frag;
   z->record_b = up(z->at_ds + state);
-  // Runs: as many as give every CU a workgroup of the second pass, of 16 chunks at least; each costs delta_join a step
-  // of 1.6 us, and the first pass does (d_k + d_v) / d_v times the work of the second.
+  // Runs: as many as give every CU a workgroup of the second pass, of 8 chunks at least; each costs delta_join a step, and the first
+  // pass does (d_k + d_v) / d_v times the work of the second.  us of the scans in runs : in one, bf16, heads of 64: 64 x 4096 tokens in 2
+  // 141 : 103, 40 x 4096 in 3 103 : 85, 32 x 8192 in 4 162 : 164, 24 x 8192 in 5 127 : 145, 20 x 8192 in 6 106 : 130; heads of 128: 16 x
+  // 8192 in 4 306 : 264, 8 x 8192 in 8 182 : 210.  In 5 of 8 chunks, 4 x 2560 tokens, heads of 64: 26 : 36.
   const long long scans = z->heads * ((z->dvb + 1) / 2);
   long long runs = lfh::num_cu() / scans;
-  if (runs > z->nc / 16) runs = z->nc / 16;
+  if (runs > z->nc / 8) runs = z->nc / 8;
   if (runs > 32) runs = 32;
-  if (runs < 3) runs = 1;
+  if (runs < 5) runs = 1;
   z->run = (int)((z->nc + runs - 1) / runs);
   z->runs = (int)((z->nc + z->run - 1) / z->run);
   const size_t blocks = z->runs > 1 ? (size_t)z->heads * z->runs * z->dkb * 1024 : 0;
@@ -150,7 +152,9 @@ void place_backward(lf::DeltaArgs* a, const Sizes& z, void* at) {
     default: X(5) break;                                                                          \
   }
 
-// 32 value channels a workgroup where that still gives three quarters of the CUs one
+// 32 value channels a workgroup where that still gives three quarters of the CUs one: the slices' common reads from the L2 halve.  us a
+// call with 16 / 32: 10 heads of 64, 65536 tokens 813 / 720, 96 heads of 40, 4096 tokens, forward and backward 843 / 821; with fewer
+// workgroups it would leave CUs idle along a chain that is no shorter.
 template <int NI, int KS, bool PARTIAL> void launch_scan(const lf::DeltaArgs& a, int slices, int runs, hipStream_t st) {
   const int pairs = (slices + 1) / 2;
   if (slices > 1 && 4LL * pairs * a.heads * runs >= 3LL * lfh::num_cu())
@@ -290,7 +294,8 @@ int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.out = out; a.state_out = state_out; a.lengths = lengths;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.heads = (int)z.heads; a.runs = z.runs; a.run = z.run; a.scale = scale;
+  a.N = N; a.H = H; a.Hk = H_k; a.heads = (int)z.heads; a.nc = (int)z.nc; a.runs = z.runs; a.run = z.run;
+  a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
   place_forward(&a, z, saved ? saved : workspace, saved != nullptr);
   const hipStream_t st = (hipStream_t)stream;
   const int BH = (int)z.heads;
@@ -344,7 +349,8 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
   a.state_in = state_in; a.lengths = lengths; a.dout = dout; a.dstate_out = dstate_out;
   a.dq = dq; a.dk_out = dk; a.dv_out = dv; a.dg = dg; a.dbeta = dbeta; a.dstate_in = dstate_in;
-  a.N = N; a.H = H; a.Hk = H_k; a.nc = (int)z.nc; a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.heads = (int)z.heads; a.runs = z.runs; a.run = z.run; a.scale = scale;
+  a.N = N; a.H = H; a.Hk = H_k; a.heads = (int)z.heads; a.nc = (int)z.nc; a.runs = z.runs; a.run = z.run;
+  a.dk = d_k; a.dv = d_v; a.dkb = z.dkb; a.dvb = z.dvb; a.dks = z.dks; a.scale = scale;
   place_backward(&a, z, workspace);
   place_forward(&a, z, saved ? const_cast<void*>(saved) : static_cast<unsigned char*>(workspace) + z.backward(), true);
   const hipStream_t st = (hipStream_t)stream;

@@ -52,7 +52,7 @@ int check_sizes(int B, long long N, int C, int dtype) {
 }
 
 // vectors of fp32: [C], or modulation rows with `stride` elements between two batch rows
-int check_vectors(int B, int C, long long stride, std::initializer_list<const void*> mod,
+int check_vectors(int C, long long stride, std::initializer_list<const void*> mod,
                   std::initializer_list<const void*> channel) {
   if (stride < 0 || (stride != 0 && stride < C) || stride >= 1LL << 40) return LINFUSION_ERR_INVALID;
   if (stride % 4) return LINFUSION_ERR_MISALIGNED;
@@ -60,27 +60,32 @@ int check_vectors(int B, int C, long long stride, std::initializer_list<const vo
     if ((uintptr_t)p & 15) return LINFUSION_ERR_MISALIGNED;
   for (const void* p : channel)
     if ((uintptr_t)p & 15) return LINFUSION_ERR_MISALIGNED;
-  (void)B;
   return LINFUSION_OK;
 }
 
 size_t mod_bytes(int B, int C, long long stride) { return ((size_t)(B - 1) * (size_t)stride + (size_t)C) * 4; }
 
-// Threads per token and tokens per workgroup.  A wave per token where its registers hold it (`most_wave` vectors of 8 channels a
-// lane) and there are tokens for every wave of the device; a workgroup per token for wide tokens and for few.  Workgroups per CU:
-// many short ones where a token takes a workgroup, whose start (the modulation of its channels) is small against four tokens or
-// more; fewer where it takes a wave, and in the backward pass, where each leaves partial sums.
+// Threads per token and tokens per workgroup.  A wave per token where two vectors of 8 channels a lane hold it and there is a token for
+// every wave of the device; a workgroup per token for wide tokens and for few.  us forward / backward, wave : workgroup, fp16: 32768 x 640
+// 31 / 51 : 32 / 109, 2048 x 1024 4.7 / 12.9 : 6.3 / 15.0, 512 x 640 3.7 / 9.1 : 3.5 / 9.0; three vectors a lane lose to the workgroup
+// (32768 x 1280 55 : 51).
+// Workgroups per CU: forward many short ones where a token takes a workgroup, whose start (the modulation of its channels) is small
+// against four tokens or more, fewer where it takes a wave; backward, where each leaves partial sums, fewer still: but four of a
+// workgroup per token, not two, where many tokens leave much of it idle (32768 x 1280 112 : 141 us; 32768 x 2048 185 : 161, 1024 x 1280
+// 17 : 13).
 struct Shape { int lanes, vpt, rows, wgs; };
-Shape shape_of(long long tokens, long long N, int C, int most_wave, int per_cu_wave, int per_cu_whole) {
+Shape shape_of(int B, long long N, int C, bool backward) {
   Shape s;
   const int vecs = C / 8;
-  const long long cus = lfh::num_cu();
-  s.lanes = (vecs <= 64 * most_wave && (tokens >= 16 * cus || vecs <= 64)) ? 64 : 256;
+  const long long cus = lfh::num_cu(), tokens = (long long)B * N;
+  s.lanes = vecs <= 128 && (tokens >= 4 * cus || vecs <= 64) ? 64 : 256;
   s.vpt = (vecs + s.lanes - 1) / s.lanes;
   const int per = 256 / s.lanes;
-  const long long want = cus * (s.lanes == 64 ? per_cu_wave : per_cu_whole);
-  long long rows = (tokens + want - 1) / want;
-  if (per_cu_whole > 16 && rows < 4 && tokens > 4 * cus) rows = 4;
+  int per_cu;
+  if (backward) per_cu = s.lanes == 64 ? (C <= 512 ? 8 : 4) : (C <= 1536 && tokens >= 16 * cus ? 4 : 2);
+  else per_cu = s.lanes == 64 ? 16 : 64;
+  long long rows = (tokens + cus * per_cu - 1) / (cus * per_cu);
+  if (!backward && rows < 4 && tokens > 4 * cus) rows = 4;
   rows = (rows + per - 1) / per * per;
   if (rows > N) rows = (N + per - 1) / per * per;
   if (rows > 1 << 20) rows = 1 << 20;
@@ -88,10 +93,6 @@ Shape shape_of(long long tokens, long long N, int C, int most_wave, int per_cu_w
   s.wgs = (int)((N + rows - 1) / rows);
   return s;
 }
-
-
-Shape fwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, 3, 16, 64); }
-Shape bwd_shape(int B, long long N, int C) { return shape_of((long long)B * N, N, C, 2, C <= 512 ? 8 : 4, 2); }
 
 template <typename T, int LANES, int VPT, bool RMS, bool POST>
 int launch_fwd(const lf::GateNormArgs& a, int B, const Shape& s, hipStream_t st) {
@@ -114,8 +115,7 @@ int launch_bwd(const lf::GateNormBwdArgs& a, int B, const Shape& s, hipStream_t 
 template <typename T> int run_fwd(const lf::GateNormArgs& a, int B, const Shape& s, bool rms, bool post, hipStream_t st) {
   if (s.lanes == 64) {
     if (s.vpt == 1) { LF_NORM_KINDS(launch_fwd, T, 64, 1); }
-    if (s.vpt == 2) { LF_NORM_KINDS(launch_fwd, T, 64, 2); }
-    LF_NORM_KINDS(launch_fwd, T, 64, 3);
+    LF_NORM_KINDS(launch_fwd, T, 64, 2);
   }
   if (s.vpt == 1) { LF_NORM_KINDS(launch_fwd, T, 256, 1); }
   if (s.vpt == 2) { LF_NORM_KINDS(launch_fwd, T, 256, 2); }
@@ -157,7 +157,7 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
   if ((rc = make_view(f, strides ? strides[1] : nullptr, B, N, C, esz, false, &vf)) != LINFUSION_OK) return rc;
   if ((rc = make_view(y, strides ? strides[2] : nullptr, B, N, C, esz, true, &vy)) != LINFUSION_OK) return rc;
   if ((rc = make_view(h, strides ? strides[3] : nullptr, B, N, C, esz, true, &vh)) != LINFUSION_OK) return rc;
-  if ((rc = check_vectors(B, C, mod_stride, {gate, scale, shift}, {w_pre, w_post})) != LINFUSION_OK) return rc;
+  if ((rc = check_vectors(C, mod_stride, {gate, scale, shift}, {w_pre, w_post})) != LINFUSION_OK) return rc;
   if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
   // y may be x itself: a token is read whole by the threads that write it
   if ((meet(vy, vx) && !same_rows(vy, vx)) || meet(vy, vf) || meet(vh, vx) || meet(vh, vf) || meet(vh, vy))
@@ -171,7 +171,7 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
     if (lengths && overlaps(o->p, o->bytes, lengths, (size_t)B * 4)) return LINFUSION_ERR_OVERLAP;
   }
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
-  const Shape s = fwd_shape(B, N, C);
+  const Shape s = shape_of(B, N, C, false);
   const lf::GateNormArgs a{x, f, y, h, dev(vx), dev(vf), dev(vy), dev(vh), gate, scale, shift, w_pre, w_post,
                            mod_stride, lengths, N, C, s.rows, residual_scale, norm_eps};
   const hipStream_t st = (hipStream_t)stream;
@@ -184,7 +184,7 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
 
 size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C) {
   if (check_sizes(B, N, C, LINFUSION_DTYPE_F32) != LINFUSION_OK) return 0;
-  const Shape s = bwd_shape(B, N, C);
+  const Shape s = shape_of(B, N, C, true);
   return up((size_t)B * s.wgs * 3 * C * 4) + up((size_t)B * 3 * C * 4);
 }
 
@@ -212,8 +212,8 @@ int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, con
   if ((rc = make_view(dh, st2(3), B, N, C, esz, false, &vdh)) != LINFUSION_OK) return rc;
   if ((rc = make_view(dx, st2(4), B, N, C, esz, true, &vdx)) != LINFUSION_OK) return rc;
   if ((rc = make_view(df, st2(5), B, N, C, esz, true, &vdf)) != LINFUSION_OK) return rc;
-  if ((rc = check_vectors(B, C, mod_stride, {gate, scale}, {w_pre, w_post})) != LINFUSION_OK) return rc;
-  if ((rc = check_vectors(B, C, dmod_stride, {dgate, dscale, dshift}, {dw_pre, dw_post})) != LINFUSION_OK) return rc;
+  if ((rc = check_vectors(C, mod_stride, {gate, scale}, {w_pre, w_post})) != LINFUSION_OK) return rc;
+  if ((rc = check_vectors(C, dmod_stride, {dgate, dscale, dshift}, {dw_pre, dw_post})) != LINFUSION_OK) return rc;
   const bool shared = mod_stride == 0;
   if (!shared && B > 1 && dmod_stride < C && (dgate || dscale || dshift)) return LINFUSION_ERR_OVERLAP;
   if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
@@ -261,7 +261,7 @@ int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, con
       if (r.p && overlaps(workspace, need, r.p, r.n)) return LINFUSION_ERR_OVERLAP;
   }
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
-  const Shape s = bwd_shape(B, N, C);
+  const Shape s = shape_of(B, N, C, true);
   float* partials = sums ? (float*)workspace : nullptr;
   float* total = sums ? (float*)((char*)workspace + up((size_t)B * s.wgs * 3 * C * 4)) : nullptr;
   const lf::GateNormBwdArgs a{x, f, dy, dh, dx, df, dev(vx), dev(vf), dev(vdy), dev(vdh), dev(vdx), dev(vdf), gate, scale,

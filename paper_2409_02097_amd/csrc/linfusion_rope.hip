@@ -80,7 +80,7 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
     return LINFUSION_ERR_UNSUPPORTED;
   if (d % 8 || d > 2 * lf::kRopePairs) return LINFUSION_ERR_UNSUPPORTED;
   if (axes < 1 || axes > lf::kRopeAxes) return LINFUSION_ERR_UNSUPPORTED;
-  if (N > (1LL << 40) / d) return LINFUSION_ERR_INVALID;
+  if (N >= 1LL << 28) return LINFUSION_ERR_INVALID;   // (a grid has at most 2^32 threads)
   lf::RopeArgs a{};
   int at = 0;
   bool whole = true;
@@ -145,7 +145,7 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
     tokens *= 2;
   a.tokens = tokens;
   const long long wgs = (N + tokens - 1) / tokens;
-  if (wgs > 0x7fffffff) return LINFUSION_ERR_INVALID;
+  if (wgs >= 1LL << 24) return LINFUSION_ERR_INVALID;
   const int mode = (flags & LINFUSION_FLAG_ROPE_NEIGHBOURS) ? 0 : (whole ? 1 : 2);
   const hipStream_t st = (hipStream_t)stream;
   rc = dtype == LINFUSION_DTYPE_F16   ? run<lf::F16>(a, B, (unsigned)wgs, mode, st)

@@ -22,7 +22,7 @@
 
 namespace {
 
-constexpr int kVersion = 600;  // 0.6.0
+constexpr int kVersion = 700;  // 0.7.0
 constexpr int kMaxDevices = 16;
 constexpr int kDefaultCU = 256;   // compute units assumed while no device can be asked (one whole MI355X)
 

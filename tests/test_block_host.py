@@ -175,3 +175,9 @@ def test_sizes_of_refused_calls_are_zero():
         for f in (lf.linfusion_delta_workspace_bytes, lf.linfusion_delta_saved_bytes, lf.linfusion_delta_bwd_workspace_bytes):
             assert f(*sizes(**bad)) == 0
     assert lf.linfusion_gate_norm_bwd_workspace_bytes(2, 50, 12) == 0
+
+
+def test_rope_of_more_tokens_than_a_grid_takes():
+    far = dict(q=M << 20, k=None, qo=M << 20, ko=None, Hk=0, B=1, H=1, d=8, axes=1, channels=(8,), bases=(1e4,), pos=M)
+    assert rope(N=(1 << 28) - 1, **far) == OK
+    assert rope(N=1 << 28, **far) == -1

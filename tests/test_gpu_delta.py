@@ -410,3 +410,12 @@ def test_runs_with_the_state_in_place():
     lf.linfusion_delta_fwd(*(g[n] for n in ("q", "k", "v", "g", "beta")), again, scale=c["scale"], state_in=state, state_out=state,
                            lengths=g["lengths"], workspace=mem)
     assert torch.equal(again, out) and torch.equal(state, last)
+
+
+@pytest.mark.parametrize("dk,dv", [(160, 24), (128, 64)])
+def test_runs_of_wide_keys(dk, dv):
+    """Three and two blocks of state rows a wave where runs are joined."""
+    c = make(1, 2, 1, 64 * 60 + 3, dk, dv, "bf16", seed=91)
+    g = on_gpu(c)
+    out, last, _ = forward(c, g)
+    check_forward(c, out, last)

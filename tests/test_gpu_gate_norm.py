@@ -292,3 +292,12 @@ def test_refusals_on_the_device():
         with pytest.raises(lf.LinFusionError) as e:
             call(**bad)
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("size", [(2, 1030, 1000), (1, 4100, 1288), (3, 700, 1536)], ids=str)
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_many_tokens(size, dtype):
+    """Enough tokens for a wave each, and for more workgroups of the backward pass; idle lanes in both."""
+    c = make(*size, dtype, 91, False, False)
+    g = on_gpu(c)
+    check_all(c, *forward(c, g), backward(c, g))

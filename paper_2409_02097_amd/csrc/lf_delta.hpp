@@ -12,12 +12,12 @@
 // Only U and S1 depend on the chunk before: T, W, U0 are formed for all chunks at once (delta_prepare), a scan runs over the
 // chunks with a slice of 16 value channels per workgroup (delta_scan), and the outputs follow for all chunks at once
 // (delta_out).  gamma and its differences are fp64: behind a token that forgets nearly everything the differences of an
-// fp32 sum have lost the small decays that follow it.  Everything that reaches the state or an fp32 result is fp32 accurate.
+// fp32 sum have lost the small decays that follow it.
 //
-// Products run on the 16-bit matrix instruction with operands as sums of bf16 terms (lf_terms.hpp): three where a state or
-// an fp32 result depends on them, two where a 16-bit output does.  What passes between the kernels is stored as its reader
-// takes it, a contiguous kilobyte for each operand or accumulator of a wave, all of a chunk and head in one record (a workgroup
-// then touches a page or two of the workspace, not one per array):
+// Products run on the 16-bit matrix instruction with operands as sums of bf16 terms (lf_terms.hpp), as many as hold all of a
+// value: fp32 accurate for every type, because an output may be the small rest of a large state and its correction.  What
+// passes between the kernels is stored as its reader takes it, a contiguous kilobyte for each operand or accumulator of a wave,
+// all of a chunk and head in one record (a workgroup then touches a page or two of the workspace, not one per array):
 //     w      T (beta e^gamma K) as operand: [4 row blocks][d_k / 32][3 terms][64 lanes][8 steps]
 //     kt     K^T as operand: [d_k / 16][2][terms][64][8], in the record of the first value head that has the key head
 //     u      U0, then U, and s the state before the chunk, as fp32 accumulators: [d_v / 16][row blocks][64][4]
@@ -238,7 +238,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
       for (int ks = 0; ks < KS; ++ks) {
         Terms<NI> fj;
         terms_near<NI>(x + (16 * nt + col) * kLd + 32 * ks + g8, kPlane, fj);
-        acc = mul_terms<3>(fi[ks], fj, acc);
+        acc = mul_terms(fi[ks], fj, acc);
       }
       float* to = ma + block_at(wave, nt);
 #pragma unroll
@@ -321,8 +321,8 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
       if (ks >= steps) continue;
       Terms<NI> key;
       terms_across<NI>(x + 32 * ks * kLd + 16 * cb, kPlane, kLd, key);
-      acc = mul_terms<3>(key, ft[ks], acc);
-      if (a.for_backward) act = mul_terms<3>(ft[ks], key, act);
+      acc = mul_terms(key, ft[ks], acc);
+      if (a.for_backward) act = mul_terms(ft[ks], key, act);
     }
     store_operand<3>(mw + (cb >> 1) * 3 * kFrag, cb & 1, acc);
     if (a.for_backward && cb < a.dkb)
@@ -344,7 +344,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_prepa
       if (ks >= steps) continue;
       Terms<NI> val;
       terms_across<NI>(v + 32 * ks * ldv + 16 * at_vb, 64 * ldv, ldv, val);
-      acc = mul_terms<3>(val, ft[ks], acc);
+      acc = mul_terms(val, ft[ks], acc);
     }
     *reinterpret_cast<f32x4*>(part<float>(rec, a.at_u) + ((vb * 4 + wave) * 64 + lane) * 4) = acc;
   }
@@ -497,8 +497,8 @@ template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(2
         Terms<3> fs;
         if (ks == 0 && e == 0) fs = first_fs;
         else terms_near<3>(sp + (16 * e + col) * kLd + 32 * ks + g8, kPlane, fs);
-        if (COLS == 1 && (ks & 1)) acc2[e] = mul_terms<3>(fs, in.w[ks], acc2[e]);
-        else acc[e] = mul_terms<3>(fs, in.w[ks], acc[e]);
+        if (COLS == 1 && (ks & 1)) acc2[e] = mul_terms(fs, in.w[ks], acc2[e]);
+        else acc[e] = mul_terms(fs, in.w[ks], acc[e]);
       }
     f32x4 u[COLS];
 #pragma unroll
@@ -519,8 +519,8 @@ template <int NI, int KS, int COLS, bool PARTIAL> __global__ __launch_bounds__(2
       for (int t = 0; t < kBlocks; ++t) {
         f32x4 more = {0, 0, 0, 0};
         s[e][t] *= in.whole;
-        s[e][t] = mul_terms<3>(in.kt[t][0], fu[0], s[e][t]);
-        more = mul_terms<3>(in.kt[t][1], fu[1], more);
+        s[e][t] = mul_terms(in.kt[t][0], fu[0], s[e][t]);
+        more = mul_terms(in.kt[t][1], fu[1], more);
         s[e][t] += more;
       }
     }
@@ -647,19 +647,23 @@ template <int KS> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a)
 
 // ---- the outputs --------------------------------------------------------------------------------------------------------------
 // Formed transposed, so that a lane has four neighbouring channels of a token: O^T = e^gamma S0^T Q^T + U^T P^T.
-// Bound: what it reads, U and the state in fp32.  10 heads of 64 channels, 65536 tokens, bf16: 133 us for 470 MB (3.5 TB/s).
-constexpr int kOutBlocks = 4;   // of 16 value channels at a time
+// Bound: what it reads, U and the state in fp32.  10 heads of 64 channels, 65536 tokens, bf16: 143 us for 470 MB (3.3 TB/s).
+//
+// Value channels pass through LDS 32 at a time (three terms each; 64 of them leave room for fewer workgroups).  us a forward call, 32 : 64:
+// bf16 10 heads of 64, 65536 tokens 658 : 674; 8 heads of 128, 8192 tokens 215 : 231; 64 heads of 32, 4096 tokens 123 : 128; fp16 32 heads of
+// 128, 2048 tokens 141 : 154; fp32 16 heads of 64, 4096 tokens 105 : 107; fp16 8 heads of 64, 197 tokens 29.7 : 28.6.
+constexpr int kOutBlocks = 2;   // of 16 value channels
 
 template <typename T> inline int delta_out_lds(int dks) {
-  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut;
-  const int keys = NI * plane_bytes(64, dks), scores = NO * 64 * kLdP * 2, rows = keys + (keys > scores ? keys : scores);
-  const int later = kOutBlocks * NO * (plane_bytes(16, dks) + 64 * kLdU * 2);
+  constexpr int NI = TermsOf<T>::kStored;
+  const int keys = NI * plane_bytes(64, dks), scores = 3 * 64 * kLdP * 2, rows = keys + (keys > scores ? keys : scores);
+  const int later = kOutBlocks * 3 * (plane_bytes(16, dks) + 64 * kLdU * 2);
   return (rows > later ? rows : later) + 64 * 8 + 2 * 64 * 4;
 }
 
 template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(DeltaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int NI = TermsOf<T>::kStored, NO = TermsOf<T>::kOut, KB = 2 * KS, kLd = 32 * KS + 8;
+  constexpr int NI = TermsOf<T>::kStored, KB = 2 * KS, kLd = 32 * KS + 8;
   constexpr int kSPlane = 16 * kLd, kUPlane = 64 * kLdU;
   const DeltaAt w(a, blockIdx.y, blockIdx.x);
   if (w.valid == 0) return;
@@ -669,7 +673,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
   uint16_t* k = q + NI * 64 * kLd;
   uint16_t* pp = k;                                      // where the keys were
   uint16_t* sp = q;                                      // later, where all of these were
-  uint16_t* up = sp + kOutBlocks * NO * kSPlane;
+  uint16_t* up = sp + kOutBlocks * 3 * kSPlane;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15;
   const int row4 = (lane >> 4) * 4, g8 = (lane >> 4) * 8;
   unsigned char* rec = a.rec(w.bh, blockIdx.x);
@@ -711,7 +715,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
       for (int ks = 0; ks < KS; ++ks) {
         Terms<NI> fk;
         terms_near<NI>(k + (16 * jt + col) * kLd + 32 * ks + g8, 64 * kLd, fk);
-        acc = mul_terms<NO>(fk, fq[ks], acc);
+        acc = mul_terms(fk, fq[ks], acc);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -724,11 +728,11 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
   }
   __syncthreads();   // the keys are read
 #pragma unroll
-  for (int jt = 0; jt < 4; ++jt) split4_lds<NO>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, scores[jt]);
+  for (int jt = 0; jt < 4; ++jt) split4_lds<3>(pp + (16 * wave + col) * kLdP + 16 * jt + row4, 64 * kLdP, scores[jt]);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (rows that only this wave writes and reads)
-  Terms<NO> fp[2];
+  Terms<3> fp[2];
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) terms_near<NO>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
+  for (int ks = 0; ks < 2; ++ks) terms_near<3>(pp + (16 * wave + col) * kLdP + 32 * ks + g8, 64 * kLdP, fp[ks]);
   const float since = decay[16 * wave + col];
   const int n = 16 * wave + col;
   for (;;) {
@@ -736,11 +740,11 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
     if (wave < blocks) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)   // (zeros in the half block behind d_k: the queries' zeros times what is there)
-        split4_lds<NO>(sp + wave * NO * kSPlane + col * kLd + 16 * kb + row4, kSPlane, kb < a.dkb ? s_in[kb] : f32x4{0, 0, 0, 0});
+        split4_lds<3>(sp + wave * 3 * kSPlane + col * kLd + 16 * kb + row4, kSPlane, kb < a.dkb ? s_in[kb] : f32x4{0, 0, 0, 0});
     }
 #pragma unroll
     for (int i = 0; i < kOutBlocks; ++i)
-      if (i < blocks) split4_lds<NO>(up + i * NO * kUPlane + n * kLdU + row4, kUPlane, u_in[i]);
+      if (i < blocks) split4_lds<3>(up + i * 3 * kUPlane + n * kLdU + row4, kUPlane, u_in[i]);
     const int here = blocks, at_block = vb0;
     vb0 += kOutBlocks;
     blocks = a.dvb - vb0 < kOutBlocks ? a.dvb - vb0 : kOutBlocks;
@@ -750,17 +754,17 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_out(D
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        Terms<NO> fs;
-        terms_near<NO>(sp + vb * NO * kSPlane + col * kLd + 32 * ks + g8, kSPlane, fs);
-        acc = mul_terms<NO>(fs, fq[ks], acc);
+        Terms<3> fs;
+        terms_near<3>(sp + vb * 3 * kSPlane + col * kLd + 32 * ks + g8, kSPlane, fs);
+        acc = mul_terms(fs, fq[ks], acc);
       }
       acc *= since;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         if (2 * ks > wave) continue;
-        Terms<NO> fu;
-        terms_across<NO>(up + vb * NO * kUPlane + 32 * ks * kLdU, kUPlane, kLdU, fu);
-        acc = mul_terms<NO>(fu, fp[ks], acc);
+        Terms<3> fu;
+        terms_across<3>(up + vb * 3 * kUPlane + 32 * ks * kLdU, kUPlane, kLdU, fu);
+        acc = mul_terms(fu, fp[ks], acc);
       }
       const int ch = 16 * (at_block + vb) + row4;
       if (n < w.valid && ch < a.dv)

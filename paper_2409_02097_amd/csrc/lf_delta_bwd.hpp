@@ -74,7 +74,7 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
         Terms<NI> fq, fk;
         terms_near<NI>(q + (16 * it + col) * ld + 32 * ks + g8, plane, fq);
         terms_near<NI>(k + (16 * wave + col) * ld + 32 * ks + g8, plane, fk);
-        acc = mul_terms<3>(fq, fk, acc);
+        acc = mul_terms(fq, fk, acc);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -133,14 +133,14 @@ template <typename T, int KS> __global__ __launch_bounds__(256) void delta_back_
     for (int ks = 0; ks < 2; ++ks) terms_across<NI>(o + 32 * ks * ldo + 16 * at_vb, 64 * ldo, ldo, fo[ks]);
     f32x4 acc = {0, 0, 0, 0};   // rows: value channels, columns: tokens j
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) acc = mul_terms<3>(fo[ks], fp[ks], acc);
+    for (int ks = 0; ks < 2; ++ks) acc = mul_terms(fo[ks], fp[ks], acc);
     *reinterpret_cast<f32x4*>(part<float>(rec_b, 0) + ((vb * 4 + wave) * 64 + lane) * 4) = acc * a.scale;
 #pragma unroll
     for (int t = 0; t < kOwn; ++t) {
       if (wave + 4 * t >= a.dkb) continue;
       f32x4 z = {0, 0, 0, 0};
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) z = mul_terms<3>(fq[t][ks], fo[ks], z);
+      for (int ks = 0; ks < 2; ++ks) z = mul_terms(fq[t][ks], fo[ks], z);
       *reinterpret_cast<f32x4*>(part<float>(rec_b, a.at_ds) + (vb * a.dkb + wave + 4 * t) * 256 + lane * 4) = z;
     }
   }
@@ -229,8 +229,8 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
       Terms<3> fs;
       if (ks == 0) fs = first_fs;
       else terms_near<3>(sp + col * kLd + 32 * ks + g8, kPlane, fs);
-      if (ks & 1) acc2 = mul_terms<3>(fs, in.kn[ks], acc2);
-      else acc = mul_terms<3>(fs, in.kn[ks], acc);
+      if (ks & 1) acc2 = mul_terms(fs, in.kn[ks], acc2);
+      else acc = mul_terms(fs, in.kn[ks], acc);
     }
     const f32x4 u = in.du + (acc + acc2) * in.left;
     split4_lds<3>(up + (16 * wave + col) * kLdU + row4, 64 * kLdU, -u);
@@ -243,8 +243,8 @@ template <int NI, int KS> __global__ __launch_bounds__(256) void delta_back_scan
     for (int t = 0; t < kBlocks; ++t) {
       f32x4 more = in.z[t];
       s[t] *= in.whole;
-      s[t] = mul_terms<3>(in.wt[t][0], fu[0], s[t]);
-      more = mul_terms<3>(in.wt[t][1], fu[1], more);
+      s[t] = mul_terms(in.wt[t][0], fu[0], s[t]);
+      more = mul_terms(in.wt[t][1], fu[1], more);
       s[t] += more;
     }
     here -= a.size_b;
@@ -426,7 +426,7 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gr
         widen8<F32>(tt[ks], y);
         split8(y, ft);
         terms_across<3>(pv + 32 * ks * kLdV + 16 * half, kVPlane, kLdV, f);
-        dv = mul_terms<3>(f, ft, dv);
+        dv = mul_terms(f, ft, dv);
         __builtin_amdgcn_sched_barrier(0);
       }
       const float by = again(per_beta);
@@ -453,8 +453,8 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gr
         __builtin_amdgcn_sched_barrier(0);   // (one operand at a time: two workgroups per CU have 128 registers a lane)
         Terms<3> fj;
         terms_near<3>(pu + (16 * jt + col) * kLdV + g8, kVPlane, fj);
-        if (half == 0) mx[jt] = mul_terms<3>(fj, fo, mx[jt]);
-        else mx[jt] = mul_terms<3>(fj, fv, mx[jt]);
+        if (half == 0) mx[jt] = mul_terms(fj, fo, mx[jt]);
+        else mx[jt] = mul_terms(fj, fv, mx[jt]);
       }
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
@@ -462,10 +462,10 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gr
         __builtin_amdgcn_sched_barrier(0);
         Terms<3> f;
         terms_across<3>(ps + 16 * kb, kSPlane, kLd, f);
-        dq[i] = mul_terms<3>(f, fo, dq[i]);
-        dk[i] = mul_terms<3>(f, fv, dk[i]);
+        dq[i] = mul_terms(f, fo, dq[i]);
+        dk[i] = mul_terms(f, fv, dk[i]);
         terms_across<3>(pd + 16 * kb, kSPlane, kLd, f);
-        dw[i] = mul_terms<3>(f, fu, dw[i]);
+        dw[i] = mul_terms(f, fu, dw[i]);
       }
       lds_barrier();   // the planes are read
     }
@@ -508,10 +508,10 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gr
         Terms<NI> f;
         terms_across<NI>(x + 32 * ks * kLd + 16 * (2 * i + half), 64 * kLd, kLd, f);
         if (2 * ks <= wave) {
-          dq[i] = mul_terms<3>(f, fe, dq[i]);
-          dk[i] = mul_terms<3>(f, fm, dk[i]);
+          dq[i] = mul_terms(f, fe, dq[i]);
+          dk[i] = mul_terms(f, fm, dk[i]);
         }
-        if (2 * ks + 1 >= wave) dk[i] = mul_terms<3>(f, em, dk[i]);
+        if (2 * ks + 1 >= wave) dk[i] = mul_terms(f, em, dk[i]);
       }
     }
     // <dS1, S1> = e^gamma_63 <dS1, S0> + sum of k.(e^(gamma_63 - gamma) dS1 u) over the tokens
@@ -536,7 +536,7 @@ template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gr
       for (int i = 0; i < KS; ++i) {
         Terms<NI> f;
         terms_across<NI>(x + 32 * ks * kLd + 16 * (2 * i + half), 64 * kLd, kLd, f);
-        dk[i] = mul_terms<3>(f, fe, dk[i]);
+        dk[i] = mul_terms(f, fe, dk[i]);
       }
     }
     double both = -vdv;   // q.dq - v.dv, the queries from their planes

@@ -2,17 +2,16 @@
 //
 // A value is the sum of its nearest bf16, the nearest bf16 of what is left, and so on: N terms carry 8 N bits (24: all of
 // fp32; a stored bf16 is one term, a stored fp16 two, exactly).  A product of two such sums keeps the pairs of terms i, j
-// with i + j < LEVEL, every pair dropped being below 2^-8 LEVEL of the result; each pair is one instruction at 16 times the
-// rate of the fp32 one.  LEVEL 3 (six instructions, or three where one side is a stored bf16) is fp32 accurate; LEVEL 2 (16
-// bits) serves sums whose result is rounded to 16 bits at once.
+// with i + j < 3, every pair dropped being near 2^-24 of the product: fp32 accurate.  Each pair is one instruction at 16 times
+// the rate of the fp32 one (six of them, or three where one side is a stored bf16).
 #pragma once
 #include "lf_vec8.hpp"
 
 namespace lf {
 
-template <typename T> struct TermsOf { static constexpr int kStored = 1, kOut = 2; };
-template <> struct TermsOf<F16> { static constexpr int kStored = 2, kOut = 2; };
-template <> struct TermsOf<F32> { static constexpr int kStored = 3, kOut = 3; };
+template <typename T> struct TermsOf { static constexpr int kStored = 1; };
+template <> struct TermsOf<F16> { static constexpr int kStored = 2; };
+template <> struct TermsOf<F32> { static constexpr int kStored = 3; };
 
 template <int N> struct Terms { u32x4 t[N]; };   // an operand of 16 x 16 x 32: 8 contraction steps of one row (or column)
 
@@ -77,9 +76,9 @@ template <int N> LF_DEV void terms_across(const uint16_t* p, int plane, int ld, 
   }
 }
 
-template <int LEVEL, int NA, int NB> LF_DEV f32x4 mul_terms(const Terms<NA>& a, const Terms<NB>& b, f32x4 c) {
+template <int NA, int NB> LF_DEV f32x4 mul_terms(const Terms<NA>& a, const Terms<NB>& b, f32x4 c) {
 #pragma unroll
-  for (int s = LEVEL - 1; s >= 0; --s)      // the small products first
+  for (int s = 2; s >= 0; --s)      // the small products first
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
       const int j = s - i;

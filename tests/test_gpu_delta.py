@@ -419,3 +419,28 @@ def test_runs_of_wide_keys(dk, dv):
     g = on_gpu(c)
     out, last, _ = forward(c, g)
     check_forward(c, out, last)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_a_corrected_key_answers_its_value(dtype):
+    """Unit keys that are columns of the identity, beta = 1, no decay: a token's correction is its value less what the state holds
+    for the key, and a query of that key gets the value back, the small rest of two sums of 2^14 and more.
+
+    A row's correction: three products (the terms of the state) and a difference, each rounded to 2^-24 of at most 2^15.  An output:
+    three products with the state, three with the correction.  A later chunk's state: three products and a sum more, and its own
+    correction again.  Together no more than 18 roundings."""
+    N, d, dv = 70, 64, 48
+    c = make(1, 2, 2, N, d, dv, dtype, seed=7)
+    r = np.random.RandomState(8)
+    eye = np.eye(d)
+    c["cpu"]["k"], c["k"] = stored(np.broadcast_to(eye[np.arange(N) % d], (1, 2, N, d)), dtype)
+    asked = np.array([r.randint(0, min(t, d - 1) + 1) for t in range(N)])
+    c["cpu"]["q"], c["q"] = stored(np.broadcast_to(eye[asked], (1, 2, N, d)), dtype)
+    c["cpu"]["state"], c["state"] = stored(r.uniform(2.0 ** 14, 2.0 ** 15, (1, 2, d, dv)) * r.choice((-1, 1), (1, 2, d, dv)), "f32")
+    for n, x in (("g", np.zeros((1, 2, N))), ("beta", np.ones((1, 2, N)))):
+        c["cpu"][n], c[n] = stored(x, "f32")
+    c["scale"] = 1.0
+    out, _, _ = forward(c, on_gpu(c))
+    ref = oracle(c)[0]
+    assert np.abs(ref).max() < 8
+    check(out, ref, dtype, 18, "out", scale=2.0 ** 15)

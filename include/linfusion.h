@@ -446,7 +446,8 @@ int linfusion_attn_state(const void* k, const void* v, float* state_out,
  *
  *   q, q_out        [B, H, N, d] views; k, k_out: [B, H_k, N, d] views, or both NULL.  q_out == q (k_out == k) with the same
  *                   strides works in place; else an output must not overlap an input.  Views whose spans interleave
- *                   (columns of one projection) are accepted where their rows lie side by side in each token.
+ *                   are accepted where, counted modulo one of their strides, each stays within a piece of its own:
+ *                   columns of one projection (of one token for each of several batch rows too), its parts head by head.
  *   N               < 2^28.  d: multiple of 8 up to 256.  axes: 1 .. 4.  channels, bases, scales: HOST arrays of `axes` values;
  *                   channels even, positive, in all at most d; bases > 0; scales NULL = 1.
  *   positions       DEVICE int32, element {b, a, n} at b * position_strides[0] + a * position_strides[1] + n; NULL strides:

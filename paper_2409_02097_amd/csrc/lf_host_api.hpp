@@ -70,6 +70,34 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// A strided view as bytes: `width` contiguous ones at every place that {batch, head, token} strides (in bytes) lead to.
+struct Places { const void* p; long long stride[3], extent[3], width; };
+inline Places places(const void* p, const long long s[3], int B, int H, long long N, int d, size_t esz) {
+  const long long e = (long long)esz;
+  return Places{p, {s[0] * e, s[1] * e, s[2] * e}, {B, H, N}, d * e};
+}
+
+// Whether two views certainly share no byte although their spans may meet: modulo one of their strides each of them stays within a
+// piece of its own (columns of one buffer, the parts of each head of one projection, batch rows dealt in turn).  Never true of views
+// that do share one.
+inline bool apart(const Places& a, const Places& b) {
+  const Places* const v[2] = {&a, &b};
+  for (int i = 0; i < 6; ++i) {
+    const long long period = v[i / 3]->stride[i % 3];
+    if (v[i / 3]->extent[i % 3] <= 1 || period <= 0) continue;
+    long long reach[2];
+    for (int k = 0; k < 2; ++k) {
+      reach[k] = v[k]->width;
+      for (int j = 0; j < 3; ++j)
+        if (v[k]->extent[j] > 1 && v[k]->stride[j] % period) reach[k] += (v[k]->extent[j] - 1) * v[k]->stride[j];
+    }
+    long long at = (long long)((uintptr_t)b.p - (uintptr_t)a.p) % period;
+    if (at < 0) at += period;
+    if (reach[0] <= at && at + reach[1] <= period) return true;
+  }
+  return false;
+}
+
 // Workgroups may use up to 160 KiB of LDS on this device; above 64 KiB the kernel has to be told (per kernel; cheap).
 template <typename KernelT>
 inline bool allow_lds(KernelT kernel, int bytes) {

@@ -38,17 +38,11 @@ bool in_place(const Side& s) {
   return s.x == s.y && s.sx[0] == s.sy[0] && s.sx[1] == s.sy[1] && s.sx[2] == s.sy[2];
 }
 
-// Whether the rows of two views of one element size share no byte although their spans meet: columns of one buffer, the same
-// token stride in both, whose pieces of a token's row lie side by side.
-bool side_by_side(const void* p, const long long sp[3], int Hp, const void* r, const long long sr[3], int Hr, int B, int d,
-                  size_t esz) {
-  const long long token = sp[2];
-  if (token != sr[2] || token <= 0 || (B > 1 && (sp[0] != sr[0] || sp[0] % token))) return false;
-  const long long np = (Hp - 1) * sp[1] + d, nr = (Hr - 1) * sr[1] + d;
-  const long long bytes = (const char*)r - (const char*)p;
-  if (bytes % (long long)esz) return false;
-  const long long apart = bytes / (long long)esz % token, m = apart < 0 ? apart + token : apart;
-  return np <= m && m + nr <= token;
+// Whether the rows at `p` and `r` may share memory.  (q and k may be columns of one projection, each turned in place: their spans
+// interleave, their rows do not.)
+bool meet(const void* p, size_t np, const long long sp[3], int Hp, const void* r, size_t nr, const long long sr[3], int Hr, int B,
+          long long N, int d, size_t esz) {
+  return overlaps(p, np, r, nr) && !lfh::apart(lfh::places(p, sp, B, Hp, N, d, esz), lfh::places(r, sr, B, Hr, N, d, esz));
 }
 
 template <typename T, int MODE> int launch(const lf::RopeArgs& a, int B, unsigned wgs, hipStream_t st) {
@@ -111,16 +105,11 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
     if (!s[i].x) continue;
     if (overlaps(s[i].y, s[i].ny, s[i].x, s[i].nx) && !in_place(s[i])) return LINFUSION_ERR_OVERLAP;
     const Side& o = s[1 - i];
-    // (q and k may be columns of one projection, each turned in place: their spans interleave, their rows do not)
-    if (o.x && overlaps(s[i].y, s[i].ny, o.x, o.nx) &&
-        !side_by_side(s[i].y, s[i].sy, s[i].H, o.x, o.sx, o.H, B, d, esz))
-      return LINFUSION_ERR_OVERLAP;
+    if (o.x && meet(s[i].y, s[i].ny, s[i].sy, s[i].H, o.x, o.nx, o.sx, o.H, B, N, d, esz)) return LINFUSION_ERR_OVERLAP;
     if (overlaps(s[i].y, s[i].ny, positions, np)) return LINFUSION_ERR_OVERLAP;
     if (lengths && overlaps(s[i].y, s[i].ny, lengths, (size_t)B * 4)) return LINFUSION_ERR_OVERLAP;
   }
-  if (k && overlaps(q_out, s[0].ny, k_out, s[1].ny) &&
-      !side_by_side(s[0].y, s[0].sy, s[0].H, s[1].y, s[1].sy, s[1].H, B, d, esz))
-    return LINFUSION_ERR_OVERLAP;
+  if (k && meet(q_out, s[0].ny, s[0].sy, s[0].H, k_out, s[1].ny, s[1].sy, s[1].H, B, N, d, esz)) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   for (int i = 0; i < 2; ++i) {
     if (!s[i].x) continue;

@@ -181,3 +181,41 @@ def test_rope_of_more_tokens_than_a_grid_takes():
     far = dict(q=M << 20, k=None, qo=M << 20, ko=None, Hk=0, B=1, H=1, d=8, axes=1, channels=(8,), bases=(1e4,), pos=M)
     assert rope(N=(1 << 28) - 1, **far) == OK
     assert rope(N=1 << 28, **far) == -1
+
+
+@pytest.mark.parametrize("kw,status", [
+    # one token of each of many batch rows: queries and keys as columns of one [B, 1, 6 heads, 40] buffer, each in place
+    (dict(B=2, N=1, k=M + 320, sq=(240, 40, 240), sk=(240, 40, 240)), OK),
+    (dict(B=64, N=1, k=M + 320, sq=(240, 40, 7), sk=(240, 40, 9)), OK),
+    (dict(B=2, N=1, k=M + 304, sq=(240, 40, 240), sk=(240, 40, 240)), -7),
+    (dict(B=2, N=1, k=M + 336, sq=(240, 40, 240), sk=(240, 40, 240)), -7),   # the keys reach into the next row's queries
+    (dict(B=2, N=1, k=M + 320, sq=(200, 40, 240), sk=(240, 40, 240)), -7),
+    # the parts of each head side by side: [B, N, 4 heads, 3, 40]
+    (dict(Hk=4, k=M + 80, sq=(48000, 120, 480), sk=(48000, 120, 480)), OK),
+    (dict(Hk=4, k=M + 160, sq=(48000, 120, 480), sk=(48000, 120, 480)), OK),
+    (dict(Hk=4, k=M + 64, sq=(48000, 120, 480), sk=(48000, 120, 480)), -7),
+    # batch rows dealt in turn: [N, B, 6 heads, 40]
+    (dict(k=M + 320, sq=(240, 40, 480), sk=(240, 40, 480)), OK),
+    (dict(k=M + 320 + 480, sq=(480, 40, 960), sk=(480, 40, 960)), OK),
+    (dict(k=M + 336, sq=(240, 40, 480), sk=(240, 40, 480)), -7),
+], ids=str)
+def test_rope_of_interleaved_views_in_place(kw, status):
+    assert rope(qo=M, ko=kw["k"], sqo=kw["sq"], sko=kw["sk"], **kw) == status
+
+
+def test_rope_accepts_no_views_that_share_a_row():
+    """Random small views of queries and keys in place, judged element by element."""
+    import random
+    rng, taken = random.Random(3), 0
+    for _ in range(20000):
+        B, N, H, Hk, d = rng.randint(1, 3), rng.randint(1, 3), rng.randint(1, 3), rng.randint(1, 3), 8
+        strides = lambda: tuple(8 * rng.choice((0, 1, 2, 3, 4, 6, 8, 12, 16, 24)) for _ in range(3))
+        sq, sk, at = strides(), strides(), 8 * rng.randint(0, 24)
+        rows = lambda s, h, first: {first + b * s[0] + i * s[1] + n * s[2] for b in range(B) for i in range(h) for n in range(N)}
+        got = rope(B=B, N=N, H=H, Hk=Hk, d=d, channels=(8,), bases=(1e4,), axes=1, k=M + 2 * at, qo=M, ko=M + 2 * at, sq=sq, sqo=sq, sk=sk, sko=sk)
+        assert got in (OK, -7)
+        if got == OK:
+            taken += 1
+            q, k = rows(sq, H, 0), rows(sk, Hk, at)
+            assert len(q) == B * N * H and len(k) == B * N * Hk and not q & k, (B, N, H, Hk, sq, sk, at)
+    assert taken > 300

@@ -150,3 +150,19 @@ def test_refusals_on_the_device():
         a = dict(q=x, k=None, q_out=x, k_out=None, positions=pos, channels=(32,), bases=(1e4,)) | bad
         with pytest.raises(ValueError):
             lf.linfusion_rope(**a)
+
+
+@pytest.mark.parametrize("B,N,per_head", [(5, 1, False), (2, 1, True), (3, 30, True)])
+def test_interleaved_views_in_place(B, N, per_head):
+    """Queries and keys of one projection turned where they are: a token for each of several users, and the parts head by head."""
+    H, d = 4, 32
+    r = np.random.RandomState(10)
+    x, wx = stored(r.randn(*((B, N, H, 3, d) if per_head else (B, N, 3, H, d))), "bf16")
+    gx = x.cuda()
+    part = lambda t, i: t[:, :, :, i] if per_head else t[:, :, i]
+    q, k = (part(gx, i).permute(0, 2, 1, 3) for i in (0, 1))
+    pos = r.randint(0, 1000, (B, 1, N)).astype(np.int32)
+    lf.linfusion_rope(q, k, q, k, torch.from_numpy(pos).cuda(), (32,), (1e4,))
+    for i, t in ((0, q), (1, k)):
+        check(t, orc.rope(part(wx, i).transpose(0, 2, 1, 3), pos, (32,), (1e4,)), "bf16", STEPS["bf16"], str(i))
+    assert torch.equal(part(gx, 2).cpu(), part(x, 2))

@@ -489,7 +489,8 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
  * vectors are the forward call's; y and the statistics are formed again.  strides: x, f, dy, dh, dx, df.
  * Every output may be NULL (not all).  dx == dy with the same strides works in place; no other overlap.
  * dgate, dscale, dshift: fp32 rows with dmod_stride between them; with mod_stride 0 one row each, summed over the
- * batch.  dw_pre, dw_post: fp32 [C].  The workspace is needed only for these vectors (else NULL).
+ * batch.  dw_pre, dw_post: fp32 [C].  The workspace is needed only for these vectors (else NULL); its size never falls with
+ * N or B, so one of the longest sequences and the largest batch serves every call of that C.
  */
 int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, const float* scale, const float* w_pre,
                             const float* w_post, const void* dy, const void* dh, void* dx, void* df, float* dgate,

@@ -135,6 +135,14 @@ lf::NormView dev(const View& v) { return lf::NormView{v.batch, v.token}; }
 
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Workgroups of a backward call over the whole batch, at most.  shape_of's tokens per workgroup go in steps, so its number of them falls
+// here and there for a token more; this one never does, and a workspace of the longest sequence and largest batch serves all.
+size_t most_partials(int B, long long N, int C) {
+  const size_t per = C <= 512 ? 4 : 1, per_cu = C <= 512 ? 8 : (C <= 1536 ? 4 : 2);
+  const size_t by_tokens = B * (((size_t)N + per - 1) / per), by_cus = lfh::num_cu() * per_cu + B + B * ((size_t)N >> 20);
+  return by_tokens < by_cus ? by_tokens : by_cus;
+}
+
 }  // namespace
 
 extern "C" {
@@ -184,8 +192,7 @@ int linfusion_gate_norm_fwd(const void* x, const void* f, const float* gate, con
 
 size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C) {
   if (check_sizes(B, N, C, LINFUSION_DTYPE_F32) != LINFUSION_OK) return 0;
-  const Shape s = shape_of(B, N, C, true);
-  return up((size_t)B * s.wgs * 3 * C * 4) + up((size_t)B * 3 * C * 4);
+  return up(most_partials(B, N, C) * 3 * C * 4) + up((size_t)B * 3 * C * 4);
 }
 
 int linfusion_gate_norm_bwd(const void* x, const void* f, const float* gate, const float* scale, const float* w_pre,

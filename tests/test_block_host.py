@@ -219,3 +219,22 @@ def test_rope_accepts_no_views_that_share_a_row():
             q, k = rows(sq, H, 0), rows(sk, Hk, at)
             assert len(q) == B * N * H and len(k) == B * N * Hk and not q & k, (B, N, H, Hk, sq, sk, at)
     assert taken > 300
+
+
+@pytest.mark.parametrize("C", [8, 320, 512, 520, 640, 1024, 1032, 1280, 1536, 1544, 2048, 4096, 8192])
+def test_a_boundary_workspace_serves_shorter_sequences_and_smaller_batches(C):
+    size = lf.linfusion_gate_norm_bwd_workspace_bytes
+    tokens = sorted({n + e for n in [1 << i for i in range(22)] + [3 << i for i in range(20)] + list(range(1, 20000, 37)) for e in (-1, 0, 1)} - {0, -1})
+    for B in (1, 2, 3, 16, 1000):
+        held = [size(B, n, C) for n in tokens]
+        assert held == sorted(held)
+    for n in (1, 50, 513, 4097, 100000):
+        held = [size(B, n, C) for B in list(range(1, 300)) + [1000, 5000, 65535]]
+        assert held == sorted(held)
+    assert size(1, (1 << 40) // C, C) > 0
+
+
+def test_a_boundary_call_takes_a_longer_ones_workspace():
+    longest = lf.linfusion_gate_norm_bwd_workspace_bytes(1, 2000, 1280)
+    for n in (1, 512, 513, 1999, 2000):
+        assert norm_bwd(B=1, N=n, C=1280, mod=0, dmod=0, n=longest) == OK

@@ -515,7 +515,8 @@ size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C);
  *                   NULL; may be state_in itself.
  *   saved           NULL, or DEVICE memory of linfusion_delta_saved_bytes that keeps what linfusion_delta_bwd needs again.
  *   flags           0.
- *   workspace       DEVICE scratch of linfusion_delta_workspace_bytes, 16-byte aligned; not used when `saved` is given.
+ *   workspace       DEVICE scratch of linfusion_delta_workspace_bytes, 16-byte aligned; not used when `saved` is given.  The sizes
+ *                   of workspaces and saved memory never fall with B or N: the largest call's serve every call of these heads.
  * Tokens are taken in chunks of 64: an infinity or NaN in one may reach every output of its chunk, and reaches those behind.
  * No output may overlap another buffer, apart from state_out == state_in.
  */

@@ -60,14 +60,16 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   // pass does (d_k + d_v) / d_v times the work of the second.  us of the scans in runs : in one, bf16, heads of 64: 64 x 4096 tokens in 2
   // 141 : 103, 40 x 4096 in 3 103 : 85, 32 x 8192 in 4 162 : 164, 24 x 8192 in 5 127 : 145, 20 x 8192 in 6 106 : 130; heads of 128: 16 x
   // 8192 in 4 306 : 264, 8 x 8192 in 8 182 : 210.  In 5 of 8 chunks, 4 x 2560 tokens, heads of 64: 26 : 36.
-  const long long scans = z->heads * ((z->dvb + 1) / 2);
-  long long runs = lfh::num_cu() / scans;
-  if (runs > z->nc / 8) runs = z->nc / 8;
-  if (runs > 32) runs = 32;
+  const long long slices = (z->dvb + 1) / 2, few = z->nc / 8 < 32 ? z->nc / 8 : 32;
+  long long runs = lfh::num_cu() / (z->heads * slices);
+  if (runs > few) runs = few;
   if (runs < 5) runs = 1;
   z->run = (int)((z->nc + runs - 1) / runs);
   z->runs = (int)((z->nc + z->run - 1) / z->run);
-  const size_t blocks = z->runs > 1 ? (size_t)z->heads * z->runs * z->dkb * 1024 : 0;
+  // Runs come and go with the rounding of `run` and with the heads; memory is for as many as any smaller call has.
+  long long most = few < 5 ? 0 : z->heads * few;
+  if (most > lfh::num_cu() / slices) most = lfh::num_cu() / slices;
+  const size_t blocks = (size_t)most * z->dkb * 1024;
   z->parts = up(blocks * (z->dvb + z->dkb));
   z->joined = up(blocks * z->dvb);
   return LINFUSION_OK;

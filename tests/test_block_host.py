@@ -238,3 +238,20 @@ def test_a_boundary_call_takes_a_longer_ones_workspace():
     longest = lf.linfusion_gate_norm_bwd_workspace_bytes(1, 2000, 1280)
     for n in (1, 512, 513, 1999, 2000):
         assert norm_bwd(B=1, N=n, C=1280, mod=0, dmod=0, n=longest) == OK
+
+
+@pytest.mark.parametrize("dk,dv,dtype", [(8, 8, 0), (64, 64, 2), (128, 128, 2), (40, 24, 1), (160, 256, 0), (96, 16, 1)])
+def test_delta_workspaces_serve_shorter_sequences_and_smaller_batches(dk, dv, dtype):
+    tokens = sorted(set(range(1, 40000, 61)) | {64 * n + e for n in range(1, 700, 3) for e in (-1, 0, 1)} | {1 << 20, 1 << 24, (1 << 30) - 1})
+    for size in (lf.linfusion_delta_workspace_bytes, lf.linfusion_delta_saved_bytes, lf.linfusion_delta_bwd_workspace_bytes):
+        for B, H, Hk in ((1, 1, 1), (1, 2, 1), (1, 10, 10), (3, 8, 4), (40, 16, 16)):
+            held = [size(B, H, Hk, n, dk, dv, dtype) for n in tokens]
+            assert held == sorted(held)
+        for n in (1, 64, 2559, 2560, 5000, 65536):
+            held = [size(B, 2, 1, n, dk, dv, dtype) for B in list(range(1, 200)) + [1000, 32767]]
+            assert held == sorted(held)
+    last = 18496
+    longest = lf.linfusion_delta_workspace_bytes(1, 2, 2, last, dk, dv, dtype)
+    big = dict(B=1, H=2, Hk=2, dk=dk, dv=dv, dtype=dtype, ws=M << 20, out=M << 16, q=M << 12, k=M << 13, v=M << 14, g=M << 17, beta=M << 18, s1=M << 19)
+    for n in (1, 18432, 18495, last):
+        assert delta_fwd(N=n, n=longest, **big) == OK

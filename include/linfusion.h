@@ -475,6 +475,7 @@ int linfusion_rope(const void* q, const void* k, void* q_out, void* k_out, const
  *   x, f, y, h      [B, N, C] views, strides[i] of them in this order (strides NULL: all contiguous); C a multiple of 8 up to
  *                   8192.  f NULL: no block output (the first norm of a model: y = residual_scale * x).  y or h may be NULL
  *                   (not both): not written.  y == x with the same strides works in place; no other overlap.
+ *                   Rows may come in any order ([N, B, C] tensors, columns of one buffer).
  *   gate, scale, shift  fp32 modulation rows, row b at b * mod_stride (a multiple of 4; 0: one row for the batch); each may
  *                   be NULL (1, 0, 0).
  *   w_pre, w_post   fp32 [C] or NULL (1).

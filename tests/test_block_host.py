@@ -255,3 +255,35 @@ def test_delta_workspaces_serve_shorter_sequences_and_smaller_batches(dk, dv, dt
     big = dict(B=1, H=2, Hk=2, dk=dk, dv=dv, dtype=dtype, ws=M << 20, out=M << 16, q=M << 12, k=M << 13, v=M << 14, g=M << 17, beta=M << 18, s1=M << 19)
     for n in (1, 18432, 18495, last):
         assert delta_fwd(N=n, n=longest, **big) == OK
+
+
+# a batch of 2 sequences of 50 tokens of 320 channels, tokens first; and as halves of rows of 640
+TOKENS_FIRST, LEFT_HALF = (320, 640), (32000, 640)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(strides=TOKENS_FIRST * 4), OK), (dict(strides=D * 2 + TOKENS_FIRST * 2), OK), (dict(y=M, strides=TOKENS_FIRST * 4), OK),
+    (dict(B=1, mod=0, strides=(0, 320) * 4), OK), (dict(N=1, strides=(320, 0) * 4), OK), (dict(N=1, strides=(640, 320) * 4), OK),
+    (dict(h=8 * M + 640, strides=D * 2 + LEFT_HALF * 2), OK), (dict(h=8 * M + 640, strides=D * 2 + (640, 1280) * 2), OK),
+    (dict(y=M + 640, f=2 * M + 640, h=2 * M, strides=LEFT_HALF * 4), OK),
+    (dict(strides=D * 2 + (160, 640) + D), -7), (dict(strides=D * 2 + (320, 480) + D), -7), (dict(strides=D * 3 + (640, 640)), -7),
+    (dict(strides=D * 2 + (0, 320) + D), -7), (dict(strides=D * 3 + (320, 0)), -7), (dict(strides=D * 2 + (15984, 320) + D), -7),
+    (dict(N=1, strides=D * 3 + (312, 320)), -7), (dict(y=M, strides=TOKENS_FIRST + D * 3), -7),
+    (dict(h=8 * M + 624, strides=D * 2 + LEFT_HALF * 2), -7), (dict(h=8 * M + 640, strides=D * 3 + LEFT_HALF), -7), (dict(y=M + 624, strides=LEFT_HALF * 4), -7),
+], ids=str)
+def test_gate_norm_rows_of_any_order(kw, status):
+    assert norm_fwd(**kw) == status
+
+
+def norm_bwd_views(strides, **kw):
+    a = dict(dx=7 * M, df=8 * M, dy=5 * M, dh=6 * M) | kw
+    return lf.library().linfusion_gate_norm_bwd(M, 2 * M, 3 * M, 4 * M, None, None, a["dy"], a["dh"], a["dx"], a["df"], 9 * M, 10 * M, 11 * M, None, None, 2, 50,
+                                                320, 2, 1.0, 1e-6, 0, None, (ctypes.c_longlong * 12)(*strides), 320, 320, 20 * M, WS, None)
+
+
+@pytest.mark.parametrize("strides,kw,status", [
+    (TOKENS_FIRST * 6, {}, OK), (D * 4 + TOKENS_FIRST * 2, {}, OK), (TOKENS_FIRST * 6, dict(dx=5 * M), OK), (D * 4 + LEFT_HALF * 2, dict(df=7 * M + 640), OK),
+    (D * 4 + (160, 640) + D, {}, -7), (D * 5 + (320, 480), {}, -7), (D * 2 + TOKENS_FIRST + D * 3, dict(dx=5 * M), -7), (D * 4 + LEFT_HALF * 2, dict(df=7 * M + 624), -7),
+], ids=str)
+def test_gate_norm_gradients_of_any_order(strides, kw, status):
+    assert norm_bwd_views(strides, **kw) == status

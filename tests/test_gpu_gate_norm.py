@@ -301,3 +301,35 @@ def test_many_tokens(size, dtype):
     c = make(*size, dtype, 91, False, False)
     g = on_gpu(c)
     check_all(c, *forward(c, g), backward(c, g))
+
+
+@pytest.mark.parametrize("order", ["tokens first", "columns of one buffer"])
+@pytest.mark.parametrize("dims,dtype", [((3, 37, 320), "bf16"), ((2, 1, 1040), "f32"), ((1, 9, 64), "f16")], ids=str)
+def test_rows_of_any_order(dims, dtype, order):
+    """Tensors of [N, B, C], and all of them as columns of one buffer: the bits of contiguous ones, and nothing else written."""
+    B, N, C = dims
+    c = make(B, N, C, dtype, 77, rms=False, post=True)
+    g = on_gpu(c)
+    y, h = forward(c, g)
+    d = backward(c, g)
+    names = ("x", "f", "dy", "dh", "y", "h", "dx", "df")
+    if order == "tokens first":
+        room = {n: torch.full((N, B, C), 5.0, dtype=TORCH[dtype], device="cuda") for n in names}
+        view = {n: t.transpose(0, 1) for n, t in room.items()}
+    else:
+        room = torch.full((B, N, len(names) + 1, C), 5.0, dtype=TORCH[dtype], device="cuda")
+        view = {n: room[:, :, i] for i, n in enumerate(names)}
+    for n in ("x", "f", "dy", "dh"):
+        view[n].copy_(g[n])
+    lf.linfusion_gate_norm_fwd(view["x"], view["f"], g["gate"], g["scale"], g["shift"], view["y"], view["h"], **rest(c, g))
+    vectors = {n: torch.full_like(t, float("nan")) for n, t in d.items() if n not in ("dx", "df")}
+    ws = torch.empty(lf.linfusion_gate_norm_bwd_workspace_bytes(B, N, C), dtype=torch.uint8, device="cuda")
+    lf.linfusion_gate_norm_bwd(view["x"], view["f"], g["gate"], g["scale"], view["dy"], view["dh"], view["dx"], view["df"], **vectors, workspace=ws,
+                               **rest(c, g))
+    for n, want in {"y": y, "h": h, **d}.items():
+        assert torch.equal(view[n] if n in view else vectors[n], want), n
+    for n in ("x", "f", "dy", "dh"):
+        assert torch.equal(view[n], g[n])
+    if order != "tokens first":
+        assert bool((room[:, :, -1] == 5.0).all())
+    check_all(c, y, h, d)

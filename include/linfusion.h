@@ -519,7 +519,8 @@ size_t linfusion_gate_norm_bwd_workspace_bytes(int B, long long N, int C);
  *   workspace       DEVICE scratch of linfusion_delta_workspace_bytes, 16-byte aligned; not used when `saved` is given.  The sizes
  *                   of workspaces and saved memory never fall with B or N: the largest call's serve every call of these heads.
  * Tokens are taken in chunks of 64: an infinity or NaN in one may reach every output of its chunk, and reaches those behind.
- * No output may overlap another buffer, apart from state_out == state_in.
+ * No output may overlap another buffer, apart from state_out == state_in; views may be columns of one buffer (out beside q, k, v;
+ * below, dq beside dk, dv; dg beside dbeta), judged as those of linfusion_rope.
  */
 int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float* g, const float* beta,
                         const float* state_in, void* out, float* state_out, const int* lengths, void* saved,

@@ -4,7 +4,6 @@
 #include <stdint.h>
 
 #include <cmath>
-#include <initializer_list>
 
 #include "lf_delta.hpp"
 #include "lf_delta_bwd.hpp"
@@ -75,7 +74,9 @@ int make_sizes(int B, int H, int H_k, long long N, int dk, int dv, int dtype, Si
   return LINFUSION_OK;
 }
 
-struct Range { const void* p; size_t n; bool written; const void* same; };   // `same`: the one range it may coincide with
+// What a call reads or writes; `same`: the one range it may coincide with; a view's `rows` may lie between another's.
+struct Range { const void* p; size_t n; bool written; const void* same; lfh::Places rows; };
+Range plain(const void* p, size_t n, bool written, const void* same = nullptr) { return Range{p, n, written, same, lfh::Places{}}; }
 
 bool clash(const Range* r, int n) {
   for (int i = 0; i < n; ++i)
@@ -83,6 +84,7 @@ bool clash(const Range* r, int n) {
       if (!r[i].p || !r[j].p || !(r[i].written || r[j].written)) continue;
       if (!overlaps(r[i].p, r[i].n, r[j].p, r[j].n)) continue;
       if (r[i].p == r[j].p && r[i].n == r[j].n && (r[i].same == r[j].p && r[i].same)) continue;
+      if (r[i].rows.width && r[j].rows.width && lfh::apart(r[i].rows, r[j].rows)) continue;
       return true;
     }
   return false;
@@ -90,7 +92,7 @@ bool clash(const Range* r, int n) {
 
 // rows of `d` channels of the tensors' type
 int check_rows(const void* p, const long long* given, int B, int H, long long N, int d, size_t esz, bool written,
-               lf::DeltaView* v, size_t* bytes) {
+               lf::DeltaView* v, Range* range) {
   long long s[3] = {H * N * d, N * d, d};
   const long long extent[3] = {B, H, N};
   for (int i = 0; i < 3; ++i)
@@ -100,27 +102,28 @@ int check_rows(const void* p, const long long* given, int B, int H, long long N,
   const int rc = lfh::check_strides(s, B, H, N, d, esz, written);
   if (rc != LINFUSION_OK) return rc;
   *v = lf::DeltaView{s[0], s[1], s[2]};
-  *bytes = lfh::span_bytes(s, B, H, N, d, esz);
+  *range = Range{p, lfh::span_bytes(s, B, H, N, d, esz), written, nullptr, lfh::places(p, s, B, H, N, d, esz)};
   return LINFUSION_OK;
 }
 
-// one fp32 value per token and head, at any strides: judged as rows of four at four times the strides
-int check_scalars(std::initializer_list<const void*> ps, const long long* given, int B, int H, long long N, bool written,
-                  lf::DeltaView* v, size_t* bytes) {
+// two tensors of one fp32 value per token and head, at any strides: judged as rows of four at four times the strides
+int check_scalars(const void* p0, const void* p1, const long long* given, int B, int H, long long N, bool written,
+                  lf::DeltaView* v, Range* range0, Range* range1) {
   long long s[3] = {H * N, N, 1};
   const long long extent[3] = {B, H, N};
   for (int i = 0; i < 3; ++i)
     if (extent[i] == 1) s[i] = 0;
     else if (given) s[i] = given[i];
-  for (const void* p : ps)
-    if ((uintptr_t)p & 3) return LINFUSION_ERR_MISALIGNED;
+  if (((uintptr_t)p0 | (uintptr_t)p1) & 3) return LINFUSION_ERR_MISALIGNED;
   for (int i = 0; i < 3; ++i)
     if (s[i] < 0 || s[i] >= 1LL << 44) return LINFUSION_ERR_INVALID;
   const long long wide[3] = {4 * s[0], 4 * s[1], 4 * s[2]};
   const int rc = lfh::check_strides(wide, B, H, N, 4, 4, written);
   if (rc != LINFUSION_OK) return rc;
   *v = lf::DeltaView{s[0], s[1], s[2]};
-  *bytes = (size_t)((B - 1) * s[0] + (H - 1) * s[1] + (N - 1) * s[2] + 1) * 4;
+  const size_t bytes = (size_t)((B - 1) * s[0] + (H - 1) * s[1] + (N - 1) * s[2] + 1) * 4;
+  *range0 = Range{p0, bytes, written, nullptr, lfh::places(p0, s, B, H, N, 1, 4)};
+  *range1 = Range{p1, bytes, written, nullptr, lfh::places(p1, s, B, H, N, 1, 4)};
   return LINFUSION_OK;
 }
 
@@ -274,12 +277,12 @@ int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float
   int rc = make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z);
   if (rc != LINFUSION_OK) return rc;
   lf::DeltaArgs a{};
-  size_t nq, nk, nv, no, ng;
-  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &nq)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &nk)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &nv)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(out, out_strides, B, H, N, d_v, z.esz, true, &a.vo, &no)) != LINFUSION_OK) return rc;
-  if ((rc = check_scalars({g, beta}, gate_strides, B, H, N, false, &a.vg, &ng)) != LINFUSION_OK) return rc;
+  Range rq, rk, rv, ro, rg, rb;
+  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &rq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &rk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &rv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(out, out_strides, B, H, N, d_v, z.esz, true, &a.vo, &ro)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars(g, beta, gate_strides, B, H, N, false, &a.vg, &rg, &rb)) != LINFUSION_OK) return rc;
   if (((uintptr_t)state_in | (uintptr_t)state_out | (uintptr_t)saved) & 15) return LINFUSION_ERR_MISALIGNED;
   if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
   if (saved && saved_bytes < z.saved()) return LINFUSION_ERR_WORKSPACE;
@@ -288,10 +291,9 @@ int linfusion_delta_fwd(const void* q, const void* k, const void* v, const float
     if ((uintptr_t)workspace & 15) return LINFUSION_ERR_MISALIGNED;
   }
   const size_t ns = (size_t)z.heads * d_k * d_v * 4;
-  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
-                          {beta, ng, false, nullptr}, {lengths, (size_t)B * 4, false, nullptr},
-                          {state_in, ns, false, state_out}, {state_out, ns, true, state_in}, {out, no, true, nullptr},
-                          saved ? Range{saved, z.saved(), true, nullptr} : Range{workspace, z.forward(), true, nullptr}};
+  const Range ranges[] = {rq, rk, rv, rg, rb, ro, plain(lengths, (size_t)B * 4, false), plain(state_in, ns, false, state_out),
+                          plain(state_out, ns, true, state_in),
+                          saved ? plain(saved, z.saved(), true) : plain(workspace, z.forward(), true)};
   if (clash(ranges, 10)) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
@@ -322,16 +324,16 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   int rc = make_sizes(B, H, H_k, N, d_k, d_v, dtype, &z);
   if (rc != LINFUSION_OK) return rc;
   lf::DeltaArgs a{};
-  size_t nq, nk, nv, ng, ndo, ndq, ndk, ndv, ndg;
-  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &nq)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &nk)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &nv)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(dout, dout_strides, B, H, N, d_v, z.esz, false, &a.vdo, &ndo)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(dq, dq_strides, B, H_k, N, d_k, z.esz, true, &a.vdq, &ndq)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(dk, dk_strides, B, H_k, N, d_k, z.esz, true, &a.vdk, &ndk)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(dv, dv_strides, B, H, N, d_v, z.esz, true, &a.vdv, &ndv)) != LINFUSION_OK) return rc;
-  if ((rc = check_scalars({g, beta}, gate_strides, B, H, N, false, &a.vg, &ng)) != LINFUSION_OK) return rc;
-  if ((rc = check_scalars({dg, dbeta}, dgate_strides, B, H, N, true, &a.vdg, &ndg)) != LINFUSION_OK) return rc;
+  Range rq, rk, rv, rg, rb, rdo, rdq, rdk, rdv, rdg, rdb;
+  if ((rc = check_rows(q, q_strides, B, H_k, N, d_k, z.esz, false, &a.vq, &rq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, k_strides, B, H_k, N, d_k, z.esz, false, &a.vk, &rk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, v_strides, B, H, N, d_v, z.esz, false, &a.vv, &rv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dout, dout_strides, B, H, N, d_v, z.esz, false, &a.vdo, &rdo)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dq, dq_strides, B, H_k, N, d_k, z.esz, true, &a.vdq, &rdq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dk, dk_strides, B, H_k, N, d_k, z.esz, true, &a.vdk, &rdk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(dv, dv_strides, B, H, N, d_v, z.esz, true, &a.vdv, &rdv)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars(g, beta, gate_strides, B, H, N, false, &a.vg, &rg, &rb)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars(dg, dbeta, dgate_strides, B, H, N, true, &a.vdg, &rdg, &rdb)) != LINFUSION_OK) return rc;
   if (((uintptr_t)state_in | (uintptr_t)dstate_out | (uintptr_t)dstate_in | (uintptr_t)saved) & 15)
     return LINFUSION_ERR_MISALIGNED;
   if ((uintptr_t)lengths & 3) return LINFUSION_ERR_MISALIGNED;
@@ -340,12 +342,9 @@ int linfusion_delta_bwd(const void* q, const void* k, const void* v, const float
   if (!workspace || workspace_bytes < need) return LINFUSION_ERR_WORKSPACE;
   if ((uintptr_t)workspace & 15) return LINFUSION_ERR_MISALIGNED;
   const size_t ns = (size_t)z.heads * d_k * d_v * 4;
-  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
-                          {beta, ng, false, nullptr}, {lengths, (size_t)B * 4, false, nullptr}, {state_in, ns, false, nullptr},
-                          {dout, ndo, false, nullptr}, {saved, z.saved(), false, nullptr},
-                          {dstate_out, ns, false, dstate_in}, {dstate_in, ns, true, dstate_out}, {dq, ndq, true, nullptr},
-                          {dk, ndk, true, nullptr}, {dv, ndv, true, nullptr}, {dg, ndg, true, nullptr},
-                          {dbeta, ndg, true, nullptr}, {workspace, need, true, nullptr}};
+  const Range ranges[] = {rq, rk, rv, rg, rb, rdo, rdq, rdk, rdv, rdg, rdb, plain(lengths, (size_t)B * 4, false),
+                          plain(state_in, ns, false), plain(saved, z.saved(), false), plain(dstate_out, ns, false, dstate_in),
+                          plain(dstate_in, ns, true, dstate_out), plain(workspace, need, true)};
   if (clash(ranges, 17)) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta;
@@ -374,21 +373,19 @@ int linfusion_delta_step(const void* q, const void* k, const void* v, const floa
   int rc = make_sizes(B, H, H_k, 1, d_k, d_v, dtype, &z);
   if (rc != LINFUSION_OK) return rc;
   lf::DeltaView vq, vk, vv, vo, vg;
-  size_t nq, nk, nv, no, ng;
+  Range rq, rk, rv, ro, rg, rb;
   struct Three { long long s[3]; };
   auto three = [](const long long* s, int heads, int d) {
     return s ? Three{{s[0], s[1], 0}} : Three{{(long long)heads * d, d, 0}};
   };
-  if ((rc = check_rows(q, three(q_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vq, &nq)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(k, three(k_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vk, &nk)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(v, three(v_strides, H, d_v).s, B, H, 1, d_v, z.esz, false, &vv, &nv)) != LINFUSION_OK) return rc;
-  if ((rc = check_rows(out, three(out_strides, H, d_v).s, B, H, 1, d_v, z.esz, true, &vo, &no)) != LINFUSION_OK) return rc;
-  if ((rc = check_scalars({g, beta}, three(gate_strides, H, 1).s, B, H, 1, false, &vg, &ng)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(q, three(q_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vq, &rq)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(k, three(k_strides, H_k, d_k).s, B, H_k, 1, d_k, z.esz, false, &vk, &rk)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(v, three(v_strides, H, d_v).s, B, H, 1, d_v, z.esz, false, &vv, &rv)) != LINFUSION_OK) return rc;
+  if ((rc = check_rows(out, three(out_strides, H, d_v).s, B, H, 1, d_v, z.esz, true, &vo, &ro)) != LINFUSION_OK) return rc;
+  if ((rc = check_scalars(g, beta, three(gate_strides, H, 1).s, B, H, 1, false, &vg, &rg, &rb)) != LINFUSION_OK) return rc;
   if (((uintptr_t)state_in | (uintptr_t)state_out) & 15) return LINFUSION_ERR_MISALIGNED;
   const size_t ns = (size_t)z.heads * d_k * d_v * 4;
-  const Range ranges[] = {{q, nq, false, nullptr}, {k, nk, false, nullptr}, {v, nv, false, nullptr}, {g, ng, false, nullptr},
-                          {beta, ng, false, nullptr}, {state_in, ns, false, state_out}, {state_out, ns, true, state_in},
-                          {out, no, true, nullptr}};
+  const Range ranges[] = {rq, rk, rv, rg, rb, ro, plain(state_in, ns, false, state_out), plain(state_out, ns, true, state_in)};
   if (clash(ranges, 8)) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   const lf::DeltaStepArgs a{q, k, v, g, beta, state_in, out, state_out, vq.b, vq.h, vk.b, vk.h, vv.b, vv.h,

@@ -287,3 +287,42 @@ def norm_bwd_views(strides, **kw):
 ], ids=str)
 def test_gate_norm_gradients_of_any_order(strides, kw, status):
     assert norm_bwd_views(strides, **kw) == status
+
+
+# 2 rows of 100 tokens, 2 key heads of 40, 4 value heads of 64: columns of a [B, N, 416] buffer, in elements
+COLUMNS = dict(sq=(41600, 40, 416), sk=(41600, 40, 416), sv=(41600, 64, 416))
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=M, k=M + 160, v=M + 320, **COLUMNS), OK),
+    # the outputs behind the inputs in rows of 672; then one channel block too early, and across the end of a row
+    (dict(q=M, k=M + 160, v=M + 320, out=M + 832, sq=(67200, 40, 672), sk=(67200, 40, 672), sv=(67200, 64, 672), so=(67200, 64, 672)), OK),
+    (dict(q=M, k=M + 160, v=M + 320, out=M + 816, sq=(67200, 40, 672), sk=(67200, 40, 672), sv=(67200, 64, 672), so=(67200, 64, 672)), -7),
+    (dict(q=M, k=M + 160, v=M + 320, out=M + 848, sq=(67200, 40, 672), sk=(67200, 40, 672), sv=(67200, 64, 672), so=(67200, 64, 672)), -7),
+    (dict(v=3 * M, out=3 * M, sv=(41600, 64, 416), so=(41600, 64, 416)), -7),
+    (dict(v=3 * M, out=3 * M + 128, sv=(51200, 128, 512), so=(51200, 128, 512)), OK),   # each head's output beside its values
+    (dict(v=3 * M, out=3 * M + 112, sv=(51200, 128, 512), so=(51200, 128, 512)), -7),
+    (dict(s1=3 * M + 128, sv=(41600, 64, 416)), -7),   # a state between a tensor's rows: not looked into
+], ids=str)
+def test_delta_forward_columns_of_one_buffer(kw, status):
+    assert delta_fwd(**kw) == status
+
+
+def delta_bwd_views(dq, dk, dv, dg, dbeta, tokens, scalars):
+    s = SIZES
+    row = lambda head: i64x3(s["N"] * tokens, head, tokens)
+    return lf.library().linfusion_delta_bwd(M, 2 * M, 3 * M, 4 * M, 5 * M, None, 7 * M, None, None, 0, dq, dk, dv, dg, dbeta, None, None, *sizes(), 1.0, 0,
+                                            *[None] * 5, row(40), row(40), row(64), i64x3(*scalars), 20 * M, lf.linfusion_delta_bwd_workspace_bytes(*sizes()), None)
+
+
+@pytest.mark.parametrize("args,status", [
+    ((9 * M, 9 * M + 160, 9 * M + 320, 12 * M, 12 * M + 16, 416, (800, 1, 8)), OK),
+    ((9 * M + 512, 9 * M + 672, 9 * M, 12 * M + 16, 12 * M, 416, (800, 1, 8)), OK),
+    ((9 * M, 9 * M + 160, 9 * M + 320, 12 * M, 12 * M + 4, 416, (800, 2, 8)), OK),
+    ((9 * M, 9 * M + 144, 9 * M + 320, 12 * M, 12 * M + 16, 416, (800, 1, 8)), -7), ((9 * M, 9 * M + 160, 9 * M + 336, 12 * M, 12 * M + 16, 416, (800, 1, 8)), -7),
+    ((9 * M, 9 * M + 160, 9 * M + 320, 12 * M, 12 * M + 12, 416, (800, 1, 8)), -7), ((9 * M, 9 * M + 160, 9 * M + 320, 12 * M, 12 * M + 20, 416, (800, 1, 8)), -7),
+    ((9 * M, 9 * M + 160, 9 * M + 320, 12 * M, 12 * M + 8, 416, (800, 2, 8)), -7), ((9 * M, 9 * M + 160, 9 * M + 320, 9 * M + 832, 12 * M, 432, (21600, 1, 216)), OK),
+    ((9 * M, 9 * M + 160, 9 * M + 320, 9 * M + 828, 12 * M, 432, (21600, 1, 216)), -7),
+], ids=str)
+def test_delta_gradients_as_columns_of_one_buffer(args, status):
+    assert delta_bwd_views(*args) == status

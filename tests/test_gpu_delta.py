@@ -444,3 +444,37 @@ def test_a_corrected_key_answers_its_value(dtype):
     ref = oracle(c)[0]
     assert np.abs(ref).max() < 8
     check(out, ref, dtype, 18, "out", scale=2.0 ** 15)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk,N", [(4, 2, 130), (2, 2, 1)], ids=str)
+def test_columns_of_one_buffer(H, Hk, N, dtype):
+    """Outputs beside q, k and v in one [B, N, ...] buffer, and their gradients beside each other in another, as those of the scalars: the
+    bits of tensors of their own, and nothing else written."""
+    B, dk, dv = 2, 40, 56
+    c = make(B, H, Hk, N, dk, dv, dtype, seed=19)
+    g = on_gpu(c)
+    out, last, saved = forward(c, g, saved=True)
+    d = backward(c, g, saved)
+    widths = (Hk * dk, Hk * dk, H * dv, H * dv, 8)
+    room, droom = (torch.full((B, N, sum(widths)), 3.0, dtype=TORCH[dtype], device="cuda") for _ in range(2))
+    scalars = torch.full((B, N, 2 * H + 1), 3.0, device="cuda")
+    cut = lambda t: [p.unflatten(-1, (-1, w)).permute(0, 2, 1, 3) for p, w in zip(t.split(widths, -1), (dk, dk, dv, dv, 8))]
+    q, k, v, o, _ = cut(room)
+    for to, n in ((q, "q"), (k, "k"), (v, "v")):
+        to.copy_(g[n])
+    packed = dict(g, q=q, k=k, v=v)
+    end = torch.empty_like(last)
+    lf.linfusion_delta_fwd(q, k, v, g["g"], g["beta"], o, scale=c["scale"], state_in=g["state"], state_out=end, saved=torch.empty_like(saved))
+    assert torch.equal(o, out) and torch.equal(end, last)
+    dq, dk_, dv_, _, spare = cut(droom)
+    into = {"q": dq, "k": dk_, "v": dv_, "g": scalars[..., :H].permute(0, 2, 1), "beta": scalars[..., H:2 * H].permute(0, 2, 1)}
+    backward(c, packed, saved, into=into)
+    for n in ("q", "k", "v", "g", "beta"):
+        assert torch.equal(into[n], d[n]), n
+        assert n not in packed or n in ("g", "beta") or torch.equal(packed[n], g[n])
+    assert bool((cut(room)[4] == 3.0).all()) and bool((spare == 3.0).all()) and bool((scalars[..., 2 * H] == 3.0).all())
+    if N == 1:
+        o.fill_(float("nan"))
+        lf.linfusion_delta_step(q[:, :, 0], k[:, :, 0], v[:, :, 0], g["g"][:, :, 0], g["beta"][:, :, 0], g["state"], end, o[:, :, 0], scale=c["scale"])
+        check_forward(c, o, end)

@@ -6,6 +6,7 @@ import torch
 import paper_2409_02097_amd as lf
 from oracle import block_oracle as orc
 from tests.block_parity import TORCH, check, f64, stored
+from tests.delta_bounds import excess, references
 
 pytestmark = pytest.mark.gpu
 
@@ -478,3 +479,61 @@ def test_columns_of_one_buffer(H, Hk, N, dtype):
         o.fill_(float("nan"))
         lf.linfusion_delta_step(q[:, :, 0], k[:, :, 0], v[:, :, 0], g["g"][:, :, 0], g["beta"][:, :, 0], g["state"], end, o[:, :, 0], scale=c["scale"])
         check_forward(c, o, end)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1, 130, 64, 64), (1, 1, 1, 200, 32, 128), (1, 4, 2, 130, 64, 64), (2, 2, 2, 150, 128, 128), (1, 4, 1, 100, 40, 56),
+                                   (1, 2, 1, 90, 160, 40), (1, 2, 1, 90, 96, 96)], ids=str)
+def test_whole_gradients_in_fp32(shape):
+    """In the 2-norm, where an operand kept to 16 bits shows (test_delta_bounds.py)."""
+    c = make(*shape, "f32", seed=sum(shape) + 1)
+    d = backward(c, on_gpu(c))
+    worst = excess(c, {n: f64(d[n]) for n in ("q", "k", "v", "g", "beta")}, *references(c))
+    assert max(worst.values()) <= 1, worst
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dk", [40, 64, 96, 128, 160])
+def test_many_heads_of_every_width(dk, dtype):
+    """Enough heads for scans of 32 value channels: 3 workgroups for the 5 blocks of 72 channels, 64 heads; more than one chunk."""
+    c = make(8, 8, 8, 70, dk, 72, dtype, seed=dk)
+    g = on_gpu(c)
+    out, last, saved = forward(c, g, saved=True)
+    check_forward(c, out, last)
+    check_backward(c, backward(c, g, saved))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dk,dv,group", [(40, 56, 2), (64, 128, 2), (64, 64, 4), (160, 24, 2), (136, 40, 3)])
+def test_gradients_summed_over_shared_keys(dk, dv, group, dtype):
+    c = make(2, 2 * group, 2, 130, dk, dv, dtype, seed=dk + dv + group)
+    g = on_gpu(c)
+    out, last, saved = forward(c, g, saved=True)
+    check_forward(c, out, last)
+    check_backward(c, backward(c, g, saved))
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [("f32", 64, 64), ("f32", 128, 64), ("f32", 160, 24), ("f16", 128, 40), ("f32", 96, 48)])
+def test_runs_of_every_width(dtype, dk, dv):
+    """Two heads in runs, 16 value channels a workgroup."""
+    c = make(1, 2, 1, 64 * 42 + 3, dk, dv, dtype, seed=dk + dv)
+    out, last, _ = forward(c, on_gpu(c))
+    check_forward(c, out, last)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dk", [40, 64, 96, 128, 160])
+def test_runs_of_many_heads_of_every_width(dk, dtype):
+    """16 heads of 64 value channels in six runs of eight chunks: both passes take 32 channels a workgroup, the first one the columns of
+    the identity too."""
+    B, H, N, dv = 1, 16, 64 * 48 - 7, 64
+    c = make(B, H, H, N, dk, dv, dtype, seed=dk)
+    out, last, _ = forward(c, on_gpu(c))
+    ref, s = np.zeros((B, H, N, dv)), np.array(c["state"])
+    for t in range(N):   # (all heads at once; the states of all tokens would be gigabytes)
+        key, qry = c["k"][:, :, t], c["q"][:, :, t]
+        s *= np.exp(c["g"][:, :, t])[..., None, None]
+        u = c["beta"][:, :, t, None] * (c["v"][:, :, t] - np.matmul(key[:, :, None], s)[:, :, 0])
+        s += key[..., None] * u[:, :, None]
+        ref[:, :, t] = c["scale"] * np.matmul(qry[:, :, None], s)[:, :, 0]
+    check(out, ref, dtype, chain(c), "out")
+    check(last, s, "f32", chain(c), "state")

@@ -74,7 +74,7 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
     return LINFUSION_ERR_UNSUPPORTED;
   if (d % 8 || d > 2 * lf::kRopePairs) return LINFUSION_ERR_UNSUPPORTED;
   if (axes < 1 || axes > lf::kRopeAxes) return LINFUSION_ERR_UNSUPPORTED;
-  if (N >= 1LL << 28) return LINFUSION_ERR_INVALID;   // (a grid has at most 2^32 threads)
+  if (N >= 1LL << 28) return LINFUSION_ERR_INVALID;
   lf::RopeArgs a{};
   int at = 0;
   bool whole = true;
@@ -128,13 +128,13 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
   // Tokens per workgroup: 16 KB of rows, so that the angles are a small part of its work, while every CU has several workgroups
   // (us per call, 8 / 16 / 32 / 64 KB: bf16 81120 x 2 x 16 x 128 252 / 227 / 233 / 236, fp32 2 x 36503 x 2 x 8 x 40 60 / 57 / 60 / 66)
   const long long heads = H + (k ? H_k : 0), all = (long long)B * N;
+  const auto many = [&](long long t) { return (N + t - 1) / t >= 1LL << 24; };   // (a grid has at most 2^32 threads a row)
   int tokens = 1;
-  while (tokens < 64 && all / (2 * tokens) >= 4LL * lfh::num_cu() && tokens * heads * d * (long long)esz < 16384 &&
-         2 * tokens * a.pairs * 8 <= 32768)
+  while (tokens < 64 && 2 * tokens * a.pairs * 8 <= 32768 &&
+         (many(tokens) || (all / (2 * tokens) >= 4LL * lfh::num_cu() && tokens * heads * d * (long long)esz < 16384)))
     tokens *= 2;
   a.tokens = tokens;
-  const long long wgs = (N + tokens - 1) / tokens;
-  if (wgs >= 1LL << 24) return LINFUSION_ERR_INVALID;
+  const long long wgs = (N + tokens - 1) / tokens;   // (32 tokens are always possible: below 2^24)
   const int mode = (flags & LINFUSION_FLAG_ROPE_NEIGHBOURS) ? 0 : (whole ? 1 : 2);
   const hipStream_t st = (hipStream_t)stream;
   rc = dtype == LINFUSION_DTYPE_F16   ? run<lf::F16>(a, B, (unsigned)wgs, mode, st)

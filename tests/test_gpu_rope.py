@@ -166,3 +166,24 @@ def test_interleaved_views_in_place(B, N, per_head):
     for i, t in ((0, q), (1, k)):
         check(t, orc.rope(part(wx, i).transpose(0, 2, 1, 3), pos, (32,), (1e4,)), "bf16", STEPS["bf16"], str(i))
     assert torch.equal(part(gx, 2).cpu(), part(x, 2))
+
+
+def test_rows_of_many_more_tokens_than_workgroups():
+    """2^24 tokens and more of 16 KB are within the documented range; a row's length says that three of them are there."""
+    import ctypes
+    H, d, far = 32, 256, (1 << 24) + 5
+    q, wq, _, _, _ = make(1, H, 1, 3, d, "bf16", 11)
+    at = 256 + (4 * far + 255) // 256 * 256   # (what is read lies before the view that ends nowhere: a length, positions of all tokens)
+    room = torch.empty(at + 3 * H * d * 2, dtype=torch.uint8, device="cuda")
+    lengths, pos = room[:256].view(torch.int32), room[256:at].view(torch.int32)
+    pos[:3] = torch.arange(3)
+    lengths[0] = 3
+    gq = room[at:].view(torch.bfloat16).view(1, 3, H, d).permute(0, 2, 1, 3)
+    gq.copy_(q)
+    strides = (ctypes.c_longlong * 3)(0, d, H * d)
+    rc = lf.library().linfusion_rope(gq.data_ptr(), None, gq.data_ptr(), None, pos.data_ptr(), 1, (ctypes.c_int * 1)(d), (ctypes.c_double * 1)(1e4), None, 1, H,
+                                     0, far, d, lf.DTYPE_BF16, 0, lengths.data_ptr(), strides, None, strides, None, None,
+                                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0
+    check(gq, orc.rope(wq, np.arange(3)[None], (d,), (1e4,)), "bf16", STEPS["bf16"], "q")

@@ -77,7 +77,9 @@ size_t mod_bytes(int B, int C, long long stride) { return ((size_t)(B - 1) * (si
 // Workgroups per CU: forward many short ones where a token takes a workgroup, whose start (the modulation of its channels) is small
 // against four tokens or more, fewer where it takes a wave; backward, where each leaves partial sums, fewer still: but four of a
 // workgroup per token, not two, where many tokens leave much of it idle (32768 x 1280 112 : 141 us; 32768 x 2048 185 : 161, 1024 x 1280
-// 17 : 13).
+// 17 : 13), and one, not two, above 4096 channels, whose registers leave a CU room for no more (bf16 16384 x 5120 313 : 320, 20000 x 4104
+// 321 : 329, 8192 x 8192 218 : 229, fp32 2048 x 8192 101 : 118, 512 x 5120 24 : 30; 16384 x 4096 224 : 176, 8192 x 2560 92 : 64).  Forward,
+// 16, 64 and 256 of them take the same time for 2560 to 8192 channels.
 struct Shape { int lanes, vpt, rows, wgs; };
 Shape shape_of(int B, long long N, int C, bool backward) {
   Shape s;
@@ -87,7 +89,7 @@ Shape shape_of(int B, long long N, int C, bool backward) {
   s.vpt = (vecs + s.lanes - 1) / s.lanes;
   const int per = 256 / s.lanes;
   int per_cu;
-  if (backward) per_cu = s.lanes == 64 ? (C <= 512 ? 8 : 4) : (C <= 1536 && tokens >= 16 * cus ? 4 : 2);
+  if (backward) per_cu = s.lanes == 64 ? (C <= 512 ? 8 : 4) : (C <= 1536 && tokens >= 16 * cus ? 4 : (C <= 4096 ? 2 : 1));
   else per_cu = s.lanes == 64 ? 16 : 64;
   long long rows = (tokens + cus * per_cu - 1) / (cus * per_cu);
   if (!backward && rows < 4 && tokens > 4 * cus) rows = 4;

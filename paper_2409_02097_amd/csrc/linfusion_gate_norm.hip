@@ -145,7 +145,7 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 // Workgroups of a backward call over the whole batch, at most.  shape_of's tokens per workgroup go in steps, so its number of them falls
 // here and there for a token more; this one never does, and a workspace of the longest sequence and largest batch serves all.
 size_t most_partials(int B, long long N, int C) {
-  const size_t per = C <= 512 ? 4 : 1, per_cu = C <= 512 ? 8 : (C <= 1536 ? 4 : 2);
+  const size_t per = C <= 512 ? 4 : 1, per_cu = C <= 512 ? 8 : (C <= 1536 ? 4 : (C <= 4096 ? 2 : 1));
   const size_t by_tokens = B * (((size_t)N + per - 1) / per), by_cus = lfh::num_cu() * per_cu + B + B * ((size_t)N >> 20);
   return by_tokens < by_cus ? by_tokens : by_cus;
 }

@@ -297,9 +297,11 @@ template <typename X> LF_DEV X again(X x) {
 // Two workgroups per CU, which leaves 128 registers a lane, where the planes are small enough and what is held fits: a workgroup is a
 // chain of barriers.  4096 tokens, us with two : one: 12 x 8 heads of 40 channels, bf16 281 : 344; 4 x 16 heads of 64, fp16 265 : 274, of
 // 32, fp32 120 : 180, of 32 with 4 key heads, bf16 111 : 140.  Not with the sums over value heads beside keys of more than 32 (2 x 16
-// heads of 64, 4 key heads, bf16 148 : 122), nor for more than 64 (4 x 16 heads of 96, bf16 416 : 362): the rest is in scratch memory.
+// heads of 64, 4 key heads, bf16 148 : 122) or beside fp32 rows (4 x 16 heads of 32, 4 key heads, the whole call 265 : 260), nor for more
+// than 64 (4 x 16 heads of 96, bf16 416 : 362; fp32 of 64, the whole call 591 : 482): the rest is in scratch memory.
 template <typename T, int KS, bool SHARED> constexpr int gradients_waves() {   // per SIMD
-  return KS == 1 || (KS == 2 && !SHARED && TermsOf<T>::kStored < 3) ? 4 : 2;
+  constexpr bool wide = TermsOf<T>::kStored == 3;
+  return (KS == 1 && !(SHARED && wide)) || (KS == 2 && !SHARED && !wide) ? 4 : 2;
 }
 
 template <typename T, int KS, bool SHARED> __global__ __launch_bounds__(512, (gradients_waves<T, KS, SHARED>())) void delta_gradients(DeltaArgs a) {

@@ -103,7 +103,8 @@ extern "C" int linfusion_rope(const void* q, const void* k, void* q_out, void* k
   const size_t np = (size_t)((B - 1) * pb + (axes - 1) * pa + N) * 4;
   for (int i = 0; i < 2; ++i) {
     if (!s[i].x) continue;
-    if (overlaps(s[i].y, s[i].ny, s[i].x, s[i].nx) && !in_place(s[i])) return LINFUSION_ERR_OVERLAP;
+    if (!in_place(s[i]) && meet(s[i].y, s[i].ny, s[i].sy, s[i].H, s[i].x, s[i].nx, s[i].sx, s[i].H, B, N, d, esz))
+      return LINFUSION_ERR_OVERLAP;
     const Side& o = s[1 - i];
     if (o.x && meet(s[i].y, s[i].ny, s[i].sy, s[i].H, o.x, o.nx, o.sx, o.H, B, N, d, esz)) return LINFUSION_ERR_OVERLAP;
     if (overlaps(s[i].y, s[i].ny, positions, np)) return LINFUSION_ERR_OVERLAP;

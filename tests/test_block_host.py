@@ -326,3 +326,13 @@ def delta_bwd_views(dq, dk, dv, dg, dbeta, tokens, scalars):
 ], ids=str)
 def test_delta_gradients_as_columns_of_one_buffer(args, status):
     assert delta_bwd_views(*args) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(k=None, ko=None, Hk=0, qo=M + 320, sq=(32000, 40, 320), sqo=(32000, 40, 320)), OK),   # beside the queries, in rows of 320
+    (dict(k=None, ko=None, Hk=0, qo=M + 304, sq=(32000, 40, 320), sqo=(32000, 40, 320)), -7),
+    (dict(k=None, ko=None, Hk=0, qo=M + 320, sq=(32000, 40, 320), sqo=(32000, 40, 160)), -7),
+    (dict(k=M + 320, qo=M + 640, ko=M + 960, Hk=4, **{n: (64000, 40, 640) for n in ("sq", "sk", "sqo", "sko")}), OK),
+], ids=str)
+def test_rope_beside_its_inputs(kw, status):
+    assert rope(**kw) == status

@@ -187,3 +187,17 @@ def test_rows_of_many_more_tokens_than_workgroups():
     torch.cuda.synchronize()
     assert rc == 0
     check(gq, orc.rope(wq, np.arange(3)[None], (d,), (1e4,)), "bf16", STEPS["bf16"], "q")
+
+
+def test_outputs_beside_their_inputs():
+    B, N, H, d = 2, 70, 3, 40
+    r = np.random.RandomState(12)
+    x, wx = stored(r.randn(B, N, 5, H, d), "f16")
+    gx = x.cuda()
+    q, k, qo, ko = (gx[:, :, i].permute(0, 2, 1, 3) for i in range(4))
+    pos = r.randint(0, 1000, (2, N)).astype(np.int32)
+    lf.linfusion_rope(q, k, qo, ko, torch.from_numpy(pos).cuda(), (16, 20), (1e4, 1e4))
+    for i, t in ((0, qo), (1, ko)):
+        check(t, orc.rope(wx[:, :, i].transpose(0, 2, 1, 3), pos, (16, 20), (1e4, 1e4)), "f16", STEPS["f16"], str(i))
+    for i in (0, 1, 4):
+        assert torch.equal(gx[:, :, i].cpu(), x[:, :, i])

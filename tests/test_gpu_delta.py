@@ -537,3 +537,41 @@ def test_runs_of_many_heads_of_every_width(dk, dtype):
         ref[:, :, t] = c["scale"] * np.matmul(qry[:, :, None], s)[:, :, 0]
     check(out, ref, dtype, chain(c), "out")
     check(last, s, "f32", chain(c), "state")
+
+
+def test_a_captured_single_token_replayed():
+    """The state in place from replay to replay, on views of one projection; the bits of calls one after the other."""
+    B, H, Hk, dk, dv, T = 3, 4, 2, 40, 24, 5
+    c = make(B, H, Hk, T, dk, dv, "bf16", seed=23)
+    g = on_gpu(c)
+    widths = (Hk * dk, Hk * dk, H * dv)
+    cat = lambda t: torch.cat([g[n][:, :, t].reshape(B, -1) for n in ("q", "k", "v")], -1)
+    one, scalars = cat(0), torch.stack((g["g"][:, :, 0], g["beta"][:, :, 0]), 1)
+    q, k, v = (p.unflatten(-1, (-1, w)) for p, w in zip(one.split(widths, -1), (dk, dk, dv)))
+    state, out = g["state"].clone(), torch.empty((B, H, dv), dtype=torch.bfloat16, device="cuda")
+    step = lambda: lf.linfusion_delta_step(q, k, v, scalars[:, 0], scalars[:, 1], state, state, out, scale=c["scale"])
+    outs = torch.empty_like(g["v"])
+
+    def feed(t):
+        one.copy_(cat(t))
+        scalars.copy_(torch.stack((g["g"][:, :, t], g["beta"][:, :, t]), 1))
+
+    for t in range(T):
+        feed(t)
+        step()
+        outs[:, :, t] = out
+    check_forward(c, outs, state)
+    last = state.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    state.copy_(g["state"])
+    for t in range(T):
+        feed(t)
+        out.fill_(float("nan"))
+        torch.randn(1 << 18, device="cuda").sum()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, outs[:, :, t])
+    assert torch.equal(state, last)

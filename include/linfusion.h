@@ -427,7 +427,9 @@ int linfusion_attn_state(const void* k, const void* v, float* state_out,
  * pointers, caller-owned buffers and workspaces, `stream`, status codes, nothing enqueued on an error, no allocation, no
  * synchronisation, run-to-run identical results, may be recorded into a HIP graph), and these:
  *   - Element types fp16, bf16, fp32 throughout; vectors, decays, corrections and states are fp32.  Arithmetic is fp32
- *     (angles and sums of log decays fp64), every result is rounded once.
+ *     (angles and sums of log decays fp64), every result is rounded once.  Where it is less or comes to less: sines and
+ *     cosines of 16-bit positions are within 2^-20; the delta rule's products leave out parts near 2^-24 of each; dg is
+ *     a difference of sums that cancel and off by some 1e-6 of its largest value, three times a recurrence in fp32.
  *   - [B, H, N, d] views: element strides {batch, head, token} as in linfusion_attn_fwd_strided; a NULL array is the
  *     contiguous tensor.  [B, N, C] views: element strides {batch, token}.
  *   - `lengths`: NULL, or a DEVICE array of B int32: only the first lengths[b] tokens (clamped to 0 .. N) of batch row b

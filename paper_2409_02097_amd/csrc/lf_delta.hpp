@@ -10,7 +10,7 @@
 //     U = U0 - W S0,   O = scale (e^gamma Q S0 + (Q K^T * D) U),   S1 = e^gamma_63 S0 + (e^(gamma_63 - gamma) K)^T U
 //
 // Only U and S1 depend on the chunk before: T, W, U0 are formed for all chunks at once (delta_prepare), a scan runs over the
-// chunks with a slice of 16 value channels per workgroup (delta_scan), and the outputs follow for all chunks at once
+// chunks with 16 or 32 value channels per workgroup (delta_scan), and the outputs follow for all chunks at once
 // (delta_out).  gamma and its differences are fp64: behind a token that forgets nearly everything the differences of an
 // fp32 sum have lost the small decays that follow it.
 //

@@ -7,7 +7,8 @@
 // on the token and the pair, not on the head: a workgroup takes a few tokens of one batch row through all heads of q and k
 // and computes each sine and cosine once.  theta is formed in turns, in fp64: a position of 10^5 leaves an fp32 product
 // no more than 3 correct digits of the angle, and the fraction of the fp64 product is exact to 2^-36.
-// bf16, 81120 tokens of 2 x 16 heads of 128: 227 us for 1.33 GB (5.9 TB/s); fp32, 2 x 36503 tokens of 2 x 8 heads of 40: 57 us for 374 MB
+// bf16, 81120 tokens of 2 x 16 heads of 128: 214 to 234 us for 1.33 GB (6.2 to 5.7 TB/s; as one section of halves 222, as sections
+// of 44 + 42 + 42, halves, 263); fp32, 2 x 36503 tokens of 2 x 8 heads of 40: 57 us for 374 MB
 // (6.6 TB/s); fp16, 2 x 256 tokens of 2 x 8 heads of 160: 5.8 us.
 #pragma once
 #include "lf_vec8.hpp"

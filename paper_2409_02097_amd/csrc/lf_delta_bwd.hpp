@@ -8,9 +8,11 @@
 //     dK = -e^gamma dV S0^T + e^(gamma_63 - gamma) U dS1^T + (dO U^T * D)^T Q + M K + M^T K,   M = -(dV U^T * D)   (strictly lower)
 //     dg_t = sum over the chunk's tokens i >= t of (q_i.dq_i - v_i.dv_i)  +  <dS1, S1>
 //
-// dg's sums cancel: it is off by 1e-6 of its largest value where a recurrence in fp32 is off by 4e-7, whatever its products are formed in.
-// That line holds because scaling the state by a factor from token t on is the same as scaling the queries there by it
-// and the values by its inverse.  Only dU and dS0 depend on the chunk behind: P^T dO and (e^gamma Q)^T dO are formed for all
+// The last line holds because scaling the state by a factor from token t on is the same as scaling the queries there by it
+// and the values by its inverse.  Its sums cancel: dg is off by 1e-6 of its largest value where a recurrence in fp32 is off by 4e-7,
+// whatever its products are formed in.
+//
+// Only dU and dS0 depend on the chunk behind: P^T dO and (e^gamma Q)^T dO are formed for all
 // chunks at once (delta_back_prepare), a scan runs from the last chunk to the first (delta_back_scan), and the rest follows
 // for all chunks at once (delta_gradients), where the value heads that share a query and key head are summed in their order.
 // The backward pass has records of its own, two more than chunks per head:

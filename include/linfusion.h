@@ -76,6 +76,18 @@ extern "C" {
 #define LINFUSION_FLAG_NORM_RMS 1u  /* root mean square norms; else layer norms */
 #define LINFUSION_FLAG_NORM_POST 2u /* the block's output is normed before its gate */
 
+/* flags for linfusion_scan_fwd / _bwd / _step */
+#define LINFUSION_FLAG_SCAN_REVERSE 1u /* from the last token to the first */
+#define LINFUSION_FLAG_SCAN_LEAKY 2u   /* new values weigh 1 - a; else sqrt(1 - a^2) */
+#define LINFUSION_FLAG_SCAN_SUM 4u     /* new values weigh 1 */
+
+/* activations of linfusion_linear_fwd / _bwd */
+#define LINFUSION_ACT_NONE 0
+#define LINFUSION_ACT_LEAKY_RELU 1 /* z > 0 ? z : slope * z */
+#define LINFUSION_ACT_GELU 2       /* z (1 + erf(z / sqrt(2))) / 2 */
+#define LINFUSION_ACT_GELU_TANH 3  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define LINFUSION_ACT_SILU 4       /* z / (1 + exp(-z)) */
+
 #define LINFUSION_OK 0
 #define LINFUSION_ERR_INVALID (-1)     /* NULL pointer, B/H/N/d <= 0, eps < 0 or NaN, bad flags */
 #define LINFUSION_ERR_UNSUPPORTED (-2) /* d, dtype or feature_map outside the supported sets */
@@ -558,6 +570,98 @@ int linfusion_delta_step(const void* q, const void* k, const void* v, const floa
                          int dtype, float scale, unsigned flags, const long long q_strides[2],
                          const long long k_strides[2], const long long v_strides[2], const long long out_strides[2],
                          const long long gate_strides[2], void* stream);
+
+/*
+ * A gated linear recurrence, channel by channel: a mixer whose state is one value per channel.  Token after token:
+ *
+ *     a = exp(-rate sigmoid(gate_t));   h = a h + m sigmoid(input_t) x_t;   out_t = h
+ *
+ * with the weight m = sqrt(1 - a^2), so that h keeps the size of what comes in (LINFUSION_FLAG_SCAN_LEAKY: 1 - a, a running
+ * mean; LINFUSION_FLAG_SCAN_SUM: 1).
+ *
+ *   x, gate, input, out  [B, N, C] views, strides[i] of them in this order (strides NULL: all contiguous); input NULL: without its
+ *                   factor.  C a multiple of 8 up to 8192, N < 2^30.
+ *   rate            fp32 [C], >= 0 and finite.
+ *   state_in        fp32 [B, C], 16-byte aligned, or NULL (zeros).  state_out: the state behind the last token that counts, or NULL;
+ *                   may be state_in itself.
+ *   saved           NULL, or DEVICE memory of linfusion_scan_saved_bytes that keeps states for linfusion_scan_bwd.
+ *   flags           LINFUSION_FLAG_SCAN_*; REVERSE: from the last token that counts to the first, state_out is then the state behind
+ *                   token 0.  Two calls, one of them reversed, see an image from both ends.
+ *   workspace       DEVICE scratch of linfusion_scan_workspace_bytes, 16-byte aligned; its size and that of `saved` never fall with B or N.
+ * An infinity or NaN reaches every token behind it in its channel.  No output may overlap another buffer, apart from state_out ==
+ * state_in; views may be columns of one buffer.
+ */
+int linfusion_scan_fwd(const void* x, const void* gate, const void* input, const float* rate, const float* state_in, void* out,
+                       float* state_out, const int* lengths, void* saved, size_t saved_bytes, int B, long long N, int C, int dtype,
+                       unsigned flags, const long long strides[4][2], void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_scan_workspace_bytes(int B, long long N, int C);
+size_t linfusion_scan_saved_bytes(int B, long long N, int C);
+
+/*
+ * Its gradients, given dout and dstate_out (gradient of state_out; NULL: 0).  strides: x, gate, input, dout, dx, dgate, dinput;
+ * dinput is NULL where input is.  drate: fp32 [C], summed over the batch; dstate_in: fp32 [B, C] or NULL, may be dstate_out itself.
+ * Where a gate lets nothing go (a = 1) m has no derivative; it counts as 0 there.  `saved`: what the forward call with the same
+ * arguments left, or NULL: formed again.  With `saved`, linfusion_scan_saved_bytes less than linfusion_scan_bwd_workspace_bytes suffice.
+ */
+int linfusion_scan_bwd(const void* x, const void* gate, const void* input, const float* rate, const float* state_in, const void* dout,
+                       const float* dstate_out, const void* saved, size_t saved_bytes, void* dx, void* dgate, void* dinput,
+                       float* drate, float* dstate_in, const int* lengths, int B, long long N, int C, int dtype, unsigned flags,
+                       const long long strides[7][2], void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_scan_bwd_workspace_bytes(int B, long long N, int C);
+
+/*
+ * The recurrence for one new token of every batch row: x, gate, input, out [B, C] with element strides[i] between batch rows (NULL:
+ * contiguous).  LINFUSION_FLAG_SCAN_REVERSE changes nothing.  state_out may be state_in itself.  One kernel, no workspace.
+ */
+int linfusion_scan_step(const void* x, const void* gate, const void* input, const float* rate, const float* state_in, float* state_out,
+                        void* out, int B, int C, int dtype, unsigned flags, const long long strides[4], void* stream);
+
+/*
+ * A linear layer with its epilogue: z = x W^T + bias, y = residual + act(z).
+ *
+ *   x               [B, N, C_in] view; residual (or NULL), y, z: [B, N, C_out] views; strides of x, residual, y, z.  y == residual with
+ *                   the same strides works in place.  y or z may be NULL (not both): not written.  z: the values before the
+ *                   activation, which linfusion_linear_bwd needs unless there is none.  Both are formed from the unrounded sums.
+ *   w               [C_out, C_in], rows w_stride elements apart (0: C_in).  bias: [C_out] of the call's type, or NULL.
+ *   C_in, C_out     multiples of 8 up to 32768; B * N < 2^31.
+ *   activation      LINFUSION_ACT_*; slope: of LINFUSION_ACT_LEAKY_RELU below 0.  flags 0.
+ *   workspace       DEVICE scratch of linfusion_linear_workspace_bytes, 16-byte aligned; never falls with B or N.
+ * Products are of the stored values, sums fp32 (16-bit types: the 16-bit matrix instruction; fp32: the fp32 one).
+ */
+int linfusion_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, int B, long long N,
+                         int C_in, int C_out, int dtype, int activation, float slope, unsigned flags, const int* lengths,
+                         const long long strides[4][2], long long w_stride, void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_linear_workspace_bytes(int B, long long N, int C_in, int C_out, int dtype);
+
+/*
+ * Its gradients, given dy: dz = dy act'(z), dx = dz W, dw = dz^T x [C_out, C_in] with rows dw_stride elements apart, dbias = the sum of
+ * dz over the tokens, all of the call's type; each may be NULL (not all).  The gradient of the residual is dy.  z may be NULL without
+ * an activation.  x and z may be what linfusion_keep8 kept: 8-bit codes, where their exponents x_exps, z_exps are given; then views
+ * of [B, N, C_in], [B, N, C_out] bytes with 8-byte aligned rows.  strides: x, z, dy, dx, x_exps, z_exps.  Tokens that do not count add
+ * nothing to dw and dbias, whatever stands there.  For the 16-bit types dz is rounded once where there is an activation, being an
+ * operand of both products; dbias is the sum of the unrounded values.
+ */
+int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void* w, const void* z, const unsigned char* z_exps,
+                         const void* dy, void* dx, void* dw, void* dbias, int B, long long N, int C_in, int C_out, int dtype,
+                         int activation, float slope, unsigned flags, const int* lengths, const long long strides[6][2],
+                         long long w_stride, long long dw_stride, void* workspace, size_t workspace_bytes, void* stream);
+size_t linfusion_linear_bwd_workspace_bytes(int B, long long N, int C_in, int C_out, int dtype);
+
+/*
+ * Activations in 8 bits between the forward and the backward pass: every block of 32 channels of a token shares a power of two, 2^e
+ * with the least e (-126 at least) for which 127 * 2^e reaches the block's largest magnitude, and a value is the integer nearest to
+ * x / 2^e (ties to even).  exps holds e + 127; 255: the block holds an infinity or NaN and comes back as NaN.  A value comes back off by at
+ * most 1 / 127 of its block's largest (beyond the type's largest value: as that).
+ *
+ *   x               [B, N, C] view of the call's type, C a multiple of 8 up to 32768 (the last block may be shorter).
+ *   codes           int8 [B, N, C] view with 8-byte aligned rows; exps: uint8 [B, N, ceil(C / 32)] view of contiguous blocks.
+ *                   strides: in the order of the arguments.  flags 0.
+ * One kernel each, no workspace.
+ */
+int linfusion_keep8(const void* x, signed char* codes, unsigned char* exps, int B, long long N, int C, int dtype, unsigned flags,
+                    const int* lengths, const long long strides[3][2], void* stream);
+int linfusion_unkeep8(const signed char* codes, const unsigned char* exps, void* x, int B, long long N, int C, int dtype, unsigned flags,
+                      const int* lengths, const long long strides[3][2], void* stream);
 
 /* Frees the library-owned scratch buffers (synchronises).  Optional; safe to call twice. */
 void linfusion_release(void);

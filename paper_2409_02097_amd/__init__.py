@@ -18,3 +18,9 @@ from .block import (  # noqa: F401
     linfusion_delta_workspace_bytes, linfusion_gate_norm_bwd, linfusion_gate_norm_bwd_workspace_bytes,
     linfusion_gate_norm_fwd, linfusion_rope,
 )
+from .layers import (  # noqa: F401
+    ACT_GELU, ACT_GELU_TANH, ACT_LEAKY_RELU, ACT_NONE, ACT_SILU, FLAG_SCAN_LEAKY, FLAG_SCAN_REVERSE, FLAG_SCAN_SUM,
+    linfusion_keep8, linfusion_linear_bwd, linfusion_linear_bwd_workspace_bytes, linfusion_linear_fwd,
+    linfusion_linear_workspace_bytes, linfusion_scan_bwd, linfusion_scan_bwd_workspace_bytes, linfusion_scan_fwd,
+    linfusion_scan_saved_bytes, linfusion_scan_step, linfusion_scan_workspace_bytes, linfusion_unkeep8,
+)

@@ -1,0 +1,95 @@
+// Activations kept in 8 bits: every block of 32 channels of a token has an exponent, the least e with 127 * 2^e not below the
+// block's largest magnitude, and every value is the integer nearest to x / 2^e (ties to even), -127 .. 127.  The exponent's byte is
+// e + 127, e at least -126; 255 marks a block that holds an infinity or a NaN, which comes back as NaN throughout.  The scale being
+// a power of two, both ways are exact but for that one rounding: off by at most 2^e / 2, i.e. by at most 1 / 127 of the block's largest
+// magnitude.  Bound: HBM.
+#pragma once
+#include "lf_vec8.hpp"
+
+namespace lf {
+
+constexpr int kKeepBlock = 32;
+
+struct KeepArgs {
+  const void* x;              // values (keep), or codes (back)
+  void* codes;                // codes (keep), or values (back)
+  unsigned char* exps;
+  long long xb, xt, cb, ct, eb, et;   // strides {batch, token} of x, codes, exps
+  const int* lengths;
+  long long N;
+  int C, rows;                // tokens per workgroup
+};
+
+// e + 127 of a block whose largest magnitude is `most` (its bits as an integer keep the order of magnitudes, infinities and NaN last)
+LF_DEV int keep_exponent(uint32_t most) {
+  if (most >= 0x7f800000u) return 255;
+  const int power = (int)(most >> 23), fraction = (int)(most & 0x7fffffu);   // most = (1 + fraction / 2^23) 2^(power - 127)
+  const int e = power - 6 + (fraction > 0x7e0000 ? 1 : 0);                   // 127 = (1 + 0x7e0000 / 2^23) 2^6
+  return e < 1 ? 1 : e;
+}
+
+template <typename T> struct Largest { static constexpr float value = 3.40282347e38f; };
+template <> struct Largest<F16> { static constexpr float value = 65504.0f; };
+template <> struct Largest<BF16> { static constexpr float value = 3.38953139e38f; };
+
+// Eight codes as values of T, exact (the one multiple of 2^e that may lie above T's largest value, 64 * 2^e, is that value).
+template <typename T> LF_DEV void keep_values(u32x2 codes, int e, float (&x)[8]) {
+  const float scale = e == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, (uint32_t)e << 23);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = (float)(int8_t)(codes[j >> 2] >> (8 * (j & 3))) * scale;
+    constexpr float most = Largest<T>::value;
+    x[j] = v > most ? most : (v < -most ? -most : v);   // (a NaN stays one)
+  }
+}
+
+// The largest of four neighbouring lanes' values.
+LF_DEV uint32_t quad_max(uint32_t v) {
+  uint32_t w = __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);
+  v = v > w ? v : w;
+  w = __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);
+  return v > w ? v : w;
+}
+
+// 32 lanes of 8 channels and 8 tokens at a time; four lanes share a block.
+template <typename T> __global__ __launch_bounds__(256) void keep8(KeepArgs a) {
+  const int b = blockIdx.z, c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+  const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
+  const long long stop = first + a.rows < end ? first + a.rows : end;
+  const bool on = c < a.C;
+  for (long long n = first + (threadIdx.x >> 5); n < stop; n += 8) {   // (four neighbouring lanes together)
+    float x[8];
+    widen8<T>(on ? load8_raw<T>(at<T>(a.x, b * a.xb + n * a.xt + c)) : none8<T>(), x);
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu;
+      most = most > m ? most : m;
+    }
+    const int e = keep_exponent(quad_max(most));
+    if (!on) continue;
+    u32x2 codes = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int q = e == 255 ? 0 : (int)__builtin_rintf(__builtin_amdgcn_ldexpf(x[j], 127 - e));
+      codes[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+    }
+    *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.codes) + b * a.cb + n * a.ct + c) = codes;
+    if ((threadIdx.x & 3) == 0) a.exps[b * a.eb + n * a.et + c / kKeepBlock] = (unsigned char)e;
+  }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void unkeep8(KeepArgs a) {
+  const int b = blockIdx.z, c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+  const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
+  const long long stop = first + a.rows < end ? first + a.rows : end;
+  if (c >= a.C) return;
+  for (long long n = first + (threadIdx.x >> 5); n < stop; n += 8) {
+    const u32x2 codes = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.x) + b * a.xb + n * a.xt + c);
+    float x[8];
+    keep_values<T>(codes, a.exps[b * a.eb + n * a.et + c / kKeepBlock], x);
+    store8_stream<T>(at<T>(a.codes, b * a.cb + n * a.ct + c), x);
+  }
+}
+
+}  // namespace lf

@@ -1,0 +1,515 @@
+// Linear layers: z = x W^T + b, y = residual + act(z), and their gradients dx = dz W, dW = dz^T x with dz = dy act'(z).
+//
+// One tiled matrix product serves all three: out[m][n] = sum_k A(m, k) B(n, k), fp32 sums on the matrix instructions (16-bit types:
+// 16 x 16 x 32; fp32: 16 x 16 x 4, whose operands are exact).  Either operand may lie with k contiguous (x, W, dz in rows) or with
+// its own index contiguous (W for dx; dz and x for dW): the second kind is staged as rows of k and read from LDS by transposing
+// reads (fp32: word by word), so that no tensor is transposed in memory.  Tiles of 128 bytes of k go from memory to LDS without
+// passing registers, one step ahead of the products; 16-byte pieces are dealt over a row so that operand reads meet every bank
+// evenly.  Where something is not there (channels behind the last, tokens behind a row's length, the end of k) a lane copies from 16
+// bytes of zeros instead.  The result is formed transposed, so that a lane holds four neighbouring channels of a token.
+#pragma once
+#include "lf_keep8.hpp"
+
+namespace lf {
+
+constexpr int kActNone = 0, kActLeaky = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4;
+
+__device__ static const u32x4 kZeros16[1] = {};   // what absent pieces are copied from
+
+struct LinRows { long long batch, token; };   // element strides of [B, N, C] rows; a matrix of plain rows: {0, row stride}
+
+// What is done with z, and where it goes.
+struct LinOut {
+  void *y, *z;
+  const void *residual, *bias;
+  LinRows vy, vz, vr;
+  int act;
+  float slope;
+};
+
+struct LinArgs {
+  const void *A, *B;
+  LinRows va, vb;
+  long long M, K;      // rows of the result, products per element
+  int N;               // columns of the result
+  unsigned per_row;    // tokens of a batch row (which index tokens are depends on the product)
+  const int* lengths;
+  float* partials;     // [splits][M][N] where k is split, else null
+  long long k_split;   // k of a split (a multiple of the tile's)
+  int tiles_m, tiles_n, splits;
+  LinOut out;
+};
+
+// ---- activations -----------------------------------------------------------------------------------------------------
+
+// Phi(z), the normal distribution, and its density.
+LF_DEV float normal_cdf(float z) { return 0.5f * erfcf(z * -0.70710678118654752440f); }
+LF_DEV float normal_pdf(float z) { return 0.39894228040143267794f * __expf(-0.5f * z * z); }
+
+LF_DEV float act_of(float z, int act, float slope) {
+  switch (act) {
+    case kActLeaky: return z > 0.0f ? z : slope * z;
+    case kActGelu: return z * normal_cdf(z);
+    case kActGeluTanh: {
+      const float v = 1.59576912160573071176f * z * __builtin_fmaf(0.044715f * z, z, 1.0f);   // twice the tangent's argument
+      return z / (1.0f + expf(-v));
+    }
+    case kActSilu: return z / (1.0f + expf(-z));
+    default: return z;
+  }
+}
+
+LF_DEV float act_slope(float z, int act, float slope) {
+  if (act != kActLeaky) z = z > 30.0f ? 30.0f : (z < -30.0f ? -30.0f : z);   // 1 or 0 from there on, and no infinity times 0
+  switch (act) {
+    case kActLeaky: return z > 0.0f ? 1.0f : slope;
+    case kActGelu: return __builtin_fmaf(z, normal_pdf(z), normal_cdf(z));
+    case kActGeluTanh: {
+      const float z2 = z * z, v = 1.59576912160573071176f * z * __builtin_fmaf(0.044715f, z2, 1.0f);
+      const float p = 1.0f / (1.0f + expf(-v));
+      return __builtin_fmaf(z * p * (1.0f - p), 1.59576912160573071176f * __builtin_fmaf(0.134145f, z2, 1.0f), p);
+    }
+    case kActSilu: {
+      const float p = 1.0f / (1.0f + expf(-z));
+      return p * __builtin_fmaf(z, 1.0f - p, 1.0f);
+    }
+    default: return 1.0f;
+  }
+}
+
+// ---- tokens and results ----------------------------------------------------------------------------------------------
+
+// Where a token is, and whether it counts.
+struct LinToken { unsigned b, n; bool on; };
+template <bool MAPPED> LF_DEV LinToken token_at(long long m, long long count, unsigned per_row, const int* lengths) {
+  LinToken t{0, (unsigned)m, m < count};
+  if constexpr (MAPPED) {
+    if (t.on) {
+      t.b = (unsigned)m / per_row;
+      t.n = (unsigned)m - t.b * per_row;
+      if (lengths) t.on = (long long)t.n < (long long)lengths[t.b];
+    }
+  }
+  return t;
+}
+LF_DEV long long place(const LinRows& v, const LinToken& t) { return t.b * v.batch + t.n * v.token; }
+
+// z of eight channels (n ..) of a token to what the call asks for
+template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, int n, float (&z)[8]) {
+  float v[8];
+  if (o.bias) {
+    load8<T>(at<T>(o.bias, n), v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] += v[j];
+  }
+  if (o.z) store8<T>(at<T>(o.z, place(o.vz, t) + n), z);
+  if (!o.y) return;
+  if (o.act != kActNone) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = act_of(z[j], o.act, o.slope);
+  }
+  if (o.residual) {
+    load8<T>(at<T>(o.residual, place(o.vr, t) + n), v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] += v[j];
+  }
+  store8<T>(at<T>(o.y, place(o.vy, t) + n), z);
+}
+
+// ---- the tiled product -----------------------------------------------------------------------------------------------
+
+template <int N> LF_DEV void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Copies 64 x 16 bytes, lane l's from `p`, to `lds` + 16 l.
+LF_DEV void copy_kb(const unsigned char* p, unsigned char* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (LF_LDS void*)lds, 16, 0, 0);
+}
+
+constexpr int kStepBytes = 128;   // of k in a tile
+
+// An operand's tile of X rows (or columns).  KC: k contiguous, X rows of 128 bytes, 16-byte piece c of row r at c ^ (r % 8).
+// Else rows of k of X values, with groups of 16 values (16-bit: 32 bytes; fp32: 64) of row k at g ^ turn(k), for as many groups as
+// make a power of two.
+template <typename T, int X, bool KC> struct LinTile {
+  static constexpr int kSize = Stored<T>::kBytes, kVec = 16 / kSize, kK = kStepBytes / kSize;
+  static constexpr int kBytes = X * kStepBytes;
+  static constexpr int kRow = KC ? kStepBytes : X * kSize, kPieces = kRow / 16;
+  static constexpr int kGroups = X / 16, kGroupPieces = kSize;   // (transposed) groups of a row; pieces of a group: 2 or 4
+  static constexpr int kMask = (kGroups & -kGroups) - 1;
+  static_assert(kBytes % 1024 == 0, "whole copies");
+  // rows that one transposing read (16-bit: k = 8 g + r; fp32: k = 4 g + j) brings together get different turns
+  static LF_DEV int turn(int k) { return (kSize == 2 ? ((k & 3) | ((k >> 3) & 3) << 2) : ((k >> 2) & 3)) & kMask; }
+};
+
+// The copies of a tile that a thread takes part in: `COUNT` of them.
+template <typename T, int X, bool KC, int WAVES, bool MAPPED> struct LinCopy {
+  using Tile = LinTile<T, X, KC>;
+  static constexpr int kCopies = Tile::kBytes / 1024, kCount = (kCopies + WAVES - 1) / WAVES;
+  const unsigned char* p[kCount];
+  int k[kCount];   // KC: the piece's first k; else the row of k
+  bool on[kCount];
+
+  // x0: the tile's first row or column; `limit`: how many there are
+  LF_DEV void start(const void* base, const LinRows& v, long long x0, long long limit, unsigned per_row, const int* lengths, int wave) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) {
+      const int f = (wave + WAVES * j) * 64 + lane, row = f / Tile::kPieces, pos = f % Tile::kPieces;
+      if constexpr (KC) {
+        const int piece = pos ^ (row & 7);
+        const LinToken t = token_at<MAPPED>(x0 + row, limit, per_row, lengths);
+        on[j] = t.on;
+        k[j] = piece * Tile::kVec;
+        p[j] = t.on ? at<T>(base, (MAPPED ? place(v, t) : (x0 + row) * v.token) + k[j]) : nullptr;
+      } else {
+        const int group = (pos / Tile::kGroupPieces) ^ Tile::turn(row), piece = group * Tile::kGroupPieces + pos % Tile::kGroupPieces;
+        const long long x = x0 + piece * Tile::kVec;
+        on[j] = x < limit;
+        k[j] = row;
+        p[j] = at<T>(base, on[j] ? x : 0);
+      }
+    }
+  }
+  // the copies of the step that starts at k0, of k < end
+  LF_DEV void step(unsigned char* lds, const LinRows& v, long long k0, long long end, unsigned per_row, const int* lengths, int wave) const {
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) {
+      if (kCopies % WAVES && wave + WAVES * j >= kCopies) break;   // (a whole wave)
+      const unsigned char* from;
+      bool there;
+      if constexpr (KC) {
+        there = on[j] && k0 + k[j] < end;
+        from = p[j] + k0 * Tile::kSize;
+      } else if constexpr (MAPPED) {
+        const LinToken t = token_at<true>(k0 + k[j], end, per_row, lengths);
+        there = on[j] && t.on;
+        from = p[j] + place(v, t) * Tile::kSize;
+      } else {
+        there = on[j] && k0 + k[j] < end;
+        from = p[j] + (k0 + k[j]) * v.token * Tile::kSize;
+      }
+      copy_kb(there ? from : reinterpret_cast<const unsigned char*>(kZeros16), lds + (wave + WAVES * j) * 1024);
+    }
+  }
+};
+
+// Operands of 16 rows (columns) from a tile: 16-bit, 32 k of lane l's row l % 16, eight of them from 8 (l / 16) on; fp32, 16 k, four of them
+// from 4 (l / 16) on: the j-th instruction takes every lane's j-th.
+template <typename T, int X, bool KC> struct LinRead {
+  using Tile = LinTile<T, X, KC>;
+  static constexpr int kSteps = 2;   // per tile
+  int base, turn[KC ? kSteps : 1];
+  LF_DEV void start(int x) {   // x: the wave's first row or column, a multiple of 16
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    if constexpr (KC) {
+      base = (x + i) * kStepBytes;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) turn[s] = ((4 * s + g) ^ (i & 7)) * 16;
+    } else if constexpr (Tile::kSize == 2) {
+      base = (8 * g + (i >> 2)) * Tile::kRow + (i & 3) * 8;
+      turn[0] = Tile::turn(8 * g + (i >> 2));
+    } else {
+      base = 4 * g * Tile::kRow + i * 4;
+      turn[0] = 0;   // (goes by the row)
+    }
+  }
+  // tile t of 16 from x on (`x` again: transposed places depend on it), step s
+  LF_DEV u32x4 get(const unsigned char* lds, int x, int t, int s) const {
+    if constexpr (KC) {
+      return *reinterpret_cast<const u32x4*>(lds + base + turn[s] + t * 16 * kStepBytes);
+    } else if constexpr (Tile::kSize == 2) {
+      const unsigned char* q = lds + base + s * 32 * Tile::kRow + ((x / 16 + t) ^ turn[0]) * 32;
+      const u32x2 a = lds_read_tr16(reinterpret_cast<const uint16_t*>(q)), b = lds_read_tr16(reinterpret_cast<const uint16_t*>(q + 4 * Tile::kRow));
+      return u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+      const int g = (threadIdx.x & 63) >> 4;
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)   // (turn(16 s + 4 g + j) is g)
+        v[j] = *reinterpret_cast<const uint32_t*>(lds + base + (s * 16 + j) * Tile::kRow + ((x / 16 + t) ^ (g & Tile::kMask)) * 64);
+      return v;
+    }
+  }
+};
+
+template <typename T> LF_DEV f32x4 lin_product(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (Stored<T>::kBytes == 2) {
+    return mfma_16x16x32<T>(a, b, c);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+    return c;
+  }
+}
+
+// Which tile of the result, and which split of k, a workgroup takes.  Workgroups are dealt to the eight XCDs in turn: each XCD gets a
+// stretch of the list, which goes through bands of eight rows of tiles column by column, so that those on an XCD at a time share
+// operands in its L2.
+struct LinPlace {
+  int m, n, split;
+  LF_DEV LinPlace(int tiles_m, int tiles_n, int splits) {
+    const unsigned all = gridDim.x, id = blockIdx.x, xcd = id % 8, at = id / 8;
+    const unsigned each = all / 8, more = all % 8;
+    unsigned t = xcd * each + (xcd < more ? xcd : more) + at;
+    const unsigned tiles = (unsigned)tiles_m * (unsigned)tiles_n;
+    split = t / tiles;
+    t -= split * tiles;
+    const unsigned band = 8 * (unsigned)tiles_n, first = t / band * 8, in = t % band;
+    const unsigned high = (unsigned)tiles_m - first < 8 ? (unsigned)tiles_m - first : 8;
+    m = first + in % high;
+    n = in / high;
+  }
+};
+
+// WR x WC waves, each with BM / WR rows and BN / WC columns of the tile.  AK, BK: whether A, B have k contiguous.  Tokens are the rows
+// of the result where A has k contiguous, else k; MAPPED: they are tokens of batch rows (with lengths, or strides that no single one
+// describes).
+template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, bool MAPPED>
+__global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
+  constexpr int kWaves = WR * WC, WM = BM / WR, WN = BN / WC, MT = WM / 16, NT = WN / 16;
+  using TA = LinTile<T, BM, AK>;
+  using TB = LinTile<T, BN, BK>;
+  constexpr int kBuffer = TA::kBytes + TB::kBytes;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const LinPlace tile(g.tiles_m, g.tiles_n, g.splits);
+  const long long m0 = (long long)tile.m * BM;
+  const int n0 = tile.n * BN;
+  if constexpr (AK && MAPPED) {   // nothing to do where no row of the tile counts
+    if (g.lengths) {
+      bool some = false;
+      for (int r = threadIdx.x; r < BM; r += 64 * kWaves) some |= token_at<true>(m0 + r, g.M, g.per_row, g.lengths).on;
+      if (!__syncthreads_or(some)) return;
+    }
+  }
+  const long long k_first = tile.split * g.k_split;
+  const long long k_end = k_first + g.k_split < g.K ? k_first + g.k_split : g.K;
+  LinCopy<T, BM, AK, kWaves, MAPPED> ca;
+  LinCopy<T, BN, BK, kWaves, MAPPED && !AK> cb;
+  ca.start(g.A, g.va, m0, g.M, g.per_row, g.lengths, wave);
+  cb.start(g.B, g.vb, n0, g.N, g.per_row, g.lengths, wave);
+  const int wm = wave / WC * WM, wn = wave % WC * WN;
+  LinRead<T, BM, AK> ra;
+  LinRead<T, BN, BK> rb;
+  ra.start(wm);
+  rb.start(wn);
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int steps = (int)((k_end - k_first + TA::kK - 1) / TA::kK);
+  auto request = [&](int s) {
+    unsigned char* to = smem + (s & 1) * kBuffer;
+    const long long k0 = k_first + (long long)s * TA::kK;
+    ca.step(to, g.va, k0, k_end, g.per_row, g.lengths, wave);
+    cb.step(to + TA::kBytes, g.vb, k0, k_end, g.per_row, g.lengths, wave);
+  };
+  if (steps > 0) request(0);
+  for (int s = 0; s < steps; ++s) {
+    wait_copies<0>();
+    __syncthreads();   // this step's tiles are there, and nobody reads the other buffer any more
+    if (s + 1 < steps) request(s + 1);
+    const unsigned char* la = smem + (s & 1) * kBuffer;
+    const unsigned char* lb = la + TA::kBytes;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      u32x4 a[MT], b[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) b[j] = rb.get(lb, wn, j, q);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i] = ra.get(la, wm, i, q);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = lin_product<T>(b[j], a[i], acc[i][j]);
+    }
+  }
+  // Lane l has columns 4 (l / 16) .. + 3 of a tile of 16 and row l % 16: through LDS, a wave's rows for itself, into rows of eight
+  // channels a lane, so that stores are whole lines and the activation's code is there once.
+  constexpr int kUnits = WN / 4, kTurn = (kUnits & -kUnits) - 1;   // 16 bytes each; row r's unit u is at u ^ (r & kTurn)
+  constexpr int kRegion = 2 * kBuffer / kWaves, kFit = kRegion / (16 * WN * 4), kPass = kFit < MT ? kFit : MT;
+  static_assert(kPass > 0 && MT % kPass == 0, "whole passes");
+  constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes of a row; rows at a time
+  __syncthreads();
+  unsigned char* mine = smem + wave * kRegion;
+#pragma unroll
+  for (int p = 0; p < MT; p += kPass) {
+#pragma unroll
+    for (int i = 0; i < kPass; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int r = 16 * i + (lane & 15), u = 4 * j + (lane >> 4);
+        *reinterpret_cast<f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16) = acc[p + i][j];
+      }
+    asm volatile("" ::: "memory");   // (a wave's LDS operations complete in order)
+#pragma unroll 1
+    for (int r0 = 0; r0 < 16 * kPass; r0 += kRows) {
+      const int r = r0 + lane / kLanes, u = lane % kLanes * 2, n = n0 + wn + 4 * u;
+      if (lane >= kRows * kLanes || r >= 16 * kPass) continue;
+      const LinToken t = token_at<MAPPED && AK>(m0 + wm + 16 * p + r, g.M, g.per_row, g.lengths);
+      if (!t.on || n >= g.N) continue;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((u + 1) ^ (r & kTurn)) * 16);
+      if (g.partials) {
+        float* to = g.partials + (tile.split * g.M + m0 + wm + 16 * p + r) * g.N + n;
+        *reinterpret_cast<f32x4*>(to) = lo;
+        *reinterpret_cast<f32x4*>(to + 4) = hi;
+      } else {
+        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        finish8<T>(g.out, t, n, z);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// The splits' sums, eight columns a thread, in their order.
+template <typename T, bool MAPPED> __global__ __launch_bounds__(256) void linear_join(LinArgs g) {
+  const long long across = g.N / 8, id = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (id >= g.M * across) return;
+  const long long m = id / across;
+  const int n = (int)(id - m * across) * 8;
+  const LinToken t = token_at<MAPPED>(m, g.M, g.per_row, g.lengths);
+  if (!t.on) return;
+  float z[8], v[8];
+  load8_f32(g.partials + m * g.N + n, z);
+  for (int s = 1; s < g.splits; ++s) {
+    load8_f32(g.partials + (s * g.M + m) * g.N + n, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] += v[j];
+  }
+  finish8<T>(g.out, t, n, z);
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------------------------
+
+// Up to 16 MT tokens: every weight is read once, straight into operand registers, 16 channels a workgroup, whose four waves share k.
+// Bound: the weights' way from memory.
+template <typename T, int MT, bool MAPPED> __global__ __launch_bounds__(256) void linear_few(LinArgs g) {
+  constexpr int kVec = 16 / Stored<T>::kBytes, kK = 4 * kVec, kAhead = 4;   // k of a product; products requested together
+  __shared__ __attribute__((aligned(16))) float lds[4][16 * MT][20];   // (rows spread over the banks)
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  f32x4 acc[MT];
+  const unsigned char* px[MT];
+  bool on[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const LinToken m = token_at<MAPPED>(16 * t + i, g.M, g.per_row, g.lengths);
+    on[t] = m.on;
+    px[t] = at<T>(g.A, on[t] ? place(g.va, m) : 0);
+  }
+  const bool row = n0 + i < g.N;
+  const unsigned char* pw = at<T>(g.B, row ? (n0 + i) * g.vb.token : 0);
+  for (long long k0 = (long long)wave * kAhead * kK; k0 < g.K; k0 += 4 * kAhead * kK) {
+    u32x4 w[kAhead], x[MT][kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const long long k = k0 + j * kK + q * kVec;
+      const bool there = k < g.K;
+      w[j] = u32x4{0, 0, 0, 0};
+      if (row && there) w[j] = ld_stream(reinterpret_cast<const u32x4*>(at<T>(pw, k)));
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        x[t][j] = u32x4{0, 0, 0, 0};
+        if (on[t] && there) x[t][j] = *reinterpret_cast<const u32x4*>(at<T>(px[t], k));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = lin_product<T>(w[j], x[t][j], acc[t]);
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) *reinterpret_cast<f32x4*>(&lds[wave][16 * t + i][4 * q]) = acc[t];
+  __syncthreads();
+  // eight channels a thread
+  const int m = threadIdx.x >> 1, half = threadIdx.x & 1, n = n0 + 8 * half;
+  if (m >= 16 * MT || n >= g.N) return;
+  const LinToken t = token_at<MAPPED>(m, g.M, g.per_row, g.lengths);
+  if (!t.on) return;
+  float z[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z[j] = (lds[0][m][8 * half + j] + lds[1][m][8 * half + j]) + (lds[2][m][8 * half + j] + lds[3][m][8 * half + j]);
+  finish8<T>(g.out, t, n, z);
+}
+
+// ---- dz, and the bias's gradient ---------------------------------------------------------------------------------------
+
+struct LinSlopeArgs {
+  const void *dy, *z;               // z: values, or codes of eight bits with `z_exps`
+  const unsigned char* z_exps;
+  LinRows vdy, vz, ve;              // ve: of the exponents' rows
+  void* dz;                         // [B * N][C] rows, or null (no activation)
+  float* partials;                  // [workgroups][C], or null
+  const int* lengths;
+  long long rows;                   // B * N
+  unsigned per_row;
+  int C, each, act;                 // each: tokens of a workgroup
+  float slope;
+};
+
+// dz = dy act'(z), rounded once to the type (it is an operand of two products), and the sums of the unrounded values over a
+// workgroup's tokens.  32 lanes of 8 channels, 8 tokens at a time.  Bound: HBM.
+template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_slope(LinSlopeArgs a) {
+  __shared__ float lds[8][32][8];
+  const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * 8;
+  const bool on = c < a.C;
+  const long long first = (long long)blockIdx.y * a.each, stop = first + a.each < a.rows ? first + a.each : a.rows;
+  float sum[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+  for (long long m = first + row; on && m < stop; m += 8) {
+    const LinToken t = token_at<true>(m, a.rows, a.per_row, a.lengths);
+    if (!t.on) continue;
+    float d[8], z[8];
+    const Raw8<T> rd = load8_raw<T>(at<T>(a.dy, place(a.vdy, t) + c));
+    if (a.dz) {
+      if constexpr (KEPT) {
+        keep_values<T>(*reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.z) + place(a.vz, t) + c),
+                       a.z_exps[place(a.ve, t) + c / kKeepBlock], z);
+      } else {
+        load8<T>(at<T>(a.z, place(a.vz, t) + c), z);
+      }
+    }
+    widen8<T>(rd, d);
+    if (a.dz) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], a.act, a.slope);
+      store8<T>(at<T>(a.dz, m * a.C + c), d);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += d[j];
+  }
+  if (!a.partials) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) lds[row][lane][j] = sum[j];
+  __syncthreads();
+  const int cc = blockIdx.x * 256 + threadIdx.x;
+  float all = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) all += lds[r][threadIdx.x >> 3][threadIdx.x & 7];
+  if (cc < a.C) a.partials[(long long)blockIdx.y * a.C + cc] = all;
+}
+
+// The bias's gradient: the workgroups' sums in their order, in fp64.
+template <typename T> __global__ __launch_bounds__(1024) void linear_bias(const float* partials, void* dbias, int parts, int C) {
+  __shared__ double lds[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  double sum = 0.0;
+  if (c < C)
+    for (int p = wave; p < parts; p += 16) sum += (double)partials[(long long)p * C + c];
+  lds[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && c < C) {
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum += lds[w][lane];
+    if constexpr (Stored<T>::kBytes == 4) static_cast<float*>(dbias)[c] = (float)sum;
+    else static_cast<uint16_t*>(dbias)[c] = (uint16_t)pack2<T>((float)sum, 0.0f);
+  }
+}
+
+}  // namespace lf

@@ -6,7 +6,7 @@
 #include <cmath>
 
 #include "lf_gate_norm.hpp"
-#include "lf_host_api.hpp"
+#include "lf_rows_api.hpp"
 
 namespace {
 
@@ -14,38 +14,12 @@ using lfh::overlaps;
 
 constexpr int kMaxChannels = 8192;
 
-struct View { const void* p; long long batch, token; size_t bytes; lfh::Places rows; };
-
-// LINFUSION_OK when the kernels can address [B, N, C] rows at `p` with these element strides (null: dense)
-int make_view(const void* p, const long long* s, int B, long long N, int C, size_t esz, bool written, View* v) {
-  v->p = p;
-  v->batch = s ? s[0] : N * C;
-  v->token = s ? s[1] : C;
-  if (B == 1) v->batch = 0;   // (never used, whatever they say)
-  if (N == 1) v->token = 0;
-  v->bytes = 0;
-  if (!p) return LINFUSION_OK;
-  const long long vec = (long long)(16 / esz);
-  if (v->batch < 0 || v->token < 0) return LINFUSION_ERR_INVALID;
-  if (((uintptr_t)p & 15) || v->batch % vec || v->token % vec) return LINFUSION_ERR_MISALIGNED;
-  if (v->token >= 1LL << 27) return LINFUSION_ERR_INVALID;
-  const long double span = (long double)(B - 1) * v->batch + (long double)(N - 1) * v->token + C;
-  if (span >= (long double)(1LL << 45)) return LINFUSION_ERR_INVALID;
-  if (written) {   // no two rows share memory, whichever of batch and token is the outer one
-    const bool tokens_out = v->token > v->batch;
-    const long long in = tokens_out ? v->batch : v->token, out = tokens_out ? v->token : v->batch;
-    const long long n_in = tokens_out ? B : N, n_out = tokens_out ? N : B;
-    if (n_in > 1 && in < C) return LINFUSION_ERR_OVERLAP;
-    if (n_out > 1 && out < (n_in - 1) * in + C) return LINFUSION_ERR_OVERLAP;
-  }
-  v->bytes = (size_t)span * esz;
-  const long long strides[3] = {v->batch, 0, v->token};
-  v->rows = lfh::places(p, strides, B, 1, N, C, esz);
-  return LINFUSION_OK;
-}
-
-bool same_rows(const View& a, const View& b) { return a.p == b.p && a.batch == b.batch && a.token == b.token; }
-bool meet(const View& a, const View& b) { return a.p && b.p && overlaps(a.p, a.bytes, b.p, b.bytes) && !lfh::apart(a.rows, b.rows); }
+using View = lfh::RowView;
+using lfh::meet;
+using lfh::same_rows;
+constexpr auto make_view = [](const void* p, const long long* s, int B, long long N, int C, size_t esz, bool written, View* v) {
+  return lfh::row_view(p, s, B, N, C, esz, written, v);
+};
 
 int check_sizes(int B, long long N, int C, int dtype) {
   if (B <= 0 || N <= 0 || C <= 0 || B > 65535) return LINFUSION_ERR_INVALID;

@@ -1,0 +1,303 @@
+"""Linear layers on the GPU against fp64: epilogues, gradients, kept activations, odd sizes, views, ragged batches.
+
+Sums of n products in fp32 are off by at most n steps of 2^-24 of the sum of their magnitudes (16-bit products are exact in fp32, fp32
+ones off by a step more each).  An activation has a slope of at most 1.13, and is itself off by 16 steps of 1 + |z|.  dz of a 16-bit type
+is rounded once before it is multiplied: half a step of each term."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_02097_amd as lf
+from oracle import layers_oracle as orc
+from tests.layers_parity import CODE, TORCH, columns, f64, half_step, live, stored, within
+
+pytestmark = pytest.mark.gpu
+
+ACTS = {"none": lf.ACT_NONE, "leaky": lf.ACT_LEAKY_RELU, "gelu": lf.ACT_GELU, "gelu_tanh": lf.ACT_GELU_TANH, "silu": lf.ACT_SILU}
+SLOPE = 0.02
+U = 2.0 ** -24
+
+
+def make(B, N, K, C, dtype, seed, act="none", bias=True, residual=False, lengths=None):
+    r = np.random.RandomState(seed)
+    c = {"dims": (B, N, K, C), "dtype": dtype, "act": act, "lengths": lengths, "t": {}, "w": {}}
+    wide = {"x": r.randn(B, N, K), "w": r.randn(C, K) / np.sqrt(K), "bias": 0.3 * r.randn(C) if bias else None,
+            "residual": r.randn(B, N, C) if residual else None, "dy": r.randn(B, N, C)}
+    for n, x in wide.items():
+        c["t"][n], c["w"][n] = (None, None) if x is None else stored(x, dtype)
+    z, _ = orc.linear(c["w"]["x"], c["w"]["w"], c["w"]["bias"])
+    c["t"]["z"], c["w"]["z"] = stored(z, dtype)   # what the gradients go by
+    return c
+
+
+def on_gpu(c, spoil=True):
+    g = {n: None if t is None else t.cuda() for n, t in c["t"].items()}
+    g["lengths"] = None if c["lengths"] is None else torch.tensor(c["lengths"], dtype=torch.int32, device="cuda")
+    if c["lengths"] is not None and spoil:
+        dead = torch.from_numpy(~live(c["dims"][:2], c["lengths"])).cuda()
+        for n in ("x", "z", "dy", "residual"):
+            if g[n] is not None:
+                g[n][dead] = float("nan")
+    return g
+
+
+def memory(size):
+    return torch.full((size,), 255, dtype=torch.uint8, device="cuda")   # (NaN wherever it is read before it is written)
+
+
+def rest(c, g):
+    return {"activation": ACTS[c["act"]], "slope": SLOPE, "lengths": g["lengths"]}
+
+
+def forward(c, g, y=True, z=True):
+    B, N, K, C = c["dims"]
+    y = torch.full((B, N, C), 7.0, dtype=g["x"].dtype, device="cuda") if y else None
+    z = torch.full((B, N, C), 7.0, dtype=g["x"].dtype, device="cuda") if z else None
+    lf.linfusion_linear_fwd(g["x"], g["w"], g["bias"], y, residual=g["residual"] if y is not None else None, z=z,
+                            workspace=memory(lf.linfusion_linear_workspace_bytes(*c["dims"], CODE[c["dtype"]])), **rest(c, g))
+    return y, z
+
+
+def backward(c, g, want=("dx", "dw", "dbias"), x=None, z=None, **kept):
+    B, N, K, C = c["dims"]
+    T = g["dy"].dtype
+    shape = {"dx": (B, N, K), "dw": (C, K), "dbias": (C,)}
+    d = {n: torch.full(shape[n], 7.0, dtype=T, device="cuda") for n in want}
+    lf.linfusion_linear_bwd(g["x"] if x is None else x, g["w"], (g["z"] if z is None else z) if c["act"] != "none" else None, g["dy"], **d, **kept,
+                            workspace=memory(lf.linfusion_linear_bwd_workspace_bytes(*c["dims"], CODE[c["dtype"]])), **rest(c, g))
+    return d
+
+
+def check_forward(c, y, z, what=""):
+    B, N, K, C = c["dims"]
+    w, dtype = c["w"], c["dtype"]
+    on = live((B, N), c["lengths"])
+    dead = torch.from_numpy(~on).cuda()
+    ref, mag = orc.linear(w["x"], w["w"], w["bias"])
+    off = (K + 4) * U * mag
+    if z is not None:
+        within(f64(z)[on], ref[on], (half_step(ref, dtype) + off)[on], what + "z")
+        assert bool((z[dead] == 7.0).all())
+    if y is not None:
+        a = orc.act(ref, c["act"], SLOPE)[0]
+        tol = 1.13 * off + (16 * U * (1 + np.abs(ref)) if c["act"] != "none" else 0.0)
+        if w["residual"] is not None:
+            a = a + w["residual"]
+            tol = tol + 2 * U * (np.abs(a) + np.abs(w["residual"]))
+        within(f64(y)[on], a[on], (half_step(a, dtype) + tol)[on], what + "y")
+        assert bool((y[dead] == 7.0).all())
+
+
+def check_backward(c, d, what="", x=None, z=None):
+    B, N, K, C = c["dims"]
+    w, dtype = c["w"], c["dtype"]
+    on = live((B, N), c["lengths"])
+    slope = orc.act(w["z"] if z is None else z, c["act"], SLOPE)[1] if c["act"] != "none" else np.ones((B, N, C))
+    dz = np.where(on[..., None], w["dy"] * slope, 0.0)
+    off = 0.0 if c["act"] == "none" else 16 * U * np.abs(w["dy"]) * (1 + np.abs(w["z"]))
+    rounded = off if c["act"] == "none" or dtype == "f32" else off + half_step(dz, dtype)
+    x = np.where(on[..., None], w["x"] if x is None else x, 0.0).reshape(-1, K)
+    rounded = np.where(on[..., None], np.broadcast_to(rounded, dz.shape), 0.0).reshape(-1, C)
+    off = np.where(on[..., None], np.broadcast_to(off, dz.shape), 0.0).reshape(-1, C)
+    dz = dz.reshape(-1, C)
+    if "dx" in d:
+        ref = (dz @ w["w"]).reshape(B, N, K)
+        tol = ((rounded + (C + 4) * U * np.abs(dz)) @ np.abs(w["w"])).reshape(B, N, K)
+        within(f64(d["dx"])[on], ref[on], (half_step(ref, dtype) + tol)[on], what + "dx")
+        assert bool((d["dx"][torch.from_numpy(~on).cuda()] == 7.0).all())
+    if "dw" in d:
+        ref = dz.T @ x
+        within(d["dw"], ref, half_step(ref, dtype) + (rounded + (B * N + 4) * U * np.abs(dz)).T @ np.abs(x), what + "dw")
+    if "dbias" in d:
+        ref = dz.sum(0)
+        within(d["dbias"], ref, half_step(ref, dtype) + (off + (B * N + 4) * U * np.abs(dz)).sum(0), what + "dbias")
+
+
+SHAPES = [(1, 1, 8, 8), (1, 1, 1280, 328), (3, 1, 72, 40), (1, 17, 40, 72), (2, 31, 264, 16), (1, 64, 128, 256), (1, 65, 64, 64),
+          (2, 77, 768, 640), (1, 300, 320, 1000), (5, 129, 72, 136), (1, 1025, 328, 320), (1, 513, 2568, 264), (2, 2049, 64, 520)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act,bias,residual", [("none", False, False), ("none", True, True), ("leaky", True, False), ("gelu", False, True),
+                                               ("gelu_tanh", True, True), ("silu", True, False)])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_against_the_oracle(shape, act, bias, residual, dtype):
+    c = make(*shape, dtype, sum(shape), act, bias, residual)
+    g = on_gpu(c)
+    check_forward(c, *forward(c, g))
+    check_backward(c, backward(c, g))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 4099, 520, 776), (1, 9000, 328, 1288), (1, 2000, 4096, 512), (3, 1500, 160, 2568)], ids=str)
+def test_large_tiles(shape, dtype):
+    c = make(*shape, dtype, sum(shape), "silu", True, True)
+    g = on_gpu(c)
+    check_forward(c, *forward(c, g))
+    check_backward(c, backward(c, g))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,lengths", [(20, (20, 0, 1, 13)), (300, (300, 0, 1, 200)), (257, (0, 0, 0, 0)), (600, (-1, 900, 256, 512))], ids=str)
+def test_ragged_rows(N, lengths, dtype):
+    """What lies behind a row's length is NaN on the way in and untouched on the way out; dw and dbias do not see it."""
+    c = make(4, N, 328, 264, dtype, N, "gelu", True, True, lengths)
+    g = on_gpu(c)
+    check_forward(c, *forward(c, g))
+    check_backward(c, backward(c, g))
+
+
+def test_outputs_one_by_one():
+    c = make(2, 150, 72, 136, "bf16", 3, "silu", True, True)
+    g = on_gpu(c)
+    y, z = forward(c, g)
+    assert torch.equal(forward(c, g, z=False)[0], y) and torch.equal(forward(c, g, y=False)[1], z)
+    d = backward(c, g)
+    for n in d:
+        assert torch.equal(backward(c, g, (n,))[n], d[n]), n
+    y2 = g["residual"].clone()   # y in place of the residual
+    lf.linfusion_linear_fwd(g["x"], g["w"], g["bias"], y2, residual=y2, workspace=memory(lf.linfusion_linear_workspace_bytes(*c["dims"], 2)),
+                            **rest(c, g))
+    assert torch.equal(y2, y)
+
+
+@pytest.mark.parametrize("N", [9, 200])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_views(dtype, N):
+    """Columns of one buffer, [N, B, C] tensors, rows of a wider weight."""
+    c = make(3, N, 72, 136, dtype, 4, "silu", True, True)
+    g = on_gpu(c)
+    y, z = forward(c, g)
+    d = backward(c, g)
+    turned = lambda t: t.permute(1, 0, 2).contiguous().permute(1, 0, 2)
+    wide = torch.full((136, 88), float("nan"), dtype=g["w"].dtype, device="cuda")
+    w = wide[:, 8:80]
+    w.copy_(g["w"])
+    for kind in (lambda *t: columns(t, 8), lambda *t: [turned(s) for s in t]):
+        x, r, zz, dy, y2, z2 = kind(g["x"], g["residual"], g["z"], g["dy"], torch.zeros_like(y), torch.zeros_like(z))
+        dx, = kind(torch.zeros_like(g["x"]))
+        dwide = torch.full_like(wide, 7.0)
+        lf.linfusion_linear_fwd(x, w, g["bias"], y2, residual=r, z=z2, workspace=memory(lf.linfusion_linear_workspace_bytes(*c["dims"], CODE[dtype])),
+                                **rest(c, g))
+        lf.linfusion_linear_bwd(x, w, zz, dy, dx=dx, dw=dwide[:, 8:80], dbias=(db := torch.zeros_like(g["bias"])),
+                                workspace=memory(lf.linfusion_linear_bwd_workspace_bytes(*c["dims"], CODE[dtype])), **rest(c, g))
+        for got, want in ((y2, y), (z2, z), (dx, d["dx"]), (dwide[:, 8:80], d["dw"]), (db, d["dbias"])):
+            assert torch.equal(got, want)
+        assert bool((dwide[:, :8] == 7.0).all()) and bool((dwide[:, 80:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape,lengths", [((2, 70, 40, 72), None), ((3, 200, 328, 136), (200, 0, 77)), ((1, 1030, 320, 264), None)], ids=str)
+def test_gradients_from_what_was_kept_in_8_bits(shape, lengths, dtype):
+    c = make(*shape, dtype, 5, "gelu", True, False, lengths)
+    g = on_gpu(c)
+    kept, wide = {}, {}
+    for n in ("x", "z"):
+        t = g[n]
+        kept[n] = torch.full(t.shape, 55, dtype=torch.int8, device="cuda")
+        kept[n + "_exps"] = torch.full((*t.shape[:2], (t.shape[2] + 31) // 32), 255, dtype=torch.uint8, device="cuda")
+        lf.linfusion_keep8(t, kept[n], kept[n + "_exps"], lengths=g["lengths"])
+        wide[n] = orc.keep8(c["w"][n])[2]
+    d = backward(c, g, **kept)
+    check_backward(c, d, "both ", **wide)
+    # one of them kept, the other not
+    check_backward(c, backward(c, g, x=kept["x"], x_exps=kept["x_exps"]), "x ", x=wide["x"])
+    check_backward(c, backward(c, g, z=kept["z"], z_exps=kept["z_exps"]), "z ", z=wide["z"])
+
+
+@pytest.mark.parametrize("act", ["leaky", "gelu", "gelu_tanh", "silu"])
+def test_activations_far_out(act):
+    """Values whose exponentials leave fp32: finite results, slopes of exactly 0 or 1 (leaky: its slope)."""
+    zs = torch.tensor([-3e38, -1e20, -1e4, -200.0, -90.0, -31.0, 31.0, 90.0, 200.0, 1e4, 1e20, 3e38], device="cuda")
+    n = len(zs)
+    x = zs.view(1, n, 1) * torch.eye(8, device="cuda")[0].view(1, 1, 8)
+    w = torch.eye(8, device="cuda")
+    y, z = torch.empty((1, n, 8), device="cuda"), torch.empty((1, n, 8), device="cuda")
+    kind = {"activation": ACTS[act], "slope": SLOPE}
+    lf.linfusion_linear_fwd(x, w, None, y, z=z, workspace=memory(lf.linfusion_linear_workspace_bytes(1, n, 8, 8, 0)), **kind)
+    assert torch.equal(z[0, :, 0], zs)
+    low = SLOPE if act == "leaky" else 0.0
+    want = torch.where(zs > 0, zs, low * zs)
+    assert bool(torch.isfinite(y).all())
+    assert bool(((y[0, :, 0] - want).abs() <= 1e-11 + 2.0 ** -23 * want.abs()).all())   # (z Phi(z) and z sigmoid(z) at -31: below 1e-11)
+    dx, dy = torch.empty((1, n, 8), device="cuda"), torch.ones((1, n, 8), device="cuda")
+    lf.linfusion_linear_bwd(None, w, z, dy, dx=dx, workspace=memory(lf.linfusion_linear_bwd_workspace_bytes(1, n, 8, 8, 0)), **kind)
+    slope = torch.where(zs > 0, 1.0, low)
+    assert bool(((dx[0, :, 0] - slope).abs() <= 1e-11).all())
+
+
+def test_gradients_against_differences():
+    c = make(2, 37, 40, 24, "f32", 6, "gelu", True, True, (37, 11))
+    g = on_gpu(c)
+    w, r = c["w"], np.random.RandomState(2)
+    g["z"] = forward(c, g)[1]
+    d = backward(c, g)
+    on = live((2, 37), c["lengths"])[..., None]
+
+    def loss(v):
+        return (orc.act(orc.linear(v["x"], v["w"], v["bias"])[0], "gelu")[0] * w["dy"] * on).sum()
+
+    for n in ("x", "w", "bias"):
+        step = r.randn(*w[n].shape) * (on if n == "x" else 1.0)
+        want = (loss(w | {n: w[n] + 1e-6 * step}) - loss(w | {n: w[n] - 1e-6 * step})) / 2e-6
+        got = f64(d["d" + n])
+        got = (np.where(on, got, 0.0) if n == "x" else got) * step
+        assert abs(got.sum() - want) <= 1e-5 * np.abs(got).sum() + 1e-7 * abs(loss(w)), n
+
+
+@pytest.mark.parametrize("shape", [(1, 5, 320, 640), (1, 300, 640, 320), (1, 3000, 320, 640)], ids=str)
+def test_graphs_that_share_a_workspace_replayed_beside_eager_calls(shape):
+    c = make(*shape, "bf16", 7, "silu", True, True)
+    g = on_gpu(c)
+    y, z = forward(c, g)
+    d = backward(c, g)
+    ws = memory(max(lf.linfusion_linear_workspace_bytes(*shape, 2), lf.linfusion_linear_bwd_workspace_bytes(*shape, 2)))
+    y2, z2, d2 = torch.empty_like(y), torch.empty_like(z), {n: torch.empty_like(t) for n, t in d.items()}
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(stream):
+        for call in (lambda: lf.linfusion_linear_fwd(g["x"], g["w"], g["bias"], y2, residual=g["residual"], z=z2, workspace=ws, **rest(c, g)),
+                     lambda: lf.linfusion_linear_bwd(g["x"], g["w"], g["z"], g["dy"], **d2, workspace=ws, **rest(c, g))):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                call()
+        for _ in range(4):
+            ws.fill_(255)
+            for t in (y2, z2, *d2.values()):
+                t.zero_()
+            graphs[0].replay()
+            graphs[1].replay()
+            stream.synchronize()
+            assert torch.equal(y2, y) and torch.equal(z2, z) and all(torch.equal(d2[n], d[n]) for n in d)
+            assert torch.equal(forward(c, g)[0], y)
+
+
+def test_runs_are_identical():
+    c = make(1, 5000, 640, 320, "bf16", 8, "silu")
+    g = on_gpu(c)
+    want, grads = forward(c, g), backward(c, g)
+    for _ in range(3):
+        assert torch.equal(forward(c, g)[0], want[0])
+        again = backward(c, g)
+        assert all(torch.equal(again[n], grads[n]) for n in grads)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_beyond_4_gib(dtype):
+    """Views whose token stride puts their last rows more than 2^32 bytes behind their first, every operand and result."""
+    N, K, C = 300, 72, 40
+    c = make(1, N, K, C, dtype, 9, "silu", True, True)
+    g = on_gpu(c)
+    y, z = forward(c, g)
+    d = backward(c, g)
+    wide = torch.zeros((N, (1 << 24) // g["x"].element_size()), dtype=g["x"].dtype, device="cuda")   # 16 MiB a row, 4.7 GiB
+    at = lambda i, n: wide[:, 256 * i:256 * i + n].unsqueeze(0)
+    x, r, zz, dy, y2, z2, dx = at(0, K), at(1, C), at(2, C), at(3, C), at(4, C), at(5, C), at(6, K)
+    for v, s in ((x, "x"), (r, "residual"), (zz, "z"), (dy, "dy")):
+        v.copy_(g[s])
+    lf.linfusion_linear_fwd(x, g["w"], g["bias"], y2, residual=r, z=z2, workspace=memory(lf.linfusion_linear_workspace_bytes(*c["dims"], CODE[dtype])),
+                            **rest(c, g))
+    dw = torch.empty_like(g["w"])
+    lf.linfusion_linear_bwd(x, g["w"], zz, dy, dx=dx, dw=dw, workspace=memory(lf.linfusion_linear_bwd_workspace_bytes(*c["dims"], CODE[dtype])), **rest(c, g))
+    assert torch.equal(y2.contiguous(), y) and torch.equal(z2.contiguous(), z) and torch.equal(dx.contiguous(), d["dx"]) and torch.equal(dw, d["dw"])

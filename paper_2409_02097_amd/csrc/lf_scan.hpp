@@ -21,24 +21,29 @@ namespace lf {
 constexpr int kScanNorm = 0, kScanLeaky = 1, kScanSum = 2;
 constexpr int kScanWidth = 64;   // channels of a workgroup
 
-// tokens of a thread: eight of 16-bit types, four of fp32 and in the backward pass, which holds twice the values
-template <typename T> struct ScanShape {
-  static constexpr int kT = Stored<T>::kBytes == 4 ? 4 : 8, kChunk = 32 * kT;
-  static constexpr int kBackT = 4, kBackChunk = 32 * kBackT;
-};
+constexpr int kScanT = 4, kScanChunk = 32 * kScanT;   // tokens of a thread; of a chunk
 
 struct ScanView { long long batch, token; };   // element strides; channels contiguous
 
+// What the chunks of a sequence tell each other: every chunk's (A, R), and the value behind every group of chunks, as soon as they are
+// known.  All ones: not yet (scan_clear).  The workgroups take chunks by `ticket`, nearer the sequence's start (backward: its end) first, so that a workgroup
+// only ever waits for ones that have started and wait for earlier ones alone: every wait ends.
+struct ScanRecords {
+  unsigned* ticket;
+  unsigned long long* totals;   // [B][chunks][C]
+  unsigned* values;             // [B][chunks][C]
+};
+
 struct ScanArgs {
   const void *x, *gate, *input;
-  void* out;
+  void* out;                    // null: only `saved`
   ScanView vx, vg, vi, vo;
   const float *rate, *state_in;
-  float *state_out, *totals, *starts;   // totals: [B][chunks][2][C]; starts: [B][chunks][C], the state before each chunk
-  float* saved;                         // null, or the states before the chunks of the backward pass, [B][back_chunks][C]
+  float *state_out, *saved;     // saved: null, or [B][chunks of kScanChunk][C], the state before each chunk
+  ScanRecords rec;
   const int* lengths;
   long long N;
-  int C, chunks, back_chunks;
+  int B, C, chunks, saved_chunks, group;
   bool reverse;
 };
 
@@ -47,81 +52,123 @@ struct ScanBackArgs {
   void *dx, *dgate, *dinput;
   ScanView vx, vg, vi, vd, vdx, vdg, vdi;
   const float *rate, *starts, *dstate_out;
-  float *dstate_in, *totals, *ends, *partials;   // ends: [B][chunks][C], E behind each chunk; partials: [B][chunks][C], of drate
+  float *dstate_in, *partials;  // partials: [B][chunks][C], of drate
+  ScanRecords rec;
   const int* lengths;
   long long N;
-  int C, chunks;
+  int B, C, chunks, group;
   bool reverse;
 };
 
-// e^x on the hardware's exponential of 2; Precise adds back what rounding x log2(e) loses.  x is cut off where the result is 0 or
-// near the largest value anyway; a NaN stays one.
-template <bool Precise> LF_DEV float exp_of(float x) {
-  constexpr float kLog2e = 1.44269504088896340736f;
-  if constexpr (!Precise) return __builtin_amdgcn_exp2f(x * kLog2e);
-  x = x < -120.0f ? -120.0f : x;
-  x = x > 88.0f ? 88.0f : x;
-  const float t = x * kLog2e, e = __builtin_amdgcn_exp2f(t);
-  const float lost = __builtin_fmaf(x, kLog2e, -t) + x * 1.92596299112661746e-8f;
-  return __builtin_fmaf(e, lost * 0.69314718055994530942f, e);
+// v < limit ? a : b by the sign of v - limit, for v that is no NaN or where a and b both are then.  Left to itself the compiler makes
+// branches of such choices, one per element (65536 x 1280 in bf16: 142 us for what takes 60 without); it also knows this mask from a
+// compare, hence the instruction.
+LF_DEV float below(float v, float limit, float a, float b) {
+  const float d = v - limit;
+  uint32_t mask;
+  asm("v_ashrrev_i32 %0, 31, %1" : "=v"(mask) : "v"(d));
+  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, a) & mask) | (__builtin_bit_cast(uint32_t, b) & ~mask));
+}
+// c ? 0 : x, x formed in any case
+LF_DEV float unless(bool c, float x) {
+  asm volatile("" : "+v"(x));
+  return c ? 0.0f : x;
 }
 
+// 1 / (1 + e^-x), the exponential by the hardware's of 2; Precise adds back what rounding x log2(e) loses.
 template <bool Precise> LF_DEV float sigmoid_of(float x) {
-  const float s = __builtin_amdgcn_rcpf(1.0f + exp_of<Precise>(-x));
-  return Precise && x < -88.0f ? 0.0f : s;
+  constexpr float kLog2e = 1.44269504088896340736f;
+  const float t = x * -kLog2e, e = __builtin_amdgcn_exp2f(t);
+  if constexpr (!Precise) return __builtin_amdgcn_rcpf(1.0f + e);
+  const float lost = __builtin_fmaf(x, -1.92596299112661746e-8f, __builtin_fmaf(x, -kLog2e, -t));
+  const float s = __builtin_amdgcn_rcpf(1.0f + unless(x > 104.0f, __builtin_fmaf(e, lost * 0.69314718055994530942f, e)));   // (no 0 times infinity)
+  return unless(x < -88.0f, s);
 }
 
-// 1 - e^-v for v >= 0, e = e^-v given: where they are near each other by the series, whose next term is below 2^-24 of the
-// result (16-bit types: 2^-19).
-template <bool Precise> LF_DEV float one_less(float v, float e) {
-  float p;
-  if constexpr (Precise) {
-    p = __builtin_fmaf(v, -1.0f / 8, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 7, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 6, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 5, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 4, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 3, 1.0f);
-    p = __builtin_fmaf(v * p, -1.0f / 2, 1.0f);
-    return v < 0.5f ? v * p : 1.0f - e;
-  }
-  p = __builtin_fmaf(v, -1.0f / 120, 1.0f / 24);
-  p = __builtin_fmaf(v, -p, 1.0f / 6);
-  p = __builtin_fmaf(v, -p, 0.5f);
-  p = __builtin_fmaf(v, -p, 1.0f);
-  return v < 0.25f ? v * p : 1.0f - e;
+// 1 - 2^-d for d >= 0, e = 2^-d given, or with TWICE 1 - 4^-d, e = 4^-d: where e is near 1 by the series, whose next term is below 2^-24
+// of the result (16-bit types: below 2^-18.9 twice, 2^-24 once).
+template <bool Precise, bool TWICE> LF_DEV float one_less(float d, float e) {
+  constexpr float k1[10] = {0.693147181f, 0.240226507f, 0.0555041087f, 0.00961812911f, 0.00133335581f, 0.000154035304f, 1.52527338e-05f, 1.32154868e-06f, 1.0178086e-07f, 7.05491162e-09f};
+  constexpr float k2[8] = {1.38629436f, 0.960906028f, 0.444032869f, 0.153890066f, 0.0426673861f, 0.00985825945f, 0.00195234993f, 0.000338316462f};   // (ln 2)^n / n!, (2 ln 2)^n / n!
+  constexpr int kTerms = Precise ? 8 : (TWICE ? 4 : 6);
+  constexpr float kLimit = Precise ? (TWICE ? 0.36f : 0.72f) : (TWICE ? 0.09f : 0.36f);   // the exponent below 1/2; 1/8, 1/4
+  float p = TWICE ? k2[kTerms - 1] : k1[kTerms - 1];
+#pragma unroll
+  for (int i = kTerms - 2; i >= 0; --i) p = __builtin_fmaf(d, -p, TWICE ? k2[i] : k1[i]);
+  return below(d, kLimit, d * p, 1.0f - e);
 }
 
-// What a token's gates say: a, and the weight m of the new value with r so that dm/dg = -a r (kScanNorm: r = a / m, 0 where m is 0).
-struct ScanWeight { float a, m, r; };
-template <bool Precise, int MODE> LF_DEV ScanWeight weight_of(float decay) {   // decay = -g
-  ScanWeight w;
-  w.a = exp_of<Precise>(-decay);
-  if constexpr (MODE == kScanSum) {
-    w.m = 1.0f;
-    w.r = 0.0f;
-  } else if constexpr (MODE == kScanLeaky) {
-    w.m = one_less<Precise>(decay, w.a);
-    w.r = 1.0f;
-  } else {
-    const float m2 = one_less<Precise>(2.0f * decay, w.a * w.a);
-    const float q = m2 < 1.17549435e-38f ? 0.0f : __builtin_amdgcn_rsqf(m2);
-    w.m = m2 * q;
-    w.r = w.a * q;
+// The weight m of the new value for a = 2^-d, and r so that dm/dg = -a r (kScanNorm: r = a / m, 0 where m is 0).
+struct ScanWeight { float m, r; };
+template <bool Precise, int MODE, bool SLOPE> LF_DEV ScanWeight weight_of(float d, float a) {   // (without SLOPE: m alone)
+  if constexpr (MODE == kScanSum) return ScanWeight{1.0f, 0.0f};
+  if constexpr (MODE == kScanLeaky) return ScanWeight{one_less<Precise, false>(d, a), 1.0f};
+  const float m2 = one_less<Precise, true>(d, a * a);
+  if constexpr (!SLOPE) return ScanWeight{__builtin_amdgcn_sqrtf(m2), 0.0f};
+  const float q = below(m2, 1.17549435e-38f, 0.0f, __builtin_amdgcn_rsqf(m2));
+  return ScanWeight{m2 * q, a * q};
+}
+
+// What absent gates read as: minus infinity, whose sigmoid is 0, so that a = 1 and the state stays as it is.
+template <typename T> struct ShutBits;
+template <> struct ShutBits<F16> { static constexpr uint32_t value = 0xfc00fc00u; };
+template <> struct ShutBits<BF16> { static constexpr uint32_t value = 0xff80ff80u; };
+template <> struct ShutBits<F32> { static constexpr uint32_t value = 0xff800000u; };
+template <typename T> LF_DEV Raw8<T> shut8() {
+  constexpr uint32_t w = ShutBits<T>::value;
+  Raw8<T> r;
+  r.w = u32x4{w, w, w, w};
+  if constexpr (Stored<T>::kBytes == 4) r.w2 = u32x4{w, w, w, w};
+  return r;
+}
+
+// Makes the compiler take a value for a new one, so that what was formed from it is formed again and not kept in registers meanwhile.
+LF_DEV void forget(float& x) { asm("" : "+v"(x)); }
+template <typename T> LF_DEV void forget(Raw8<T>& r) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w = r.w[i];
+    asm("" : "+v"(w));
+    r.w[i] = w;
+    if constexpr (Stored<T>::kBytes == 4) {
+      w = r.w2[i];
+      asm("" : "+v"(w));
+      r.w2[i] = w;
+    }
   }
-  return w;
 }
 
 // Where a row's tokens are in the order of the recurrence.
 struct ScanRow {
-  long long n, first, step;   // tokens that count; the first one; from one to the next
-  LF_DEV ScanRow(const int* lengths, int b, long long N, bool reverse) {
-    n = tokens_of(lengths, b, N);
-    first = reverse ? n - 1 : 0;
-    step = reverse ? -1 : 1;
-  }
-  LF_DEV long long token(long long t) const { return first + step * t; }
+  long long n;       // tokens that count
+  bool reverse;
+  LF_DEV ScanRow(const int* lengths, int b, long long N, bool rev) : n(tokens_of(lengths, b, N)), reverse(rev) {}
+  LF_DEV long long token(long long t) const { return reverse ? n - 1 - t : t; }
+  // the bytes from a token's row to the next one's in this order
+  template <typename T> LF_DEV long long step(const ScanView& v) const { return (reverse ? -v.token : v.token) * Stored<T>::kBytes; }
 };
+
+LF_DEV void load_rate(const float* p, bool on, float (&rate)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) rate[k] = 0.0f;
+  if (on) load8_f32(p, rate);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) rate[k] *= 1.44269504088896340736f;
+}
+
+// The rows of a thread's tokens, the first at `p`, the next ones `step` bytes on; `absent` where there are none.
+template <typename T, int TT> LF_DEV void load_rows(const unsigned char* p, long long step, int live, bool full, const Raw8<T>& absent, Raw8<T> (&r)[TT]) {
+  if (full) {   // (a whole workgroup's)
+#pragma unroll
+    for (int j = 0; j < TT; ++j, p += step) r[j] = load8_raw<T>(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < TT; ++j, p += step) {
+      r[j] = absent;
+      if (j < live) r[j] = load8_raw<T>(p);
+    }
+  }
+}
 
 // The stretches of a chunk joined: from each thread's (A, R) of 8 channels the value its first token starts from, given the
 // chunk's; and the chunk's own (A, R).  Time lane of a thread: threadIdx.x / 8 in the recurrence's order (BACK: 31 minus that).
@@ -199,233 +246,235 @@ LF_DEV void spread8(float* lds, float v, float (&x)[8]) {
   }
 }
 
-constexpr int kScanWhole = 0, kScanTotals = 1, kScanApply = 2;
+// ---- between chunks ----------------------------------------------------------------------------------------------------
 
-// PASS kScanTotals leaves every chunk's (A, R), scan_starts turns them into the states between the chunks, and kScanApply goes
-// from those; a sequence of one chunk is kScanWhole alone.
-template <typename T, int MODE, bool INPUT, int PASS>
+constexpr unsigned kNotYet = 0xffffffffu;
+LF_DEV unsigned told(float v) { return v != v ? 0x7fc00000u : __builtin_bit_cast(unsigned, v); }   // (never kNotYet)
+
+LF_DEV void tell_totals(const ScanRecords& r, long long i, float A, float R) {
+  __hip_atomic_store(r.totals + i, (unsigned long long)told(R) << 32 | told(A), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+LF_DEV void tell_value(const ScanRecords& r, long long i, float h) {
+  __hip_atomic_store(r.values + i, told(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+constexpr int kScanGroup = 32;   // chunks of a group, at most
+struct ScanFound { float value[kScanWidth]; };
+
+// The value that a chunk starts from, lane c's for its channel: from the value behind the group of chunks before its own (its row's first
+// one, `start`, in the first group) through the totals of its group's chunks before it, one after the other.  Only a group's last chunk
+// tells its value, so that results do not depend on who was first, and a chunk reads 16 totals or fewer, not a row's.  `order`: the chunk's
+// place in its row's order (backward: from the row's end); `i0`: its record for this channel, `next`: from a chunk's record to the one's
+// after it in the order.  `totals`: 16 KB of LDS.
+LF_DEV float look_back(const ScanRecords& r, ScanFound& lds, float (&totals)[32][2][kScanWidth], int group, int order, long long i0, long long next,
+                       float start, bool on) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int before = order % group;   // chunks of the group before this one
+  if (wave == 0) {
+    float v = start;
+    if (order >= group) {
+      const unsigned* p = r.values + i0 - next * (before + 1);
+      unsigned w = 0;
+      if (on) w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      while (__any(w == kNotYet)) {
+        __builtin_amdgcn_s_sleep(1);
+        if (w == kNotYet) w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      v = __builtin_bit_cast(float, w);
+    }
+    lds.value[lane] = v;
+  }
+  // the waves take the chunks in turn, from the furthest on; those of a wave are requested together, four at a time
+  for (int e0 = wave; e0 < before; e0 += 16) {
+    unsigned long long t[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      t[k] = 0;
+      if (on && e0 + 4 * k < before)
+        t[k] = __hip_atomic_load(r.totals + i0 - next * (before - e0 - 4 * k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      while (__any((unsigned)t[k] == kNotYet)) {
+        __builtin_amdgcn_s_sleep(1);
+        if ((unsigned)t[k] == kNotYet)
+          t[k] = __hip_atomic_load(r.totals + i0 - next * (before - e0 - 4 * k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      if (e0 + 4 * k < before) {
+        totals[e0 + 4 * k][0][lane] = __builtin_bit_cast(float, (unsigned)t[k]);
+        totals[e0 + 4 * k][1][lane] = __builtin_bit_cast(float, (unsigned)(t[k] >> 32));
+      }
+    }
+  }
+  __syncthreads();
+  float h = lds.value[lane];
+  for (int e = 0; e < before; ++e) h = __builtin_fmaf(totals[e][0][lane], h, totals[e][1][lane]);
+  return h;
+}
+
+// Records to "not yet", the ticket to 0.
+__global__ __launch_bounds__(256) void scan_clear(ScanRecords r, long long count) {
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 2;
+  if (i == 0) *r.ticket = 0;
+  if (i >= count) return;   // (count is even)
+  *reinterpret_cast<u32x4*>(r.totals + i) = u32x4{kNotYet, kNotYet, kNotYet, kNotYet};
+  *reinterpret_cast<u32x2*>(r.values + i) = u32x2{kNotYet, kNotYet};
+}
+
+// Which chunk, batch row and channels a workgroup takes.
+struct ScanPlace {
+  int chunk, b, c0;
+  template <bool ONE, bool BACK> LF_DEV void take(const ScanRecords& r, int B, int C, int chunks, int& lds) {
+    unsigned id = blockIdx.x;
+    if constexpr (!ONE) {
+      if (threadIdx.x == 0) lds = (int)__hip_atomic_fetch_add(r.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      id = (unsigned)__builtin_amdgcn_readfirstlane(lds);
+    }
+    const unsigned blocks = (unsigned)(C + kScanWidth - 1) / kScanWidth, per = blocks * (unsigned)B;
+    const unsigned at = id / per, rest = id - at * per;
+    b = (int)(rest / blocks);
+    c0 = (int)(rest - (unsigned)b * blocks) * kScanWidth;
+    chunk = BACK ? chunks - 1 - (int)at : (int)at;
+  }
+};
+
+// ---- forward -----------------------------------------------------------------------------------------------------------
+
+// TT tokens a thread; ONE: the whole sequence is one chunk.
+// Bound: HBM and vector instructions, nearly level (46 issue slots a value with the norm's weight, six of them transcendental).
+template <typename T, int MODE, bool INPUT, int TT, bool ONE>
 __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
-  constexpr int TT = ScanShape<T>::kT, L = ScanShape<T>::kChunk;
+  constexpr int L = 32 * TT;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanJoin lds;
+  __shared__ ScanFound found;
   __shared__ float spread[4][kScanWidth];
-  const int b = blockIdx.z, blocks = (a.C + kScanWidth - 1) / kScanWidth;
-  const int chunk = blockIdx.x / blocks, c0 = (blockIdx.x - chunk * blocks) * kScanWidth;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = c0 + (lane & 7) * 8;
+  __shared__ int id;
+  ScanPlace p;
+  p.take<ONE, false>(a.rec, a.B, a.C, a.chunks, id);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
   const bool on = c < a.C;
-  const ScanRow row(a.lengths, b, a.N, a.reverse);
-  const long long t0 = (long long)chunk * L + (threadIdx.x >> 3) * TT;
-  if (chunk && (long long)chunk * L >= row.n) return;   // (the whole workgroup)
-  Raw8<T> rx[TT], rg[TT], ri[TT];
-#pragma unroll
-  for (int j = 0; j < TT; ++j) {
-    rx[j] = rg[j] = ri[j] = none8<T>();
-    if (!on || t0 + j >= row.n) continue;
-    const long long n = row.token(t0 + j);
-    rx[j] = load8_raw<T>(at<T>(a.x, b * a.vx.batch + n * a.vx.token + c));
-    rg[j] = load8_raw<T>(at<T>(a.gate, b * a.vg.batch + n * a.vg.token + c));
-    if constexpr (INPUT) ri[j] = load8_raw<T>(at<T>(a.input, b * a.vi.batch + n * a.vi.token + c));
+  const ScanRow row(a.lengths, p.b, a.N, a.reverse);
+  const int t0 = p.chunk * L + (threadIdx.x >> 3) * TT;
+  if (p.chunk && (long long)p.chunk * L >= row.n) return;   // (the whole workgroup)
+  const int live = on ? (row.n - t0 < TT ? (int)(row.n - t0) : TT) : 0;   // this thread's tokens that count (below 0: none)
+  Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1];
+  const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
+  {
+    const long long n = row.token(t0);
+    load_rows(at<T>(a.gate, p.b * a.vg.batch + n * a.vg.token + c), row.step<T>(a.vg), live, full, shut8<T>(), rg);
+    load_rows(at<T>(a.x, p.b * a.vx.batch + n * a.vx.token + c), row.step<T>(a.vx), live, full, none8<T>(), rx);
+    if constexpr (INPUT) load_rows(at<T>(a.input, p.b * a.vi.batch + n * a.vi.token + c), row.step<T>(a.vi), live, full, none8<T>(), ri);
   }
-  float rate[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) rate[k] = 0.0f;
-  if (on) load8_f32(a.rate + c, rate);
+  float rate[8];   // of powers of two
+  load_rate(a.rate + c, on, rate);
   float da[TT][8], u[TT][8], A[8], R[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
     float x[8], g[8], in[8];
     widen8<T>(rx[j], x);
     widen8<T>(rg[j], g);
-    widen8<T>(ri[j], in);
-    const bool live = on && t0 + j < row.n;
+    if constexpr (INPUT) widen8<T>(ri[j], in);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const ScanWeight w = weight_of<kPrecise, MODE>(rate[k] * sigmoid_of<kPrecise>(g[k]));
-      float v = w.m * x[k];
-      if constexpr (INPUT) v *= sigmoid_of<kPrecise>(in[k]);
-      da[j][k] = live ? w.a : 1.0f;
-      u[j][k] = live ? v : 0.0f;
+      const float d = rate[k] * sigmoid_of<kPrecise>(g[k]);
+      da[j][k] = __builtin_amdgcn_exp2f(-d);
+      u[j][k] = weight_of<kPrecise, MODE, false>(d, da[j][k]).m * x[k];
+      if constexpr (INPUT) u[j][k] *= sigmoid_of<kPrecise>(in[k]);
       R[k] = j ? __builtin_fmaf(da[j][k], R[k], u[j][k]) : u[j][k];
       A[k] = j ? A[k] * da[j][k] : da[j][k];
     }
   }
   join_wave<false>(lds, A, R);
   __syncthreads();
-  const long long at0 = ((long long)b * a.chunks + chunk) * a.C;
-  const int cl = c0 + lane;
-  float ca, cr;
-  if constexpr (PASS == kScanTotals) {
+  float ca, cr, h0 = 0.0f;
+  const long long row0 = (long long)p.b * a.chunks * a.C + cl;
+  const bool whole = wave == 0 && cl < a.C;   // the threads that speak for the chunk
+  if (cl < a.C && a.state_in && (ONE || p.chunk < a.group)) h0 = a.state_in[(long long)p.b * a.C + cl];
+  const long long i0 = row0 + (long long)p.chunk * a.C;
+  if constexpr (!ONE) {
     join_chunk<false>(lds, 4, ca, cr);
-    if (wave == 0 && cl < a.C) {
-      a.totals[2 * at0 + cl] = ca;
-      a.totals[2 * at0 + a.C + cl] = cr;
-    }
-    return;
+    if (whole) tell_totals(a.rec, i0, ca, cr);
+    h0 = look_back(a.rec, found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
   }
-  float h0 = 0.0f;
-  if (cl < a.C) {
-    if constexpr (PASS == kScanApply) h0 = a.starts[at0 + cl];
-    else h0 = a.state_in ? a.state_in[(long long)b * a.C + cl] : 0.0f;
+  if (whole) {
+    join_chunk<false>(lds, 4, ca, cr);
+    const float end = __builtin_fmaf(ca, h0, cr);
+    if (!ONE && p.chunk % a.group == a.group - 1) tell_value(a.rec, i0, end);
+    if (a.state_out && (long long)(p.chunk + 1) * L >= row.n) a.state_out[(long long)p.b * a.C + cl] = end;   // the last token is here
   }
   join_chunk<false>(lds, wave, ca, cr);
-  float h[8];
   const float mine = __builtin_fmaf(ca, h0, cr);   // the state before the wave's tokens
-  constexpr int kEvery = ScanShape<T>::kBackChunk / (8 * TT);   // waves of a chunk of the backward pass
-  if (a.saved && cl < a.C && wave % kEvery == 0) {
-    const long long t = (long long)chunk * L + wave * 8 * TT;
-    if (t == 0 || t < row.n) a.saved[((long long)b * a.back_chunks + t / ScanShape<T>::kBackChunk) * a.C + cl] = mine;
+  if (a.saved && cl < a.C && wave * 8 * TT % kScanChunk == 0) {
+    const long long t = (long long)p.chunk * L + wave * 8 * TT;
+    if (t == 0 || t < row.n) a.saved[((long long)p.b * a.saved_chunks + t / kScanChunk) * a.C + cl] = mine;
   }
+  if (!a.out) return;
+  float h[8];
   spread8(spread[wave], mine, h);
+  unsigned char* po = at<T>(a.out, p.b * a.vo.batch + row.token(t0) * a.vo.token + c);
+  const long long so = row.step<T>(a.vo);
 #pragma unroll
   for (int k = 0; k < 8; ++k) h[k] = __builtin_fmaf(A[k], h[k], R[k]);
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) h[k] = __builtin_fmaf(da[j][k], h[k], u[j][k]);
-    if (a.out && on && t0 + j < row.n) store8_stream<T>(at<T>(a.out, b * a.vo.batch + row.token(t0 + j) * a.vo.token + c), h);
-  }
-  if (wave == 3 && cl < a.C && a.state_out && (long long)(chunk + 1) * L >= row.n) {   // the chunk with the last token that counts
-    join_chunk<false>(lds, 4, ca, cr);
-    a.state_out[(long long)b * a.C + cl] = __builtin_fmaf(ca, h0, cr);
+    if (j < live) store8_stream<T>(po, h);
+    po += so;
   }
 }
 
-// The values that the chunks of one (batch, channel) start from, one after the other (BACK: from the last one that counts).
-template <bool BACK>
-__global__ __launch_bounds__(64) void scan_starts(const float* totals, const float* first, float* starts, const int* lengths,
-                                                  long long N, int C, int chunks, int L) {
-  const int b = blockIdx.y, c = blockIdx.x * 64 + threadIdx.x;
-  if (c >= C) return;
-  long long used = (tokens_of(lengths, b, N) + L - 1) / L;
-  if (used < 1) used = 1;
-  float h = first ? first[(long long)b * C + c] : 0.0f;
-  const long long row = (long long)b * chunks;
-  constexpr int kAhead = 8;
-  for (long long j0 = 0; j0 < used; j0 += kAhead) {
-    float ta[kAhead], tr[kAhead];
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      const long long j = BACK ? used - 1 - j0 - q : j0 + q;
-      ta[q] = tr[q] = 0.0f;
-      if (j0 + q >= used) continue;
-      ta[q] = totals[2 * (row + j) * C + c];
-      tr[q] = totals[2 * (row + j) * C + C + c];
-    }
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      const long long j = BACK ? used - 1 - j0 - q : j0 + q;
-      if (j0 + q >= used) break;
-      starts[(row + j) * C + c] = h;
-      h = __builtin_fmaf(ta[q], h, tr[q]);
-    }
-  }
-}
+// ---- backward ----------------------------------------------------------------------------------------------------------
 
-// What backward's chunks do to E: E = a (dout + E) from a chunk's last token to its first.
-template <typename T>
-__global__ __launch_bounds__(256) void scan_back_totals(ScanBackArgs a) {
-  constexpr int TT = ScanShape<T>::kBackT, L = ScanShape<T>::kBackChunk;
-  constexpr bool kPrecise = Stored<T>::kBytes == 4;
-  __shared__ ScanJoin lds;
-  const int b = blockIdx.z, blocks = (a.C + kScanWidth - 1) / kScanWidth;
-  const int chunk = blockIdx.x / blocks, c0 = (blockIdx.x - chunk * blocks) * kScanWidth;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = c0 + (lane & 7) * 8;
-  const bool on = c < a.C;
-  const ScanRow row(a.lengths, b, a.N, a.reverse);
-  const long long t0 = (long long)chunk * L + (threadIdx.x >> 3) * TT;
-  if (chunk && (long long)chunk * L >= row.n) return;
-  Raw8<T> rg[TT], rd[TT];
-#pragma unroll
-  for (int j = 0; j < TT; ++j) {
-    rg[j] = rd[j] = none8<T>();
-    if (!on || t0 + j >= row.n) continue;
-    const long long n = row.token(t0 + j);
-    rg[j] = load8_raw<T>(at<T>(a.gate, b * a.vg.batch + n * a.vg.token + c));
-    rd[j] = load8_raw<T>(at<T>(a.dout, b * a.vd.batch + n * a.vd.token + c));
-  }
-  float rate[8], A[8], R[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) { rate[k] = 0.0f; A[k] = 1.0f; R[k] = 0.0f; }
-  if (on) load8_f32(a.rate + c, rate);
-#pragma unroll
-  for (int j = TT - 1; j >= 0; --j) {
-    float g[8], d[8];
-    widen8<T>(rg[j], g);
-    widen8<T>(rd[j], d);
-    const bool live = on && t0 + j < row.n;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float da = live ? exp_of<kPrecise>(-rate[k] * sigmoid_of<kPrecise>(g[k])) : 1.0f;
-      R[k] = da * (R[k] + (live ? d[k] : 0.0f));
-      A[k] *= da;
-    }
-  }
-  join_wave<true>(lds, A, R);
-  __syncthreads();
-  const int cl = c0 + lane;
-  if (wave == 0 && cl < a.C) {
-    float ca, cr;
-    join_chunk<true>(lds, 4, ca, cr);
-    const long long at0 = 2 * ((long long)b * a.chunks + chunk) * a.C + cl;
-    a.totals[at0] = ca;
-    a.totals[at0 + a.C] = cr;
-  }
-}
-
-// The gradients of a chunk, from the state in front of it and E behind it (ends; null: one chunk, dstate_out).
-template <typename T, int MODE, bool INPUT>
-__global__ __launch_bounds__(256) void scan_bwd(ScanBackArgs a) {
-  constexpr int TT = ScanShape<T>::kBackT, L = ScanShape<T>::kBackChunk;
+// The gradients of a chunk, from the state in front of it and E behind it, which comes from the chunks behind as the state does from
+// those before.
+template <typename T, int MODE, bool INPUT, bool ONE>
+__global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
+  constexpr int TT = kScanT, L = kScanChunk;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanJoin there, back;
+  __shared__ ScanFound found;
   __shared__ float spread[2][4][kScanWidth];
-  const int b = blockIdx.z, blocks = (a.C + kScanWidth - 1) / kScanWidth;
-  const int chunk = blockIdx.x / blocks, c0 = (blockIdx.x - chunk * blocks) * kScanWidth;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = c0 + (lane & 7) * 8;
+  __shared__ int id;
+  ScanPlace p;
+  p.take<ONE, true>(a.rec, a.B, a.C, a.chunks, id);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
   const bool on = c < a.C;
-  const ScanRow row(a.lengths, b, a.N, a.reverse);
-  const long long t0 = (long long)chunk * L + (threadIdx.x >> 3) * TT;
-  const int cl = c0 + lane;
-  const long long at0 = ((long long)b * a.chunks + chunk) * a.C;
-  if (chunk && (long long)chunk * L >= row.n) {
-    if (wave == 0 && cl < a.C) a.partials[at0 + cl] = 0.0f;
+  const ScanRow row(a.lengths, p.b, a.N, a.reverse);
+  const long long row0 = (long long)p.b * a.chunks * a.C + cl, at0 = row0 + (long long)p.chunk * a.C;
+  const int last = row.n ? (int)((row.n - 1) / L) : 0;
+  if (p.chunk > last) {   // (the whole workgroup)
+    if (wave == 0 && cl < a.C) a.partials[at0] = 0.0f;
     return;
   }
-  Raw8<T> rx[TT], rg[TT], ri[TT], rd[TT];
-#pragma unroll
-  for (int j = 0; j < TT; ++j) {
-    rx[j] = rg[j] = ri[j] = rd[j] = none8<T>();
-    if (!on || t0 + j >= row.n) continue;
-    const long long n = row.token(t0 + j);
-    rx[j] = load8_raw<T>(at<T>(a.x, b * a.vx.batch + n * a.vx.token + c));
-    rg[j] = load8_raw<T>(at<T>(a.gate, b * a.vg.batch + n * a.vg.token + c));
-    if constexpr (INPUT) ri[j] = load8_raw<T>(at<T>(a.input, b * a.vi.batch + n * a.vi.token + c));
-    rd[j] = load8_raw<T>(at<T>(a.dout, b * a.vd.batch + n * a.vd.token + c));
-  }
+  const int t0 = p.chunk * L + (threadIdx.x >> 3) * TT;
+  const int live = on ? (row.n - t0 < TT ? (int)(row.n - t0) : TT) : 0;
+  const long long n0 = row.token(t0);
+  Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1], rd[TT];
+  const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
+  load_rows(at<T>(a.gate, p.b * a.vg.batch + n0 * a.vg.token + c), row.step<T>(a.vg), live, full, shut8<T>(), rg);
+  load_rows(at<T>(a.dout, p.b * a.vd.batch + n0 * a.vd.token + c), row.step<T>(a.vd), live, full, none8<T>(), rd);
+  load_rows(at<T>(a.x, p.b * a.vx.batch + n0 * a.vx.token + c), row.step<T>(a.vx), live, full, none8<T>(), rx);
+  if constexpr (INPUT) load_rows(at<T>(a.input, p.b * a.vi.batch + n0 * a.vi.token + c), row.step<T>(a.vi), live, full, none8<T>(), ri);
   float rate[8], h0 = 0.0f, e0 = 0.0f;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) rate[k] = 0.0f;
-  if (on) load8_f32(a.rate + c, rate);
-  if (cl < a.C) {
-    h0 = a.starts[at0 + cl];
-    e0 = a.ends ? a.ends[at0 + cl] : (a.dstate_out ? a.dstate_out[(long long)b * a.C + cl] : 0.0f);
-  }
+  load_rate(a.rate + c, on, rate);
+  if (cl < a.C) h0 = a.starts[at0];
   float da[TT][8], u[TT][8], sg[TT][8], A[8], R[8], BA[8], BR[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
     float x[8], g[8], in[8];
     widen8<T>(rx[j], x);
     widen8<T>(rg[j], g);
-    widen8<T>(ri[j], in);
-    const bool live = on && t0 + j < row.n;
+    if constexpr (INPUT) widen8<T>(ri[j], in);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       sg[j][k] = sigmoid_of<kPrecise>(g[k]);
-      const ScanWeight w = weight_of<kPrecise, MODE>(rate[k] * sg[j][k]);
-      float v = w.m * x[k];
-      if constexpr (INPUT) v *= sigmoid_of<kPrecise>(in[k]);
-      da[j][k] = live ? w.a : 1.0f;
-      u[j][k] = live ? v : 0.0f;
+      const float dk = rate[k] * sg[j][k];
+      da[j][k] = __builtin_amdgcn_exp2f(-dk);
+      u[j][k] = weight_of<kPrecise, MODE, false>(dk, da[j][k]).m * x[k];
+      if constexpr (INPUT) u[j][k] *= sigmoid_of<kPrecise>(in[k]);
       R[k] = j ? __builtin_fmaf(da[j][k], R[k], u[j][k]) : u[j][k];
       A[k] = j ? A[k] * da[j][k] : da[j][k];
     }
@@ -441,17 +490,37 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBackArgs a) {
   }
   join_wave<false>(there, A, R);
   join_wave<true>(back, BA, BR);
+#pragma unroll
+  for (int j = 0; j < TT; ++j) {
+    forget(rx[j]);
+    forget(rd[j]);
+    if constexpr (INPUT) forget(ri[j]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      forget(sg[j][k]);
+      forget(da[j][k]);
+    }
+  }
   __syncthreads();
   float ca, cr;
+  const bool whole = wave == 0 && cl < a.C;
+  if (cl < a.C && a.dstate_out && (ONE || last - p.chunk < a.group)) e0 = a.dstate_out[(long long)p.b * a.C + cl];
+  if constexpr (!ONE) {
+    join_chunk<true>(back, 4, ca, cr);
+    if (whole) tell_totals(a.rec, at0, ca, cr);
+    e0 = look_back(a.rec, found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
+  }
+  if (whole) {
+    join_chunk<true>(back, 4, ca, cr);
+    const float end = __builtin_fmaf(ca, e0, cr);
+    if (!ONE && (last - p.chunk) % a.group == a.group - 1) tell_value(a.rec, at0, end);
+    if (a.dstate_in && p.chunk == 0) a.dstate_in[(long long)p.b * a.C + cl] = end;
+  }
   float h[8], E[8];
   join_chunk<false>(there, wave, ca, cr);
   spread8(spread[0][wave], __builtin_fmaf(ca, h0, cr), h);
   join_chunk<true>(back, 3 - wave, ca, cr);
   spread8(spread[1][wave], __builtin_fmaf(ca, e0, cr), E);
-  if (a.dstate_in && chunk == 0 && wave == 0 && cl < a.C) {
-    join_chunk<true>(back, 4, ca, cr);
-    a.dstate_in[(long long)b * a.C + cl] = __builtin_fmaf(ca, e0, cr);
-  }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     h[k] = __builtin_fmaf(A[k], h[k], R[k]);
@@ -468,33 +537,40 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBackArgs a) {
   float by_rate[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) by_rate[k] = 0.0f;
+  const long long sdx = row.step<T>(a.vdx), sdg = row.step<T>(a.vdg), sdi = row.step<T>(a.vdi);
+  unsigned char* pdx = at<T>(a.dx, p.b * a.vdx.batch + n0 * a.vdx.token + c) + (TT - 1) * sdx;
+  unsigned char* pdg = at<T>(a.dgate, p.b * a.vdg.batch + n0 * a.vdg.token + c) + (TT - 1) * sdg;
+  unsigned char* pdi = at<T>(a.dinput, p.b * a.vdi.batch + n0 * a.vdi.token + c) + (TT - 1) * sdi;
 #pragma unroll
   for (int j = TT - 1; j >= 0; --j) {
     float x[8], in[8], d[8], dx[8], dg[8], di[8];
     widen8<T>(rx[j], x);
-    widen8<T>(ri[j], in);
+    if constexpr (INPUT) widen8<T>(ri[j], in);
     widen8<T>(rd[j], d);
-    const bool live = on && t0 + j < row.n;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float D = d[k] + E[k], s = sg[j][k], decay = rate[k] * s, ak = da[j][k];
-      const ScanWeight w = weight_of<kPrecise, MODE>(decay);
+    for (int k = 0; k < 8; ++k) {   // (a token that does not count: D = E, s = m = 0, a = 1)
+      const float D = d[k] + E[k], s = sg[j][k], ak = da[j][k];
+      const ScanWeight w = weight_of<kPrecise, MODE, true>(rate[k] * s, ak);
       float i = 1.0f;
       if constexpr (INPUT) i = sigmoid_of<kPrecise>(in[k]);
       const float Di = D * i, Dmi = w.m * Di;
       dx[k] = Dmi;
       if constexpr (INPUT) di[k] = Dmi * x[k] * (1.0f - i);
-      // dg = a (D h' - r D i x)
-      const float by_log = ak * __builtin_fmaf(D, u[j][k], -w.r * Di * x[k]);
-      dg[k] = -by_log * decay * (1.0f - s);
-      by_rate[k] = live ? __builtin_fmaf(-by_log, s, by_rate[k]) : by_rate[k];
+      // -dg = a (r D i x - D h')
+      const float less = ak * __builtin_fmaf(w.r * Di, x[k], -D * u[j][k]);
+      const float part = less * s;
+      by_rate[k] += part;
+      dg[k] = part * (rate[k] * 0.69314718055994530942f) * (1.0f - s);
       E[k] = ak * D;
     }
-    if (!live) continue;
-    const long long n = row.token(t0 + j);
-    store8_stream<T>(at<T>(a.dx, b * a.vdx.batch + n * a.vdx.token + c), dx);
-    store8_stream<T>(at<T>(a.dgate, b * a.vdg.batch + n * a.vdg.token + c), dg);
-    if constexpr (INPUT) store8_stream<T>(at<T>(a.dinput, b * a.vdi.batch + n * a.vdi.token + c), di);
+    if (j < live) {
+      store8_stream<T>(pdx, dx);
+      store8_stream<T>(pdg, dg);
+      if constexpr (INPUT) store8_stream<T>(pdi, di);
+    }
+    pdx -= sdx;
+    pdg -= sdg;
+    pdi -= sdi;
   }
   __syncthreads();   // the stretches' LDS takes the sums
 #pragma unroll
@@ -502,28 +578,20 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBackArgs a) {
     *reinterpret_cast<f32x4*>(&there.stretch[threadIdx.x >> 3][0][(lane & 7) * 8 + 4 * q]) =
         f32x4{by_rate[4 * q], by_rate[4 * q + 1], by_rate[4 * q + 2], by_rate[4 * q + 3]};
   __syncthreads();
-  if (wave == 0 && cl < a.C) {
+  if (whole) {
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < 32; ++j) sum += there.stretch[j][0][lane];
-    a.partials[at0 + cl] = sum;
+    a.partials[at0] = sum;
   }
 }
 
-// drate: the chunks' sums of every batch row, in a fixed order, in fp64 (a long sequence has thousands of them).
+// drate: the chunks' sums of every batch row.
 __global__ __launch_bounds__(1024) void scan_rate_sums(const float* partials, float* drate, long long parts, int C) {
-  __shared__ double lds[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-  double sum = 0.0;
-  if (c < C)
-    for (long long p = wave; p < parts; p += 16) sum += (double)partials[p * C + c];
-  lds[wave][lane] = sum;
-  __syncthreads();
-  if (wave == 0 && c < C) {
-#pragma unroll
-    for (int w = 1; w < 16; ++w) sum += lds[w][lane];
-    drate[c] = (float)sum;
-  }
+  __shared__ double lds[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+  const double sum = column_sum(lds, partials, parts, C, c);
+  if (threadIdx.x < 32 && c < C) drate[c] = (float)sum;
 }
 
 struct ScanStepArgs {
@@ -555,10 +623,10 @@ __global__ __launch_bounds__(64) void scan_step(ScanStepArgs a) {
   widen8<T>(ri, in);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const ScanWeight w = weight_of<kPrecise, MODE>(rate[k] * sigmoid_of<kPrecise>(g[k]));
-    float v = w.m * x[k];
+    const float d = rate[k] * 1.44269504088896340736f * sigmoid_of<kPrecise>(g[k]), da = __builtin_amdgcn_exp2f(-d);
+    float v = weight_of<kPrecise, MODE, false>(d, da).m * x[k];
     if constexpr (INPUT) v *= sigmoid_of<kPrecise>(in[k]);
-    h[k] = __builtin_fmaf(w.a, h[k], v);
+    h[k] = __builtin_fmaf(da, h[k], v);
   }
   if (a.state_out) store8<F32>(reinterpret_cast<unsigned char*>(a.state_out + at0), h);
   store8<T>(at<T>(a.out, b * a.so + c), h);

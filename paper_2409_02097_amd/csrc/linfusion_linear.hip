@@ -39,26 +39,47 @@ lf::LinRows dev(const RowView& v) { return lf::LinRows{v.batch, v.token}; }
 
 struct Plan { int kind, splits; long long k_split; };   // kind: index into the tile shapes below
 
-constexpr int kShapes = 3;
-constexpr int kTileM[kShapes] = {256, 128, 64}, kTileN[kShapes] = {256, 128, 64}, kPerCu[kShapes] = {1, 2, 4};
+// Tile shapes: rows, columns, waves along each, workgroups that share a CU (LDS).  The first for 16-bit types only.
+#define LF_LINEAR_SHAPES(DO) \
+  DO(0, 256, 256, 2, 4, 1) DO(1, 128, 160, 2, 2, 2) DO(2, 128, 128, 2, 2, 2) DO(3, 128, 64, 2, 2, 3) DO(4, 64, 64, 2, 2, 4)
+constexpr int kShapes = 5;
+struct Shape { int m, n, per_cu; };
+constexpr Shape kShape[kShapes] = {
+#define LF_ROW(I, M, N, WR, WC, PER) {M, N, PER},
+    LF_LINEAR_SHAPES(LF_ROW)
+#undef LF_ROW
+};
 
-// Time in arbitrary units of a product with these tiles.
-Plan plan(long long M, int N, long long K, int dtype) {
-  const int k_step = dtype == LINFUSION_DTYPE_F32 ? 32 : 64;
+// What a product takes, in us: rounds of workgroups, each a start and end (`over`) and its steps of 128 bytes of k (`step`, of a CU full of
+// such tiles), the last round by how full it is; another launch where k is split, and the sums' way out and in.  Fitted to 380
+// measured times of 16-bit products and 108 of fp32 ones (rows 154 to 81120, columns 320 to 8192, k 320 to 81120, all shapes, 1 to 32
+// splits; off by 11 % and 4 % at the root mean square; the shape it chooses takes 1.00 to 1.16 times the best one's time, 1.3 for one product of
+// 13 us).  A rule by the number of tiles alone chose 256 x 256 for 49152 x 1280 -> 320: 74 us where 128 x 160 takes 49.
+struct Cost { double step[kShapes], over[kShapes], fill, join, join_mb, turned; };
+constexpr Cost kCost16{{1.56, 1.09, 0.89, 0.78, 0.63}, {4.2, 3.6, 2.9, 2.3, 1.7}, 0.4, 4.1, 0.69, 1.23};
+constexpr Cost kCost32{{0.0, 4.81, 3.82, 3.11, 2.16}, {0.0, 3.3, 2.2, 0.3, 0.0}, 0.9, 2.3, 1.02, 1.03};
+
+// `turned`: whether an operand has its own index contiguous.
+Plan plan(long long M, int N, long long K, int dtype, bool turned) {
+  const bool wide = dtype == LINFUSION_DTYPE_F32;
+  const Cost& c = wide ? kCost32 : kCost16;
+  const int k_step = lf::kStepBytes / (wide ? 4 : 2);
   const long long steps = (K + k_step - 1) / k_step, cus = lfh::num_cu();
-  const double rate[kShapes] = {1.0, 0.7, 0.35};   // of a CU full of such tiles
-  Plan best{0, 1, steps * k_step};
+  const int only = lfh::env_int("LINFUSION_LINEAR_TILES", 0) - 1, only_splits = lfh::env_int("LINFUSION_LINEAR_SPLITS", 0);
+  Plan best{4, 1, steps * k_step};
   double least = 1e300;
-  for (int s = dtype == LINFUSION_DTYPE_F32 ? 1 : 0; s < kShapes; ++s) {
-    const long long tiles = ((M + kTileM[s] - 1) / kTileM[s]) * ((N + kTileN[s] - 1) / kTileN[s]), room = cus * kPerCu[s];
-    for (long long splits = 1; splits <= 64 && splits <= steps; splits *= 2) {
-      if (splits > 1 && tiles * (splits / 2) >= room) break;
+  for (int s = wide ? 1 : 0; s < kShapes; ++s) {
+    if (only >= 0 && s != only) continue;
+    const long long tiles = ((M + kShape[s].m - 1) / kShape[s].m) * ((N + kShape[s].n - 1) / kShape[s].n), room = cus * kShape[s].per_cu;
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (splits > steps || (splits > 1 && tiles * splits >= 2 * room)) break;   // (what most_partials counts on)
+      if (only_splits && splits != only_splits) continue;
       const long long per = (steps + splits - 1) / splits, used = (steps + per - 1) / per;
-      if (used != splits && splits > 1 && used <= splits / 2) continue;
-      const double rounds = (double)((tiles * used + room - 1) / room);
-      const double step_time = (double)kTileM[s] * kTileN[s] * kPerCu[s] / rate[s] / 65536.0;   // of all of a CU's tiles
-      double t = rounds * (per + 3) * step_time;
-      if (used > 1) t += (double)M * N * (used + 1) * 8 / 65536.0 / 64.0 + 4.0;   // the sums out and in again, and a launch
+      const double each = per * c.step[s] * (turned ? c.turned : 1.0) + c.over[s];
+      const long long all = tiles * used, rest = all % room;
+      double t = (double)(all / room) * each;
+      if (rest) t += each * std::pow((double)((rest + cus - 1) / cus) / kShape[s].per_cu, c.fill);
+      if (used > 1) t += c.join + c.join_mb * 1e-6 * (double)M * N * (used + 1);
       if (t < least) {
         least = t;
         best = Plan{s, (int)used, per * k_step};
@@ -87,17 +108,17 @@ int launch_tiles(const lf::LinArgs& g, hipStream_t st) {
 
 template <typename T, bool AK, bool BK, bool MAPPED>
 int product(lf::LinArgs g, const Plan& p, hipStream_t st) {
-  g.tiles_m = (int)((g.M + kTileM[p.kind] - 1) / kTileM[p.kind]);
-  g.tiles_n = (g.N + kTileN[p.kind] - 1) / kTileN[p.kind];
+  g.tiles_m = (int)((g.M + kShape[p.kind].m - 1) / kShape[p.kind].m);
+  g.tiles_n = (g.N + kShape[p.kind].n - 1) / kShape[p.kind].n;
   g.splits = p.splits;
   g.k_split = p.k_split;
   if (p.splits == 1) g.partials = nullptr;
   int rc = LINFUSION_ERR_UNSUPPORTED;
-  if constexpr (lf::Stored<T>::kBytes == 2) {
-    if (p.kind == 0) rc = launch_tiles<T, 256, 256, 2, 4, AK, BK, MAPPED>(g, st);
-  }
-  if (p.kind == 1) rc = launch_tiles<T, 128, 128, 2, 2, AK, BK, MAPPED>(g, st);
-  if (p.kind == 2) rc = launch_tiles<T, 64, 64, 2, 2, AK, BK, MAPPED>(g, st);
+#define LF_CASE(I, TM, TN, WR, WC, PER)                                                       \
+  if constexpr (lf::Stored<T>::kBytes == 2 || I > 0)                           \
+    if (p.kind == I) rc = launch_tiles<T, TM, TN, WR, WC, AK, BK, MAPPED>(g, st);
+  LF_LINEAR_SHAPES(LF_CASE)
+#undef LF_CASE
   if (rc != LINFUSION_OK) return rc;
   if (p.splits > 1) {
     const long long threads = g.M * (g.N / 8);
@@ -135,14 +156,14 @@ template <typename T, int MT> int launch_few(const lf::LinArgs& g, bool mapped, 
 // Workgroups along the tokens of linear_slope and their tokens.
 struct Slices { int count, each; };
 Slices slices(long long rows, int C) {
-  const long long across = (C + 255) / 256, most = 16LL * lfh::num_cu() / across + 1;
+  const long long across = (C + 255) / 256, most = 4LL * lfh::num_cu() / across + 1;
   long long each = (rows + most - 1) / most;
   each = (each + 7) / 8 * 8;
   if (each < 32) each = 32;
   return Slices{(int)((rows + each - 1) / each), (int)each};
 }
 size_t most_slices(long long rows, int C) {   // never falls with the rows
-  const long long across = (C + 255) / 256, most = 16LL * lfh::num_cu() / across + 1, by_rows = (rows + 31) / 32;
+  const long long across = (C + 255) / 256, most = 4LL * lfh::num_cu() / across + 1, by_rows = (rows + 31) / 32;
   return lfh::up256((size_t)(most < by_rows ? most : by_rows) * C * 4);
 }
 
@@ -197,7 +218,7 @@ int linfusion_linear_fwd(const void* x, const void* w, const void* bias, const v
     if (g.M <= 16) return launch_few<T, 1>(g, mapped, st);
     if (g.M <= 32) return launch_few<T, 2>(g, mapped, st);
     if (g.M <= kFew) return launch_few<T, 4>(g, mapped, st);
-    return product<T, true, true>(g, mapped, plan(g.M, g.N, g.K, dtype), st);
+    return product<T, true, true>(g, mapped, plan(g.M, g.N, g.K, dtype, false), st);
   });
   if (rc != LINFUSION_OK) return rc;
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
@@ -266,7 +287,7 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
       using T = decltype(t);
       if (z_exps) lf::linear_slope<T, true><<<grid, 256, 0, st>>>(a);
       else lf::linear_slope<T, false><<<grid, 256, 0, st>>>(a);
-      if (dbias) lf::linear_bias<T><<<(C_out + 63) / 64, 1024, 0, st>>>(sums, dbias, s.count, C_out);
+      if (dbias) lf::linear_bias<T><<<(C_out + 31) / 32, 1024, 0, st>>>(sums, dbias, s.count, C_out);
       return LINFUSION_OK;
     });
   }
@@ -283,7 +304,7 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     g.A = vd.p, g.va = flat(vd, B, N, mapped), g.B = w, g.vb = lf::LinRows{0, ws[1]};
     g.M = M, g.K = C_out, g.N = C_in;
     g.out = lf::LinOut{dx, nullptr, nullptr, nullptr, flat(vdx, B, N, mapped), {}, {}, lf::kActNone, 0.0f};
-    rc = by_type(dtype, [&](auto t) { return product<decltype(t), true, false>(g, mapped, plan(g.M, g.N, g.K, dtype), st); });
+    rc = by_type(dtype, [&](auto t) { return product<decltype(t), true, false>(g, mapped, plan(g.M, g.N, g.K, dtype, true), st); });
     if (rc != LINFUSION_OK) return rc;
   }
   if (dw) {
@@ -298,7 +319,7 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     g.A = vd.p, g.va = flat(vd, B, N, mapped), g.B = vx.p, g.vb = flat(vx, B, N, mapped);
     g.M = C_out, g.K = M, g.N = C_in;
     g.out = lf::LinOut{dw, nullptr, nullptr, nullptr, lf::LinRows{0, dws[1]}, {}, {}, lf::kActNone, 0.0f};
-    rc = by_type(dtype, [&](auto t) { return product<decltype(t), false, false>(g, mapped, plan(g.M, g.N, g.K, dtype), st); });
+    rc = by_type(dtype, [&](auto t) { return product<decltype(t), false, false>(g, mapped, plan(g.M, g.N, g.K, dtype, true), st); });
     if (rc != LINFUSION_OK) return rc;
   }
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;

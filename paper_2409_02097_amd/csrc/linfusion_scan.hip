@@ -14,8 +14,6 @@ using lfh::span;
 
 constexpr int kMaxChannels = 8192;
 constexpr unsigned kFlags = LINFUSION_FLAG_SCAN_REVERSE | LINFUSION_FLAG_SCAN_LEAKY | LINFUSION_FLAG_SCAN_SUM;
-constexpr int kBackChunk = lf::ScanShape<lf::F32>::kBackChunk;   // the same for all types
-
 int check(int B, long long N, int C, int dtype, unsigned flags) {
   if (B <= 0 || N <= 0 || C <= 0 || B > 65535 || N >= 1LL << 30) return LINFUSION_ERR_INVALID;
   if (dtype != LINFUSION_DTYPE_F32 && dtype != LINFUSION_DTYPE_F16 && dtype != LINFUSION_DTYPE_BF16) return LINFUSION_ERR_UNSUPPORTED;
@@ -60,41 +58,56 @@ bool clash(std::initializer_list<RowView> in, std::initializer_list<RowView> out
 
 lf::ScanView dev(const RowView& v) { return lf::ScanView{v.batch, v.token}; }
 
-long long back_chunks(long long N) { return (N + kBackChunk - 1) / kBackChunk; }
-size_t states(int B, long long N, int C) { return lfh::up256((size_t)B * back_chunks(N) * C * 4); }   // one value per chunk and channel
+long long chunks_of(long long N) { return (N + lf::kScanChunk - 1) / lf::kScanChunk; }
+size_t states(int B, long long N, int C) { return lfh::up256((size_t)B * chunks_of(N) * C * 4); }   // one value per chunk and channel
 
-template <typename T, int MODE, bool INPUT>
-int forward(const lf::ScanArgs& a0, int B, hipStream_t st) {
+constexpr size_t kTicketBytes = 256;
+
+// Chunks of a group.
+int group_of(int B, int C) {
+  (void)B, (void)C;
+  return lfh::env_int("LINFUSION_SCAN_GROUP", 16);
+}
+
+lf::ScanRecords records(void* workspace, int B, long long N, int C) {
+  char* w = (char*)workspace;
+  return lf::ScanRecords{(unsigned*)w, (unsigned long long*)(w + kTicketBytes), (unsigned*)(w + kTicketBytes + 2 * states(B, N, C))};
+}
+
+void clear(const lf::ScanRecords& r, int B, long long chunks, int C, hipStream_t st) {
+  const long long count = (long long)B * chunks * C;
+  lf::scan_clear<<<(unsigned)((count / 2 + 255) / 256), 256, 0, st>>>(r, count);
+}
+
+template <typename T, int MODE, bool INPUT, int TT, bool ONE>
+int forward(const lf::ScanArgs& a0, hipStream_t st) {
   lf::ScanArgs a = a0;
-  constexpr int L = lf::ScanShape<T>::kChunk;
-  const long long chunks = (a.N + L - 1) / L, blocks = (a.C + lf::kScanWidth - 1) / lf::kScanWidth;
-  if (chunks * blocks > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
+  const long long chunks = (a.N + 32 * TT - 1) / (32 * TT), wgs = chunks * ((a.C + lf::kScanWidth - 1) / lf::kScanWidth) * a.B;
+  if (wgs > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   a.chunks = (int)chunks;
-  const dim3 grid((unsigned)(chunks * blocks), 1, B);
-  if (chunks == 1) {
-    lf::scan_fwd<T, MODE, INPUT, lf::kScanWhole><<<grid, 256, 0, st>>>(a);
-    return LINFUSION_OK;
-  }
-  lf::scan_fwd<T, MODE, INPUT, lf::kScanTotals><<<grid, 256, 0, st>>>(a);
-  lf::scan_starts<false><<<dim3((unsigned)blocks, B), 64, 0, st>>>(a.totals, a.state_in, a.starts, a.lengths, a.N, a.C, a.chunks, L);
-  lf::scan_fwd<T, MODE, INPUT, lf::kScanApply><<<grid, 256, 0, st>>>(a);
+  if constexpr (!ONE) clear(a.rec, a.B, chunks, a.C, st);
+  lf::scan_fwd<T, MODE, INPUT, TT, ONE><<<(unsigned)wgs, 256, 0, st>>>(a);
   return LINFUSION_OK;
+}
+// One chunk holds up to 128 tokens, or 256 of 16-bit types with eight a thread.
+template <typename T, int MODE, bool INPUT>
+int forward(const lf::ScanArgs& a, hipStream_t st) {
+  constexpr int kLong = lf::Stored<T>::kBytes == 4 ? lf::kScanT : 2 * lf::kScanT;
+  if (a.N <= lf::kScanChunk) return forward<T, MODE, INPUT, lf::kScanT, true>(a, st);
+  if (kLong > lf::kScanT && a.N <= 32 * kLong) return forward<T, MODE, INPUT, kLong, true>(a, st);
+  return forward<T, MODE, INPUT, lf::kScanT, false>(a, st);
 }
 
 template <typename T, int MODE, bool INPUT>
-int backward(const lf::ScanBackArgs& a0, int B, hipStream_t st) {
-  lf::ScanBackArgs a = a0;
-  constexpr int L = lf::ScanShape<T>::kBackChunk;
-  const long long blocks = (a.C + lf::kScanWidth - 1) / lf::kScanWidth;
-  if (a.chunks * blocks > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
-  const dim3 grid((unsigned)(a.chunks * blocks), 1, B);
-  if (a.chunks > 1) {
-    lf::scan_back_totals<T><<<grid, 256, 0, st>>>(a);
-    lf::scan_starts<true><<<dim3((unsigned)blocks, B), 64, 0, st>>>(a.totals, a.dstate_out, a.ends, a.lengths, a.N, a.C, a.chunks, L);
-  } else {
-    a.ends = nullptr;
+int backward(const lf::ScanBackArgs& a, hipStream_t st) {
+  const long long wgs = a.chunks * (long long)((a.C + lf::kScanWidth - 1) / lf::kScanWidth) * a.B;
+  if (wgs > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
+  if (a.chunks == 1) {
+    lf::scan_bwd<T, MODE, INPUT, true><<<(unsigned)wgs, 256, 0, st>>>(a);
+    return LINFUSION_OK;
   }
-  lf::scan_bwd<T, MODE, INPUT><<<grid, 256, 0, st>>>(a);
+  clear(a.rec, a.B, a.chunks, a.C, st);
+  lf::scan_bwd<T, MODE, INPUT, false><<<(unsigned)wgs, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
 
@@ -115,9 +128,9 @@ template <typename F> int with(int dtype, int mode, bool input, F f) {
   return dtype == LINFUSION_DTYPE_F16 ? by_mode(lf::F16{}) : dtype == LINFUSION_DTYPE_BF16 ? by_mode(lf::BF16{}) : by_mode(lf::F32{});
 }
 
-int launch_forward(const lf::ScanArgs& a, int B, int dtype, int mode, hipStream_t st) {
+int launch_forward(const lf::ScanArgs& a, int dtype, int mode, hipStream_t st) {
   return with(dtype, mode, a.input != nullptr, [&](auto t, auto m, auto i) {
-    return forward<decltype(t), decltype(m)::value, decltype(i)::value>(a, B, st);
+    return forward<decltype(t), decltype(m)::value, decltype(i)::value>(a, st);
   });
 }
 
@@ -127,7 +140,7 @@ extern "C" {
 
 size_t linfusion_scan_workspace_bytes(int B, long long N, int C) {
   if (check(B, N, C, LINFUSION_DTYPE_F32, 0) != LINFUSION_OK) return 0;
-  return N <= kBackChunk ? 0 : 3 * states(B, N, C);
+  return N <= lf::kScanChunk ? 0 : kTicketBytes + 3 * states(B, N, C);
 }
 
 size_t linfusion_scan_saved_bytes(int B, long long N, int C) {
@@ -137,7 +150,7 @@ size_t linfusion_scan_saved_bytes(int B, long long N, int C) {
 
 size_t linfusion_scan_bwd_workspace_bytes(int B, long long N, int C) {
   if (check(B, N, C, LINFUSION_DTYPE_F32, 0) != LINFUSION_OK) return 0;
-  return 5 * states(B, N, C) + linfusion_scan_workspace_bytes(B, N, C);
+  return kTicketBytes + 5 * states(B, N, C);
 }
 
 int linfusion_scan_fwd(const void* x, const void* gate, const void* input, const float* rate, const float* state_in, void* out,
@@ -160,13 +173,9 @@ int linfusion_scan_fwd(const void* x, const void* gate, const void* input, const
   if (clash({vx, vg, vi}, {vo}, {Range{rate, (size_t)C * 4}, Range{lengths, (size_t)B * 4}}, {s_out, ws, kept})) return LINFUSION_ERR_OVERLAP;
   if (meet(span(vo), s_in) || meet(ws, s_in) || meet(kept, s_in) || (state_in != state_out && meet(s_in, s_out))) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
-  lf::ScanArgs a{x, gate, input, out, dev(vx), dev(vg), dev(vi), dev(vo), rate, state_in, state_out, nullptr, nullptr, (float*)saved,
-                 lengths, N, C, 0, (int)back_chunks(N), (flags & LINFUSION_FLAG_SCAN_REVERSE) != 0};
-  if (need) {
-    a.totals = (float*)workspace;
-    a.starts = (float*)((char*)workspace + 2 * states(B, N, C));
-  }
-  if ((rc = launch_forward(a, B, dtype, mode_of(flags), (hipStream_t)stream)) != LINFUSION_OK) return rc;
+  const lf::ScanArgs a{x, gate, input, out, dev(vx), dev(vg), dev(vi), dev(vo), rate, state_in, state_out, (float*)saved,
+                       records(workspace, B, N, C), lengths, N, B, C, 0, (int)chunks_of(N), group_of(B, C), (flags & LINFUSION_FLAG_SCAN_REVERSE) != 0};
+  if ((rc = launch_forward(a, dtype, mode_of(flags), (hipStream_t)stream)) != LINFUSION_OK) return rc;
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }
 
@@ -196,23 +205,23 @@ int linfusion_scan_bwd(const void* x, const void* gate, const void* input, const
   if (meet(ws, ds_out) || meet(Range{drate, (size_t)C * 4}, ds_out) || (dstate_in != dstate_out && meet(ds_in, ds_out))) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   const hipStream_t st = (hipStream_t)stream;
-  char* w = (char*)workspace;
+  char* const w = (char*)workspace + kTicketBytes + 3 * one;   // behind the records
+  const lf::ScanRecords rec = records(workspace, B, N, C);
   const bool reverse = (flags & LINFUSION_FLAG_SCAN_REVERSE) != 0;
   const float* starts = (const float*)saved;
   if (!saved) {   // the states between the chunks again
-    lf::ScanArgs f{x, gate, input, nullptr, dev(v[0]), dev(v[1]), dev(v[2]), lf::ScanView{0, 0}, rate, state_in, nullptr, (float*)(w + 5 * one),
-                   (float*)(w + 7 * one), (float*)(w + 4 * one), lengths, N, C, 0, (int)back_chunks(N), reverse};
-    if ((rc = launch_forward(f, B, dtype, mode_of(flags), st)) != LINFUSION_OK) return rc;
+    const lf::ScanArgs f{x, gate, input, nullptr, dev(v[0]), dev(v[1]), dev(v[2]), lf::ScanView{0, 0}, rate, state_in, nullptr, (float*)(w + one),
+                         rec, lengths, N, B, C, 0, (int)chunks_of(N), group_of(B, C), reverse};
+    if ((rc = launch_forward(f, dtype, mode_of(flags), st)) != LINFUSION_OK) return rc;
     starts = f.saved;
   }
-  lf::ScanBackArgs a{x, gate, input, dout, dx, dgate, dinput, dev(v[0]), dev(v[1]), dev(v[2]), dev(v[3]), dev(v[4]), dev(v[5]), dev(v[6]),
-                     rate, starts, dstate_out, dstate_in, (float*)w, (float*)(w + 2 * one), (float*)(w + 3 * one), lengths, N, C,
-                     (int)back_chunks(N), reverse};
+  const lf::ScanBackArgs a{x, gate, input, dout, dx, dgate, dinput, dev(v[0]), dev(v[1]), dev(v[2]), dev(v[3]), dev(v[4]), dev(v[5]), dev(v[6]),
+                           rate, starts, dstate_out, dstate_in, (float*)w, rec, lengths, N, B, C, (int)chunks_of(N), group_of(B, C), reverse};
   rc = with(dtype, mode_of(flags), input != nullptr, [&](auto t, auto m, auto i) {
-    return backward<decltype(t), decltype(m)::value, decltype(i)::value>(a, B, st);
+    return backward<decltype(t), decltype(m)::value, decltype(i)::value>(a, st);
   });
   if (rc != LINFUSION_OK) return rc;
-  lf::scan_rate_sums<<<(C + 63) / 64, 1024, 0, st>>>(a.partials, drate, (long long)B * a.chunks, C);
+  lf::scan_rate_sums<<<(C + 31) / 32, 1024, 0, st>>>(a.partials, drate, (long long)B * a.chunks, C);
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }
 

@@ -60,14 +60,11 @@ struct ScanBackArgs {
   bool reverse;
 };
 
-// v < limit ? a : b by the sign of v - limit, for v that is no NaN or where a and b both are then.  Left to itself the compiler makes
-// branches of such choices, one per element (65536 x 1280 in bf16: 142 us for what takes 60 without); it also knows this mask from a
-// compare, hence the instruction.
+// v < limit ? a : b, both formed in any case: left to itself the compiler makes branches of such choices, one per element (65536 x 1280 in
+// bf16: 142 us for what takes 60 without).
 LF_DEV float below(float v, float limit, float a, float b) {
-  const float d = v - limit;
-  uint32_t mask;
-  asm("v_ashrrev_i32 %0, 31, %1" : "=v"(mask) : "v"(d));
-  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, a) & mask) | (__builtin_bit_cast(uint32_t, b) & ~mask));
+  asm volatile("" : "+v"(a));
+  return v < limit ? a : b;
 }
 // c ? 0 : x, x formed in any case
 LF_DEV float unless(bool c, float x) {
@@ -98,15 +95,11 @@ template <bool Precise, bool TWICE> LF_DEV float one_less(float d, float e) {
   return below(d, kLimit, d * p, 1.0f - e);
 }
 
-// The weight m of the new value for a = 2^-d, and r so that dm/dg = -a r (kScanNorm: r = a / m, 0 where m is 0).
-struct ScanWeight { float m, r; };
-template <bool Precise, int MODE, bool SLOPE> LF_DEV ScanWeight weight_of(float d, float a) {   // (without SLOPE: m alone)
-  if constexpr (MODE == kScanSum) return ScanWeight{1.0f, 0.0f};
-  if constexpr (MODE == kScanLeaky) return ScanWeight{one_less<Precise, false>(d, a), 1.0f};
-  const float m2 = one_less<Precise, true>(d, a * a);
-  if constexpr (!SLOPE) return ScanWeight{__builtin_amdgcn_sqrtf(m2), 0.0f};
-  const float q = below(m2, 1.17549435e-38f, 0.0f, __builtin_amdgcn_rsqf(m2));
-  return ScanWeight{m2 * q, a * q};
+// The weight m of the new value for a = 2^-d.
+template <bool Precise, int MODE> LF_DEV float weight_of(float d, float a) {
+  if constexpr (MODE == kScanSum) return 1.0f;
+  if constexpr (MODE == kScanLeaky) return one_less<Precise, false>(d, a);
+  return __builtin_amdgcn_sqrtf(one_less<Precise, true>(d, a * a));
 }
 
 // What absent gates read as: minus infinity, whose sigmoid is 0, so that a = 1 and the state stays as it is.
@@ -122,8 +115,7 @@ template <typename T> LF_DEV Raw8<T> shut8() {
   return r;
 }
 
-// Makes the compiler take a value for a new one, so that what was formed from it is formed again and not kept in registers meanwhile.
-LF_DEV void forget(float& x) { asm("" : "+v"(x)); }
+// Makes the compiler take a row for a new one, so that what was formed from it is formed again and not kept in registers meanwhile.
 template <typename T> LF_DEV void forget(Raw8<T>& r) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -152,22 +144,33 @@ LF_DEV void load_rate(const float* p, bool on, float (&rate)[8]) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) rate[k] = 0.0f;
   if (on) load8_f32(p, rate);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) rate[k] *= 1.44269504088896340736f;
 }
 
-// The rows of a thread's tokens, the first at `p`, the next ones `step` bytes on; `absent` where there are none.
-template <typename T, int TT> LF_DEV void load_rows(const unsigned char* p, long long step, int live, bool full, const Raw8<T>& absent, Raw8<T> (&r)[TT]) {
+// The rows of a thread's tokens of up to four tensors, token after token, so that work on the first can begin while the others are on
+// their way; `absent` where there are none.
+template <typename T> struct ScanLoad {
+  const unsigned char* p;   // the first token's
+  long long step;           // bytes to the next one's
+  Raw8<T> absent;
+};
+template <typename T> LF_DEV void load_token(bool there, int j, ScanLoad<T>& l, Raw8<T>* r) {
+  r[j] = l.absent;
+  if (there) r[j] = load8_raw<T>(l.p);
+  l.p += l.step;
+}
+template <typename T, int TT, typename... More> LF_DEV void load_rows(int live, bool full, More&&... more) {
+  auto all = [&](bool there, int j) { (load_token<T>(there, j, more.first, more.second), ...); };
   if (full) {   // (a whole workgroup's)
 #pragma unroll
-    for (int j = 0; j < TT; ++j, p += step) r[j] = load8_raw<T>(p);
+    for (int j = 0; j < TT; ++j) all(true, j);
   } else {
 #pragma unroll
-    for (int j = 0; j < TT; ++j, p += step) {
-      r[j] = absent;
-      if (j < live) r[j] = load8_raw<T>(p);
-    }
+    for (int j = 0; j < TT; ++j) all(j < live, j);
   }
+}
+template <typename T> struct ScanPair { ScanLoad<T> first; Raw8<T>* second; };
+template <typename T> LF_DEV ScanPair<T> rows_of(const void* base, const ScanView& v, const ScanRow& row, int b, long long n, int c, const Raw8<T>& absent, Raw8<T>* r) {
+  return ScanPair<T>{ScanLoad<T>{at<T>(base, b * v.batch + n * v.token + c), row.step<T>(v), absent}, r};
 }
 
 // The stretches of a chunk joined: from each thread's (A, R) of 8 channels the value its first token starts from, given the
@@ -246,6 +249,8 @@ LF_DEV void spread8(float* lds, float v, float (&x)[8]) {
   }
 }
 
+struct ScanPlace { int chunk, b, c0; };
+
 // ---- between chunks ----------------------------------------------------------------------------------------------------
 
 constexpr unsigned kNotYet = 0xffffffffu;
@@ -321,38 +326,39 @@ __global__ __launch_bounds__(256) void scan_clear(ScanRecords r, long long count
   *reinterpret_cast<u32x2*>(r.values + i) = u32x2{kNotYet, kNotYet};
 }
 
-// Which chunk, batch row and channels a workgroup takes.
-struct ScanPlace {
-  int chunk, b, c0;
-  template <bool ONE, bool BACK> LF_DEV void take(const ScanRecords& r, int B, int C, int chunks, int& lds) {
-    unsigned id = blockIdx.x;
-    if constexpr (!ONE) {
-      if (threadIdx.x == 0) lds = (int)__hip_atomic_fetch_add(r.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __syncthreads();
-      id = (unsigned)__builtin_amdgcn_readfirstlane(lds);
-    }
-    const unsigned blocks = (unsigned)(C + kScanWidth - 1) / kScanWidth, per = blocks * (unsigned)B;
-    const unsigned at = id / per, rest = id - at * per;
-    b = (int)(rest / blocks);
-    c0 = (int)(rest - (unsigned)b * blocks) * kScanWidth;
-    chunk = BACK ? chunks - 1 - (int)at : (int)at;
+// A workgroup's tile: a chunk of a batch row and 64 channels, by ticket (ONE: by its index): a chunk of all rows and channels, then the
+// next one.  Waiting for the ticket costs 17 of 160 us (65536 x 1280 bf16); workgroups that stay and draw their next ticket early hold it while
+// others wait for its tile (218 us, 176 when drawn as late as the results' way out), and several tiles a ticket leave fewer chunks under way
+// (two 190, four 214).
+template <bool ONE, bool BACK> LF_DEV ScanPlace take_tile(const ScanRecords& r, int B, int C, int chunks, unsigned& lds) {
+  unsigned id = blockIdx.x;
+  if constexpr (!ONE) {
+    if (threadIdx.x == 0) lds = __hip_atomic_fetch_add(r.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    id = (unsigned)__builtin_amdgcn_readfirstlane((int)lds);
   }
-};
+  const unsigned blocks = (unsigned)(C + kScanWidth - 1) / kScanWidth, per = blocks * (unsigned)B;
+  const unsigned at = id / per, rest = id - at * per, b = rest / blocks;
+  return ScanPlace{BACK ? chunks - 1 - (int)at : (int)at, (int)b, (int)(rest - b * blocks) * kScanWidth};
+}
 
 // ---- forward -----------------------------------------------------------------------------------------------------------
 
 // TT tokens a thread; ONE: the whole sequence is one chunk.
 // Bound: HBM and vector instructions, nearly level (46 issue slots a value with the norm's weight, six of them transcendental).
+struct ScanForwardLds {
+  ScanJoin join;
+  ScanFound found;
+  float spread[4][kScanWidth];
+  unsigned id;
+};
 template <typename T, int MODE, bool INPUT, int TT, bool ONE>
 __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   constexpr int L = 32 * TT;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
-  __shared__ ScanJoin lds;
-  __shared__ ScanFound found;
-  __shared__ float spread[4][kScanWidth];
-  __shared__ int id;
-  ScanPlace p;
-  p.take<ONE, false>(a.rec, a.B, a.C, a.chunks, id);
+  __shared__ ScanForwardLds shared;
+  ScanJoin& lds = shared.join;
+  const ScanPlace p = take_tile<ONE, false>(a.rec, a.B, a.C, a.chunks, shared.id);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
   const bool on = c < a.C;
   const ScanRow row(a.lengths, p.b, a.N, a.reverse);
@@ -361,14 +367,14 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   const int live = on ? (row.n - t0 < TT ? (int)(row.n - t0) : TT) : 0;   // this thread's tokens that count (below 0: none)
   Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1];
   const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
+  float rate[8];   // (requested first: loads are waited for in their order)
+  load_rate(a.rate + c, on, rate);
   {
     const long long n = row.token(t0);
-    load_rows(at<T>(a.gate, p.b * a.vg.batch + n * a.vg.token + c), row.step<T>(a.vg), live, full, shut8<T>(), rg);
-    load_rows(at<T>(a.x, p.b * a.vx.batch + n * a.vx.token + c), row.step<T>(a.vx), live, full, none8<T>(), rx);
-    if constexpr (INPUT) load_rows(at<T>(a.input, p.b * a.vi.batch + n * a.vi.token + c), row.step<T>(a.vi), live, full, none8<T>(), ri);
+    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, p.b, n, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, p.b, n, c, none8<T>(), rx);
+    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, p.b, n, c, none8<T>(), ri));
+    else load_rows<T, TT>(live, full, g, x);
   }
-  float rate[8];   // of powers of two
-  load_rate(a.rate + c, on, rate);
   float da[TT][8], u[TT][8], A[8], R[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
@@ -378,9 +384,9 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
     if constexpr (INPUT) widen8<T>(ri[j], in);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float d = rate[k] * sigmoid_of<kPrecise>(g[k]);
+      const float d = rate[k] * 1.44269504088896340736f * sigmoid_of<kPrecise>(g[k]);
       da[j][k] = __builtin_amdgcn_exp2f(-d);
-      u[j][k] = weight_of<kPrecise, MODE, false>(d, da[j][k]).m * x[k];
+      u[j][k] = weight_of<kPrecise, MODE>(d, da[j][k]) * x[k];
       if constexpr (INPUT) u[j][k] *= sigmoid_of<kPrecise>(in[k]);
       R[k] = j ? __builtin_fmaf(da[j][k], R[k], u[j][k]) : u[j][k];
       A[k] = j ? A[k] * da[j][k] : da[j][k];
@@ -396,7 +402,7 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   if constexpr (!ONE) {
     join_chunk<false>(lds, 4, ca, cr);
     if (whole) tell_totals(a.rec, i0, ca, cr);
-    h0 = look_back(a.rec, found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
+    h0 = look_back(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
   }
   if (whole) {
     join_chunk<false>(lds, 4, ca, cr);
@@ -412,7 +418,7 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   }
   if (!a.out) return;
   float h[8];
-  spread8(spread[wave], mine, h);
+  spread8(shared.spread[wave], mine, h);
   unsigned char* po = at<T>(a.out, p.b * a.vo.batch + row.token(t0) * a.vo.token + c);
   const long long so = row.step<T>(a.vo);
 #pragma unroll
@@ -430,16 +436,20 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
 
 // The gradients of a chunk, from the state in front of it and E behind it, which comes from the chunks behind as the state does from
 // those before.
+struct ScanBackLds {
+  ScanJoin there, back;
+  ScanFound found;
+  float spread[2][4][kScanWidth];
+  f32x4 weights[kScanT][2][256];
+  unsigned id;
+};
 template <typename T, int MODE, bool INPUT, bool ONE>
 __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   constexpr int TT = kScanT, L = kScanChunk;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
-  __shared__ ScanJoin there, back;
-  __shared__ ScanFound found;
-  __shared__ float spread[2][4][kScanWidth];
-  __shared__ int id;
-  ScanPlace p;
-  p.take<ONE, true>(a.rec, a.B, a.C, a.chunks, id);
+  __shared__ ScanBackLds shared;
+  ScanJoin &there = shared.there, &back = shared.back;
+  const ScanPlace p = take_tile<ONE, true>(a.rec, a.B, a.C, a.chunks, shared.id);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
   const bool on = c < a.C;
   const ScanRow row(a.lengths, p.b, a.N, a.reverse);
@@ -454,30 +464,36 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   const long long n0 = row.token(t0);
   Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1], rd[TT];
   const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
-  load_rows(at<T>(a.gate, p.b * a.vg.batch + n0 * a.vg.token + c), row.step<T>(a.vg), live, full, shut8<T>(), rg);
-  load_rows(at<T>(a.dout, p.b * a.vd.batch + n0 * a.vd.token + c), row.step<T>(a.vd), live, full, none8<T>(), rd);
-  load_rows(at<T>(a.x, p.b * a.vx.batch + n0 * a.vx.token + c), row.step<T>(a.vx), live, full, none8<T>(), rx);
-  if constexpr (INPUT) load_rows(at<T>(a.input, p.b * a.vi.batch + n0 * a.vi.token + c), row.step<T>(a.vi), live, full, none8<T>(), ri);
   float rate[8], h0 = 0.0f, e0 = 0.0f;
   load_rate(a.rate + c, on, rate);
   if (cl < a.C) h0 = a.starts[at0];
+  {
+    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, p.b, n0, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, p.b, n0, c, none8<T>(), rx);
+    ScanPair<T> d = rows_of<T>(a.dout, a.vd, row, p.b, n0, c, none8<T>(), rd);
+    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, p.b, n0, c, none8<T>(), ri), d);
+    else load_rows<T, TT>(live, full, g, x, d);
+  }
+  // (m i waits in LDS: with it and what follows from it in registers 75 of them spill)
   float da[TT][8], u[TT][8], sg[TT][8], A[8], R[8], BA[8], BR[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
-    float x[8], g[8], in[8];
+    float x[8], g[8], in[8], mi[8];
     widen8<T>(rx[j], x);
     widen8<T>(rg[j], g);
     if constexpr (INPUT) widen8<T>(ri[j], in);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      sg[j][k] = sigmoid_of<kPrecise>(g[k]);
-      const float dk = rate[k] * sg[j][k];
-      da[j][k] = __builtin_amdgcn_exp2f(-dk);
-      u[j][k] = weight_of<kPrecise, MODE, false>(dk, da[j][k]).m * x[k];
-      if constexpr (INPUT) u[j][k] *= sigmoid_of<kPrecise>(in[k]);
-      R[k] = j ? __builtin_fmaf(da[j][k], R[k], u[j][k]) : u[j][k];
-      A[k] = j ? A[k] * da[j][k] : da[j][k];
+      const float s = sigmoid_of<kPrecise>(g[k]), d = rate[k] * 1.44269504088896340736f * s, ak = __builtin_amdgcn_exp2f(-d);
+      sg[j][k] = s;
+      da[j][k] = ak;
+      mi[k] = weight_of<kPrecise, MODE>(d, ak);
+      if constexpr (INPUT) mi[k] *= sigmoid_of<kPrecise>(in[k]);
+      u[j][k] = mi[k] * x[k];
+      R[k] = j ? __builtin_fmaf(ak, R[k], u[j][k]) : u[j][k];
+      A[k] = j ? A[k] * ak : ak;
     }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) shared.weights[j][q][threadIdx.x] = f32x4{mi[4 * q], mi[4 * q + 1], mi[4 * q + 2], mi[4 * q + 3]};
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) { BA[k] = A[k]; BR[k] = 0.0f; }
@@ -490,17 +506,6 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   }
   join_wave<false>(there, A, R);
   join_wave<true>(back, BA, BR);
-#pragma unroll
-  for (int j = 0; j < TT; ++j) {
-    forget(rx[j]);
-    forget(rd[j]);
-    if constexpr (INPUT) forget(ri[j]);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      forget(sg[j][k]);
-      forget(da[j][k]);
-    }
-  }
   __syncthreads();
   float ca, cr;
   const bool whole = wave == 0 && cl < a.C;
@@ -508,7 +513,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   if constexpr (!ONE) {
     join_chunk<true>(back, 4, ca, cr);
     if (whole) tell_totals(a.rec, at0, ca, cr);
-    e0 = look_back(a.rec, found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
+    e0 = look_back(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
   }
   if (whole) {
     join_chunk<true>(back, 4, ca, cr);
@@ -518,9 +523,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   }
   float h[8], E[8];
   join_chunk<false>(there, wave, ca, cr);
-  spread8(spread[0][wave], __builtin_fmaf(ca, h0, cr), h);
+  spread8(shared.spread[0][wave], __builtin_fmaf(ca, h0, cr), h);
   join_chunk<true>(back, 3 - wave, ca, cr);
-  spread8(spread[1][wave], __builtin_fmaf(ca, e0, cr), E);
+  spread8(shared.spread[1][wave], __builtin_fmaf(ca, e0, cr), E);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     h[k] = __builtin_fmaf(A[k], h[k], R[k]);
@@ -544,24 +549,29 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
 #pragma unroll
   for (int j = TT - 1; j >= 0; --j) {
     float x[8], in[8], d[8], dx[8], dg[8], di[8];
+    forget(rx[j]);
     widen8<T>(rx[j], x);
-    if constexpr (INPUT) widen8<T>(ri[j], in);
+    if constexpr (INPUT) {
+      forget(ri[j]);
+      widen8<T>(ri[j], in);
+    }
     widen8<T>(rd[j], d);
+    const f32x4 w0 = shared.weights[j][0][threadIdx.x], w1 = shared.weights[j][1][threadIdx.x];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {   // (a token that does not count: D = E, s = m = 0, a = 1)
-      const float D = d[k] + E[k], s = sg[j][k], ak = da[j][k];
-      const ScanWeight w = weight_of<kPrecise, MODE, true>(rate[k] * s, ak);
+      const float D = d[k] + E[k], s = sg[j][k], mi = k < 4 ? w0[k & 3] : w1[k & 3];
       float i = 1.0f;
       if constexpr (INPUT) i = sigmoid_of<kPrecise>(in[k]);
-      const float Di = D * i, Dmi = w.m * Di;
-      dx[k] = Dmi;
-      if constexpr (INPUT) di[k] = Dmi * x[k] * (1.0f - i);
-      // -dg = a (r D i x - D h')
-      const float less = ak * __builtin_fmaf(w.r * Di, x[k], -D * u[j][k]);
-      const float part = less * s;
+      dx[k] = D * mi;
+      if constexpr (INPUT) di[k] = dx[k] * x[k] * (1.0f - i);
+      E[k] = da[j][k] * D;
+      // -dg = a D (r i x - h') with dm/dg = -a r: r = a / m, 1, 0
+      float rix = 0.0f;
+      if constexpr (MODE == kScanLeaky) rix = i * x[k];
+      if constexpr (MODE == kScanNorm) rix = below(mi, 1.17549435e-38f, 0.0f, da[j][k] * (i * __builtin_amdgcn_rcpf(mi))) * (i * x[k]);
+      const float part = E[k] * (rix - u[j][k]) * s;
       by_rate[k] += part;
-      dg[k] = part * (rate[k] * 0.69314718055994530942f) * (1.0f - s);
-      E[k] = ak * D;
+      dg[k] = part * rate[k] * (1.0f - s);
     }
     if (j < live) {
       store8_stream<T>(pdx, dx);
@@ -624,7 +634,7 @@ __global__ __launch_bounds__(64) void scan_step(ScanStepArgs a) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const float d = rate[k] * 1.44269504088896340736f * sigmoid_of<kPrecise>(g[k]), da = __builtin_amdgcn_exp2f(-d);
-    float v = weight_of<kPrecise, MODE, false>(d, da).m * x[k];
+    float v = weight_of<kPrecise, MODE>(d, da) * x[k];
     if constexpr (INPUT) v *= sigmoid_of<kPrecise>(in[k]);
     h[k] = __builtin_fmaf(da, h[k], v);
   }

@@ -79,14 +79,17 @@ void clear(const lf::ScanRecords& r, int B, long long chunks, int C, hipStream_t
   lf::scan_clear<<<(unsigned)((count / 2 + 255) / 256), 256, 0, st>>>(r, count);
 }
 
+long long tiles_of(long long chunks, int B, int C) { return chunks * ((C + lf::kScanWidth - 1) / lf::kScanWidth) * B; }
+
 template <typename T, int MODE, bool INPUT, int TT, bool ONE>
 int forward(const lf::ScanArgs& a0, hipStream_t st) {
   lf::ScanArgs a = a0;
-  const long long chunks = (a.N + 32 * TT - 1) / (32 * TT), wgs = chunks * ((a.C + lf::kScanWidth - 1) / lf::kScanWidth) * a.B;
-  if (wgs > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
+  const long long chunks = (a.N + 32 * TT - 1) / (32 * TT);
+  const long long tiles = tiles_of(chunks, a.B, a.C);
+  if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   a.chunks = (int)chunks;
   if constexpr (!ONE) clear(a.rec, a.B, chunks, a.C, st);
-  lf::scan_fwd<T, MODE, INPUT, TT, ONE><<<(unsigned)wgs, 256, 0, st>>>(a);
+  lf::scan_fwd<T, MODE, INPUT, TT, ONE><<<(unsigned)tiles, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
 // One chunk holds up to 128 tokens, or 256 of 16-bit types with eight a thread.
@@ -100,14 +103,14 @@ int forward(const lf::ScanArgs& a, hipStream_t st) {
 
 template <typename T, int MODE, bool INPUT>
 int backward(const lf::ScanBackArgs& a, hipStream_t st) {
-  const long long wgs = a.chunks * (long long)((a.C + lf::kScanWidth - 1) / lf::kScanWidth) * a.B;
-  if (wgs > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
+  const long long tiles = tiles_of(a.chunks, a.B, a.C);
+  if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   if (a.chunks == 1) {
-    lf::scan_bwd<T, MODE, INPUT, true><<<(unsigned)wgs, 256, 0, st>>>(a);
+    lf::scan_bwd<T, MODE, INPUT, true><<<(unsigned)tiles, 256, 0, st>>>(a);
     return LINFUSION_OK;
   }
   clear(a.rec, a.B, a.chunks, a.C, st);
-  lf::scan_bwd<T, MODE, INPUT, false><<<(unsigned)wgs, 256, 0, st>>>(a);
+  lf::scan_bwd<T, MODE, INPUT, false><<<(unsigned)tiles, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
 

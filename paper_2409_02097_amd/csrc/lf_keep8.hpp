@@ -36,10 +36,12 @@ template <> struct Largest<BF16> { static constexpr float value = 3.38953139e38f
 template <typename T> LF_DEV void keep_values(u32x2 codes, int e, float (&x)[8]) {
   const float scale = e == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, (uint32_t)e << 23);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float v = (float)(int8_t)(codes[j >> 2] >> (8 * (j & 3))) * scale;
-    constexpr float most = Largest<T>::value;
-    x[j] = v > most ? most : (v < -most ? -most : v);   // (a NaN stays one)
+  for (int j = 0; j < 8; ++j) x[j] = (float)(int8_t)(codes[j >> 2] >> (8 * (j & 3))) * scale;
+  constexpr float most = Largest<T>::value;
+  constexpr int kTop = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 5;   // the exponent byte of 2^e where 64 * 2^e is above `most`
+  if (e >= kTop) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x[j] > most ? most : (x[j] < -most ? -most : x[j]);   // (a NaN stays one)
   }
 }
 
@@ -51,31 +53,43 @@ LF_DEV uint32_t quad_max(uint32_t v) {
   return v > w ? v : w;
 }
 
-// 32 lanes of 8 channels and 8 tokens at a time; four lanes share a block.
+// 32 lanes of 8 channels and 8 tokens at a time, four of them under way; four lanes share a block.
+constexpr int kKeepAhead = 4;
+
 template <typename T> __global__ __launch_bounds__(256) void keep8(KeepArgs a) {
   const int b = blockIdx.z, c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
   const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
   const long long stop = first + a.rows < end ? first + a.rows : end;
   const bool on = c < a.C;
-  for (long long n = first + (threadIdx.x >> 5); n < stop; n += 8) {   // (four neighbouring lanes together)
-    float x[8];
-    widen8<T>(on ? load8_raw<T>(at<T>(a.x, b * a.xb + n * a.xt + c)) : none8<T>(), x);
-    uint32_t most = 0;
+  for (long long n0 = first + (threadIdx.x >> 5); n0 < stop; n0 += 8 * kKeepAhead) {   // (four neighbouring lanes together)
+    Raw8<T> raw[kKeepAhead];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu;
-      most = most > m ? most : m;
+    for (int q = 0; q < kKeepAhead; ++q) {
+      raw[q] = none8<T>();
+      if (on && n0 + 8 * q < stop) raw[q] = load8_raw<T>(at<T>(a.x, b * a.xb + (n0 + 8 * q) * a.xt + c));
     }
-    const int e = keep_exponent(quad_max(most));
-    if (!on) continue;
-    u32x2 codes = {0, 0};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int q = e == 255 ? 0 : (int)__builtin_rintf(__builtin_amdgcn_ldexpf(x[j], 127 - e));
-      codes[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+    for (int q = 0; q < kKeepAhead; ++q) {
+      const long long n = n0 + 8 * q;
+      float x[8];
+      widen8<T>(raw[q], x);
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t m = __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu;
+        most = most > m ? most : m;
+      }
+      const int e = keep_exponent(quad_max(most));
+      if (!on || n >= stop) continue;
+      u32x2 codes = {0, 0};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int v = e == 255 ? 0 : (int)__builtin_rintf(__builtin_amdgcn_ldexpf(x[j], 127 - e));
+        codes[j >> 2] |= (uint32_t)(v & 255) << (8 * (j & 3));
+      }
+      *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.codes) + b * a.cb + n * a.ct + c) = codes;
+      if ((threadIdx.x & 3) == 0) a.exps[b * a.eb + n * a.et + c / kKeepBlock] = (unsigned char)e;
     }
-    *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.codes) + b * a.cb + n * a.ct + c) = codes;
-    if ((threadIdx.x & 3) == 0) a.exps[b * a.eb + n * a.et + c / kKeepBlock] = (unsigned char)e;
   }
 }
 
@@ -84,11 +98,24 @@ template <typename T> __global__ __launch_bounds__(256) void unkeep8(KeepArgs a)
   const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
   const long long stop = first + a.rows < end ? first + a.rows : end;
   if (c >= a.C) return;
-  for (long long n = first + (threadIdx.x >> 5); n < stop; n += 8) {
-    const u32x2 codes = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.x) + b * a.xb + n * a.xt + c);
-    float x[8];
-    keep_values<T>(codes, a.exps[b * a.eb + n * a.et + c / kKeepBlock], x);
-    store8_stream<T>(at<T>(a.codes, b * a.cb + n * a.ct + c), x);
+  for (long long n0 = first + (threadIdx.x >> 5); n0 < stop; n0 += 8 * kKeepAhead) {
+    u32x2 codes[kKeepAhead];
+    int e[kKeepAhead];
+#pragma unroll
+    for (int q = 0; q < kKeepAhead; ++q) {
+      const long long n = n0 + 8 * q;
+      if (n >= stop) continue;
+      codes[q] = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.x) + b * a.xb + n * a.xt + c);
+      e[q] = a.exps[b * a.eb + n * a.et + c / kKeepBlock];
+    }
+#pragma unroll
+    for (int q = 0; q < kKeepAhead; ++q) {
+      const long long n = n0 + 8 * q;
+      if (n >= stop) continue;
+      float x[8];
+      keep_values<T>(codes[q], e[q], x);
+      store8_stream<T>(at<T>(a.codes, b * a.cb + n * a.ct + c), x);
+    }
   }
 }
 

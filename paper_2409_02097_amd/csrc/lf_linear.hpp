@@ -79,7 +79,6 @@ template <bool Precise> LF_DEV float act_of(float z, int act, float slope) {
 }
 
 template <bool Precise> LF_DEV float act_slope(float z, int act, float slope) {
-  if (act != kActLeaky) z = z > 30.0f ? 30.0f : (z < -30.0f ? -30.0f : z);   // 1 or 0 from there on, and no infinity times 0
   switch (act) {
     case kActLeaky: return z > 0.0f ? 1.0f : slope;
     case kActGelu: {
@@ -90,6 +89,7 @@ template <bool Precise> LF_DEV float act_slope(float z, int act, float slope) {
       return __builtin_fmaf(z, kDensity * e, z > 0.0f ? 1.0f - q : q);
     }
     case kActGeluTanh: {
+      z = z > 30.0f ? 30.0f : (z < -30.0f ? -30.0f : z);   // 1 or 0 from there on, and no infinity times 0
       const float z2 = z * z, p = logistic<Precise>(1.59576912160573071176f * z * __builtin_fmaf(0.044715f, z2, 1.0f));
       return __builtin_fmaf(z * p * (1.0f - p), 1.59576912160573071176f * __builtin_fmaf(0.134145f, z2, 1.0f), p);
     }
@@ -118,14 +118,10 @@ template <bool MAPPED> LF_DEV LinToken token_at(long long m, long long count, un
 }
 LF_DEV long long place(const LinRows& v, const LinToken& t) { return t.b * v.batch + t.n * v.token; }
 
-// z of eight channels (n ..) of a token to what the call asks for
-template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, int n, float (&z)[8]) {
-  float v[8];
-  if (o.bias) {
-    load8<T>(at<T>(o.bias, n), v);
+// z of eight channels (n ..) of a token to what the call asks for, bias and residual (where there is one) at hand
+template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, int n, float (&z)[8], const float (&bias)[8], const Raw8<T>& residual) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] += v[j];
-  }
+  for (int j = 0; j < 8; ++j) z[j] += bias[j];
   if (o.z) store8<T>(at<T>(o.z, place(o.vz, t) + n), z);
   if (!o.y) return;
   if (o.act != kActNone) {
@@ -133,21 +129,40 @@ template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, in
     for (int j = 0; j < 8; ++j) z[j] = act_of<Stored<T>::kBytes == 4>(z[j], o.act, o.slope);
   }
   if (o.residual) {
-    load8<T>(at<T>(o.residual, place(o.vr, t) + n), v);
+    float v[8];
+    widen8<T>(residual, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] += v[j];
   }
   store8<T>(at<T>(o.y, place(o.vy, t) + n), z);
+}
+template <typename T> LF_DEV void bias8(const LinOut& o, int n, float (&bias)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bias[j] = 0.0f;
+  if (o.bias) load8<T>(at<T>(o.bias, n), bias);
+}
+template <typename T> LF_DEV Raw8<T> residual8(const LinOut& o, const LinToken& t, int n) {
+  return o.residual ? load8_raw<T>(at<T>(o.residual, place(o.vr, t) + n)) : none8<T>();
+}
+template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, int n, float (&z)[8]) {
+  const Raw8<T> residual = residual8<T>(o, t, n);
+  float bias[8];
+  bias8<T>(o, n, bias);
+  finish8<T>(o, t, n, z, bias, residual);
 }
 
 // ---- the tiled product -----------------------------------------------------------------------------------------------
 
 template <int N> LF_DEV void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// Copies 64 x 16 bytes, lane l's from `p`, to `lds` + 16 l.
-LF_DEV void copy_kb(const unsigned char* p, unsigned char* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (LF_LDS void*)lds, 16, 0, 0);
+// Copies 64 x 16 bytes, lane l's from `p`, to the LDS address `lds` + 16 l.  Written out: before a transposing read the compiler waits for
+// every copy of its own that is under way, though it goes to the other buffer (8192^3 with B's own index contiguous, bf16: 1093 us so, 905
+// without).  (m0, which nothing else here uses, has to be written an
+// instruction before it is read.)  No register receives anything, and wait_copies stands before the barrier behind which the copy is read.
+LF_DEV void copy_kb(const unsigned char* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
 }
+LF_DEV unsigned lds_address(unsigned char* p) { return (unsigned)(uintptr_t)(LF_LDS unsigned char*)p; }
 
 constexpr int kStepBytes = 128;   // of k in a tile
 
@@ -165,8 +180,54 @@ template <typename T, int X, bool KC> struct LinTile {
   static LF_DEV int turn(int k) { return (kSize == 2 ? ((k & 3) | ((k >> 3) & 3) << 2) : ((k >> 2) & 3)) & kMask; }
 };
 
+// How tokens are found.  kFlat: one stride leads through all of them.  kRows: batch row and token; where tokens are k, a step's are all of one
+// batch row, whose length a wave reads once (a division and a length for every copy: 101 us for 3 x 1000 x 640 to 1280 in fp32, 62 so).
+// kLanes (tokens are k, batch rows of a few tokens, of which a step takes several): every lane for itself.
+constexpr int kFlat = 0, kRows = 1, kLanes = 2;
+
+// The steps of a tile's k.
+struct LinStep { long long k0, end; int b, len; };   // k from k0 to end; kRows: tokens of batch row b, from token k0 on, that count below len
+template <int K, bool ROWS> struct LinSteps {
+  long long at, stop;   // steps
+  long long k_end;
+  unsigned per, n;      // ROWS: steps of a batch row, its tokens
+  const int* lengths;
+  LF_DEV LinSteps(long long k_first, long long k_split, long long k_all, unsigned per_row, const int* len) {
+    k_end = k_first + k_split < k_all ? k_first + k_split : k_all;
+    at = k_first / K;
+    stop = (k_end + K - 1) / K;
+    n = per_row;
+    per = (per_row + K - 1) / K;
+    lengths = len;
+  }
+  // the next step with something in it; false: none left
+  LF_DEV bool next(LinStep& s) {
+    if constexpr (!ROWS) {
+      if (at >= stop) return false;
+      s = LinStep{at * K, k_end, 0, 0};
+      ++at;
+      return true;
+    }
+    while (at < stop) {
+      const unsigned b = (unsigned)at / per, first = ((unsigned)at - b * per) * K;
+      int len = (int)n;
+      if (lengths) {   // (a scalar load: it must not wait for the copies under way)
+        len = *(const __attribute__((address_space(4))) int*)(lengths + b);
+        len = len < 0 ? 0 : (len > (int)n ? (int)n : len);
+      }
+      if ((int)first < len) {
+        s = LinStep{first, 0, (int)b, len};
+        ++at;
+        return true;
+      }
+      at = (long long)(b + 1) * per;
+    }
+    return false;
+  }
+};
+
 // The copies of a tile that a thread takes part in: `COUNT` of them.
-template <typename T, int X, bool KC, int WAVES, bool MAPPED> struct LinCopy {
+template <typename T, int X, bool KC, int WAVES, int MAPPED> struct LinCopy {
   using Tile = LinTile<T, X, KC>;
   static constexpr int kCopies = Tile::kBytes / 1024, kCount = (kCopies + WAVES - 1) / WAVES;
   const unsigned char* p[kCount];
@@ -181,10 +242,10 @@ template <typename T, int X, bool KC, int WAVES, bool MAPPED> struct LinCopy {
       const int f = (wave + WAVES * j) * 64 + lane, row = f / Tile::kPieces, pos = f % Tile::kPieces;
       if constexpr (KC) {
         const int piece = pos ^ (row & 7);
-        const LinToken t = token_at<MAPPED>(x0 + row, limit, per_row, lengths);
+        const LinToken t = token_at<MAPPED != kFlat>(x0 + row, limit, per_row, lengths);
         on[j] = t.on;
         k[j] = piece * Tile::kVec;
-        p[j] = t.on ? at<T>(base, (MAPPED ? place(v, t) : (x0 + row) * v.token) + k[j]) : nullptr;
+        p[j] = t.on ? at<T>(base, (MAPPED != kFlat ? place(v, t) : (x0 + row) * v.token) + k[j]) : nullptr;
       } else {
         const int group = (pos / Tile::kGroupPieces) ^ Tile::turn(row), piece = group * Tile::kGroupPieces + pos % Tile::kGroupPieces;
         const long long x = x0 + piece * Tile::kVec;
@@ -194,23 +255,25 @@ template <typename T, int X, bool KC, int WAVES, bool MAPPED> struct LinCopy {
       }
     }
   }
-  // the copies of the step that starts at k0, of k < end
-  LF_DEV void step(unsigned char* lds, const LinRows& v, long long k0, long long end, unsigned per_row, const int* lengths, int wave) const {
+  LF_DEV void step(unsigned lds, const LinRows& v, const LinStep& s, unsigned per_row, const int* lengths, int wave) const {
 #pragma unroll
     for (int j = 0; j < kCount; ++j) {
       if (kCopies % WAVES && wave + WAVES * j >= kCopies) break;   // (a whole wave)
       const unsigned char* from;
       bool there;
       if constexpr (KC) {
-        there = on[j] && k0 + k[j] < end;
-        from = p[j] + k0 * Tile::kSize;
-      } else if constexpr (MAPPED) {
-        const LinToken t = token_at<true>(k0 + k[j], end, per_row, lengths);
+        there = on[j] && s.k0 + k[j] < s.end;
+        from = p[j] + s.k0 * Tile::kSize;
+      } else if constexpr (MAPPED == kLanes) {
+        const LinToken t = token_at<true>(s.k0 + k[j], s.end, per_row, lengths);
         there = on[j] && t.on;
         from = p[j] + place(v, t) * Tile::kSize;
+      } else if constexpr (MAPPED == kRows) {
+        there = on[j] && (int)s.k0 + k[j] < s.len;
+        from = p[j] + (s.b * v.batch + s.k0 * v.token) * Tile::kSize + k[j] * v.token * Tile::kSize;
       } else {
-        there = on[j] && k0 + k[j] < end;
-        from = p[j] + (k0 + k[j]) * v.token * Tile::kSize;
+        there = on[j] && s.k0 + k[j] < s.end;
+        from = p[j] + s.k0 * v.token * Tile::kSize + k[j] * v.token * Tile::kSize;
       }
       copy_kb(there ? from : reinterpret_cast<const unsigned char*>(kZeros16), lds + (wave + WAVES * j) * 1024);
     }
@@ -287,9 +350,8 @@ struct LinPlace {
 };
 
 // WR x WC waves, each with BM / WR rows and BN / WC columns of the tile.  AK, BK: whether A, B have k contiguous.  Tokens are the rows
-// of the result where A has k contiguous, else k; MAPPED: they are tokens of batch rows (with lengths, or strides that no single one
-// describes).
-template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, bool MAPPED>
+// of the result where A has k contiguous, else k.
+template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, int MAPPED>
 __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
   constexpr int kWaves = WR * WC, WM = BM / WR, WN = BN / WC, MT = WM / 16, NT = WN / 16;
   using TA = LinTile<T, BM, AK>;
@@ -300,17 +362,17 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
   const LinPlace tile(g.tiles_m, g.tiles_n, g.splits);
   const long long m0 = (long long)tile.m * BM;
   const int n0 = tile.n * BN;
-  if constexpr (AK && MAPPED) {   // nothing to do where no row of the tile counts
+  if constexpr (AK && MAPPED != kFlat) {   // nothing to do where no row of the tile counts
     if (g.lengths) {
       bool some = false;
       for (int r = threadIdx.x; r < BM; r += 64 * kWaves) some |= token_at<true>(m0 + r, g.M, g.per_row, g.lengths).on;
       if (!__syncthreads_or(some)) return;
     }
   }
-  const long long k_first = tile.split * g.k_split;
-  const long long k_end = k_first + g.k_split < g.K ? k_first + g.k_split : g.K;
+  constexpr bool kByRows = !AK && MAPPED == kRows;
+  LinSteps<TA::kK, kByRows> steps(tile.split * g.k_split, g.k_split, g.K, g.per_row, g.lengths);
   LinCopy<T, BM, AK, kWaves, MAPPED> ca;
-  LinCopy<T, BN, BK, kWaves, MAPPED && !AK> cb;
+  LinCopy<T, BN, BK, kWaves, AK ? kFlat : MAPPED> cb;
   ca.start(g.A, g.va, m0, g.M, g.per_row, g.lengths, wave);
   cb.start(g.B, g.vb, n0, g.N, g.per_row, g.lengths, wave);
   const int wm = wave / WC * WM, wn = wave % WC * WN;
@@ -323,19 +385,23 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int steps = (int)((k_end - k_first + TA::kK - 1) / TA::kK);
-  auto request = [&](int s) {
-    unsigned char* to = smem + (s & 1) * kBuffer;
-    const long long k0 = k_first + (long long)s * TA::kK;
-    ca.step(to, g.va, k0, k_end, g.per_row, g.lengths, wave);
-    cb.step(to + TA::kBytes, g.vb, k0, k_end, g.per_row, g.lengths, wave);
+  int side = 0;
+  const unsigned base = lds_address(smem);
+  auto request = [&](const LinStep& s) {
+    const unsigned to = base + side * kBuffer;
+    ca.step(to, g.va, s, g.per_row, g.lengths, wave);
+    cb.step(to + TA::kBytes, g.vb, s, g.per_row, g.lengths, wave);
   };
-  if (steps > 0) request(0);
-  for (int s = 0; s < steps; ++s) {
+  LinStep s;
+  bool more = steps.next(s);
+  if (more) request(s);
+  while (more) {
     wait_copies<0>();
     __syncthreads();   // this step's tiles are there, and nobody reads the other buffer any more
-    if (s + 1 < steps) request(s + 1);
-    const unsigned char* la = smem + (s & 1) * kBuffer;
+    const unsigned char* la = smem + side * kBuffer;
+    side ^= 1;
+    more = steps.next(s);
+    if (more) request(s);
     const unsigned char* lb = la + TA::kBytes;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -357,33 +423,49 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
   constexpr int kPass = kFit >= MT ? MT : (kFit >= (MT + 1) / 2 && MT % 2 == 0 ? MT / 2 : (kFit >= 2 && MT % 2 == 0 ? 2 : 1));
   static_assert(kFit >= kPass && MT % kPass == 0, "whole passes");
   constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes of a row; rows at a time
+  constexpr int kAtOnce = 4;   // rows of a lane whose residuals are requested together
   __syncthreads();
   unsigned char* mine = smem + wave * kRegion;
+  const int row = lane / kLanes, u = lane % kLanes * 2, n = n0 + wn + 4 * u;
+  const bool on = lane < kRows * kLanes && n < g.N;
+  float bias[8];
+  if (on && !g.partials) bias8<T>(g.out, n, bias);
 #pragma unroll
   for (int p = 0; p < MT; p += kPass) {
 #pragma unroll
     for (int i = 0; i < kPass; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        const int r = 16 * i + (lane & 15), u = 4 * j + (lane >> 4);
-        *reinterpret_cast<f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16) = acc[p + i][j];
+        const int r = 16 * i + (lane & 15), v = 4 * j + (lane >> 4);
+        *reinterpret_cast<f32x4*>(mine + r * (WN * 4) + (v ^ (r & kTurn)) * 16) = acc[p + i][j];
       }
     asm volatile("" ::: "memory");   // (a wave's LDS operations complete in order)
 #pragma unroll 1
-    for (int r0 = 0; r0 < 16 * kPass; r0 += kRows) {
-      const int r = r0 + lane / kLanes, u = lane % kLanes * 2, n = n0 + wn + 4 * u;
-      if (lane >= kRows * kLanes || r >= 16 * kPass) continue;
-      const LinToken t = token_at<MAPPED && AK>(m0 + wm + 16 * p + r, g.M, g.per_row, g.lengths);
-      if (!t.on || n >= g.N) continue;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((u + 1) ^ (r & kTurn)) * 16);
-      if (g.partials) {
-        float* to = g.partials + (tile.split * g.M + m0 + wm + 16 * p + r) * g.N + n;
-        *reinterpret_cast<f32x4*>(to) = lo;
-        *reinterpret_cast<f32x4*>(to + 4) = hi;
-      } else {
-        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish8<T>(g.out, t, n, z);
+    for (int r0 = 0; r0 < 16 * kPass; r0 += kRows * kAtOnce) {
+      LinToken t[kAtOnce];
+      Raw8<T> residual[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        const int r = r0 + q * kRows + row;
+        t[q] = token_at<MAPPED != kFlat && AK>(m0 + wm + 16 * p + r, g.M, g.per_row, g.lengths);
+        t[q].on = t[q].on && on && r < 16 * kPass;
+        residual[q] = none8<T>();
+        if (t[q].on && !g.partials) residual[q] = residual8<T>(g.out, t[q], n);
+      }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (!t[q].on) continue;
+        const int r = r0 + q * kRows + row;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((u + 1) ^ (r & kTurn)) * 16);
+        if (g.partials) {
+          float* to = g.partials + (tile.split * g.M + m0 + wm + 16 * p + r) * g.N + n;
+          *reinterpret_cast<f32x4*>(to) = lo;
+          *reinterpret_cast<f32x4*>(to + 4) = hi;
+        } else {
+          float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          finish8<T>(g.out, t[q], n, z, bias, residual[q]);
+        }
       }
     }
     asm volatile("" ::: "memory");
@@ -469,45 +551,75 @@ struct LinSlopeArgs {
   const unsigned char* z_exps;
   LinRows vdy, vz, ve;              // ve: of the exponents' rows
   void* dz;                         // [B * N][C] rows, or null (no activation)
-  float* partials;                  // [workgroups][C], or null
+  float* partials;                  // [workgroups along the tokens][C], or null
   const int* lengths;
-  long long rows;                   // B * N
-  unsigned per_row;
-  int C, each, act;                 // each: tokens of a workgroup
+  long long N;
+  int B, C, each, act;              // each: tokens of a piece of a batch row; a workgroup takes pieces in turn
   float slope;
 };
 
 // dz = dy act'(z), rounded once to the type (it is an operand of two products), and the sums of the unrounded values over a
-// workgroup's tokens.  32 lanes of 8 channels, 8 tokens at a time.  Bound: HBM.
+// workgroup's tokens.  32 lanes of 8 channels, 8 tokens at a time, four of them under way (absent ones from 16 bytes of zeros, without
+// branches).  Bound: HBM (49152 x 1280 bf16 from kept z: 315 MB), with GELU the vector instructions too.
 template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_slope(LinSlopeArgs a) {
   __shared__ float lds[8][32][8];
+  constexpr int kAhead = 4;
   const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * 8;
   const bool on = c < a.C;
-  const long long first = (long long)blockIdx.y * a.each, stop = first + a.each < a.rows ? first + a.each : a.rows;
+  const unsigned char* const none = reinterpret_cast<const unsigned char*>(kZeros16);
+  const long long per = (a.N + a.each - 1) / a.each, pieces = per * a.B;
   float sum[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-  for (long long m = first + row; on && m < stop; m += 8) {
-    const LinToken t = token_at<true>(m, a.rows, a.per_row, a.lengths);
-    if (!t.on) continue;
-    float d[8], z[8];
-    const Raw8<T> rd = load8_raw<T>(at<T>(a.dy, place(a.vdy, t) + c));
-    if (a.dz) {
-      if constexpr (KEPT) {
-        keep_values<T>(*reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.z) + place(a.vz, t) + c),
-                       a.z_exps[place(a.ve, t) + c / kKeepBlock], z);
-      } else {
-        load8<T>(at<T>(a.z, place(a.vz, t) + c), z);
+  for (long long piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
+    const unsigned b = (unsigned)piece / (unsigned)per;
+    const long long first = (long long)((unsigned)piece - b * (unsigned)per) * a.each, len = tokens_of(a.lengths, b, a.N);
+    const long long end = first + a.each < len ? first + a.each : len;
+    const unsigned char *pd = at<T>(a.dy, b * a.vdy.batch + c), *pe = a.z_exps + b * a.ve.batch + c / kKeepBlock;
+    const unsigned char* pz = KEPT ? static_cast<const unsigned char*>(a.z) + b * a.vz.batch + c : at<T>(a.z, b * a.vz.batch + c);
+    unsigned char* po = at<T>(a.dz, b * a.N * a.C + c);
+    for (long long n0 = first; n0 < end; n0 += 8 * kAhead) {
+      Raw8<T> rd[kAhead], rz[KEPT ? 1 : kAhead];
+      u32x2 codes[KEPT ? kAhead : 1];
+      int exps[KEPT ? kAhead : 1];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const long long n = n0 + row + 8 * q;
+        const bool there = on && n < end;
+        if constexpr (Stored<T>::kBytes == 4) {
+          rd[q] = none8<T>();
+          if (there) rd[q] = load8_raw<T>(pd + n * a.vdy.token * 4);
+        } else {
+          rd[q].w = *reinterpret_cast<const u32x4*>(there ? pd + n * a.vdy.token * 2 : none);
+        }
+        if (!a.dz) continue;
+        if constexpr (KEPT) {
+          codes[q] = *reinterpret_cast<const u32x2*>(there ? pz + n * a.vz.token : none);
+          exps[q] = *(there ? pe + n * a.ve.token : none);
+        } else if constexpr (Stored<T>::kBytes == 4) {
+          rz[q] = none8<T>();
+          if (there) rz[q] = load8_raw<T>(pz + n * a.vz.token * 4);
+        } else {
+          rz[q].w = *reinterpret_cast<const u32x4*>(there ? pz + n * a.vz.token * 2 : none);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const long long n = n0 + row + 8 * q;
+        float d[8];
+        widen8<T>(rd[q], d);
+        if (a.dz) {
+          float z[8];
+          if constexpr (KEPT) keep_values<T>(codes[q], exps[q], z);
+          else widen8<T>(rz[q], z);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] *= act_slope<Stored<T>::kBytes == 4>(z[j], a.act, a.slope);
+          if (on && n < end) store8<T>(po + n * a.C * Stored<T>::kBytes, d);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += d[j];
       }
     }
-    widen8<T>(rd, d);
-    if (a.dz) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] *= act_slope<Stored<T>::kBytes == 4>(z[j], a.act, a.slope);
-      store8<T>(at<T>(a.dz, m * a.C + c), d);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += d[j];
   }
   if (!a.partials) return;
 #pragma unroll

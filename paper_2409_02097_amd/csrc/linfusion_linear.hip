@@ -95,7 +95,7 @@ size_t most_partials(long long M, int N) {
   return lfh::up256(by_rows < by_tiles ? by_rows : by_tiles);
 }
 
-template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, bool MAPPED>
+template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, int MAPPED>
 int launch_tiles(const lf::LinArgs& g, hipStream_t st) {
   auto kernel = lf::linear_tiles<T, BM, BN, WR, WC, AK, BK, MAPPED>;
   constexpr int lds = 2 * (BM + BN) * lf::kStepBytes;
@@ -106,7 +106,7 @@ int launch_tiles(const lf::LinArgs& g, hipStream_t st) {
   return LINFUSION_OK;
 }
 
-template <typename T, bool AK, bool BK, bool MAPPED>
+template <typename T, bool AK, bool BK, int MAPPED>
 int product(lf::LinArgs g, const Plan& p, hipStream_t st) {
   g.tiles_m = (int)((g.M + kShape[p.kind].m - 1) / kShape[p.kind].m);
   g.tiles_n = (g.N + kShape[p.kind].n - 1) / kShape[p.kind].n;
@@ -122,14 +122,21 @@ int product(lf::LinArgs g, const Plan& p, hipStream_t st) {
   if (rc != LINFUSION_OK) return rc;
   if (p.splits > 1) {
     const long long threads = g.M * (g.N / 8);
-    lf::linear_join<T, MAPPED && AK><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(g);
+    lf::linear_join<T, MAPPED != lf::kFlat && AK><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(g);
   }
   return LINFUSION_OK;
 }
 
+// Tokens of a batch row from which on a step of k takes those of one row alone.
+constexpr unsigned kRowTokens = 32;
+
 template <typename T, bool AK, bool BK>
 int product(const lf::LinArgs& g, bool mapped, const Plan& p, hipStream_t st) {
-  return mapped ? product<T, AK, BK, true>(g, p, st) : product<T, AK, BK, false>(g, p, st);
+  if (!mapped) return product<T, AK, BK, lf::kFlat>(g, p, st);
+  if constexpr (!AK) {
+    if (g.per_row < kRowTokens) return product<T, AK, BK, lf::kLanes>(g, p, st);
+  }
+  return product<T, AK, BK, lf::kRows>(g, p, st);
 }
 
 template <typename F> int by_type(int dtype, F f) {
@@ -153,18 +160,20 @@ template <typename T, int MT> int launch_few(const lf::LinArgs& g, bool mapped, 
   return LINFUSION_OK;
 }
 
-// Workgroups along the tokens of linear_slope and their tokens.
+// Workgroups along the tokens of linear_slope, and the tokens of a piece of a batch row.
 struct Slices { int count, each; };
-Slices slices(long long rows, int C) {
-  const long long across = (C + 255) / 256, most = 4LL * lfh::num_cu() / across + 1;
-  long long each = (rows + most - 1) / most;
-  each = (each + 7) / 8 * 8;
-  if (each < 32) each = 32;
-  return Slices{(int)((rows + each - 1) / each), (int)each};
+long long most_workgroups(int C) { return 4LL * lfh::num_cu() / ((C + 255) / 256) + 1; }
+Slices slices(int B, long long N, int C) {
+  const long long most = most_workgroups(C);
+  long long each = (B * N + most - 1) / most;
+  each = (each + 31) / 32 * 32;
+  if (each > N) each = (N + 31) / 32 * 32;
+  const long long pieces = (N + each - 1) / each * B;
+  return Slices{(int)(pieces < most ? pieces : most), (int)each};
 }
 size_t most_slices(long long rows, int C) {   // never falls with the rows
-  const long long across = (C + 255) / 256, most = 4LL * lfh::num_cu() / across + 1, by_rows = (rows + 31) / 32;
-  return lfh::up256((size_t)(most < by_rows ? most : by_rows) * C * 4);
+  const long long most = most_workgroups(C);
+  return lfh::up256((size_t)(most < rows ? most : rows) * C * 4);
 }
 
 }  // namespace
@@ -279,9 +288,13 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
   float* const partials = (float*)at_ws;
   const bool act = activation != LINFUSION_ACT_NONE;
   if (act || dbias) {
-    const Slices s = slices(M, C_out);
-    const lf::LinSlopeArgs a{dy, z, z_exps, dev(vdy), dev(vz), dev(vze), act ? dz : nullptr, dbias ? sums : nullptr, lengths, M, (unsigned)N, C_out,
-                             s.each, activation, slope};
+    const bool one = !lengths && plain(vdy, B, N) && plain(vz, B, N) && plain(vze, B, N);   // one stride leads through all tokens
+    const int rows_b = one ? 1 : B;
+    const long long rows_n = one ? M : N;
+    auto rows = [&](const RowView& v) { return flat(v, B, N, !one); };
+    const Slices s = slices(rows_b, rows_n, C_out);
+    const lf::LinSlopeArgs a{dy, z, z_exps, rows(vdy), rows(vz), rows(vze), act ? dz : nullptr, dbias ? sums : nullptr, lengths, rows_n, rows_b,
+                             C_out, s.each, activation, slope};
     const dim3 grid((C_out + 255) / 256, s.count);
     rc = by_type(dtype, [&](auto t) {
       using T = decltype(t);
@@ -318,6 +331,10 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     const bool mapped = lengths || !plain(vd, B, N) || !plain(vx, B, N);
     g.A = vd.p, g.va = flat(vd, B, N, mapped), g.B = vx.p, g.vb = flat(vx, B, N, mapped);
     g.M = C_out, g.K = M, g.N = C_in;
+    if (mapped && N >= kRowTokens) {   // whole steps for every batch row
+      const long long k_step = lf::kStepBytes / (long long)esz;
+      g.K = (N + k_step - 1) / k_step * k_step * B;
+    }
     g.out = lf::LinOut{dw, nullptr, nullptr, nullptr, lf::LinRows{0, dws[1]}, {}, {}, lf::kActNone, 0.0f};
     rc = by_type(dtype, [&](auto t) { return product<decltype(t), false, false>(g, mapped, plan(g.M, g.N, g.K, dtype, true), st); });
     if (rc != LINFUSION_OK) return rc;

@@ -181,8 +181,9 @@ def test_views(dtype, N):
                                 **rest(c, g))
         lf.linfusion_linear_bwd(x, w, zz, dy, dx=dx, dw=dwide[:, 8:80], dbias=(db := torch.zeros_like(g["bias"])),
                                 workspace=memory(lf.linfusion_linear_bwd_workspace_bytes(*c["dims"], CODE[dtype])), **rest(c, g))
-        for got, want in ((y2, y), (z2, z), (dx, d["dx"]), (dwide[:, 8:80], d["dw"]), (db, d["dbias"])):
+        for got, want in ((y2, y), (z2, z), (dx, d["dx"])):
             assert torch.equal(got, want)
+        check_backward(c, {"dw": dwide[:, 8:80], "dbias": db})   # (not bit for bit: tokens are summed by batch rows where no single stride leads through them)
         assert bool((dwide[:, :8] == 7.0).all()) and bool((dwide[:, 80:] == 7.0).all())
 
 

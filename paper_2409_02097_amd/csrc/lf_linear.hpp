@@ -3,7 +3,7 @@
 // One tiled matrix product serves all three: out[m][n] = sum_k A(m, k) B(n, k), fp32 sums on the matrix instructions (16-bit types:
 // 16 x 16 x 32; fp32: 16 x 16 x 4, whose operands are exact).  Either operand may lie with k contiguous (x, W, dz in rows) or with
 // its own index contiguous (W for dx; dz and x for dW): the second kind is staged as rows of k and read from LDS by transposing
-// reads (fp32: word by word), so that no tensor is transposed in memory.  Tiles of 128 bytes of k go from memory to LDS without
+// reads (fp32: word by word), so that no tensor is transposed in memory.  Tiles of 128 or 64 bytes of k go from memory to LDS without
 // passing registers, one step ahead of the products; 16-byte pieces are dealt over a row so that operand reads meet every bank
 // evenly.  Where something is not there (channels behind the last, tokens behind a row's length, the end of k) a lane copies from 16
 // bytes of zeros instead.  The result is formed transposed, so that a lane holds four neighbouring channels of a token.
@@ -122,7 +122,7 @@ LF_DEV long long place(const LinRows& v, const LinToken& t) { return t.b * v.bat
 template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, int n, float (&z)[8], const float (&bias)[8], const Raw8<T>& residual) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) z[j] += bias[j];
-  if (o.z) store8<T>(at<T>(o.z, place(o.vz, t) + n), z);
+  if (o.z) store8_stream<T>(at<T>(o.z, place(o.vz, t) + n), z);
   if (!o.y) return;
   if (o.act != kActNone) {
 #pragma unroll
@@ -134,7 +134,7 @@ template <typename T> LF_DEV void finish8(const LinOut& o, const LinToken& t, in
 #pragma unroll
     for (int j = 0; j < 8; ++j) z[j] += v[j];
   }
-  store8<T>(at<T>(o.y, place(o.vy, t) + n), z);
+  store8_stream<T>(at<T>(o.y, place(o.vy, t) + n), z);
 }
 template <typename T> LF_DEV void bias8(const LinOut& o, int n, float (&bias)[8]) {
 #pragma unroll
@@ -164,15 +164,14 @@ LF_DEV void copy_kb(const unsigned char* p, unsigned lds) {
 }
 LF_DEV unsigned lds_address(unsigned char* p) { return (unsigned)(uintptr_t)(LF_LDS unsigned char*)p; }
 
-constexpr int kStepBytes = 128;   // of k in a tile
-
-// An operand's tile of X rows (or columns).  KC: k contiguous, X rows of 128 bytes, 16-byte piece c of row r at c ^ (r % 8).
-// Else rows of k of X values, with groups of 16 values (16-bit: 32 bytes; fp32: 64) of row k at g ^ turn(k), for as many groups as
-// make a power of two.
-template <typename T, int X, bool KC> struct LinTile {
-  static constexpr int kSize = Stored<T>::kBytes, kVec = 16 / kSize, kK = kStepBytes / kSize;
-  static constexpr int kBytes = X * kStepBytes;
-  static constexpr int kRow = KC ? kStepBytes : X * kSize, kPieces = kRow / 16;
+// An operand's tile of X rows (or columns) and STEP bytes of k, 128 or 64.  KC: k contiguous, X rows of STEP bytes, 16-byte piece c of row r
+// at c ^ turn_row(r).  Else rows of k of X values, with groups of 16 values (16-bit: 32 bytes; fp32: 64) of row k at g ^ turn(k), for as
+// many groups as make a power of two.
+template <typename T, int X, bool KC, int STEP> struct LinTile {
+  static constexpr int kSize = Stored<T>::kBytes, kVec = 16 / kSize, kK = STEP / kSize;
+  static constexpr int kBytes = X * STEP;
+  static constexpr int kRow = KC ? STEP : X * kSize, kPieces = kRow / 16;
+  static LF_DEV int turn_row(int r) { return STEP == 128 ? r & 7 : (r >> 2) & 3; }
   static constexpr int kGroups = X / 16, kGroupPieces = kSize;   // (transposed) groups of a row; pieces of a group: 2 or 4
   static constexpr int kMask = (kGroups & -kGroups) - 1;
   static_assert(kBytes % 1024 == 0, "whole copies");
@@ -227,8 +226,8 @@ template <int K, bool ROWS> struct LinSteps {
 };
 
 // The copies of a tile that a thread takes part in: `COUNT` of them.
-template <typename T, int X, bool KC, int WAVES, int MAPPED> struct LinCopy {
-  using Tile = LinTile<T, X, KC>;
+template <typename T, int X, bool KC, int STEP, int WAVES, int MAPPED> struct LinCopy {
+  using Tile = LinTile<T, X, KC, STEP>;
   static constexpr int kCopies = Tile::kBytes / 1024, kCount = (kCopies + WAVES - 1) / WAVES;
   const unsigned char* p[kCount];
   int k[kCount];   // KC: the piece's first k; else the row of k
@@ -241,7 +240,7 @@ template <typename T, int X, bool KC, int WAVES, int MAPPED> struct LinCopy {
     for (int j = 0; j < kCount; ++j) {
       const int f = (wave + WAVES * j) * 64 + lane, row = f / Tile::kPieces, pos = f % Tile::kPieces;
       if constexpr (KC) {
-        const int piece = pos ^ (row & 7);
+        const int piece = pos ^ Tile::turn_row(row);
         const LinToken t = token_at<MAPPED != kFlat>(x0 + row, limit, per_row, lengths);
         on[j] = t.on;
         k[j] = piece * Tile::kVec;
@@ -282,16 +281,16 @@ template <typename T, int X, bool KC, int WAVES, int MAPPED> struct LinCopy {
 
 // Operands of 16 rows (columns) from a tile: 16-bit, 32 k of lane l's row l % 16, eight of them from 8 (l / 16) on; fp32, 16 k, four of them
 // from 4 (l / 16) on: the j-th instruction takes every lane's j-th.
-template <typename T, int X, bool KC> struct LinRead {
-  using Tile = LinTile<T, X, KC>;
-  static constexpr int kSteps = 2;   // per tile
+template <typename T, int X, bool KC, int STEP> struct LinRead {
+  using Tile = LinTile<T, X, KC, STEP>;
+  static constexpr int kSteps = STEP / 64;   // per tile
   int base, turn[KC ? kSteps : 1];
   LF_DEV void start(int x) {   // x: the wave's first row or column, a multiple of 16
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     if constexpr (KC) {
-      base = (x + i) * kStepBytes;
+      base = (x + i) * STEP;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) turn[s] = ((4 * s + g) ^ (i & 7)) * 16;
+      for (int s = 0; s < kSteps; ++s) turn[s] = ((4 * s + g) ^ Tile::turn_row(i)) * 16;
     } else if constexpr (Tile::kSize == 2) {
       base = (8 * g + (i >> 2)) * Tile::kRow + (i & 3) * 8;
       turn[0] = Tile::turn(8 * g + (i >> 2));
@@ -303,7 +302,7 @@ template <typename T, int X, bool KC> struct LinRead {
   // tile t of 16 from x on (`x` again: transposed places depend on it), step s
   LF_DEV u32x4 get(const unsigned char* lds, int x, int t, int s) const {
     if constexpr (KC) {
-      return *reinterpret_cast<const u32x4*>(lds + base + turn[s] + t * 16 * kStepBytes);
+      return *reinterpret_cast<const u32x4*>(lds + base + turn[s] + t * 16 * STEP);
     } else if constexpr (Tile::kSize == 2) {
       const unsigned char* q = lds + base + s * 32 * Tile::kRow + ((x / 16 + t) ^ turn[0]) * 32;
       const u32x2 a = lds_read_tr16(reinterpret_cast<const uint16_t*>(q)), b = lds_read_tr16(reinterpret_cast<const uint16_t*>(q + 4 * Tile::kRow));
@@ -351,11 +350,11 @@ struct LinPlace {
 
 // WR x WC waves, each with BM / WR rows and BN / WC columns of the tile.  AK, BK: whether A, B have k contiguous.  Tokens are the rows
 // of the result where A has k contiguous, else k.
-template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, int MAPPED>
-__global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
+template <typename T, int BM, int BN, int WR, int WC, int STEP, bool AK, bool BK, int MAPPED>
+__global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 4 : 1) void linear_tiles(LinArgs g) {
   constexpr int kWaves = WR * WC, WM = BM / WR, WN = BN / WC, MT = WM / 16, NT = WN / 16;
-  using TA = LinTile<T, BM, AK>;
-  using TB = LinTile<T, BN, BK>;
+  using TA = LinTile<T, BM, AK, STEP>;
+  using TB = LinTile<T, BN, BK, STEP>;
   constexpr int kBuffer = TA::kBytes + TB::kBytes;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -371,13 +370,13 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
   }
   constexpr bool kByRows = !AK && MAPPED == kRows;
   LinSteps<TA::kK, kByRows> steps(tile.split * g.k_split, g.k_split, g.K, g.per_row, g.lengths);
-  LinCopy<T, BM, AK, kWaves, MAPPED> ca;
-  LinCopy<T, BN, BK, kWaves, AK ? kFlat : MAPPED> cb;
+  LinCopy<T, BM, AK, STEP, kWaves, MAPPED> ca;
+  LinCopy<T, BN, BK, STEP, kWaves, AK ? kFlat : MAPPED> cb;
   ca.start(g.A, g.va, m0, g.M, g.per_row, g.lengths, wave);
   cb.start(g.B, g.vb, n0, g.N, g.per_row, g.lengths, wave);
   const int wm = wave / WC * WM, wn = wave % WC * WN;
-  LinRead<T, BM, AK> ra;
-  LinRead<T, BN, BK> rb;
+  LinRead<T, BM, AK, STEP> ra;
+  LinRead<T, BN, BK, STEP> rb;
   ra.start(wm);
   rb.start(wn);
   f32x4 acc[MT][NT];
@@ -404,7 +403,7 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_tiles(LinArgs g) {
     if (more) request(s);
     const unsigned char* lb = la + TA::kBytes;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < STEP / 64; ++q) {
       u32x4 a[MT], b[NT];
 #pragma unroll
       for (int j = 0; j < NT; ++j) b[j] = rb.get(lb, wn, j, q);

@@ -39,43 +39,46 @@ lf::LinRows dev(const RowView& v) { return lf::LinRows{v.batch, v.token}; }
 
 struct Plan { int kind, splits; long long k_split; };   // kind: index into the tile shapes below
 
-// Tile shapes: rows, columns, waves along each, workgroups that share a CU (LDS).  The first for 16-bit types only.
+// Tile shapes: rows, columns, waves along each, bytes of k of a step, workgroups that share a CU (LDS, registers).  The first for
+// 16-bit types only.  Half steps leave room for more workgroups, whose starts and ends overlap more: for short k (49152 x 320 -> 1280 in bf16
+// 60 us, whole steps 74), while long k loses (8192^3 1274, 1043).
 #define LF_LINEAR_SHAPES(DO) \
-  DO(0, 256, 256, 2, 4, 1) DO(1, 128, 160, 2, 2, 2) DO(2, 128, 128, 2, 2, 2) DO(3, 128, 64, 2, 2, 3) DO(4, 64, 64, 2, 2, 4)
-constexpr int kShapes = 5;
-struct Shape { int m, n, per_cu; };
+  DO(0, 256, 256, 2, 4, 128, 1) DO(1, 128, 160, 2, 2, 128, 2) DO(2, 128, 128, 2, 2, 128, 2) DO(3, 128, 64, 2, 2, 128, 3) \
+  DO(4, 64, 64, 2, 2, 128, 4) DO(5, 128, 128, 2, 2, 64, 4) DO(6, 128, 160, 2, 2, 64, 3) DO(7, 128, 64, 2, 2, 64, 5)
+constexpr int kShapes = 8;
+struct Shape { int m, n, step, per_cu; };
 constexpr Shape kShape[kShapes] = {
-#define LF_ROW(I, M, N, WR, WC, PER) {M, N, PER},
+#define LF_ROW(I, M, N, WR, WC, STEP, PER) {M, N, STEP, PER},
     LF_LINEAR_SHAPES(LF_ROW)
 #undef LF_ROW
 };
 
-// What a product takes, in us: rounds of workgroups, each a start and end (`over`) and its steps of 128 bytes of k (`step`, of a CU full of
-// such tiles), the last round by how full it is; another launch where k is split, and the sums' way out and in.  Fitted to 380
-// measured times of 16-bit products and 108 of fp32 ones (rows 154 to 81120, columns 320 to 8192, k 320 to 81120, all shapes, 1 to 32
-// splits; off by 11 % and 4 % at the root mean square; the shape it chooses takes 1.00 to 1.16 times the best one's time, 1.3 for one product of
-// 13 us).  A rule by the number of tiles alone chose 256 x 256 for 49152 x 1280 -> 320: 74 us where 128 x 160 takes 49.
-struct Cost { double step[kShapes], over[kShapes], fill, join, join_mb, turned; };
-constexpr Cost kCost16{{1.56, 1.09, 0.89, 0.78, 0.63}, {4.2, 3.6, 2.9, 2.3, 1.7}, 0.4, 4.1, 0.69, 1.23};
-constexpr Cost kCost32{{0.0, 4.81, 3.82, 3.11, 2.16}, {0.0, 3.3, 2.2, 0.3, 0.0}, 0.9, 2.3, 1.02, 1.03};
+// What a product takes, in us: rounds of workgroups, each a start and end (`over`) and its steps (`step`, of a CU full of such
+// tiles), the last round by how full it is; another launch where k is split, and the sums' way out and in.  Fitted to 449
+// measured times of 16-bit products and 210 of fp32 ones (rows 154 to 81120, columns 64 to 5120, k 64 to 49152, all shapes, 1 to 32
+// splits; off by 10 % and 3 % at the root mean square; of 47 products it chooses the best shape or one within 5 % for 44, and 1.25 times the
+// best one's time at most).  The number of tiles alone chose 256 x 256 for 49152 x 1280 -> 320: 74 us where 128 x 160 takes 49.
+struct Cost { double step[kShapes], over[kShapes], fill, join, join_mb; };
+constexpr Cost kCost16{{1.55, 1.10, 0.91, 0.81, 0.68, 0.90, 0.88, 0.78}, {5.6, 6.1, 3.9, 2.9, 1.8, 4.2, 6.2, 3.0}, 0.58, 3.4, 0.79};
+constexpr Cost kCost32{{0.0, 5.00, 3.87, 3.19, 2.22, 3.76, 3.80, 2.69}, {0.0, 4.9, 4.1, 0.2, 0.0, 3.0, 3.4, 0.0}, 0.87, 2.7, 1.01};
 
-// `turned`: whether an operand has its own index contiguous.
-Plan plan(long long M, int N, long long K, int dtype, bool turned) {
+Plan plan(long long M, int N, long long K, int dtype) {
   const bool wide = dtype == LINFUSION_DTYPE_F32;
   const Cost& c = wide ? kCost32 : kCost16;
-  const int k_step = lf::kStepBytes / (wide ? 4 : 2);
-  const long long steps = (K + k_step - 1) / k_step, cus = lfh::num_cu();
+  const long long cus = lfh::num_cu();
   const int only = lfh::env_int("LINFUSION_LINEAR_TILES", 0) - 1, only_splits = lfh::env_int("LINFUSION_LINEAR_SPLITS", 0);
-  Plan best{4, 1, steps * k_step};
+  Plan best{4, 1, K};
   double least = 1e300;
   for (int s = wide ? 1 : 0; s < kShapes; ++s) {
     if (only >= 0 && s != only) continue;
+    const int k_step = kShape[s].step / (wide ? 4 : 2);
+    const long long steps = (K + k_step - 1) / k_step;
     const long long tiles = ((M + kShape[s].m - 1) / kShape[s].m) * ((N + kShape[s].n - 1) / kShape[s].n), room = cus * kShape[s].per_cu;
     for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (splits > steps || (splits > 1 && tiles * splits >= 2 * room)) break;   // (what most_partials counts on)
       if (only_splits && splits != only_splits) continue;
       const long long per = (steps + splits - 1) / splits, used = (steps + per - 1) / per;
-      const double each = per * c.step[s] * (turned ? c.turned : 1.0) + c.over[s];
+      const double each = per * c.step[s] + c.over[s];
       const long long all = tiles * used, rest = all % room;
       double t = (double)(all / room) * each;
       if (rest) t += each * std::pow((double)((rest + cus - 1) / cus) / kShape[s].per_cu, c.fill);
@@ -95,10 +98,10 @@ size_t most_partials(long long M, int N) {
   return lfh::up256(by_rows < by_tiles ? by_rows : by_tiles);
 }
 
-template <typename T, int BM, int BN, int WR, int WC, bool AK, bool BK, int MAPPED>
+template <typename T, int BM, int BN, int WR, int WC, int STEP, bool AK, bool BK, int MAPPED>
 int launch_tiles(const lf::LinArgs& g, hipStream_t st) {
-  auto kernel = lf::linear_tiles<T, BM, BN, WR, WC, AK, BK, MAPPED>;
-  constexpr int lds = 2 * (BM + BN) * lf::kStepBytes;
+  auto kernel = lf::linear_tiles<T, BM, BN, WR, WC, STEP, AK, BK, MAPPED>;
+  constexpr int lds = 2 * (BM + BN) * STEP;
   if (!lfh::allow_lds(kernel, lds)) return LINFUSION_ERR_HIP;
   const long long all = (long long)g.tiles_m * g.tiles_n * g.splits;
   if (all > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
@@ -107,16 +110,22 @@ int launch_tiles(const lf::LinArgs& g, hipStream_t st) {
 }
 
 template <typename T, bool AK, bool BK, int MAPPED>
-int product(lf::LinArgs g, const Plan& p, hipStream_t st) {
+int product(lf::LinArgs g, Plan p, hipStream_t st) {
+  if constexpr (!AK && MAPPED == lf::kRows) {   // whole steps for every batch row
+    const long long k_step = kShape[p.kind].step / lf::Stored<T>::kBytes, steps = (g.per_row + k_step - 1) / k_step * (g.K / g.per_row);
+    const long long per = (steps + p.splits - 1) / p.splits;
+    g.K = steps * k_step;
+    p = Plan{p.kind, (int)((steps + per - 1) / per), per * k_step};
+  }
   g.tiles_m = (int)((g.M + kShape[p.kind].m - 1) / kShape[p.kind].m);
   g.tiles_n = (g.N + kShape[p.kind].n - 1) / kShape[p.kind].n;
   g.splits = p.splits;
   g.k_split = p.k_split;
   if (p.splits == 1) g.partials = nullptr;
   int rc = LINFUSION_ERR_UNSUPPORTED;
-#define LF_CASE(I, TM, TN, WR, WC, PER)                                                       \
+#define LF_CASE(I, TM, TN, WR, WC, STEP, PER)                                                    \
   if constexpr (lf::Stored<T>::kBytes == 2 || I > 0)                           \
-    if (p.kind == I) rc = launch_tiles<T, TM, TN, WR, WC, AK, BK, MAPPED>(g, st);
+    if (p.kind == I) rc = launch_tiles<T, TM, TN, WR, WC, STEP, AK, BK, MAPPED>(g, st);
   LF_LINEAR_SHAPES(LF_CASE)
 #undef LF_CASE
   if (rc != LINFUSION_OK) return rc;
@@ -227,7 +236,7 @@ int linfusion_linear_fwd(const void* x, const void* w, const void* bias, const v
     if (g.M <= 16) return launch_few<T, 1>(g, mapped, st);
     if (g.M <= 32) return launch_few<T, 2>(g, mapped, st);
     if (g.M <= kFew) return launch_few<T, 4>(g, mapped, st);
-    return product<T, true, true>(g, mapped, plan(g.M, g.N, g.K, dtype, false), st);
+    return product<T, true, true>(g, mapped, plan(g.M, g.N, g.K, dtype), st);
   });
   if (rc != LINFUSION_OK) return rc;
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
@@ -317,7 +326,7 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     g.A = vd.p, g.va = flat(vd, B, N, mapped), g.B = w, g.vb = lf::LinRows{0, ws[1]};
     g.M = M, g.K = C_out, g.N = C_in;
     g.out = lf::LinOut{dx, nullptr, nullptr, nullptr, flat(vdx, B, N, mapped), {}, {}, lf::kActNone, 0.0f};
-    rc = by_type(dtype, [&](auto t) { return product<decltype(t), true, false>(g, mapped, plan(g.M, g.N, g.K, dtype, true), st); });
+    rc = by_type(dtype, [&](auto t) { return product<decltype(t), true, false>(g, mapped, plan(g.M, g.N, g.K, dtype), st); });
     if (rc != LINFUSION_OK) return rc;
   }
   if (dw) {
@@ -331,12 +340,8 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     const bool mapped = lengths || !plain(vd, B, N) || !plain(vx, B, N);
     g.A = vd.p, g.va = flat(vd, B, N, mapped), g.B = vx.p, g.vb = flat(vx, B, N, mapped);
     g.M = C_out, g.K = M, g.N = C_in;
-    if (mapped && N >= kRowTokens) {   // whole steps for every batch row
-      const long long k_step = lf::kStepBytes / (long long)esz;
-      g.K = (N + k_step - 1) / k_step * k_step * B;
-    }
     g.out = lf::LinOut{dw, nullptr, nullptr, nullptr, lf::LinRows{0, dws[1]}, {}, {}, lf::kActNone, 0.0f};
-    rc = by_type(dtype, [&](auto t) { return product<decltype(t), false, false>(g, mapped, plan(g.M, g.N, g.K, dtype, true), st); });
+    rc = by_type(dtype, [&](auto t) { return product<decltype(t), false, false>(g, mapped, plan(g.M, g.N, g.K, dtype), st); });
     if (rc != LINFUSION_OK) return rc;
   }
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;

@@ -17,7 +17,7 @@ struct KeepArgs {
   long long xb, xt, cb, ct, eb, et;   // strides {batch, token} of x, codes, exps
   const int* lengths;
   long long N;
-  int C, rows;                // tokens per workgroup
+  int C, rows, lanes;         // tokens of a workgroup; lanes of a token, a multiple of four
 };
 
 // e + 127 of a block whose largest magnitude is `most` (its bits as an integer keep the order of magnitudes, infinities and NaN last)
@@ -32,16 +32,24 @@ template <typename T> struct Largest { static constexpr float value = 3.40282347
 template <> struct Largest<F16> { static constexpr float value = 65504.0f; };
 template <> struct Largest<BF16> { static constexpr float value = 3.38953139e38f; };
 
-// Eight codes as values of T, exact (the one multiple of 2^e that may lie above T's largest value, 64 * 2^e, is that value).
+// Eight codes as values of T, exact (the one multiple of 2^e that may lie above T's largest value, 64 * 2^e, is that value).  A code is
+// read as the unsigned byte code + 128: (byte - 128) 2^e in one exact multiply-add.
 template <typename T> LF_DEV void keep_values(u32x2 codes, int e, float (&x)[8]) {
-  const float scale = e == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, (uint32_t)e << 23);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (float)(int8_t)(codes[j >> 2] >> (8 * (j & 3))) * scale;
   constexpr float most = Largest<T>::value;
   constexpr int kTop = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 5;   // the exponent byte of 2^e where 64 * 2^e is above `most`
-  if (e >= kTop) {
+  constexpr int kFar = kTop < 247 ? kTop : 247;                               // (or 128 * 2^e above fp32's)
+  const float scale = e == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, (uint32_t)e << 23), off = -128.0f * scale;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] > most ? most : (x[j] < -most ? -most : x[j]);   // (a NaN stays one)
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t w = codes[j >> 2] ^ 0x80808080u;
+    x[j] = __builtin_fmaf((float)(w >> (8 * (j & 3)) & 255u), scale, off);
+  }
+  if (e >= kFar) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = (float)(int8_t)(codes[j >> 2] >> (8 * (j & 3))) * scale;
+      x[j] = v > most ? most : (v < -most ? -most : v);   // (a NaN stays one)
+    }
   }
 }
 
@@ -53,24 +61,26 @@ LF_DEV uint32_t quad_max(uint32_t v) {
   return v > w ? v : w;
 }
 
-// 32 lanes of 8 channels and 8 tokens at a time, four of them under way; four lanes share a block.
+// `lanes` lanes of 8 channels a token, as many tokens at a time as that leaves, four times as many under way; four lanes share a block.
 constexpr int kKeepAhead = 4;
 
 template <typename T> __global__ __launch_bounds__(256) void keep8(KeepArgs a) {
-  const int b = blockIdx.z, c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+  const int row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, together = 256 / a.lanes;
+  const int b = blockIdx.z, c = (blockIdx.x * a.lanes + lane) * 8;
   const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
   const long long stop = first + a.rows < end ? first + a.rows : end;
+  if (row >= together) return;
   const bool on = c < a.C;
-  for (long long n0 = first + (threadIdx.x >> 5); n0 < stop; n0 += 8 * kKeepAhead) {   // (four neighbouring lanes together)
+  for (long long n0 = first + row; n0 < stop; n0 += together * kKeepAhead) {   // (four neighbouring lanes together)
     Raw8<T> raw[kKeepAhead];
 #pragma unroll
     for (int q = 0; q < kKeepAhead; ++q) {
       raw[q] = none8<T>();
-      if (on && n0 + 8 * q < stop) raw[q] = load8_raw<T>(at<T>(a.x, b * a.xb + (n0 + 8 * q) * a.xt + c));
+      if (on && n0 + together * q < stop) raw[q] = load8_raw<T>(at<T>(a.x, b * a.xb + (n0 + together * q) * a.xt + c));
     }
 #pragma unroll
     for (int q = 0; q < kKeepAhead; ++q) {
-      const long long n = n0 + 8 * q;
+      const long long n = n0 + together * q;
       float x[8];
       widen8<T>(raw[q], x);
       uint32_t most = 0;
@@ -88,29 +98,30 @@ template <typename T> __global__ __launch_bounds__(256) void keep8(KeepArgs a) {
         codes[j >> 2] |= (uint32_t)(v & 255) << (8 * (j & 3));
       }
       *reinterpret_cast<u32x2*>(static_cast<unsigned char*>(a.codes) + b * a.cb + n * a.ct + c) = codes;
-      if ((threadIdx.x & 3) == 0) a.exps[b * a.eb + n * a.et + c / kKeepBlock] = (unsigned char)e;
+      if ((lane & 3) == 0) a.exps[b * a.eb + n * a.et + c / kKeepBlock] = (unsigned char)e;
     }
   }
 }
 
 template <typename T> __global__ __launch_bounds__(256) void unkeep8(KeepArgs a) {
-  const int b = blockIdx.z, c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+  const int row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, together = 256 / a.lanes;
+  const int b = blockIdx.z, c = (blockIdx.x * a.lanes + lane) * 8;
   const long long end = tokens_of(a.lengths, b, a.N), first = (long long)blockIdx.y * a.rows;
   const long long stop = first + a.rows < end ? first + a.rows : end;
-  if (c >= a.C) return;
-  for (long long n0 = first + (threadIdx.x >> 5); n0 < stop; n0 += 8 * kKeepAhead) {
+  if (c >= a.C || row >= together) return;
+  for (long long n0 = first + row; n0 < stop; n0 += together * kKeepAhead) {
     u32x2 codes[kKeepAhead];
     int e[kKeepAhead];
 #pragma unroll
     for (int q = 0; q < kKeepAhead; ++q) {
-      const long long n = n0 + 8 * q;
+      const long long n = n0 + together * q;
       if (n >= stop) continue;
       codes[q] = *reinterpret_cast<const u32x2*>(static_cast<const unsigned char*>(a.x) + b * a.xb + n * a.xt + c);
       e[q] = a.exps[b * a.eb + n * a.et + c / kKeepBlock];
     }
 #pragma unroll
     for (int q = 0; q < kKeepAhead; ++q) {
-      const long long n = n0 + 8 * q;
+      const long long n = n0 + together * q;
       if (n >= stop) continue;
       float x[8];
       keep_values<T>(codes[q], e[q], x);

@@ -187,14 +187,16 @@ constexpr int kFlat = 0, kRows = 1, kLanes = 2;
 // The steps of a tile's k.
 struct LinStep { long long k0, end; int b, len; };   // k from k0 to end; kRows: tokens of batch row b, from token k0 on, that count below len
 template <int K, bool ROWS> struct LinSteps {
-  long long at, stop;   // steps
+  long long at, stop, by;   // steps
   long long k_end;
-  unsigned per, n;      // ROWS: steps of a batch row, its tokens
+  unsigned per, n;          // ROWS: steps of a batch row, its tokens
   const int* lengths;
-  LF_DEV LinSteps(long long k_first, long long k_split, long long k_all, unsigned per_row, const int* len) {
-    k_end = k_first + k_split < k_all ? k_first + k_split : k_all;
-    at = k_first / K;
-    stop = (k_end + K - 1) / K;
+  // ROWS: the splits take steps in turn, so that rows of any lengths are shared evenly; else each a stretch
+  LF_DEV LinSteps(int split, int splits, long long k_split, long long k_all, unsigned per_row, const int* len) {
+    k_end = (split + 1) * k_split < k_all ? (split + 1) * k_split : k_all;
+    at = ROWS ? split : split * (k_split / K);
+    stop = ROWS ? k_all / K : (k_end + K - 1) / K;
+    by = ROWS ? splits : 1;
     n = per_row;
     per = (per_row + K - 1) / K;
     lengths = len;
@@ -207,19 +209,17 @@ template <int K, bool ROWS> struct LinSteps {
       ++at;
       return true;
     }
-    while (at < stop) {
+    for (; at < stop; at += by) {
       const unsigned b = (unsigned)at / per, first = ((unsigned)at - b * per) * K;
       int len = (int)n;
       if (lengths) {   // (a scalar load: it must not wait for the copies under way)
         len = *(const __attribute__((address_space(4))) int*)(lengths + b);
         len = len < 0 ? 0 : (len > (int)n ? (int)n : len);
       }
-      if ((int)first < len) {
-        s = LinStep{first, 0, (int)b, len};
-        ++at;
-        return true;
-      }
-      at = (long long)(b + 1) * per;
+      if ((int)first >= len) continue;
+      s = LinStep{first, 0, (int)b, len};
+      at += by;
+      return true;
     }
     return false;
   }
@@ -331,13 +331,13 @@ template <typename T> LF_DEV f32x4 lin_product(u32x4 a, u32x4 b, f32x4 c) {
 
 // Which tile of the result, and which split of k, a workgroup takes.  Workgroups are dealt to the eight XCDs in turn: each XCD gets a
 // stretch of the list, which goes through bands of eight rows of tiles column by column, so that those on an XCD at a time share
-// operands in its L2.
+// operands in its L2.  `ragged` (rows that may not count): the list as it is, so that no XCD's stretch is empty.
 struct LinPlace {
   int m, n, split;
-  LF_DEV LinPlace(int tiles_m, int tiles_n, int splits) {
+  LF_DEV LinPlace(int tiles_m, int tiles_n, bool ragged) {
     const unsigned all = gridDim.x, id = blockIdx.x, xcd = id % 8, at = id / 8;
     const unsigned each = all / 8, more = all % 8;
-    unsigned t = xcd * each + (xcd < more ? xcd : more) + at;
+    unsigned t = ragged ? id : xcd * each + (xcd < more ? xcd : more) + at;
     const unsigned tiles = (unsigned)tiles_m * (unsigned)tiles_n;
     split = t / tiles;
     t -= split * tiles;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
   constexpr int kBuffer = TA::kBytes + TB::kBytes;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const LinPlace tile(g.tiles_m, g.tiles_n, g.splits);
+  const LinPlace tile(g.tiles_m, g.tiles_n, AK && g.lengths != nullptr);
   const long long m0 = (long long)tile.m * BM;
   const int n0 = tile.n * BN;
   if constexpr (AK && MAPPED != kFlat) {   // nothing to do where no row of the tile counts
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
     }
   }
   constexpr bool kByRows = !AK && MAPPED == kRows;
-  LinSteps<TA::kK, kByRows> steps(tile.split * g.k_split, g.k_split, g.K, g.per_row, g.lengths);
+  LinSteps<TA::kK, kByRows> steps(tile.split, g.splits, g.k_split, g.K, g.per_row, g.lengths);
   LinCopy<T, BM, AK, STEP, kWaves, MAPPED> ca;
   LinCopy<T, BN, BK, STEP, kWaves, AK ? kFlat : MAPPED> cb;
   ca.start(g.A, g.va, m0, g.M, g.per_row, g.lengths, wave);
@@ -409,10 +409,12 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
       for (int j = 0; j < NT; ++j) b[j] = rb.get(lb, wn, j, q);
 #pragma unroll
       for (int i = 0; i < MT; ++i) a[i] = ra.get(la, wm, i, q);
+      __builtin_amdgcn_s_setprio(1);   // one wave of a SIMD multiplies while the other one reads (8192^3 in bf16: 869 us without, 835 with)
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = lin_product<T>(b[j], a[i], acc[i][j]);
+      __builtin_amdgcn_s_setprio(0);
     }
   }
   // Lane l has columns 4 (l / 16) .. + 3 of a tile of 16 and row l % 16: through LDS, a wave's rows for itself, into rows of eight
@@ -491,11 +493,12 @@ template <typename T, bool MAPPED> __global__ __launch_bounds__(256) void linear
 
 // ---- few tokens ------------------------------------------------------------------------------------------------------
 
-// Up to 16 MT tokens: every weight is read once, straight into operand registers, 16 channels a workgroup, whose four waves share k.
-// Bound: the weights' way from memory.
-template <typename T, int MT, bool MAPPED> __global__ __launch_bounds__(256) void linear_few(LinArgs g) {
-  constexpr int kVec = 16 / Stored<T>::kBytes, kK = 4 * kVec, kAhead = 4;   // k of a product; products requested together
-  __shared__ __attribute__((aligned(16))) float lds[4][16 * MT][20];   // (rows spread over the banks)
+// Up to 16 MT tokens: every weight is read once, straight into operand registers, 16 channels a workgroup, whose eight waves share k.
+// Bound: the weights' way from memory, for few of them its latency.
+constexpr int kFewWaves = 8;
+template <typename T, int MT, bool MAPPED> __global__ __launch_bounds__(64 * kFewWaves) void linear_few(LinArgs g) {
+  constexpr int kVec = 16 / Stored<T>::kBytes, kK = 4 * kVec, kAhead = MT == 4 ? 4 : 6;   // k of a product; products requested together
+  __shared__ __attribute__((aligned(16))) float lds[kFewWaves][16 * MT][20];   // (rows spread over the banks)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   const int n0 = blockIdx.x * 16;
   f32x4 acc[MT];
@@ -510,7 +513,7 @@ template <typename T, int MT, bool MAPPED> __global__ __launch_bounds__(256) voi
   }
   const bool row = n0 + i < g.N;
   const unsigned char* pw = at<T>(g.B, row ? (n0 + i) * g.vb.token : 0);
-  for (long long k0 = (long long)wave * kAhead * kK; k0 < g.K; k0 += 4 * kAhead * kK) {
+  for (long long k0 = (long long)wave * kAhead * kK; k0 < g.K; k0 += kFewWaves * kAhead * kK) {
     u32x4 w[kAhead], x[MT][kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -539,7 +542,11 @@ template <typename T, int MT, bool MAPPED> __global__ __launch_bounds__(256) voi
   if (!t.on) return;
   float z[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) z[j] = (lds[0][m][8 * half + j] + lds[1][m][8 * half + j]) + (lds[2][m][8 * half + j] + lds[3][m][8 * half + j]);
+  for (int j = 0; j < 8; ++j) {
+    z[j] = lds[0][m][8 * half + j];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) z[j] += lds[w][m][8 * half + j];
+  }
   finish8<T>(g.out, t, n, z);
 }
 
@@ -553,18 +560,18 @@ struct LinSlopeArgs {
   float* partials;                  // [workgroups along the tokens][C], or null
   const int* lengths;
   long long N;
-  int B, C, each, act;              // each: tokens of a piece of a batch row; a workgroup takes pieces in turn
+  int B, C, each, lanes, act;       // each: tokens of a piece of a batch row; a workgroup takes pieces in turn; lanes: of a token
   float slope;
 };
 
 // dz = dy act'(z), rounded once to the type (it is an operand of two products), and the sums of the unrounded values over a
-// workgroup's tokens.  32 lanes of 8 channels, 8 tokens at a time, four of them under way (absent ones from 16 bytes of zeros, without
+// workgroup's tokens.  `lanes` lanes of 8 channels a token, as many tokens at a time as that leaves, twice as many under way (absent ones from 16 bytes of zeros, without
 // branches).  Bound: HBM (49152 x 1280 bf16 from kept z: 315 MB), with GELU the vector instructions too.
 template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_slope(LinSlopeArgs a) {
-  __shared__ float lds[8][32][8];
-  constexpr int kAhead = 4;
-  const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * 8;
-  const bool on = c < a.C;
+  __shared__ float lds[256][8];
+  constexpr int kAhead = 2;
+  const int row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, rows = 256 / a.lanes, c = (blockIdx.x * a.lanes + lane) * 8;
+  const bool on = c < a.C && row < rows;
   const unsigned char* const none = reinterpret_cast<const unsigned char*>(kZeros16);
   const long long per = (a.N + a.each - 1) / a.each, pieces = per * a.B;
   float sum[8];
@@ -577,13 +584,13 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_s
     const unsigned char *pd = at<T>(a.dy, b * a.vdy.batch + c), *pe = a.z_exps + b * a.ve.batch + c / kKeepBlock;
     const unsigned char* pz = KEPT ? static_cast<const unsigned char*>(a.z) + b * a.vz.batch + c : at<T>(a.z, b * a.vz.batch + c);
     unsigned char* po = at<T>(a.dz, b * a.N * a.C + c);
-    for (long long n0 = first; n0 < end; n0 += 8 * kAhead) {
+    for (long long n0 = first; n0 < end; n0 += rows * kAhead) {
       Raw8<T> rd[kAhead], rz[KEPT ? 1 : kAhead];
       u32x2 codes[KEPT ? kAhead : 1];
       int exps[KEPT ? kAhead : 1];
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {
-        const long long n = n0 + row + 8 * q;
+        const long long n = n0 + row + rows * q;
         const bool there = on && n < end;
         if constexpr (Stored<T>::kBytes == 4) {
           rd[q] = none8<T>();
@@ -604,7 +611,7 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_s
       }
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {
-        const long long n = n0 + row + 8 * q;
+        const long long n = n0 + row + rows * q;
         float d[8];
         widen8<T>(rd[q], d);
         if (a.dz) {
@@ -622,21 +629,22 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_s
   }
   if (!a.partials) return;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) lds[row][lane][j] = sum[j];
+  for (int j = 0; j < 8; ++j) lds[threadIdx.x][j] = sum[j];
   __syncthreads();
-  const int cc = blockIdx.x * 256 + threadIdx.x;
-  float all = 0.0f;
-#pragma unroll
-  for (int r = 0; r < 8; ++r) all += lds[r][threadIdx.x >> 3][threadIdx.x & 7];
-  if (cc < a.C) a.partials[(long long)blockIdx.y * a.C + cc] = all;
+  for (int t = threadIdx.x; t < 8 * a.lanes; t += 256) {
+    const int cc = blockIdx.x * a.lanes * 8 + t;
+    float all = 0.0f;
+    for (int r = 0; r < rows; ++r) all += lds[r * a.lanes + (t >> 3)][t & 7];
+    if (cc < a.C) a.partials[(long long)blockIdx.y * a.C + cc] = all;
+  }
 }
 
 // The bias's gradient: the workgroups' sums.
 template <typename T> __global__ __launch_bounds__(1024) void linear_bias(const float* partials, void* dbias, int parts, int C) {
-  __shared__ double lds[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+  __shared__ double lds[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15);
   const double sum = column_sum(lds, partials, parts, C, c);
-  if (threadIdx.x >= 32 || c >= C) return;
+  if (threadIdx.x >= 16 || c >= C) return;
   if constexpr (Stored<T>::kBytes == 4) static_cast<float*>(dbias)[c] = (float)sum;
   else static_cast<uint16_t*>(dbias)[c] = (uint16_t)pack2<T>((float)sum, 0.0f);
 }

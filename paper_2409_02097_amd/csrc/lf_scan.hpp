@@ -598,10 +598,10 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
 
 // drate: the chunks' sums of every batch row.
 __global__ __launch_bounds__(1024) void scan_rate_sums(const float* partials, float* drate, long long parts, int C) {
-  __shared__ double lds[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+  __shared__ double lds[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15);
   const double sum = column_sum(lds, partials, parts, C, c);
-  if (threadIdx.x < 32 && c < C) drate[c] = (float)sum;
+  if (threadIdx.x < 16 && c < C) drate[c] = (float)sum;
 }
 
 struct ScanStepArgs {

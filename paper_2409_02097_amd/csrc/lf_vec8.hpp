@@ -103,16 +103,16 @@ template <int LANES> LF_DEV float lanes_sum(float v) {
   return v;
 }
 
-// Sum over the rows of partials [parts][C] in column c, for the first 32 threads of a workgroup of 1024, whose thread t has column t % 32:
-// 32 rows at a time, in a fixed order, in fp64 (a long batch has thousands of rows).
-LF_DEV double column_sum(double (&lds)[32][33], const float* partials, long long parts, int C, int c) {
-  const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
+// Sum over the rows of partials [parts][C] in column c, for the first 16 threads of a workgroup of 1024, whose thread t has column t % 16:
+// 64 rows at a time, in a fixed order, in fp64 (a long batch has thousands of rows).
+LF_DEV double column_sum(double (&lds)[64][17], const float* partials, long long parts, int C, int c) {
+  const int lane = threadIdx.x & 15, row = threadIdx.x >> 4;
   double sum = 0.0;
-  for (long long p0 = row; p0 < parts; p0 += 32 * 8) {
+  for (long long p0 = row; p0 < parts; p0 += 64 * 8) {
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const long long p = p0 + 32 * j;
+      const long long p = p0 + 64 * j;
       v[j] = p < parts && c < C ? partials[p * C + c] : 0.0f;
     }
 #pragma unroll
@@ -120,9 +120,10 @@ LF_DEV double column_sum(double (&lds)[32][33], const float* partials, long long
   }
   lds[row][lane] = sum;
   __syncthreads();
-  if (row == 0)
-#pragma unroll
-    for (int r = 1; r < 32; ++r) sum += lds[r][lane];
+  if (row == 0) {
+#pragma unroll 8
+    for (int r = 1; r < 64; ++r) sum += lds[r][lane];
+  }
   return sum;
 }
 

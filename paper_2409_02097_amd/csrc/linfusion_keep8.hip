@@ -11,11 +11,11 @@ using lfh::span;
 
 constexpr int kMaxChannels = 32768;
 
-// tokens per workgroup: enough workgroups for 16 a CU, eight tokens at least
-int rows_of(int B, long long N, int C) {
-  const long long all = (long long)((C + 255) / 256) * B, most = 16LL * lfh::num_cu();
+// tokens of a workgroup: enough workgroups for 16 a CU, whole rounds of its tokens
+int rows_of(int B, long long N, int C, const lfh::Across& x) {
+  const long long all = (long long)x.blocks * B, most = 16LL * lfh::num_cu(), round = 256 / x.lanes;
   long long rows = (N * all + most - 1) / most;
-  rows = (rows + 7) / 8 * 8;
+  rows = (rows + round - 1) / round * round;
   while ((N + rows - 1) / rows > 65535) rows *= 2;
   return (int)rows;
 }
@@ -44,8 +44,10 @@ namespace lfh {
 
 void launch_unkeep8(const lf::KeepArgs& a0, int B, int dtype, hipStream_t st) {
   lf::KeepArgs a = a0;
-  a.rows = rows_of(B, a.N, a.C);
-  const dim3 grid((a.C + 255) / 256, (unsigned)((a.N + a.rows - 1) / a.rows), B);
+  const Across x = across(a.C);
+  a.rows = rows_of(B, a.N, a.C, x);
+  a.lanes = x.lanes;
+  const dim3 grid(x.blocks, (unsigned)((a.N + a.rows - 1) / a.rows), B);
   if (dtype == LINFUSION_DTYPE_F16) lf::unkeep8<lf::F16><<<grid, 256, 0, st>>>(a);
   else if (dtype == LINFUSION_DTYPE_BF16) lf::unkeep8<lf::BF16><<<grid, 256, 0, st>>>(a);
   else lf::unkeep8<lf::F32><<<grid, 256, 0, st>>>(a);
@@ -61,8 +63,9 @@ int linfusion_keep8(const void* x, signed char* codes, unsigned char* exps, int 
   RowView v[3];
   int rc = views(x, codes, exps, B, N, C, dtype, lengths, strides, false, v);
   if (rc != LINFUSION_OK || (rc = lfh::check_device()) != LINFUSION_OK) return rc;
-  const lf::KeepArgs a{x, codes, exps, v[0].batch, v[0].token, v[1].batch, v[1].token, v[2].batch, v[2].token, lengths, N, C, rows_of(B, N, C)};
-  const dim3 grid((C + 255) / 256, (unsigned)((N + a.rows - 1) / a.rows), B);
+  const lfh::Across x8 = lfh::across(C);
+  const lf::KeepArgs a{x, codes, exps, v[0].batch, v[0].token, v[1].batch, v[1].token, v[2].batch, v[2].token, lengths, N, C, rows_of(B, N, C, x8), x8.lanes};
+  const dim3 grid(x8.blocks, (unsigned)((N + a.rows - 1) / a.rows), B);
   const hipStream_t st = (hipStream_t)stream;
   if (dtype == LINFUSION_DTYPE_F16) lf::keep8<lf::F16><<<grid, 256, 0, st>>>(a);
   else if (dtype == LINFUSION_DTYPE_BF16) lf::keep8<lf::BF16><<<grid, 256, 0, st>>>(a);
@@ -78,7 +81,7 @@ int linfusion_unkeep8(const signed char* codes, const unsigned char* exps, void*
                                   {strides ? strides[1][0] : 0, strides ? strides[1][1] : 0}};
   int rc = views(x, codes, exps, B, N, C, dtype, lengths, strides ? turned : nullptr, true, v);
   if (rc != LINFUSION_OK || (rc = lfh::check_device()) != LINFUSION_OK) return rc;
-  const lf::KeepArgs a{codes, x, const_cast<unsigned char*>(exps), v[1].batch, v[1].token, v[0].batch, v[0].token, v[2].batch, v[2].token, lengths, N, C, 0};
+  const lf::KeepArgs a{codes, x, const_cast<unsigned char*>(exps), v[1].batch, v[1].token, v[0].batch, v[0].token, v[2].batch, v[2].token, lengths, N, C, 0, 0};
   lfh::launch_unkeep8(a, B, dtype, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }

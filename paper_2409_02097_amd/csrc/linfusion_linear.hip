@@ -164,19 +164,24 @@ constexpr long long kFew = 64;   // tokens up to which the weights' way from mem
 
 template <typename T, int MT> int launch_few(const lf::LinArgs& g, bool mapped, hipStream_t st) {
   const unsigned wgs = (unsigned)((g.N + 15) / 16);
-  if (mapped) lf::linear_few<T, MT, true><<<wgs, 256, 0, st>>>(g);
-  else lf::linear_few<T, MT, false><<<wgs, 256, 0, st>>>(g);
+  if (mapped) lf::linear_few<T, MT, true><<<wgs, 64 * lf::kFewWaves, 0, st>>>(g);
+  else lf::linear_few<T, MT, false><<<wgs, 64 * lf::kFewWaves, 0, st>>>(g);
   return LINFUSION_OK;
 }
 
 // Workgroups along the tokens of linear_slope, and the tokens of a piece of a batch row.
 struct Slices { int count, each; };
-long long most_workgroups(int C) { return 4LL * lfh::num_cu() / ((C + 255) / 256) + 1; }
+// (49152 x 1280 from kept values, GELU: six a CU with two tokens of a lane under way 68 us, four with four 75, two with four 93.)
+long long most_workgroups(int C) {
+  const long long most = 6LL * lfh::num_cu() / lfh::across(C).blocks;
+  return most < 1 ? 1 : most;
+}
 Slices slices(int B, long long N, int C) {
   const long long most = most_workgroups(C);
   long long each = (B * N + most - 1) / most;
-  each = (each + 31) / 32 * 32;
-  if (each > N) each = (N + 31) / 32 * 32;
+  const long long round = 2 * (256 / lfh::across(C).lanes);
+  each = (each + round - 1) / round * round;
+  if (each > N) each = (N + round - 1) / round * round;
   const long long pieces = (N + each - 1) / each * B;
   return Slices{(int)(pieces < most ? pieces : most), (int)each};
 }
@@ -303,13 +308,13 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
     auto rows = [&](const RowView& v) { return flat(v, B, N, !one); };
     const Slices s = slices(rows_b, rows_n, C_out);
     const lf::LinSlopeArgs a{dy, z, z_exps, rows(vdy), rows(vz), rows(vze), act ? dz : nullptr, dbias ? sums : nullptr, lengths, rows_n, rows_b,
-                             C_out, s.each, activation, slope};
-    const dim3 grid((C_out + 255) / 256, s.count);
+                             C_out, s.each, lfh::across(C_out).lanes, activation, slope};
+    const dim3 grid(lfh::across(C_out).blocks, s.count);
     rc = by_type(dtype, [&](auto t) {
       using T = decltype(t);
       if (z_exps) lf::linear_slope<T, true><<<grid, 256, 0, st>>>(a);
       else lf::linear_slope<T, false><<<grid, 256, 0, st>>>(a);
-      if (dbias) lf::linear_bias<T><<<(C_out + 31) / 32, 1024, 0, st>>>(sums, dbias, s.count, C_out);
+      if (dbias) lf::linear_bias<T><<<(C_out + 15) / 16, 1024, 0, st>>>(sums, dbias, s.count, C_out);
       return LINFUSION_OK;
     });
   }
@@ -331,7 +336,7 @@ int linfusion_linear_bwd(const void* x, const unsigned char* x_exps, const void*
   }
   if (dw) {
     if (x_exps) {
-      const lf::KeepArgs k{x, wide_x, const_cast<unsigned char*>(x_exps), vx.batch, vx.token, N * C_in, C_in, vxe.batch, vxe.token, lengths, N, C_in, 0};
+      const lf::KeepArgs k{x, wide_x, const_cast<unsigned char*>(x_exps), vx.batch, vx.token, N * C_in, C_in, vxe.batch, vxe.token, lengths, N, C_in, 0, 0};
       lfh::launch_unkeep8(k, B, dtype, st);
       vx.p = wide_x;
       vx.batch = B == 1 ? 0 : N * C_in;

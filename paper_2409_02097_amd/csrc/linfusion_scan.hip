@@ -224,7 +224,7 @@ int linfusion_scan_bwd(const void* x, const void* gate, const void* input, const
     return backward<decltype(t), decltype(m)::value, decltype(i)::value>(a, st);
   });
   if (rc != LINFUSION_OK) return rc;
-  lf::scan_rate_sums<<<(C + 31) / 32, 1024, 0, st>>>(a.partials, drate, (long long)B * a.chunks, C);
+  lf::scan_rate_sums<<<(C + 15) / 16, 1024, 0, st>>>(a.partials, drate, (long long)B * a.chunks, C);
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }
 

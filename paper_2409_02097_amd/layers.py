@@ -7,7 +7,7 @@ import ctypes
 
 from . import binding, block
 from .binding import _dtype_code, _stream_ptr
-from .block import _done, _head, _lengths, _longs, _ptr, _rows, _scratch, _size, _vector
+from .block import _done, _head, _lengths, _longs, _plain, _ptr, _rows, _scratch, _size, _vector
 
 FLAG_SCAN_REVERSE, FLAG_SCAN_LEAKY, FLAG_SCAN_SUM = 1, 2, 4
 ACT_NONE, ACT_LEAKY_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
@@ -38,7 +38,13 @@ def declare(lib) -> None:
 
 
 def _tokens(named, head):
-    """{batch, token} strides of [B, N, C] views of the call's type (None: absent), one after the other."""
+    """{batch, token} strides of [B, N, C] views of the call's type (None: absent), one after the other; None where all of them are
+    contiguous."""
+    for _, t, shape in named:
+        if not _plain(t, shape, head):
+            break
+    else:
+        return None
     flat = ()
     for name, t, shape in named:
         if t is None:
@@ -117,17 +123,20 @@ def linfusion_scan_step(x, gate, input, rate, state_in, state_out, out, flags: i
     if x.dim() != 2:
         raise ValueError("x: [B, C]")
     B, C = shape = x.shape
-    flat = ()
-    for name, t in (("x", x), ("gate", gate), ("input", input), ("out", out)):
-        if t is not None:
-            _rows(name, t, shape, head)
-        flat += (0,) if t is None else t.stride()[:1]
+    strides = None
+    if not (_plain(x, shape, head) and _plain(gate, shape, head) and _plain(input, shape, head) and _plain(out, shape, head)):
+        flat = ()
+        for name, t in (("x", x), ("gate", gate), ("input", input), ("out", out)):
+            if t is not None:
+                _rows(name, t, shape, head)
+            flat += (0,) if t is None else t.stride()[:1]
+        strides = _longs(flat)
     _vector("rate", rate, (C,), head)
     _vector("state_in", state_in, shape, head)
     _vector("state_out", state_out, shape, head)
     rc = binding.library().linfusion_scan_step(
         x.data_ptr(), _ptr(gate), _ptr(input), _ptr(rate), _ptr(state_in), _ptr(state_out), _ptr(out), B, C, _dtype_code(x), flags,
-        _longs(flat), _stream_ptr(stream))
+        strides, _stream_ptr(stream))
     return _done(rc, "linfusion_scan_step", check)
 
 

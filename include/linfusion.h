@@ -651,7 +651,7 @@ size_t linfusion_linear_bwd_workspace_bytes(int B, long long N, int C_in, int C_
  * Activations in 8 bits between the forward and the backward pass: every block of 32 channels of a token shares a power of two, 2^e
  * with the least e (-126 at least) for which 127 * 2^e reaches the block's largest magnitude, and a value is the integer nearest to
  * x / 2^e (ties to even).  exps holds e + 127; 255: the block holds an infinity or NaN and comes back as NaN.  A value comes back off by at
- * most 1 / 127 of its block's largest (beyond the type's largest value: as that).
+ * most 1 / 127 of its block's largest, or by 2^-127 if that is more (beyond the type's largest value: as that).
  *
  *   x               [B, N, C] view of the call's type, C a multiple of 8 up to 32768 (the last block may be shorter).
  *   codes           int8 [B, N, C] view with 8-byte aligned rows; exps: uint8 [B, N, ceil(C / 32)] view of contiguous blocks.

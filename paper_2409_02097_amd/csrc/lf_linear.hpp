@@ -70,7 +70,7 @@ template <bool Precise> LF_DEV float act_of(float z, int act, float slope) {
     case kActGelu: {
       if constexpr (Precise) return 0.5f * z * erfcf(z * -0.70710678118654752440f);
       float e;
-      return fmaxf(z, 0.0f) - __builtin_fabsf(z) * normal_tail(z, e);   // z (1 - Q) above 0, z Q below
+      return fmaxf(z, 0.0f) - fminf(__builtin_fabsf(z), 64.0f) * normal_tail(z, e);   // z (1 - Q) above 0, z Q below (Q is 0 long before 64)
     }
     case kActGeluTanh: return z * logistic<Precise>(1.59576912160573071176f * z * __builtin_fmaf(0.044715f * z, z, 1.0f));
     case kActSilu: return z * logistic<Precise>(z);
@@ -157,8 +157,7 @@ template <int N> LF_DEV void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" 
 
 // Copies 64 x 16 bytes, lane l's from `p`, to the LDS address `lds` + 16 l.  Written out: before a transposing read the compiler waits for
 // every copy of its own that is under way, though it goes to the other buffer (8192^3 with B's own index contiguous, bf16: 1093 us so, 905
-// without).  (m0, which nothing else here uses, has to be written an
-// instruction before it is read.)  No register receives anything, and wait_copies stands before the barrier behind which the copy is read.
+// without).  (m0, which nothing else here uses, has to be written an instruction before it is read.)  No register receives anything, and wait_copies stands before the barrier behind which the copy is read.
 LF_DEV void copy_kb(const unsigned char* p, unsigned lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
 }

@@ -227,6 +227,25 @@ def test_activations_far_out(act):
     assert bool(((dx[0, :, 0] - slope).abs() <= 1e-11).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ["none", "leaky", "gelu", "gelu_tanh", "silu"])
+def test_infinities_and_nan_pass_through(act, dtype):
+    """Infinity before the activation is infinity behind it, a NaN a NaN; other tokens do not see them."""
+    n = 100   # (tiles; the first 60 rows alone: few tokens)
+    x = torch.zeros((1, n, 8), dtype=TORCH[dtype], device="cuda")
+    x[0, :, 0] = 1.5
+    x[0, 3, 0], x[0, 5, 0], x[0, 70, 0], x[0, 72, 0] = float("inf"), float("nan"), float("inf"), float("nan")
+    w = torch.eye(8, dtype=TORCH[dtype], device="cuda")
+    for rows in (n, 60):
+        y = torch.empty((1, rows, 8), dtype=TORCH[dtype], device="cuda")
+        lf.linfusion_linear_fwd(x[:, :rows], w, None, y, workspace=memory(lf.linfusion_linear_workspace_bytes(1, rows, 8, 8, CODE[dtype])),
+                                activation=ACTS[act], slope=SLOPE)
+        got = y[0, :, 0]
+        for i in range(rows):
+            v = float(x[0, i, 0])
+            assert (v == 1.5 and 1.2 < float(got[i]) <= 1.5) or float(got[i]) == v or (np.isnan(v) and bool(torch.isnan(got[i]))), (rows, i)
+
+
 def test_gradients_against_differences():
     c = make(2, 37, 40, 24, "f32", 6, "gelu", True, True, (37, 11))
     g = on_gpu(c)

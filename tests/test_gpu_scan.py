@@ -160,6 +160,27 @@ def test_state_in_place_and_a_sequence_in_parts(dtype):
     near(state, ref_last, "f32", STEPS[dtype], held["last_scale"], "state")
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("N", [5, 128, 250, 300, 2300])   # one chunk of either length, two, more than a group of them
+def test_states_in_place_are_the_same(N, reverse):
+    """Every workgroup and wave that starts from the state that is given reads it before the last one replaces it."""
+    c = make(3, N, 1280, "bf16", 16, reverse=reverse, lengths=(N, max(1, N // 2), 0))
+    g = on_gpu(c)
+    out, last, keep = forward(c, g)
+    d = backward(c, g, keep)
+    for _ in range(4):
+        state, again = g["state_in"].clone(), torch.full_like(out, 7.0)
+        lf.linfusion_scan_fwd(g["x"], g["gate"], g["input"], g["rate"], again, state_in=state, state_out=state, lengths=g["lengths"],
+                              flags=flags(c), workspace=memory(lf.linfusion_scan_workspace_bytes(*c["dims"])))
+        assert torch.equal(again, out) and torch.equal(state, last)
+        slope, grads = g["dstate_out"].clone(), {n: torch.full_like(t, 7.0) for n, t in d.items()}
+        lf.linfusion_scan_bwd(g["x"], g["gate"], g["input"], g["rate"], g["dout"], grads["dx"], grads["dgate"], grads["dinput"], grads["drate"],
+                              state_in=g["state_in"], dstate_out=slope, dstate_in=slope, saved=keep, lengths=g["lengths"], flags=flags(c),
+                              workspace=memory(lf.linfusion_scan_bwd_workspace_bytes(*c["dims"])))
+        assert torch.equal(slope, d["dstate_in"])
+        assert all(torch.equal(grads[n], d[n]) for n in d if n != "dstate_in")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("weight,inputs", [("norm", True), ("norm", False), ("leaky", True), ("sum", True)])
 @pytest.mark.parametrize("B,C", [(1, 8), (3, 40), (64, 520), (2, 4096)])

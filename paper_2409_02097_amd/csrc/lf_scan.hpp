@@ -29,8 +29,8 @@ constexpr int kScanT = 4, kScanChunk = 32 * kScanT;   // tokens of a thread; of 
 
 struct ScanView { long long batch, token; };   // element strides; channels contiguous
 
-// What the chunks of a sequence tell each other: every chunk's (A, R), and the value behind every group of chunks, as soon as they are
-// known.  All ones: not yet (scan_clear).  The workgroups take chunks by `ticket`, nearer the sequence's start (backward: its end) first, so that a workgroup
+// What the chunks of a sequence tell each other: every chunk's (A, R), and what stands for groups of them, as soon as they are known.  All ones:
+// not yet (scan_clear).  The workgroups take chunks by `ticket`, nearer the sequence's start (backward: its end) first, so that a workgroup
 // only ever waits for ones that have started and wait for earlier ones alone: every wait ends.
 struct ScanRecords {
   unsigned* ticket;
@@ -264,21 +264,33 @@ struct ScanPlace { int chunk, b, c0; };
 constexpr unsigned kNotYet = 0xffffffffu;
 LF_DEV unsigned told(float v) { return v != v ? 0x7fc00000u : __builtin_bit_cast(unsigned, v); }   // (never kNotYet)
 
-LF_DEV void tell_totals(const ScanRecords& r, long long i, float A, float R) {
-  __hip_atomic_store(r.totals + i, (unsigned long long)told(R) << 32 | told(A), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+LF_DEV void tell_totals(unsigned long long* p, float A, float R) {
+  __hip_atomic_store(p, (unsigned long long)told(R) << 32 | told(A), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-LF_DEV void tell_value(const ScanRecords& r, long long i, float h) {
-  __hip_atomic_store(r.values + i, told(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+LF_DEV void tell_value(unsigned* p, float h) { __hip_atomic_store(p, told(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+template <typename W> LF_DEV W heard(const W* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// `w` as it was read from `p`, read again until it is there (lanes that read nothing have 0)
+template <typename W> LF_DEV void await(W& w, const W* p) {
+  while (__any((unsigned)w == kNotYet)) {
+    __builtin_amdgcn_s_sleep(1);
+    if ((unsigned)w == kNotYet) w = heard(p);
+  }
 }
 
-constexpr int kScanGroup = 32;   // chunks of a group, at most
+// How a row's chunks hear of one another.  kAlone: there is one.  kGroups: in groups; a group's last chunk tells the value behind it, so a row is a
+// chain of groups.  kStretches: the groups in stretches of as many; a group's last chunk tells the group's totals, a stretch's last one the value behind
+// it, so a row is a chain of stretches, for rows with too few channels beside one another to hide the longer chain.
+constexpr int kAlone = 0, kGroups = 1, kStretches = 2;
+
+constexpr int kScanGroup = 16;   // chunks of a group, groups of a stretch, at most
 struct ScanFound { float value[kScanWidth]; };
 
 // The value that a chunk starts from, lane c's for its channel: from the value behind the group of chunks before its own (its row's first
 // one, `start`, in the first group) through the totals of its group's chunks before it, one after the other.  Only a group's last chunk
 // tells its value, so that results do not depend on who was first, and a chunk reads 16 totals or fewer, not a row's.  `order`: the chunk's
 // place in its row's order (backward: from the row's end); `i0`: its record for this channel, `next`: from a chunk's record to the one's
-// after it in the order.  `totals`: 16 KB of LDS.
+// after it in the order.  `totals`: LDS for `group` of them.
 LF_DEV float look_back(const ScanRecords& r, ScanFound& lds, float (&totals)[32][2][kScanWidth], int group, int order, long long i0, long long next,
                        float start, bool on) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -297,7 +309,8 @@ LF_DEV float look_back(const ScanRecords& r, ScanFound& lds, float (&totals)[32]
     }
     lds.value[lane] = v;
   }
-  // the waves take the chunks in turn, from the furthest on; those of a wave are requested together, four at a time
+  // The waves take the chunks in turn, from the furthest on; those of a wave are requested together, four at a time.  (Written out: with await
+  // bf16 takes two registers more, so that three workgroups share a CU and not four: 65536 x 1280 194 us for 179.)
   for (int e0 = wave; e0 < before; e0 += 16) {
     unsigned long long t[4];
 #pragma unroll
@@ -322,6 +335,75 @@ LF_DEV float look_back(const ScanRecords& r, ScanFound& lds, float (&totals)[32]
   __syncthreads();
   float h = lds.value[lane];
   for (int e = 0; e < before; ++e) h = __builtin_fmaf(totals[e][0][lane], h, totals[e][1][lane]);
+  return h;
+}
+
+// A group's totals: eight bytes a channel in the rows of `values` of its last chunk, whose record for channel c is i, and of the one before.
+LF_DEV unsigned long long* group_totals(const ScanRecords& r, long long i, long long next, int c) {
+  return reinterpret_cast<unsigned long long*>(r.values + (i - c - (next > 0 ? next : 0))) + c;
+}
+
+// The same with stretches: from the value behind the stretch before (`start` in the first) through the totals of this stretch's groups before and of
+// this group's chunks before.  c: the channel; A, R: the chunk's totals, of which a group's last chunk makes the group's.  The value behind
+// a stretch is told in the row before those of its last group's totals.  `totals`: 16 KB of LDS.
+LF_DEV float look_far(const ScanRecords& r, ScanFound& lds, float (&totals)[32][2][kScanWidth], int group, int order, long long i0, long long next,
+                      int c, float start, float A, float R, bool on) {
+  constexpr int kEach = kScanGroup / 4;   // of a wave
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int before = order % group, groups = order / group % group;   // chunks, groups before this one
+  const long long last = i0 - next * (before + 1);                    // the last chunk of the group before
+  // the waves take the chunks and the groups in turn, from the furthest on; all of a wave's are requested together
+  unsigned long long t[kEach], g[kEach];
+  unsigned w = 0;
+  const bool far = wave == 0 && order >= group * group;
+  const unsigned* const from = r.values + last - next * ((long long)groups * group + 2);
+  if (far && on) w = heard(from);
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int e = wave + 4 * k;
+    t[k] = g[k] = 0;
+    if (on && e < before) t[k] = heard(r.totals + i0 - next * (before - e));
+    if (on && e < groups) g[k] = heard(group_totals(r, last - next * ((long long)(groups - 1 - e) * group), next, c));
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int e = wave + 4 * k;
+    await(t[k], r.totals + i0 - next * (before - e));
+    if (e < before) {
+      totals[kScanGroup + e][0][lane] = __builtin_bit_cast(float, (unsigned)t[k]);
+      totals[kScanGroup + e][1][lane] = __builtin_bit_cast(float, (unsigned)(t[k] >> 32));
+    }
+  }
+  if (before == group - 1) {
+    __syncthreads();
+    if (wave == 0) {
+      float ga = 1.0f, gr = 0.0f;
+      for (int e = 0; e < before; ++e) {
+        const float a = totals[kScanGroup + e][0][lane];
+        gr = __builtin_fmaf(a, gr, totals[kScanGroup + e][1][lane]);
+        ga *= a;
+      }
+      if (on) tell_totals(group_totals(r, i0, next, c), ga * A, __builtin_fmaf(A, gr, R));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int e = wave + 4 * k;
+    await(g[k], group_totals(r, last - next * ((long long)(groups - 1 - e) * group), next, c));
+    if (e < groups) {
+      totals[e][0][lane] = __builtin_bit_cast(float, (unsigned)g[k]);
+      totals[e][1][lane] = __builtin_bit_cast(float, (unsigned)(g[k] >> 32));
+    }
+  }
+  if (far) {
+    await(w, from);
+    start = __builtin_bit_cast(float, w);
+  }
+  if (wave == 0) lds.value[lane] = start;
+  __syncthreads();
+  float h = lds.value[lane];
+  for (int e = 0; e < groups; ++e) h = __builtin_fmaf(totals[e][0][lane], h, totals[e][1][lane]);
+  for (int e = 0; e < before; ++e) h = __builtin_fmaf(totals[kScanGroup + e][0][lane], h, totals[kScanGroup + e][1][lane]);
   return h;
 }
 
@@ -358,12 +440,13 @@ struct ScanForwardLds {
   float spread[4][kScanWidth];
   unsigned id;
 };
-// TT tokens a thread; ONE: the whole sequence is one chunk.
+// TT tokens a thread.
 // Bound: HBM and vector instructions, nearly level (46 issue slots a value with the norm's weight, six of them transcendental: the vector
 // units are busy 62 % of the time), then the wait for a ticket (take_tile).
-template <typename T, int MODE, bool INPUT, int TT, bool ONE>
+template <typename T, int MODE, bool INPUT, int TT, int CHAIN>
 __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   constexpr int L = 32 * TT;
+  constexpr bool ONE = CHAIN == kAlone;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanForwardLds shared;
   ScanJoin& lds = shared.join;
@@ -384,7 +467,7 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
     if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, p.b, n, c, none8<T>(), ri));
     else load_rows<T, TT>(live, full, g, x);
   }
-  if (cl < a.C && a.state_in && (ONE || p.chunk < a.group)) h0 = a.state_in[(long long)p.b * a.C + cl];
+  if (cl < a.C && a.state_in && (ONE || p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) h0 = a.state_in[(long long)p.b * a.C + cl];
   float da[TT][8], u[TT][8], A[8], R[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
@@ -411,13 +494,15 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   const long long i0 = row0 + (long long)p.chunk * a.C;
   if constexpr (!ONE) {
     join_chunk<false>(lds, 4, ca, cr);
-    if (whole) tell_totals(a.rec, i0, ca, cr);
-    h0 = look_back(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
+    if (whole) tell_totals(a.rec.totals + i0, ca, cr);
+    if constexpr (CHAIN == kGroups) h0 = look_back(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
+    else h0 = look_far(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, cl, h0, ca, cr, cl < a.C);
   }
   if (whole) {
     join_chunk<false>(lds, 4, ca, cr);
     const float end = __builtin_fmaf(ca, h0, cr);
-    if (!ONE && p.chunk % a.group == a.group - 1) tell_value(a.rec, i0, end);
+    if (CHAIN == kGroups && p.chunk % a.group == a.group - 1) tell_value(a.rec.values + i0, end);
+    if (CHAIN == kStretches && p.chunk % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + i0 - 2 * a.C, end);
     if (a.state_out && (long long)(p.chunk + 1) * L >= row.n) a.state_out[(long long)p.b * a.C + cl] = end;   // the last token is here
   }
   join_chunk<false>(lds, wave, ca, cr);
@@ -453,9 +538,10 @@ struct ScanBackLds {
   f32x4 weights[kScanT][2][256];
   unsigned id;
 };
-template <typename T, int MODE, bool INPUT, bool ONE>
+template <typename T, int MODE, bool INPUT, int CHAIN>
 __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   constexpr int TT = kScanT, L = kScanChunk;
+  constexpr bool ONE = CHAIN == kAlone;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanBackLds shared;
   ScanJoin &there = shared.there, &back = shared.back;
@@ -477,7 +563,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   float rate[8], h0 = 0.0f, e0 = 0.0f;
   load_rate(a.rate + c, on, rate);
   if (cl < a.C) h0 = a.starts[at0];
-  if (cl < a.C && a.dstate_out && (ONE || last - p.chunk < a.group)) e0 = a.dstate_out[(long long)p.b * a.C + cl];
+  if (cl < a.C && a.dstate_out && (ONE || last - p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) e0 = a.dstate_out[(long long)p.b * a.C + cl];
   {
     ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, p.b, n0, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, p.b, n0, c, none8<T>(), rx);
     ScanPair<T> d = rows_of<T>(a.dout, a.vd, row, p.b, n0, c, none8<T>(), rd);
@@ -523,13 +609,15 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   const bool whole = wave == 0 && cl < a.C;
   if constexpr (!ONE) {
     join_chunk<true>(back, 4, ca, cr);
-    if (whole) tell_totals(a.rec, at0, ca, cr);
-    e0 = look_back(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
+    if (whole) tell_totals(a.rec.totals + at0, ca, cr);
+    if constexpr (CHAIN == kGroups) e0 = look_back(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
+    else e0 = look_far(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, cl, e0, ca, cr, cl < a.C);
   }
   if (whole) {
     join_chunk<true>(back, 4, ca, cr);
     const float end = __builtin_fmaf(ca, e0, cr);
-    if (!ONE && (last - p.chunk) % a.group == a.group - 1) tell_value(a.rec, at0, end);
+    if (CHAIN == kGroups && (last - p.chunk) % a.group == a.group - 1) tell_value(a.rec.values + at0, end);
+    if (CHAIN == kStretches && (last - p.chunk) % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + at0 + 2 * a.C, end);
     if (a.dstate_in && p.chunk == 0) a.dstate_in[(long long)p.b * a.C + cl] = end;
   }
   float h[8], E[8];

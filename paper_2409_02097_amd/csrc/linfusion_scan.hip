@@ -63,11 +63,17 @@ size_t states(int B, long long N, int C) { return lfh::up256((size_t)B * chunks_
 
 constexpr size_t kTicketBytes = 256;
 
-// Chunks of a group (up to 32): few mean many values that wait for one another, many that a chunk reads many totals (65536 x 1280 bf16: 4
-// 235 us, 8 172, 16 162, 32 164).
+// Chunks of a group, groups of a stretch: few mean many values that wait for one another, many that a chunk reads many totals (65536 x 1280 bf16
+// in groups of 4 235 us, 8 172, 16 162, 32 164; 2^20 x 64 in stretches of 4 547 us, 8 226, 16 174).
 int group_size() {
-  const int g = lfh::env_int("LINFUSION_SCAN_GROUP", 16);
-  return g < 1 ? 1 : (g > lf::kScanGroup ? lf::kScanGroup : g);
+  const int g = lfh::env_int("LINFUSION_SCAN_GROUP", lf::kScanGroup);
+  return g < 4 ? 4 : (g > lf::kScanGroup ? lf::kScanGroup : g);
+}
+// Whether the chain from group to group (1.8 us each) takes longer than the chunks themselves (16 ns each where all CUs have some): stretches
+// then (bf16, 65536 x 64: 22 us, 67 by groups; 2^20 x 64: 174, 922), groups else (65536 x 1280: 162, stretches 10 % more).
+constexpr int kNarrow = 8;   // chunks side by side
+bool narrow(long long chunks, int B, int C) {
+  return chunks > group_size() && (long long)B * ((C + lf::kScanWidth - 1) / lf::kScanWidth) < kNarrow;
 }
 
 lf::ScanRecords records(void* workspace, int B, long long N, int C) {
@@ -82,24 +88,25 @@ void clear(const lf::ScanRecords& r, int B, long long chunks, int C, hipStream_t
 
 long long tiles_of(long long chunks, int B, int C) { return chunks * ((C + lf::kScanWidth - 1) / lf::kScanWidth) * B; }
 
-template <typename T, int MODE, bool INPUT, int TT, bool ONE>
+template <typename T, int MODE, bool INPUT, int TT, int CHAIN>
 int forward(const lf::ScanArgs& a0, hipStream_t st) {
   lf::ScanArgs a = a0;
   const long long chunks = (a.N + 32 * TT - 1) / (32 * TT);
   const long long tiles = tiles_of(chunks, a.B, a.C);
   if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   a.chunks = (int)chunks;
-  if constexpr (!ONE) clear(a.rec, a.B, chunks, a.C, st);
-  lf::scan_fwd<T, MODE, INPUT, TT, ONE><<<(unsigned)tiles, 256, 0, st>>>(a);
+  if constexpr (CHAIN != lf::kAlone) clear(a.rec, a.B, chunks, a.C, st);
+  lf::scan_fwd<T, MODE, INPUT, TT, CHAIN><<<(unsigned)tiles, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
 // One chunk holds up to 128 tokens, or 256 of 16-bit types with eight a thread.
 template <typename T, int MODE, bool INPUT>
 int forward(const lf::ScanArgs& a, hipStream_t st) {
   constexpr int kLong = lf::Stored<T>::kBytes == 4 ? lf::kScanT : 2 * lf::kScanT;
-  if (a.N <= lf::kScanChunk) return forward<T, MODE, INPUT, lf::kScanT, true>(a, st);
-  if (kLong > lf::kScanT && a.N <= 32 * kLong) return forward<T, MODE, INPUT, kLong, true>(a, st);
-  return forward<T, MODE, INPUT, lf::kScanT, false>(a, st);
+  if (a.N <= lf::kScanChunk) return forward<T, MODE, INPUT, lf::kScanT, lf::kAlone>(a, st);
+  if (kLong > lf::kScanT && a.N <= 32 * kLong) return forward<T, MODE, INPUT, kLong, lf::kAlone>(a, st);
+  if (narrow(chunks_of(a.N), a.B, a.C)) return forward<T, MODE, INPUT, lf::kScanT, lf::kStretches>(a, st);
+  return forward<T, MODE, INPUT, lf::kScanT, lf::kGroups>(a, st);
 }
 
 template <typename T, int MODE, bool INPUT>
@@ -107,11 +114,12 @@ int backward(const lf::ScanBackArgs& a, hipStream_t st) {
   const long long tiles = tiles_of(a.chunks, a.B, a.C);
   if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   if (a.chunks == 1) {
-    lf::scan_bwd<T, MODE, INPUT, true><<<(unsigned)tiles, 256, 0, st>>>(a);
+    lf::scan_bwd<T, MODE, INPUT, lf::kAlone><<<(unsigned)tiles, 256, 0, st>>>(a);
     return LINFUSION_OK;
   }
   clear(a.rec, a.B, a.chunks, a.C, st);
-  lf::scan_bwd<T, MODE, INPUT, false><<<(unsigned)tiles, 256, 0, st>>>(a);
+  if (narrow(a.chunks, a.B, a.C)) lf::scan_bwd<T, MODE, INPUT, lf::kStretches><<<(unsigned)tiles, 256, 0, st>>>(a);
+  else lf::scan_bwd<T, MODE, INPUT, lf::kGroups><<<(unsigned)tiles, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
 

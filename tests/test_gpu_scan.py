@@ -121,6 +121,23 @@ def test_ragged_rows(N, lengths, reverse, dtype):
         assert torch.equal(last[at], g["state_in"][at])
 
 
+@pytest.mark.parametrize("dtype,reverse", [("f32", False), ("bf16", True)])
+def test_long_rows_of_few_channels(dtype, reverse):
+    """Hundreds of chunks with few beside them: more than a stretch of groups, and exactly one; the same from run to run, states in place."""
+    c = make(2, 40000, 72, dtype, 12, reverse=reverse, lengths=(40000, 32768))
+    g = on_gpu(c)
+    out, last, keep = forward(c, g)
+    grads = backward(c, g, keep)
+    check_all(c, out, last, grads)
+    for _ in range(3):
+        again, state = torch.full_like(out, 7.0), g["state_in"].clone()
+        lf.linfusion_scan_fwd(g["x"], g["gate"], g["input"], g["rate"], again, state_in=state, state_out=state, lengths=g["lengths"],
+                              flags=flags(c), workspace=memory(lf.linfusion_scan_workspace_bytes(*c["dims"])))
+        assert torch.equal(again, out) and torch.equal(state, last)
+        more = backward(c, g, None)
+        assert all(torch.equal(grads[n], more[n]) for n in grads)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_columns_of_one_buffer(dtype):
     c = make(2, 400, 72, dtype, 5)

@@ -47,7 +47,7 @@ struct ScanArgs {
   ScanRecords rec;
   const int* lengths;
   long long N;
-  int B, C, chunks, saved_chunks, group;
+  int B, C, chunks, saved_chunks, group, seg;
   bool reverse;
 };
 
@@ -60,7 +60,7 @@ struct ScanBackArgs {
   ScanRecords rec;
   const int* lengths;
   long long N;
-  int B, C, chunks, group;
+  int B, C, chunks, group, seg;
   bool reverse;
 };
 
@@ -191,8 +191,8 @@ struct ScanJoin {
 // A wave's LDS operations complete in the order in which they are issued: between its lanes no barrier is needed, only the order.
 LF_DEV void lds_in_order() { asm volatile("" ::: "memory"); }
 
-// before the barrier: `A`, `R` are replaced by those of the wave's stretches in front of this thread's
-template <bool BACK> LF_DEV void join_wave(ScanJoin& s, float (&A)[8], float (&R)[8]) {
+// before the barrier: `A`, `R` are replaced by those of the wave's stretches in front of this thread's (of the `seg` among which it is)
+template <bool BACK> LF_DEV void join_wave(ScanJoin& s, float (&A)[8], float (&R)[8], int seg = 8) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = threadIdx.x >> 3, c = (lane & 7) * 8;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -211,6 +211,10 @@ template <bool BACK> LF_DEV void join_wave(ScanJoin& s, float (&A)[8], float (&R
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int t = wave * 8 + (BACK ? 7 - j : j);
+    if ((j & (seg - 1)) == 0) {
+      pa = 1.0f;
+      pr = 0.0f;
+    }
     s.stretch[t][0][lane] = pa;
     s.stretch[t][1][lane] = pr;
     pr = __builtin_fmaf(a[j], pr, r[j]);
@@ -258,6 +262,25 @@ LF_DEV void spread8(float* lds, float v, float (&x)[8]) {
 }
 
 struct ScanPlace { int chunk, b, c0; };
+inline __host__ __device__ int packed_tiles(int B, int seg) { return (int)(((long long)B * seg + 31) / 32); }
+
+// A thread's batch row and its first token; packed: of the rows of a workgroup its own (`on`: whether there is one).
+template <bool PACKED> struct ScanThread {
+  int b, t0;
+  bool on;
+  LF_DEV ScanThread(const ScanPlace& p, int c, int B, int C, int seg, int tokens, int chunk) : b(p.b), on(c < C) {
+    const int at = threadIdx.x >> 3;
+    if constexpr (PACKED) {
+      b = p.b * (32 / seg) + at / seg;
+      on = on && b < B;
+      b = b < B ? b : B - 1;
+      t0 = (at & (seg - 1)) * tokens;
+    } else {
+      t0 = p.chunk * chunk + at * tokens;
+    }
+  }
+};
+
 
 // ---- between chunks ----------------------------------------------------------------------------------------------------
 
@@ -280,8 +303,9 @@ template <typename W> LF_DEV void await(W& w, const W* p) {
 
 // How a row's chunks hear of one another.  kAlone: there is one.  kGroups: in groups; a group's last chunk tells the value behind it, so a row is a
 // chain of groups.  kStretches: the groups in stretches of as many; a group's last chunk tells the group's totals, a stretch's last one the value behind
-// it, so a row is a chain of stretches, for rows with too few channels beside one another to hide the longer chain.
-constexpr int kAlone = 0, kGroups = 1, kStretches = 2;
+// it, so a row is a chain of stretches, for rows with too few channels beside one another to hide the longer chain.  kPacked: rows of 32 tokens or
+// fewer, several in a workgroup: `seg` time lanes (1, 2, 4 or 8) each, nothing to be told and no barrier.
+constexpr int kAlone = 0, kGroups = 1, kStretches = 2, kPacked = 3;
 
 constexpr int kScanGroup = 16;   // chunks of a group, groups of a stretch, at most
 struct ScanFound { float value[kScanWidth]; };
@@ -446,28 +470,29 @@ struct ScanForwardLds {
 template <typename T, int MODE, bool INPUT, int TT, int CHAIN>
 __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
   constexpr int L = 32 * TT;
-  constexpr bool ONE = CHAIN == kAlone;
+  constexpr bool ONE = CHAIN == kAlone || CHAIN == kPacked;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanForwardLds shared;
   ScanJoin& lds = shared.join;
-  const ScanPlace p = take_tile<ONE, false>(a.rec, a.B, a.C, a.chunks, shared.id);
+  const ScanPlace p = take_tile<ONE, false>(a.rec, CHAIN == kPacked ? packed_tiles(a.B, a.seg) : a.B, a.C, a.chunks, shared.id);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
-  const bool on = c < a.C;
-  const ScanRow row(a.lengths, p.b, a.N, a.reverse);
-  const int t0 = p.chunk * L + (threadIdx.x >> 3) * TT;
+  const ScanThread<CHAIN == kPacked> me(p, c, a.B, a.C, a.seg, TT, L);
+  const bool on = me.on;
+  const ScanRow row(a.lengths, me.b, a.N, a.reverse);
+  const int t0 = me.t0;
   if (p.chunk && (long long)p.chunk * L >= row.n) return;   // (the whole workgroup)
   const int live = on ? (row.n - t0 < TT ? (int)(row.n - t0) : TT) : 0;   // this thread's tokens that count (below 0: none)
   Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1];
-  const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
+  const bool full = CHAIN != kPacked && (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
   float rate[8], h0 = 0.0f;   // (rate requested first: loads are waited for in their order)
   load_rate(a.rate + c, on, rate);
   {
     const long long n = row.token(t0);
-    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, p.b, n, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, p.b, n, c, none8<T>(), rx);
-    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, p.b, n, c, none8<T>(), ri));
+    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, me.b, n, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, me.b, n, c, none8<T>(), rx);
+    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, me.b, n, c, none8<T>(), ri));
     else load_rows<T, TT>(live, full, g, x);
   }
-  if (cl < a.C && a.state_in && (ONE || p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) h0 = a.state_in[(long long)p.b * a.C + cl];
+  if (CHAIN != kPacked && cl < a.C && a.state_in && (ONE || p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) h0 = a.state_in[(long long)p.b * a.C + cl];
   float da[TT][8], u[TT][8], A[8], R[8];
 #pragma unroll
   for (int j = 0; j < TT; ++j) {
@@ -485,36 +510,44 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
       A[k] = j ? A[k] * da[j][k] : da[j][k];
     }
   }
-  join_wave<false>(lds, A, R);
-  arrive(h0);
-  __syncthreads();
-  float ca, cr;
-  const long long row0 = (long long)p.b * a.chunks * a.C + cl;
-  const bool whole = wave == 0 && cl < a.C;   // the threads that speak for the chunk
-  const long long i0 = row0 + (long long)p.chunk * a.C;
-  if constexpr (!ONE) {
-    join_chunk<false>(lds, 4, ca, cr);
-    if (whole) tell_totals(a.rec.totals + i0, ca, cr);
-    if constexpr (CHAIN == kGroups) h0 = look_back(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
-    else h0 = look_far(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, cl, h0, ca, cr, cl < a.C);
-  }
-  if (whole) {
-    join_chunk<false>(lds, 4, ca, cr);
-    const float end = __builtin_fmaf(ca, h0, cr);
-    if (CHAIN == kGroups && p.chunk % a.group == a.group - 1) tell_value(a.rec.values + i0, end);
-    if (CHAIN == kStretches && p.chunk % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + i0 - 2 * a.C, end);
-    if (a.state_out && (long long)(p.chunk + 1) * L >= row.n) a.state_out[(long long)p.b * a.C + cl] = end;   // the last token is here
-  }
-  join_chunk<false>(lds, wave, ca, cr);
-  const float mine = __builtin_fmaf(ca, h0, cr);   // the state before the wave's tokens
-  if (a.saved && cl < a.C && wave * 8 * TT % kScanChunk == 0) {
-    const long long t = (long long)p.chunk * L + wave * 8 * TT;
-    if (t == 0 || t < row.n) a.saved[((long long)p.b * a.saved_chunks + t / kScanChunk) * a.C + cl] = mine;
+  float h[8];
+  if constexpr (CHAIN == kPacked) {
+    join_wave<false>(lds, A, R, a.seg);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = 0.0f;
+    if (on && a.state_in) load8_f32(a.state_in + (long long)me.b * a.C + c, h);
+    if (on && a.saved && t0 == 0) store8<F32>(reinterpret_cast<unsigned char*>(a.saved + (long long)me.b * a.C + c), h);
+  } else {
+    join_wave<false>(lds, A, R);
+    arrive(h0);
+    __syncthreads();
+    float ca, cr;
+    const long long row0 = (long long)p.b * a.chunks * a.C + cl;
+    const bool whole = wave == 0 && cl < a.C;   // the threads that speak for the chunk
+    const long long i0 = row0 + (long long)p.chunk * a.C;
+    if constexpr (!ONE) {
+      join_chunk<false>(lds, 4, ca, cr);
+      if (whole) tell_totals(a.rec.totals + i0, ca, cr);
+      if constexpr (CHAIN == kGroups) h0 = look_back(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, h0, cl < a.C);
+      else h0 = look_far(a.rec, shared.found, lds.stretch, a.group, p.chunk, i0, a.C, cl, h0, ca, cr, cl < a.C);
+    }
+    if (whole) {
+      join_chunk<false>(lds, 4, ca, cr);
+      const float end = __builtin_fmaf(ca, h0, cr);
+      if (CHAIN == kGroups && p.chunk % a.group == a.group - 1) tell_value(a.rec.values + i0, end);
+      if (CHAIN == kStretches && p.chunk % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + i0 - 2 * a.C, end);
+      if (a.state_out && (long long)(p.chunk + 1) * L >= row.n) a.state_out[(long long)p.b * a.C + cl] = end;   // the last token is here
+    }
+    join_chunk<false>(lds, wave, ca, cr);
+    const float mine = __builtin_fmaf(ca, h0, cr);   // the state before the wave's tokens
+    if (a.saved && cl < a.C && wave * 8 * TT % kScanChunk == 0) {
+      const long long t = (long long)p.chunk * L + wave * 8 * TT;
+      if (t == 0 || t < row.n) a.saved[((long long)p.b * a.saved_chunks + t / kScanChunk) * a.C + cl] = mine;
+    }
+    spread8(shared.spread[wave], mine, h);
   }
   if (!a.out) return;
-  float h[8];
-  spread8(shared.spread[wave], mine, h);
-  unsigned char* po = at<T>(a.out, p.b * a.vo.batch + row.token(t0) * a.vo.token + c);
+  unsigned char* po = at<T>(a.out, me.b * a.vo.batch + row.token(t0) * a.vo.token + c);
   const long long so = row.step<T>(a.vo);
 #pragma unroll
   for (int k = 0; k < 8; ++k) h[k] = __builtin_fmaf(A[k], h[k], R[k]);
@@ -524,6 +557,10 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
     for (int k = 0; k < 8; ++k) h[k] = __builtin_fmaf(da[j][k], h[k], u[j][k]);
     if (j < live) store8_stream<T>(po, h);
     po += so;
+  }
+  if constexpr (CHAIN == kPacked) {   // whose tokens reach the last that counts (without any: the first)
+    const bool ends = row.n > t0 ? row.n <= t0 + TT : (row.n == 0 && t0 == 0);
+    if (on && a.state_out && ends) store8<F32>(reinterpret_cast<unsigned char*>(a.state_out + (long long)me.b * a.C + c), h);
   }
 }
 
@@ -541,33 +578,34 @@ struct ScanBackLds {
 template <typename T, int MODE, bool INPUT, int CHAIN>
 __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
   constexpr int TT = kScanT, L = kScanChunk;
-  constexpr bool ONE = CHAIN == kAlone;
+  constexpr bool ONE = CHAIN == kAlone || CHAIN == kPacked;
   constexpr bool kPrecise = Stored<T>::kBytes == 4;
   __shared__ ScanBackLds shared;
   ScanJoin &there = shared.there, &back = shared.back;
-  const ScanPlace p = take_tile<ONE, true>(a.rec, a.B, a.C, a.chunks, shared.id);
+  const ScanPlace p = take_tile<ONE, true>(a.rec, CHAIN == kPacked ? packed_tiles(a.B, a.seg) : a.B, a.C, a.chunks, shared.id);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = p.c0 + (lane & 7) * 8, cl = p.c0 + lane;
-  const bool on = c < a.C;
-  const ScanRow row(a.lengths, p.b, a.N, a.reverse);
+  const ScanThread<CHAIN == kPacked> me(p, c, a.B, a.C, a.seg, TT, L);
+  const bool on = me.on;
+  const ScanRow row(a.lengths, me.b, a.N, a.reverse);
   const long long row0 = (long long)p.b * a.chunks * a.C + cl, at0 = row0 + (long long)p.chunk * a.C;
-  const int last = row.n ? (int)((row.n - 1) / L) : 0;
+  const int last = row.n ? (int)((row.n - 1) / L) : 0;   // (packed: 0)
   if (p.chunk > last) {   // (the whole workgroup)
     if (wave == 0 && cl < a.C) a.partials[at0] = 0.0f;
     return;
   }
-  const int t0 = p.chunk * L + (threadIdx.x >> 3) * TT;
+  const int t0 = me.t0;
   const int live = on ? (row.n - t0 < TT ? (int)(row.n - t0) : TT) : 0;
   const long long n0 = row.token(t0);
   Raw8<T> rx[TT], rg[TT], ri[INPUT ? TT : 1], rd[TT];
-  const bool full = (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
+  const bool full = CHAIN != kPacked && (long long)(p.chunk + 1) * L <= row.n && p.c0 + kScanWidth <= a.C;
   float rate[8], h0 = 0.0f, e0 = 0.0f;
   load_rate(a.rate + c, on, rate);
-  if (cl < a.C) h0 = a.starts[at0];
-  if (cl < a.C && a.dstate_out && (ONE || last - p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) e0 = a.dstate_out[(long long)p.b * a.C + cl];
+  if (CHAIN != kPacked && cl < a.C) h0 = a.starts[at0];
+  if (CHAIN != kPacked && cl < a.C && a.dstate_out && (ONE || last - p.chunk < (CHAIN == kStretches ? a.group * a.group : a.group))) e0 = a.dstate_out[(long long)p.b * a.C + cl];
   {
-    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, p.b, n0, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, p.b, n0, c, none8<T>(), rx);
-    ScanPair<T> d = rows_of<T>(a.dout, a.vd, row, p.b, n0, c, none8<T>(), rd);
-    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, p.b, n0, c, none8<T>(), ri), d);
+    ScanPair<T> g = rows_of<T>(a.gate, a.vg, row, me.b, n0, c, shut8<T>(), rg), x = rows_of<T>(a.x, a.vx, row, me.b, n0, c, none8<T>(), rx);
+    ScanPair<T> d = rows_of<T>(a.dout, a.vd, row, me.b, n0, c, none8<T>(), rd);
+    if constexpr (INPUT) load_rows<T, TT>(live, full, g, x, rows_of<T>(a.input, a.vi, row, me.b, n0, c, none8<T>(), ri), d);
     else load_rows<T, TT>(live, full, g, x, d);
   }
   // (m i waits in LDS: with it and what follows from it in registers 75 of them spill)
@@ -601,30 +639,40 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) BR[k] = da[j][k] * (BR[k] + d[k]);
   }
-  join_wave<false>(there, A, R);
-  join_wave<true>(back, BA, BR);
-  arrive(e0);
-  __syncthreads();
-  float ca, cr;
-  const bool whole = wave == 0 && cl < a.C;
-  if constexpr (!ONE) {
-    join_chunk<true>(back, 4, ca, cr);
-    if (whole) tell_totals(a.rec.totals + at0, ca, cr);
-    if constexpr (CHAIN == kGroups) e0 = look_back(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
-    else e0 = look_far(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, cl, e0, ca, cr, cl < a.C);
-  }
-  if (whole) {
-    join_chunk<true>(back, 4, ca, cr);
-    const float end = __builtin_fmaf(ca, e0, cr);
-    if (CHAIN == kGroups && (last - p.chunk) % a.group == a.group - 1) tell_value(a.rec.values + at0, end);
-    if (CHAIN == kStretches && (last - p.chunk) % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + at0 + 2 * a.C, end);
-    if (a.dstate_in && p.chunk == 0) a.dstate_in[(long long)p.b * a.C + cl] = end;
-  }
   float h[8], E[8];
-  join_chunk<false>(there, wave, ca, cr);
-  spread8(shared.spread[0][wave], __builtin_fmaf(ca, h0, cr), h);
-  join_chunk<true>(back, 3 - wave, ca, cr);
-  spread8(shared.spread[1][wave], __builtin_fmaf(ca, e0, cr), E);
+  const bool whole = wave == 0 && cl < a.C;
+  if constexpr (CHAIN == kPacked) {
+    join_wave<false>(there, A, R, a.seg);
+    join_wave<true>(back, BA, BR, a.seg);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = E[k] = 0.0f;
+    const long long of = (long long)me.b * a.C + c;
+    if (on) load8_f32(a.starts + of, h);
+    if (on && a.dstate_out) load8_f32(a.dstate_out + of, E);
+  } else {
+    join_wave<false>(there, A, R);
+    join_wave<true>(back, BA, BR);
+    arrive(e0);
+    __syncthreads();
+    float ca, cr;
+    if constexpr (!ONE) {
+      join_chunk<true>(back, 4, ca, cr);
+      if (whole) tell_totals(a.rec.totals + at0, ca, cr);
+      if constexpr (CHAIN == kGroups) e0 = look_back(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, e0, cl < a.C);
+      else e0 = look_far(a.rec, shared.found, back.stretch, a.group, last - p.chunk, at0, -(long long)a.C, cl, e0, ca, cr, cl < a.C);
+    }
+    if (whole) {
+      join_chunk<true>(back, 4, ca, cr);
+      const float end = __builtin_fmaf(ca, e0, cr);
+      if (CHAIN == kGroups && (last - p.chunk) % a.group == a.group - 1) tell_value(a.rec.values + at0, end);
+      if (CHAIN == kStretches && (last - p.chunk) % (a.group * a.group) == a.group * a.group - 1) tell_value(a.rec.values + at0 + 2 * a.C, end);
+      if (a.dstate_in && p.chunk == 0) a.dstate_in[(long long)p.b * a.C + cl] = end;
+    }
+    join_chunk<false>(there, wave, ca, cr);
+    spread8(shared.spread[0][wave], __builtin_fmaf(ca, h0, cr), h);
+    join_chunk<true>(back, 3 - wave, ca, cr);
+    spread8(shared.spread[1][wave], __builtin_fmaf(ca, e0, cr), E);
+  }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     h[k] = __builtin_fmaf(A[k], h[k], R[k]);
@@ -642,9 +690,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) by_rate[k] = 0.0f;
   const long long sdx = row.step<T>(a.vdx), sdg = row.step<T>(a.vdg), sdi = row.step<T>(a.vdi);
-  unsigned char* pdx = at<T>(a.dx, p.b * a.vdx.batch + n0 * a.vdx.token + c) + (TT - 1) * sdx;
-  unsigned char* pdg = at<T>(a.dgate, p.b * a.vdg.batch + n0 * a.vdg.token + c) + (TT - 1) * sdg;
-  unsigned char* pdi = at<T>(a.dinput, p.b * a.vdi.batch + n0 * a.vdi.token + c) + (TT - 1) * sdi;
+  unsigned char* pdx = at<T>(a.dx, me.b * a.vdx.batch + n0 * a.vdx.token + c) + (TT - 1) * sdx;
+  unsigned char* pdg = at<T>(a.dgate, me.b * a.vdg.batch + n0 * a.vdg.token + c) + (TT - 1) * sdg;
+  unsigned char* pdi = at<T>(a.dinput, me.b * a.vdi.batch + n0 * a.vdi.token + c) + (TT - 1) * sdi;
 #pragma unroll
   for (int j = TT - 1; j >= 0; --j) {
     float x[8], in[8], d[8], dx[8], dg[8], di[8];
@@ -681,6 +729,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
     pdg -= sdg;
     pdi -= sdi;
   }
+  if (CHAIN == kPacked && on && a.dstate_in && t0 == 0) store8<F32>(reinterpret_cast<unsigned char*>(a.dstate_in + (long long)me.b * a.C + c), E);
   __syncthreads();   // the stretches' LDS takes the sums
 #pragma unroll
   for (int q = 0; q < 2; ++q)

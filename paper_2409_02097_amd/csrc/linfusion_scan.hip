@@ -76,6 +76,15 @@ bool narrow(long long chunks, int B, int C) {
   return chunks > group_size() && (long long)B * ((C + lf::kScanWidth - 1) / lf::kScanWidth) < kNarrow;
 }
 
+// Time lanes of a row of up to 32 tokens where several share a workgroup, else 0 (bf16 forward, 65535 x 2 x 64: 23 us, 503 with a workgroup
+// for every row; 6240 x 13 x 2048 285 us, 1.33 GB).
+int packed(int B, long long N) {
+  if (B == 1 || N > 32) return 0;
+  int seg = 1;
+  while (seg * lf::kScanT < N) seg *= 2;
+  return seg;
+}
+
 lf::ScanRecords records(void* workspace, int B, long long N, int C) {
   char* w = (char*)workspace;
   return lf::ScanRecords{(unsigned*)w, (unsigned long long*)(w + kTicketBytes), (unsigned*)(w + kTicketBytes + 2 * states(B, N, C))};
@@ -92,10 +101,10 @@ template <typename T, int MODE, bool INPUT, int TT, int CHAIN>
 int forward(const lf::ScanArgs& a0, hipStream_t st) {
   lf::ScanArgs a = a0;
   const long long chunks = (a.N + 32 * TT - 1) / (32 * TT);
-  const long long tiles = tiles_of(chunks, a.B, a.C);
+  const long long tiles = tiles_of(chunks, CHAIN == lf::kPacked ? lf::packed_tiles(a.B, a.seg) : a.B, a.C);
   if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
   a.chunks = (int)chunks;
-  if constexpr (CHAIN != lf::kAlone) clear(a.rec, a.B, chunks, a.C, st);
+  if constexpr (CHAIN == lf::kGroups || CHAIN == lf::kStretches) clear(a.rec, a.B, chunks, a.C, st);
   lf::scan_fwd<T, MODE, INPUT, TT, CHAIN><<<(unsigned)tiles, 256, 0, st>>>(a);
   return LINFUSION_OK;
 }
@@ -103,6 +112,7 @@ int forward(const lf::ScanArgs& a0, hipStream_t st) {
 template <typename T, int MODE, bool INPUT>
 int forward(const lf::ScanArgs& a, hipStream_t st) {
   constexpr int kLong = lf::Stored<T>::kBytes == 4 ? lf::kScanT : 2 * lf::kScanT;
+  if (a.seg) return forward<T, MODE, INPUT, lf::kScanT, lf::kPacked>(a, st);
   if (a.N <= lf::kScanChunk) return forward<T, MODE, INPUT, lf::kScanT, lf::kAlone>(a, st);
   if (kLong > lf::kScanT && a.N <= 32 * kLong) return forward<T, MODE, INPUT, kLong, lf::kAlone>(a, st);
   if (narrow(chunks_of(a.N), a.B, a.C)) return forward<T, MODE, INPUT, lf::kScanT, lf::kStretches>(a, st);
@@ -111,8 +121,12 @@ int forward(const lf::ScanArgs& a, hipStream_t st) {
 
 template <typename T, int MODE, bool INPUT>
 int backward(const lf::ScanBackArgs& a, hipStream_t st) {
-  const long long tiles = tiles_of(a.chunks, a.B, a.C);
+  const long long tiles = tiles_of(a.chunks, a.seg ? lf::packed_tiles(a.B, a.seg) : a.B, a.C);
   if (tiles > 0x7fffffffLL) return LINFUSION_ERR_INVALID;
+  if (a.seg) {
+    lf::scan_bwd<T, MODE, INPUT, lf::kPacked><<<(unsigned)tiles, 256, 0, st>>>(a);
+    return LINFUSION_OK;
+  }
   if (a.chunks == 1) {
     lf::scan_bwd<T, MODE, INPUT, lf::kAlone><<<(unsigned)tiles, 256, 0, st>>>(a);
     return LINFUSION_OK;
@@ -186,7 +200,7 @@ int linfusion_scan_fwd(const void* x, const void* gate, const void* input, const
   if (meet(span(vo), s_in) || meet(ws, s_in) || meet(kept, s_in) || (state_in != state_out && meet(s_in, s_out))) return LINFUSION_ERR_OVERLAP;
   if ((rc = lfh::check_device()) != LINFUSION_OK) return rc;
   const lf::ScanArgs a{x, gate, input, out, dev(vx), dev(vg), dev(vi), dev(vo), rate, state_in, state_out, (float*)saved,
-                       records(workspace, B, N, C), lengths, N, B, C, 0, (int)chunks_of(N), group_size(), (flags & LINFUSION_FLAG_SCAN_REVERSE) != 0};
+                       records(workspace, B, N, C), lengths, N, B, C, 0, (int)chunks_of(N), group_size(), packed(B, N), (flags & LINFUSION_FLAG_SCAN_REVERSE) != 0};
   if ((rc = launch_forward(a, dtype, mode_of(flags), (hipStream_t)stream)) != LINFUSION_OK) return rc;
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }
@@ -223,17 +237,17 @@ int linfusion_scan_bwd(const void* x, const void* gate, const void* input, const
   const float* starts = (const float*)saved;
   if (!saved) {   // the states between the chunks again
     const lf::ScanArgs f{x, gate, input, nullptr, dev(v[0]), dev(v[1]), dev(v[2]), lf::ScanView{0, 0}, rate, state_in, nullptr, (float*)(w + one),
-                         rec, lengths, N, B, C, 0, (int)chunks_of(N), group_size(), reverse};
+                         rec, lengths, N, B, C, 0, (int)chunks_of(N), group_size(), packed(B, N), reverse};
     if ((rc = launch_forward(f, dtype, mode_of(flags), st)) != LINFUSION_OK) return rc;
     starts = f.saved;
   }
   const lf::ScanBackArgs a{x, gate, input, dout, dx, dgate, dinput, dev(v[0]), dev(v[1]), dev(v[2]), dev(v[3]), dev(v[4]), dev(v[5]), dev(v[6]),
-                           rate, starts, dstate_out, dstate_in, (float*)w, rec, lengths, N, B, C, (int)chunks_of(N), group_size(), reverse};
+                           rate, starts, dstate_out, dstate_in, (float*)w, rec, lengths, N, B, C, (int)chunks_of(N), group_size(), packed(B, N), reverse};
   rc = with(dtype, mode_of(flags), input != nullptr, [&](auto t, auto m, auto i) {
     return backward<decltype(t), decltype(m)::value, decltype(i)::value>(a, st);
   });
   if (rc != LINFUSION_OK) return rc;
-  lf::scan_rate_sums<<<(C + 15) / 16, 1024, 0, st>>>(a.partials, drate, (long long)B * a.chunks, C);
+  lf::scan_rate_sums<<<(C + 15) / 16, 1024, 0, st>>>(a.partials, drate, a.seg ? lf::packed_tiles(B, a.seg) : (long long)B * a.chunks, C);
   return hipGetLastError() == hipSuccess ? LINFUSION_OK : LINFUSION_ERR_HIP;
 }
 

@@ -108,6 +108,31 @@ def test_against_the_oracle(shape, weight, inputs, state, reverse, dtype):
     assert torch.equal(plain[0], out) and torch.equal(plain[1], last)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("weight,inputs,state,reverse,ragged", [("norm", True, True, False, False), ("norm", True, True, True, True), ("leaky", False, False, True, False),
+                                                                ("sum", True, True, False, True)])
+@pytest.mark.parametrize("shape", [(5, 1, 72), (33, 2, 8), (7, 4, 64), (70, 5, 40), (65, 8, 136), (33, 13, 136), (6, 16, 8), (17, 17, 72), (11, 32, 200)], ids=str)
+def test_many_rows_of_a_few_tokens(shape, weight, inputs, state, reverse, ragged, dtype):
+    """Several rows share a workgroup; the last one has some to spare."""
+    B, N, C = shape
+    c = make(B, N, C, dtype, sum(shape), weight, inputs, state, reverse, tuple((5 * b + 3) % (N + 1) for b in range(B)) if ragged else None)
+    g = on_gpu(c)
+    out, last, keep = forward(c, g)
+    grads = backward(c, g, keep)
+    check_all(c, out, last, grads)
+    again = backward(c, g, None)
+    assert all(torch.equal(grads[n], again[n]) for n in grads)
+    if state:
+        held, slope = g["state_in"].clone(), g["dstate_out"].clone()
+        more = {n: torch.full_like(t, 7.0) for n, t in grads.items()}
+        lf.linfusion_scan_fwd(g["x"], g["gate"], g["input"], g["rate"], torch.empty_like(out), state_in=held, state_out=held, lengths=g["lengths"],
+                              flags=flags(c), workspace=memory(lf.linfusion_scan_workspace_bytes(*c["dims"])))
+        lf.linfusion_scan_bwd(g["x"], g["gate"], g["input"], g["rate"], g["dout"], more["dx"], more["dgate"], more.get("dinput"), more["drate"],
+                              state_in=g["state_in"], dstate_out=slope, dstate_in=slope, lengths=g["lengths"], flags=flags(c),
+                              workspace=memory(lf.linfusion_scan_bwd_workspace_bytes(*c["dims"])))
+        assert torch.equal(held, last) and torch.equal(slope, grads["dstate_in"])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("reverse", [False, True])
 @pytest.mark.parametrize("N,lengths", [(300, (300, 0, 1, 129)), (700, (128, 256, 257, 699)), (100, (0, 0, 5, 100)), (1100, (-3, 2000, 1024, 513))], ids=str)

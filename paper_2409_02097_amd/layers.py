@@ -157,6 +157,8 @@ def _matrix(name, t, shape, head):
         raise ValueError(f"{name} must be a {list(shape)} tensor of the call's type and device")
     if shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: a row's elements must be contiguous")
+    if shape[0] > 1 and t.stride(0) < shape[1]:   # (one row for all of them has stride 0, which the library takes for contiguous rows)
+        raise ValueError(f"{name}: the rows must lie one behind the other")
     return t.stride(0) if shape[0] > 1 else shape[1]
 
 

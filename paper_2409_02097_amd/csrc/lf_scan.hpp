@@ -77,13 +77,32 @@ LF_DEV float unless(bool c, float x) {
 }
 
 // 1 / (1 + e^-x), the exponential by the hardware's of 2; Precise adds back what rounding x log2(e) loses.
-template <bool Precise> LF_DEV float sigmoid_of(float x) {
+// `e`: e^-x.
+template <bool Precise> LF_DEV float sigmoid_of(float x, float& e) {
   constexpr float kLog2e = 1.44269504088896340736f;
-  const float t = x * -kLog2e, e = __builtin_amdgcn_exp2f(t);
+  const float t = x * -kLog2e;
+  e = __builtin_amdgcn_exp2f(t);
   if constexpr (!Precise) return __builtin_amdgcn_rcpf(1.0f + e);
   const float lost = __builtin_fmaf(x, -1.92596299112661746e-8f, __builtin_fmaf(x, -kLog2e, -t));
-  const float s = __builtin_amdgcn_rcpf(1.0f + unless(x > 104.0f, __builtin_fmaf(e, lost * 0.69314718055994530942f, e)));   // (no 0 times infinity)
+  e = unless(x > 104.0f, __builtin_fmaf(e, lost * 0.69314718055994530942f, e));   // (no 0 times infinity)
+  const float s = __builtin_amdgcn_rcpf(1.0f + e);
   return unless(x < -88.0f, s);
+}
+template <bool Precise> LF_DEV float sigmoid_of(float x) {
+  float e;
+  return sigmoid_of<Precise>(x, e);
+}
+
+// A sigmoid and one less it in one number, the smaller of the two, as next to 1 a sigmoid no longer holds what is left: s below x = 0, else s - 1, whose sign
+// says which (a zero's too).  s (1 - s) is |v| (1 - |v|) either way.
+template <bool Precise> LF_DEV float smaller_sigmoid(float x, float& s) {
+  float e;
+  s = sigmoid_of<Precise>(x, e);
+  float v = -(e * s);
+  asm("" : "+v"(v));   // (no branch)
+  v = x < 0.0f ? s : v;
+  asm volatile("" : "+v"(v));   // (or what it is chosen from is kept until it is needed)
+  return v;
 }
 
 // 1 - 2^-d for d >= 0, e = 2^-d given, or with TWICE 1 - 4^-d, e = 4^-d: where e is near 1 by the series, whose next term is below 2^-24
@@ -618,8 +637,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
     if constexpr (INPUT) widen8<T>(ri[j], in);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float s = sigmoid_of<kPrecise>(g[k]), d = rate[k] * 1.44269504088896340736f * s, ak = __builtin_amdgcn_exp2f(-d);
-      sg[j][k] = s;
+      float s;
+      sg[j][k] = smaller_sigmoid<kPrecise>(g[k], s);
+      const float d = rate[k] * 1.44269504088896340736f * s, ak = __builtin_amdgcn_exp2f(-d);
       da[j][k] = ak;
       mi[k] = weight_of<kPrecise, MODE>(d, ak);
       if constexpr (INPUT) mi[k] *= sigmoid_of<kPrecise>(in[k]);
@@ -706,19 +726,23 @@ __global__ __launch_bounds__(256, 2) void scan_bwd(ScanBackArgs a) {
     const f32x4 w0 = shared.weights[j][0][threadIdx.x], w1 = shared.weights[j][1][threadIdx.x];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {   // (a token that does not count: D = E, s = m = 0, a = 1)
-      const float D = d[k] + E[k], s = sg[j][k], mi = k < 4 ? w0[k & 3] : w1[k & 3];
+      const float D = d[k] + E[k], mi = k < 4 ? w0[k & 3] : w1[k & 3];
+      const float v = sg[j][k], other = 1.0f - __builtin_fabsf(v), s = __builtin_bit_cast(int, v) < 0 ? other : v;
       float i = 1.0f;
-      if constexpr (INPUT) i = sigmoid_of<kPrecise>(in[k]);
       dx[k] = D * mi;
-      if constexpr (INPUT) di[k] = dx[k] * x[k] * (1.0f - i);
+      if constexpr (INPUT) {
+        float e;
+        i = sigmoid_of<kPrecise>(in[k], e);
+        di[k] = dx[k] * x[k] * (__builtin_fminf(e, 0x1p126f) * i);   // 1 - i = e i (and no infinity times 0 where i, and so dx, is 0)
+      }
       E[k] = da[j][k] * D;
       // -dg = a D (r i x - h') with dm/dg = -a r: r = a / m, 1, 0
       float rix = 0.0f;
       if constexpr (MODE == kScanLeaky) rix = i * x[k];
       if constexpr (MODE == kScanNorm) rix = below(mi, 1.17549435e-38f, 0.0f, da[j][k] * (i * __builtin_amdgcn_rcpf(mi))) * (i * x[k]);
-      const float part = E[k] * (rix - u[j][k]) * s;
-      by_rate[k] += part;
-      dg[k] = part * rate[k] * (1.0f - s);
+      const float part = E[k] * (rix - u[j][k]);
+      by_rate[k] = __builtin_fmaf(part, s, by_rate[k]);
+      dg[k] = part * rate[k] * (__builtin_fabsf(v) * other);
     }
     if (j < live) {
       store8_stream<T>(pdx, dx);

@@ -424,12 +424,12 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
   constexpr int kRegion = 2 * kBuffer / kWaves, kFit = kRegion / (16 * WN * 4);
   constexpr int kPass = kFit >= MT ? MT : (kFit >= (MT + 1) / 2 && MT % 2 == 0 ? MT / 2 : (kFit >= 2 && MT % 2 == 0 ? 2 : 1));
   static_assert(kFit >= kPass && MT % kPass == 0, "whole passes");
-  constexpr int kLanes = WN / 8, kRows = 64 / kLanes;   // lanes of a row; rows at a time
+  constexpr int kRowLanes = WN / 8, kTogether = 64 / kRowLanes;   // lanes of a row; rows at a time
   constexpr int kAtOnce = 4;   // rows of a lane whose residuals are requested together
   __syncthreads();
   unsigned char* mine = smem + wave * kRegion;
-  const int row = lane / kLanes, u = lane % kLanes * 2, n = n0 + wn + 4 * u;
-  const bool on = lane < kRows * kLanes && n < g.N;
+  const int row = lane / kRowLanes, u = lane % kRowLanes * 2, n = n0 + wn + 4 * u;
+  const bool on = lane < kTogether * kRowLanes && n < g.N;
   float bias[8];
   if (on && !g.partials) bias8<T>(g.out, n, bias);
 #pragma unroll
@@ -443,12 +443,12 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
       }
     asm volatile("" ::: "memory");   // (a wave's LDS operations complete in order)
 #pragma unroll 1
-    for (int r0 = 0; r0 < 16 * kPass; r0 += kRows * kAtOnce) {
+    for (int r0 = 0; r0 < 16 * kPass; r0 += kTogether * kAtOnce) {
       LinToken t[kAtOnce];
       Raw8<T> residual[kAtOnce];
 #pragma unroll
       for (int q = 0; q < kAtOnce; ++q) {
-        const int r = r0 + q * kRows + row;
+        const int r = r0 + q * kTogether + row;
         t[q] = token_at<MAPPED != kFlat && AK>(m0 + wm + 16 * p + r, g.M, g.per_row, g.lengths);
         t[q].on = t[q].on && on && r < 16 * kPass;
         residual[q] = none8<T>();
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(64 * WR * WC, STEP == 64 && BM * BN <= 128 * 128 ? 
 #pragma unroll
       for (int q = 0; q < kAtOnce; ++q) {
         if (!t[q].on) continue;
-        const int r = r0 + q * kRows + row;
+        const int r = r0 + q * kTogether + row;
         const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + (u ^ (r & kTurn)) * 16);
         const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * (WN * 4) + ((u + 1) ^ (r & kTurn)) * 16);
         if (g.partials) {

@@ -441,7 +441,9 @@ int linfusion_attn_state(const void* k, const void* v, float* state_out,
  *   - Element types fp16, bf16, fp32 throughout; vectors, decays, corrections and states are fp32.  Arithmetic is fp32
  *     (angles and sums of log decays fp64), every result is rounded once.  Where it is less or comes to less: sines and
  *     cosines of 16-bit positions are within 2^-20; the delta rule's products leave out parts near 2^-24 of each; dg is
- *     a difference of sums that cancel and off by some 1e-6 of its largest value, three times a recurrence in fp32.
+ *     a difference of sums that cancel and off by some 1e-6 of its largest value, three times a recurrence in fp32; exponentials
+ *     of 16-bit recurrences and activations are the hardware's (steps of 2^-24, as many as their argument is large), GELU's tail there is
+ *     within 2.3e-5 of itself; linear_bwd rounds dz of 16-bit types before the products, so that dx and dw carry two roundings.
  *   - [B, H, N, d] views: element strides {batch, head, token} as in linfusion_attn_fwd_strided; a NULL array is the
  *     contiguous tensor.  [B, N, C] views: element strides {batch, token}.
  *   - `lengths`: NULL, or a DEVICE array of B int32: only the first lengths[b] tokens (clamped to 0 .. N) of batch row b
@@ -580,7 +582,7 @@ int linfusion_delta_step(const void* q, const void* k, const void* v, const floa
  * mean; LINFUSION_FLAG_SCAN_SUM: 1).
  *
  *   x, gate, input, out  [B, N, C] views, strides[i] of them in this order (strides NULL: all contiguous); input NULL: without its
- *                   factor.  C a multiple of 8 up to 8192, N < 2^30.
+ *                   factor.  B up to 65535, C a multiple of 8 up to 8192, N < 2^30.
  *   rate            fp32 [C], >= 0 and finite.
  *   state_in        fp32 [B, C], 16-byte aligned, or NULL (zeros).  state_out: the state behind the last token that counts, or NULL;
  *                   may be state_in itself.
@@ -623,7 +625,7 @@ int linfusion_scan_step(const void* x, const void* gate, const void* input, cons
  *                   the same strides works in place.  y or z may be NULL (not both): not written.  z: the values before the
  *                   activation, which linfusion_linear_bwd needs unless there is none.  Both are formed from the unrounded sums.
  *   w               [C_out, C_in], rows w_stride elements apart (0: C_in).  bias: [C_out] of the call's type, or NULL.
- *   C_in, C_out     multiples of 8 up to 32768; B * N < 2^31.
+ *   C_in, C_out     multiples of 8 up to 32768; B up to 65535, B * N < 2^31.
  *   activation      LINFUSION_ACT_*; slope: of LINFUSION_ACT_LEAKY_RELU below 0.  flags 0.
  *   workspace       DEVICE scratch of linfusion_linear_workspace_bytes, 16-byte aligned; never falls with B or N.
  * Products are of the stored values, sums fp32 (16-bit types: the 16-bit matrix instruction; fp32: the fp32 one).
@@ -653,7 +655,7 @@ size_t linfusion_linear_bwd_workspace_bytes(int B, long long N, int C_in, int C_
  * x / 2^e (ties to even).  exps holds e + 127; 255: the block holds an infinity or NaN and comes back as NaN.  A value comes back off by at
  * most 1 / 127 of its block's largest, or by 2^-127 if that is more (beyond the type's largest value: as that).
  *
- *   x               [B, N, C] view of the call's type, C a multiple of 8 up to 32768 (the last block may be shorter).
+ *   x               [B, N, C] view of the call's type, B up to 65535, C a multiple of 8 up to 32768 (the last block may be shorter).
  *   codes           int8 [B, N, C] view with 8-byte aligned rows; exps: uint8 [B, N, ceil(C / 32)] view of contiguous blocks.
  *                   strides: in the order of the arguments.  flags 0.
  * One kernel each, no workspace.

@@ -566,7 +566,10 @@ struct LinSlopeArgs {
 };
 
 // dz = dy act'(z), rounded once to the type (it is an operand of two products), and the sums of the unrounded values over a
-// workgroup's tokens.  `lanes` lanes of 8 channels a token, as many tokens at a time as that leaves, twice as many under way (absent ones from 16 bytes of zeros, without
+// workgroup's tokens.  That rounding is beside the results' own in dx and dw of 16-bit types: bf16 2.4e-3 of their norm off, 1.7e-3 with dz as two terms of the
+// type.  Those double the products' work: dx and dw of 49152 x 1280 to 320 take 101 and 101 us for 71 and 57, of 320 to 1280 115 and 108 for 48 and 57, of 16384 x
+// 1280 to 5120 405 and 381 for 204 and 221, and the way out of dz of 1280 channels 24 us more.  One term is also what a layer hands back whose activation is a call
+// of its own.  `lanes` lanes of 8 channels a token, as many tokens at a time as that leaves, twice as many under way (absent ones from 16 bytes of zeros, without
 // branches).  Bound: HBM (49152 x 1280 bf16 from kept z: 315 MB), with GELU the vector instructions too.
 template <typename T, bool KEPT> __global__ __launch_bounds__(256) void linear_slope(LinSlopeArgs a) {
   __shared__ float lds[256][8];

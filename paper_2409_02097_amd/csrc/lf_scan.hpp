@@ -15,7 +15,7 @@
 // the four waves joined through LDS.  The chunks of a long sequence tell each other theirs inside the launch (ScanRecords), so that
 // every tensor is read once and written once.  Everything is fp32, results are rounded once.
 // One MI355X: 65536 x 1280 bf16 with a gate on the inputs 162 us with the records' clearing, 671 MB at 4.2 TB/s, where a copy of
-// 1 GiB makes 5.2; 12 x 4096 x 320 bf16, 46 us forward and 60 back (189 MB at 3.2 TB/s).
+// 1 GiB makes 5.2; 12 x 4096 x 320 bf16, 46 us forward (126 MB) and 63 back (220 MB at 3.5 TB/s).
 #pragma once
 #include "lf_vec8.hpp"
 
@@ -586,7 +586,8 @@ __global__ __launch_bounds__(256) void scan_fwd(ScanArgs a) {
 // ---- backward ----------------------------------------------------------------------------------------------------------
 
 // The gradients of a chunk, from the state in front of it and E behind it, which comes from the chunks behind as the state does from
-// those before.  Bound: registers, which leave two workgroups a CU (three spill: 100 us where two take 60, 12 x 4096 x 320 bf16).
+// those before.  Bound: registers, which leave two workgroups a CU (three spill: 100 us where two take 60, 12 x 4096 x 320 bf16), and for fp32 with a gate on
+// the inputs not even those: 3 to 9 values a lane go through scratch, 23 to 27 in a chain of stretches.
 struct ScanBackLds {
   ScanJoin there, back;
   ScanFound found;

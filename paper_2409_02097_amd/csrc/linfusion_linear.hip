@@ -45,6 +45,7 @@ struct Plan { int kind, splits; long long k_split; };   // kind: index into the 
 #define LF_LINEAR_SHAPES(DO) \
   DO(0, 256, 256, 2, 4, 128, 1) DO(1, 128, 160, 2, 2, 128, 2) DO(2, 128, 128, 2, 2, 128, 2) DO(3, 128, 64, 2, 2, 128, 3) \
   DO(4, 64, 64, 2, 2, 128, 4) DO(5, 128, 128, 2, 2, 64, 4) DO(6, 128, 160, 2, 2, 64, 3) DO(7, 128, 64, 2, 2, 64, 5)
+// (Where every lane finds its tokens, dW by 128 x 128 in half steps spills 14 to 16 registers.)
 constexpr int kShapes = 8;
 struct Shape { int m, n, step, per_cu; };
 constexpr Shape kShape[kShapes] = {
